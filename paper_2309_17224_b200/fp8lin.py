@@ -27,13 +27,15 @@ MM_FWD, MM_DGRAD, MM_WGRAD = 0, 1, 2
 ACT_NONE = 0
 ACT_GELU = 1
 ACT_SWIGLU = 2
-FLAG_NONFINITE_AMAX, FLAG_ZERO_AMAX, FLAG_SATURATED, FLAG_TIMEOUT = 1, 2, 4, 8
+FLAG_NONFINITE_AMAX, FLAG_ZERO_AMAX, FLAG_SATURATED, FLAG_TIMEOUT, FLAG_BAD_INDEX = 1, 2, 4, 8, 16
+KV_BIAS_NONFINITE, KV_BIAS_MAX = -128, 64
 
 SYMBOLS = (
     "fp8_create", "fp8_destroy", "fp8_status_string", "fp8_device_flags", "fp8_amax", "fp8_scaling_bias",
     "fp8_scaling_bias_host", "fp8_cast_e4", "fp8_cast_e5", "fp8_ptq_weights", "fp8_linear_fwd", "fp8_linear_dgrad",
     "fp8_linear_wgrad", "fp8_amax_noalloc", "fp8_linear_fwd_act", "fp8_cast_predicted", "fp8_prediction_stats",
     "fp8_linear_dgrad_act", "fp8_selftest_wait_expiry", "fp8_range_stats", "fp8_linear_fwd_q", "fp8_linear_dgrad_q", "fp8_amax_history_bias", "fp8_launch_count", "fp8_cast_group", "fp8_selftest_mma_ceiling", "fp8_bias_log_append", "fp8_bias_mode", "fp8_linear_f16acc", "fp8_linear_infer", "fp8_linear_infer_cast", "fp8_linear_group",
+    "fp8_kv_append", "fp8_kv_read", "fp8_attn_paged",
     "fp8h_gelu", "fp8h_gelu_backward", "fp8h_mse_grad", "fp8h_sgd",
 )
 
@@ -98,6 +100,25 @@ class MatmulItem(ctypes.Structure):
 
 
 _lib.fp8_linear_group.argtypes = [_P, POINTER(MatmulItem), c_int32, c_int, _P]
+
+
+class KvCacheDesc(ctypes.Structure):
+    """``fp8_kv_cache_t``."""
+    _fields_ = [("k8", c_void_p), ("v8", c_void_p), ("bk", c_void_p), ("bv", c_void_p), ("page_stride", c_int64),
+                ("bias_stride", c_int64), ("pages", c_int32), ("kv_heads", c_int32), ("page_size", c_int32),
+                ("head_dim", c_int32)]
+
+
+class SeqBatchDesc(ctypes.Structure):
+    """``fp8_seq_batch_t``."""
+    _fields_ = [("d_q_start", c_void_p), ("d_kv_len", c_void_p), ("d_page_table", c_void_p), ("table_stride", c_int64),
+                ("seqs", c_int32), ("tokens", c_int32), ("max_q_len", c_int32), ("max_kv_len", c_int32)]
+
+
+_lib.fp8_kv_append.argtypes = [_P, POINTER(KvCacheDesc), POINTER(SeqBatchDesc), _P, _P, c_int, c_int64, c_int64, c_int, _P]
+_lib.fp8_kv_read.argtypes = _lib.fp8_kv_append.argtypes
+_lib.fp8_attn_paged.argtypes = [_P, POINTER(KvCacheDesc), POINTER(SeqBatchDesc), _P, c_int64, c_int32, _P, c_int64, _P,
+                                c_float, c_int32, c_int, _P]
 _lib.fp8h_gelu.argtypes = [_P, _P, c_int64, _P]
 _lib.fp8h_gelu_backward.argtypes = [_P, _P, _P, c_int64, _P]
 _lib.fp8h_mse_grad.argtypes = [_P, _P, ctypes.c_float, _P, c_int64, _P]
@@ -173,6 +194,55 @@ def group_items(tensors):
         it.d_amax = d_amax.data_ptr() if d_amax is not None else None
         it.d_bias, it.y = d_bias.data_ptr(), (y.data_ptr() if y is not None else None)
     return arr
+
+
+class KvCache:
+    """The pages of one layer's cache (``fp8_kv_cache_t``): k8, v8 uint8 [pages, kv_heads, page_size, head_dim], bk, bv
+    int8 [pages, kv_heads, page_size].  The first dimension may be strided (keys and values of a page in one buffer)."""
+
+    def __init__(self, k8, v8, bk, bv, conv=CONV_PAPER):
+        pages, heads, size, dim = k8.shape
+        for t, shape, dt in ((k8, k8.shape, torch.uint8), (v8, k8.shape, torch.uint8), (bk, k8.shape[:3], torch.int8),
+                             (bv, k8.shape[:3], torch.int8)):
+            if t.shape != shape or t.dtype != dt or not t[0].is_contiguous() or not t.is_cuda:
+                raise ValueError("k8, v8: uint8 [pages, kv_heads, page_size, head_dim]; bk, bv: int8 [pages, kv_heads, "
+                                 "page_size]; on the GPU, each page contiguous")
+        if _page_stride(k8) != _page_stride(v8) or _page_stride(bk) != _page_stride(bv):
+            raise ValueError("k8 and v8, bk and bv have their pages equally far apart")
+        self.k8, self.v8, self.bk, self.bv, self.conv = k8, v8, bk, bv, conv
+        self._desc = KvCacheDesc(k8.data_ptr(), v8.data_ptr(), bk.data_ptr(), bv.data_ptr(), _page_stride(k8),
+                                 _page_stride(bk), pages, heads, size, dim)
+        self._ref = byref(self._desc)
+
+
+def _page_stride(t):
+    return t.stride(0) if t.shape[0] > 1 else t[0].numel()
+
+
+class SeqBatch:
+    """The sequences of one call (``fp8_seq_batch_t``): q_start int32 [seqs + 1], kv_len int32 [seqs], page_table int32
+    [seqs, table width], all on the GPU; the bounds of rows and tokens per sequence are host numbers."""
+
+    def __init__(self, q_start, kv_len, page_table, max_q_len, max_kv_len):
+        seqs = kv_len.shape[0]
+        for t in (q_start, kv_len, page_table):
+            if t.dtype != torch.int32 or (t.shape[-1] > 1 and t.stride(-1) != 1) or not t.is_cuda:
+                raise ValueError("q_start, kv_len and page_table are int32 tensors on the GPU")
+        if q_start.shape != (seqs + 1,) or page_table.dim() != 2 or page_table.shape[0] != seqs:
+            raise ValueError("q_start [seqs + 1], kv_len [seqs], page_table [seqs, width]")
+        self.q_start, self.kv_len, self.page_table = q_start, kv_len, page_table
+        self._width = page_table.shape[1]
+        self._desc = SeqBatchDesc(q_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(),
+                                  page_table.stride(0) if seqs > 1 else self._width, seqs, 0, max_q_len, max_kv_len)
+        self._ref = byref(self._desc)
+
+
+def _rows3(t, heads, dim, what):
+    """Check a [tokens, heads, head_dim] tensor whose heads are contiguous; its row distance in elements."""
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim or t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim):
+        raise ValueError(f"{what}: [tokens, {heads}, {dim}] with contiguous heads expected, got {tuple(t.shape)} "
+                         f"strides {t.stride()}")
+    return t.stride(0) if t.shape[0] > 1 else heads * dim
 
 
 MATMUL_FWD, MATMUL_DGRAD, MATMUL_WGRAD = 0, 1, 2
@@ -423,6 +493,42 @@ class Context:
         N, K = dw.shape
         _check(_lib.fp8_linear_wgrad(self._h, _ptr(dy8), _ptr(dy8_t), _ptr(d_bg), _ptr(x8), _ptr(x8_t), _ptr(d_bx),
                                      _ptr(dw), _DT[dw.dtype], T, K, N, conv, _stream()), "fp8_linear_wgrad")
+
+    # -- paged FP8 cache ----------------------------------------------------------
+    def _kv(self, fn, name, cache, batch, k, v):
+        d = cache._desc
+        some = k if k is not None else v
+        if some is None:
+            raise ValueError("keys, values or both")
+        ld_k = _rows3(k, d.kv_heads, d.head_dim, "keys") if k is not None else 0
+        ld_v = _rows3(v, d.kv_heads, d.head_dim, "values") if v is not None else 0
+        if k is not None and v is not None and (k.dtype != v.dtype or k.shape != v.shape):
+            raise ValueError("keys and values of one shape and type")
+        batch._desc.tokens = some.shape[0]
+        _check(fn(self._h, cache._ref, batch._ref, _ptr(k), _ptr(v), _DT[some.dtype], ld_k, ld_v, cache.conv, _stream()), name)
+
+    def kv_append(self, cache, batch, k, v):
+        """``fp8_kv_append``: quantise the new tokens' keys and values, [tokens, kv_heads, head_dim], into the cache."""
+        self._kv(_lib.fp8_kv_append, "fp8_kv_append", cache, batch, k, v)
+
+    def kv_read(self, cache, batch, k, v):
+        """``fp8_kv_read``: the numbers that the cache holds, into k and v (either may be None)."""
+        self._kv(_lib.fp8_kv_read, "fp8_kv_read", cache, batch, k, v)
+
+    def attn_paged(self, cache, batch, q, out, scale=None, causal=True, lse=None):
+        """``fp8_attn_paged``: q, out [tokens, q_heads, head_dim] bf16, lse float32 [tokens, q_heads] or None; scale
+        1 / sqrt(head_dim) by default."""
+        d = cache._desc
+        heads, dim = q.shape[1], d.head_dim
+        ld_q, ld_o = _rows3(q, heads, dim, "q"), _rows3(out, heads, dim, "out")
+        if q.dtype != torch.bfloat16 or out.dtype != torch.bfloat16 or out.shape != q.shape:
+            raise ValueError("q and out: bf16 tensors of one shape")
+        if lse is not None and (lse.dtype != torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous()):
+            raise ValueError("lse: contiguous float32 [tokens, q_heads]")
+        batch._desc.tokens = q.shape[0]
+        _check(_lib.fp8_attn_paged(self._h, cache._ref, batch._ref, q.data_ptr(), ld_q, heads, out.data_ptr(), ld_o,
+                                   _ptr(lse), dim ** -0.5 if scale is None else scale, 1 if causal else 0, cache.conv,
+                                   _stream()), "fp8_attn_paged")
 
 
 def raw():
