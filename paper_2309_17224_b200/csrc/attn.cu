@@ -2,19 +2,11 @@
 //
 // One CTA per query row (token, head): a thread takes every 128th cached token, holds its score, and the CTA keeps the
 // running maximum and sum of the softmax (statistics and sums in FP32) over blocks of 128 tokens.
-#include "kv_common.cuh"
+#include "attn_common.cuh"
 
 namespace fp8lin {
 
-struct AttnParams {
-    KvParams kv;
-    const uint16_t *q;
-    uint16_t *out;
-    float *lse;
-    int64_t ld_q, ld_o;
-    int32_t q_heads, causal;
-    float scale;
-};
+fp8_status_t attn_decode(const fp8_ctx *ctx, const AttnParams &p, int head_dim, int rows, cudaStream_t st);   // attn_decode.cu
 
 __device__ __forceinline__ float e4_number(uint8_t c)
 {
@@ -54,9 +46,9 @@ __global__ void __launch_bounds__(128) attn_row_kernel(const AttnParams p)
     const int64_t last = (int64_t)len - n + (t - first);
     len = min(max(len, 0), kv.max_kv_len);
     if (p.causal) len = (int)min((int64_t)len, max((int64_t)0, last + 1));
-    const int hk = head / (p.q_heads / kv.kv_heads);
+    const int hk = head / p.group;
     for (int i = threadIdx.x; i < D; i += 128)
-        q[i] = __uint_as_float((uint32_t)p.q[t * p.ld_q + (int64_t)head * D + i] << 16) * p.scale;
+        q[i] = __uint_as_float((uint32_t)p.q[t * p.ld_q + (int64_t)head * D + i] << 16) * (p.c * kLn2);
     __syncthreads();
     bool q_bad = false;
     for (int i = 0; i < D; ++i) q_bad |= !(fabsf(q[i]) < INFINITY);
@@ -130,9 +122,14 @@ fp8_status_t fp8_attn_paged(fp8_ctx *ctx, const fp8_kv_cache_t *c, const fp8_seq
     p.lse = d_lse;
     p.ld_q = ld_q;
     p.ld_o = ld_o;
+    p.part = ctx->d_partial;
+    p.count = ctx->d_attn_count;
     p.q_heads = q_heads;
+    p.group = q_heads / c->kv_heads;
     p.causal = causal != 0;
-    p.scale = scale;
+    p.c = scale * 1.44269504088896341f;
+    const int64_t rows = (int64_t)batch->max_q_len * p.group;
+    if (rows <= 16) return attn_decode(ctx, p, c->head_dim, (int)rows, (cudaStream_t)stream);
     const dim3 grid((unsigned)batch->tokens, (unsigned)q_heads);
     count_launch();
     if (c->head_dim == 128) attn_row_kernel<128><<<grid, 128, 0, (cudaStream_t)stream>>>(p);

@@ -1,0 +1,464 @@
+// Attention over the paged FP8 cache for few query rows: at most 16 rows share a key/value head (one new token with up
+// to 16 query heads per key/value head, or a few tokens with fewer).
+//
+// Bound by the cache's bytes.  Every byte goes from global memory into the registers of the lane that feeds it to the
+// matrix instruction: no shared memory on the way, no barrier, no swizzle.  A warp takes blocks of 16 tokens (never
+// across a page); tokens are the rows of the first product and head dimensions the rows of the second, queries are the
+// columns of both (m16n8k16, fp16 operands, FP32 sums), so eight queries cost one instruction and none is padded to 16:
+//   S^T[16 tokens x 8 rows] = K[16 x D] Q^T:   lane (g = lane / 4, t = lane % 4) holds 16 contiguous bytes of tokens g and
+//       g + 8 per 64 dimensions; which dimension meets which contraction index is free as long as Q agrees, so the
+//       bytes are used in memory order
+//   O^T[D x 8 rows] += V^T P^T:   lane (g, t) holds 16 contiguous dimensions of tokens 2t, 2t+1, 2t+8, 2t+9; two byte
+//       permutes interleave two tokens, one conversion makes an fp16 pair of E4 bytes.  P^T comes out of S^T by two 8x8
+//       transposes (movmatrix).
+// Two blocks are in flight per warp, each re-requested as soon as its registers are free: with 12 warps on an SM about
+// 80 KB.  The blocks of all (sequence, head) units form one list, cut evenly between the CTAs (a sequence's length
+// changes nothing in the balance); a unit that lies in several CTAs leaves partial sums in the workspace, joined in
+// order by the CTA that arrives last, so results do not depend on the order of arrival.
+#include "attn_common.cuh"
+
+namespace fp8lin {
+
+constexpr int kDecodeWarps = 4;
+constexpr int kDecodeThreads = 32 * kDecodeWarps;
+constexpr int kBlockTokens = 16;
+
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t v)
+{
+    uint32_t r;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
+}
+
+// One block's bytes as a lane holds them.
+template <int D>
+struct KvBlock {
+    static constexpr int kKChunks = D / 64;
+    static constexpr int kVWords = D / 32;       // words of each of the four value rows
+    uint32_t k[2][kKChunks][4];
+    uint32_t v[4][kVWords];
+    int bk[2], bv[2];
+    int bad;                                     // the block's page number is out of range
+};
+
+template <int D>
+__device__ __forceinline__ void load_k(KvBlock<D> &x, const uint8_t *k, const int8_t *bk, const int8_t *bv, int g, int t)
+{
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+#pragma unroll
+        for (int i = 0; i < KvBlock<D>::kKChunks; ++i) {
+            const uint4 w = ldg_stream(k + (g + 8 * r) * D + (t + 4 * i) * 16);
+            x.k[r][i][0] = w.x; x.k[r][i][1] = w.y; x.k[r][i][2] = w.z; x.k[r][i][3] = w.w;
+        }
+        x.bk[r] = bk[g + 8 * r];
+        x.bv[r] = bv[g + 8 * r];
+    }
+}
+template <int D>
+__device__ __forceinline__ void load_v(KvBlock<D> &x, const uint8_t *v, int g, int t)
+{
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const uint8_t *src = v + (2 * t + (r & 1) + 8 * (r >> 1)) * D + g * (D / 8);
+        if constexpr (D == 128) {
+            const uint4 w = ldg_stream(src);
+            x.v[r][0] = w.x; x.v[r][1] = w.y; x.v[r][2] = w.z; x.v[r][3] = w.w;
+        } else {
+            const uint2 w = ldg_stream2(src);
+            x.v[r][0] = w.x; x.v[r][1] = w.y;
+        }
+    }
+}
+
+// Where the CTA stands in the list of blocks: a unit (sequence b, head h) and the range of its blocks.
+struct Unit {
+    int b, h;
+    SeqShape s;
+    int blocks;           // of the whole unit, at least one where the sequence has rows
+    int64_t first_block;  // of the unit, in the list
+};
+
+__device__ __forceinline__ int unit_blocks(const SeqShape &s) { return s.n > 0 ? max(1, (s.len + kBlockTokens - 1) / kBlockTokens) : 0; }
+
+template <int D, int NT>
+__global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 3 : 2) attn_decode_kernel(const AttnParams p)
+{
+    constexpr int kRows = 8 * NT;
+    constexpr int kPart = kRows * (D + 2);       // floats of a partial result
+    __shared__ __align__(16) float s_o[kDecodeWarps][kRows][D];
+    __shared__ float s_m[kDecodeWarps][kRows], s_l[kDecodeWarps][kRows];
+    __shared__ unsigned s_last;
+    const KvParams &kv = p.kv;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+
+    // ---- the CTA's share of the list (every warp computes it for itself) ----
+    int64_t total = 0;
+    bool any_cut = false;
+    for (int b0 = 0; b0 < kv.seqs; b0 += 32) {
+        int n = 0;
+        if (b0 + lane < kv.seqs) {
+            bool cut;
+            n = unit_blocks(seq_shape(kv, b0 + lane, cut));
+            any_cut |= cut;
+        }
+        total += __reduce_add_sync(0xFFFFFFFFu, n);
+    }
+    if (blockIdx.x == 0 && warp == 0 && __any_sync(0xFFFFFFFFu, any_cut) && lane == 0) raise_flags(kv.d_status, FP8_FLAG_BAD_INDEX);
+    total *= kv.kv_heads;
+    // at least one block per warp, so that short lists are not spread over CTAs that then wait for one another's sums
+    const int64_t share = max((total + gridDim.x - 1) / (int64_t)gridDim.x, (int64_t)kDecodeWarps);
+    int64_t at = blockIdx.x * share;
+    const int64_t end = min(total, at + share);
+    if (at >= end) return;
+
+    Unit u;
+    {
+        int64_t before = 0;
+        for (int b0 = 0;; b0 += 32) {
+            SeqShape s = {0, 0, 0};
+            int n = 0;
+            if (b0 + lane < kv.seqs) {
+                bool cut;
+                s = seq_shape(kv, b0 + lane, cut);
+                n = unit_blocks(s);
+            }
+            int64_t upto = (int64_t)n * kv.kv_heads;   // inclusive sums
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int64_t x = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+                if (lane >= o) upto += x;
+            }
+            const unsigned hit = __ballot_sync(0xFFFFFFFFu, at < before + upto);
+            if (hit) {
+                const int l = __ffs(hit) - 1;
+                u.b = b0 + l;
+                u.s.first = __shfl_sync(0xFFFFFFFFu, s.first, l);
+                u.s.n = __shfl_sync(0xFFFFFFFFu, s.n, l);
+                u.s.len = __shfl_sync(0xFFFFFFFFu, s.len, l);
+                u.blocks = __shfl_sync(0xFFFFFFFFu, n, l);
+                const int64_t start = before + __shfl_sync(0xFFFFFFFFu, upto, l) - (int64_t)u.blocks * kv.kv_heads;
+                u.h = (int)((at - start) / u.blocks);
+                u.first_block = start + (int64_t)u.h * u.blocks;
+                break;
+            }
+            before += __shfl_sync(0xFFFFFFFFu, upto, 31);
+        }
+    }
+
+    const int size = 1 << kv.page_shift, blocks_per_page_shift = kv.page_shift - 4;
+    while (true) {
+        const int lo = (int)(at - u.first_block), hi = (int)min((int64_t)u.blocks, end - u.first_block);
+        const int rows = u.s.n * p.group;
+
+        // ---- queries: fp16 under a power of two per row (exact for bf16 unless 2^28 below the row's largest) ----
+        uint32_t q[NT][D / 16][2];
+        float rc[NT][2];          // c / that power, for the rows of S^T's columns
+        int limit[NT][2];         // tokens those rows see
+        int all_see = u.s.len;    // tokens that every row sees
+        {
+            float mine[NT];
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                const int r = 8 * j + g;
+                uint32_t w[D / 64][8];
+                uint32_t m = 0;
+#pragma unroll
+                for (int i = 0; i < D / 64; ++i) {
+                    uint4 x = make_uint4(0, 0, 0, 0), y = x;
+                    if (r < rows) {
+                        const uint16_t *src = p.q + (int64_t)(u.s.first + r / p.group) * p.ld_q +
+                                              (int64_t)(u.h * p.group + r % p.group) * D + (t + 4 * i) * 16;
+                        x = *reinterpret_cast<const uint4 *>(src);
+                        y = *reinterpret_cast<const uint4 *>(src + 8);
+                    }
+                    w[i][0] = x.x; w[i][1] = x.y; w[i][2] = x.z; w[i][3] = x.w;
+                    w[i][4] = y.x; w[i][5] = y.y; w[i][6] = y.z; w[i][7] = y.w;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) m = max(m, max((w[i][k] << 16) & 0x7FFF0000u, w[i][k] & 0x7FFF0000u));
+                }
+                m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
+                m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
+                // the row's largest lands in [2^14, 2^15)
+                const int e = m == 0 ? 0 : max(-113, min(126, 14 + 127 - (int)(m >> 23)));
+                const float f = pow2_normal(e);
+                mine[j] = m >= 0x7F800000u ? __int_as_float(0x7FFFFFFF) : p.c * pow2_normal(-e);
+#pragma unroll
+                for (int i = 0; i < D / 64; ++i)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        q[j][4 * i + k / 2][k & 1] = pack_f16(__uint_as_float(w[i][k] << 16) * f, __uint_as_float(w[i][k] & 0xFFFF0000u) * f);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    rc[j][k] = __shfl_sync(0xFFFFFFFFu, mine[j], (2 * t + k) * 4);
+                    limit[j][k] = u.s.len;
+                    if (p.causal) limit[j][k] = min(u.s.len, max(0, u.s.len - u.s.n + (8 * j + 2 * t + k) / p.group + 1));
+                }
+            }
+            if (p.causal) all_see = max(0, u.s.len - u.s.n + 1);
+        }
+
+        float o[NT][D / 16][4], top[NT][2], l[NT][2];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+#pragma unroll
+            for (int m = 0; m < D / 16; ++m) o[j][m][0] = o[j][m][1] = o[j][m][2] = o[j][m][3] = 0.0f;
+            top[j][0] = top[j][1] = kNoMax;
+            l[j][0] = l[j][1] = 0.0f;
+        }
+
+        // ---- this warp's blocks: lo + warp, every fourth ----
+        const int32_t *table = kv.table + (int64_t)u.b * kv.table_stride;
+        const int mine = max(0, (hi - lo - warp + kDecodeWarps - 1) / kDecodeWarps);
+        const int count = u.s.len > 0 ? mine : 0;
+        int pages = 0;            // lane i: page of the warp's block (32 * round + i)
+        auto fetch_pages = [&](int i0) {
+            const int blk = lo + warp + (i0 + lane) * kDecodeWarps;
+            pages = i0 + lane < count ? __ldg(table + (blk >> blocks_per_page_shift)) : 0;
+        };
+        int64_t v_at[2];
+        auto request_k = [&](KvBlock<D> &x, int i, int64_t &v_off) {
+            if ((i & 31) == 0) fetch_pages(i);
+            const int page = __shfl_sync(0xFFFFFFFFu, pages, i & 31);
+            const int blk = lo + warp + i * kDecodeWarps;
+            x.bad = (unsigned)page >= (unsigned)kv.pages;
+            const int64_t row = ((int64_t)u.h << kv.page_shift) + ((blk * kBlockTokens) & (size - 1));
+            const int64_t pg = x.bad ? 0 : page;
+            v_off = pg * kv.page_stride + row * D;
+            const int64_t b_off = pg * kv.bias_stride + row;
+            load_k<D>(x, kv.k8 + v_off, kv.bk + b_off, kv.bv + b_off, g, t);
+        };
+        KvBlock<D> x[2];
+        if (count > 0) { request_k(x[0], 0, v_at[0]); load_v<D>(x[0], kv.v8 + v_at[0], g, t); }
+        if (count > 1) { request_k(x[1], 1, v_at[1]); load_v<D>(x[1], kv.v8 + v_at[1], g, t); }
+
+        auto step = [&](KvBlock<D> &cur, int64_t &v_off, int i) {
+            const int j0 = (lo + warp + i * kDecodeWarps) * kBlockTokens;
+            // S^T
+            float s[NT][4];
+#pragma unroll
+            for (int j = 0; j < NT; ++j) s[j][0] = s[j][1] = s[j][2] = s[j][3] = 0.0f;
+#pragma unroll
+            for (int c = 0; c < D / 64; ++c)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    uint32_t a0, a1, a2, a3;
+                    e4_to_f16(cur.k[0][c][k], a0, a2);
+                    e4_to_f16(cur.k[1][c][k], a1, a3);
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) mma_f16(s[j], a0, a1, a2, a3, q[j][4 * c + k][0], q[j][4 * c + k][1]);
+                }
+            // a page out of range is read as page 0 and then taken as non-finite
+            int bk[2] = {cur.bk[0], cur.bk[1]}, bv[2] = {cur.bv[0], cur.bv[1]};
+            if (cur.bad) bk[0] = bk[1] = bv[0] = bv[1] = FP8_KV_BIAS_NONFINITE;
+            const int bad = cur.bad;
+            // the registers of K are free: the block after next
+            if (i + 2 < count) request_k(cur, i + 2, v_off);
+            if (bad && lane == 0) raise_flags(kv.d_status, FP8_FLAG_BAD_INDEX);
+            const bool marked0 = bk[0] == FP8_KV_BIAS_NONFINITE || bv[0] == FP8_KV_BIAS_NONFINITE;
+            const bool marked1 = bk[1] == FP8_KV_BIAS_NONFINITE || bv[1] == FP8_KV_BIAS_NONFINITE;
+            const float f0 = marked0 ? __int_as_float(0x7FFFFFFF) : pow2_normal(min(126, -(bk[0] + kv.delta)));
+            const float f1 = marked1 ? __int_as_float(0x7FFFFFFF) : pow2_normal(min(126, -(bk[1] + kv.delta)));
+            const float d0 = (float)bv[0], d1 = (float)bv[1];
+            // w = s - d; beyond what a row sees -infinity
+            bool above = false;
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    s[j][k] = fmaf(s[j][k] * f0, rc[j][k], -d0);
+                    s[j][2 + k] = fmaf(s[j][2 + k] * f1, rc[j][k], -d1);
+                    if (j0 + kBlockTokens > all_see) {
+                        if (j0 + g >= limit[j][k]) s[j][k] = -INFINITY;
+                        if (j0 + g + 8 >= limit[j][k]) s[j][2 + k] = -INFINITY;
+                    }
+                    above |= fmaxf(s[j][k], s[j][2 + k]) > top[j][k] + kSlack;
+                }
+            if (__any_sync(0xFFFFFFFFu, above)) {
+#pragma unroll
+                for (int j = 0; j < NT; ++j)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        float m = fmaxf(s[j][k], s[j][2 + k]);
+                        m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 4));
+                        m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 8));
+                        m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 16));
+                        const float next = fmaxf(top[j][k], m - kLift);
+                        const float shrink = exp2_approx(top[j][k] - next);
+                        top[j][k] = next;
+                        l[j][k] *= shrink;
+#pragma unroll
+                        for (int m2 = 0; m2 < D / 16; ++m2) {
+                            o[j][m2][k] *= shrink;
+                            o[j][m2][2 + k] *= shrink;
+                        }
+                    }
+            }
+            // p, the denominator, and P^T as the second product's operand
+            const float e0 = pow2_normal(max(-126, bv[0] + kv.delta)), e1 = pow2_normal(max(-126, bv[1] + kv.delta));
+            uint32_t pt[NT][2];
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    s[j][k] = exp2_approx(s[j][k] - top[j][k]);
+                    s[j][2 + k] = exp2_approx(s[j][2 + k] - top[j][k]);
+                    l[j][k] = fmaf(s[j][k], e0, fmaf(s[j][2 + k], e1, l[j][k]));
+                }
+                pt[j][0] = transpose8x8(pack_f16(s[j][0], s[j][1]));
+                pt[j][1] = transpose8x8(pack_f16(s[j][2], s[j][3]));
+            }
+            // values that no weight may meet, because 0 times a NaN is one: tokens behind the end, marked rows
+            const unsigned marks = __ballot_sync(0xFFFFFFFFu, marked0) | 0u, marks8 = __ballot_sync(0xFFFFFFFFu, marked1);
+            if ((marks | marks8) != 0u || j0 + kBlockTokens > u.s.len) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int row = 2 * t + (r & 1);
+                    const bool drop = ((((r >> 1) ? marks8 : marks) >> (4 * row)) & 1u) || j0 + row + 8 * (r >> 1) >= u.s.len;
+                    if (drop) {
+#pragma unroll
+                        for (int k = 0; k < KvBlock<D>::kVWords; ++k) cur.v[r][k] = 0u;
+                    }
+                }
+            }
+#pragma unroll
+            for (int m = 0; m < D / 16; ++m) {
+                // dimensions 2m and 2m + 1 of the lane's sixteen (or eight), four tokens
+                uint32_t a0, a1, a2, a3;
+                const uint32_t sel = (m & 1) ? 0x7362u : 0x5140u;
+                e4_to_f16(__byte_perm(cur.v[0][m >> 1], cur.v[1][m >> 1], sel), a0, a1);
+                e4_to_f16(__byte_perm(cur.v[2][m >> 1], cur.v[3][m >> 1], sel), a2, a3);
+#pragma unroll
+                for (int j = 0; j < NT; ++j) mma_f16(o[j][m], a0, a1, a2, a3, pt[j][0], pt[j][1]);
+            }
+            if (i + 2 < count) load_v<D>(cur, kv.v8 + v_off, g, t);
+        };
+        for (int i = 0; i < count; i += 2) {
+            step(x[0], v_at[0], i);
+            if (i + 1 < count) step(x[1], v_at[1], i + 1);
+        }
+
+        // ---- join the warps ----
+        __syncthreads();   // the previous unit's sums have been read
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                float v = l[j][k];
+                v += __shfl_xor_sync(0xFFFFFFFFu, v, 4);
+                v += __shfl_xor_sync(0xFFFFFFFFu, v, 8);
+                v += __shfl_xor_sync(0xFFFFFFFFu, v, 16);
+                const int r = 8 * j + 2 * t + k;
+                if (g == 0) { s_l[warp][r] = v; s_m[warp][r] = top[j][k]; }
+                float *dst = &s_o[warp][r][g * (D / 8)];
+#pragma unroll
+                for (int m = 0; m < D / 16; m += 2)
+                    *reinterpret_cast<float4 *>(dst + 2 * m) = make_float4(o[j][m][k], o[j][m][2 + k], o[j][m + 1][k], o[j][m + 1][2 + k]);
+            }
+        __syncthreads();
+        const bool whole = lo == 0 && hi == u.blocks;
+        const int64_t first_cta = u.first_block / share, last_cta = (u.first_block + u.blocks - 1) / share;
+        float *slot = p.part + ((int64_t)blockIdx.x * 2 + (lo == 0 ? 1 : 0)) * kPart;
+        auto store_row = [&](int r, int d, float4 v, float m, float sum) {
+            const int64_t row = u.s.first + r / p.group;
+            const int head = u.h * p.group + r % p.group;
+            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+            *reinterpret_cast<uint2 *>(p.out + row * p.ld_o + (int64_t)head * D + d) =
+                make_uint2(pack_bf16x2(v.x * inv, v.y * inv), pack_bf16x2(v.z * inv, v.w * inv));
+            if (p.lse && d == 0)
+                p.lse[row * p.q_heads + head] = sum == 0.0f ? -INFINITY : (m - (float)kv.delta + log2_approx(sum)) * kLn2;
+        };
+        for (int idx = threadIdx.x; idx < kRows * (D / 4); idx += kDecodeThreads) {
+            const int r = idx / (D / 4), d = idx % (D / 4) * 4;
+            if (r >= rows) break;
+            float m = s_m[0][r];
+#pragma unroll
+            for (int w = 1; w < kDecodeWarps; ++w) m = fmaxf(m, s_m[w][r]);
+            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            float sum = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kDecodeWarps; ++w) {
+                const float f = exp2_approx(s_m[w][r] - m);
+                const float4 y = *reinterpret_cast<const float4 *>(&s_o[w][r][d]);
+                v.x = fmaf(y.x, f, v.x); v.y = fmaf(y.y, f, v.y); v.z = fmaf(y.z, f, v.z); v.w = fmaf(y.w, f, v.w);
+                sum = fmaf(s_l[w][r], f, sum);
+            }
+            if (whole) {
+                store_row(r, d, v, m, sum);
+            } else {
+                *reinterpret_cast<float4 *>(slot + r * D + d) = v;
+                if (d == 0) { slot[kRows * D + r] = m; slot[kRows * D + kRows + r] = sum; }
+            }
+        }
+        if (!whole) {
+            __threadfence();
+            __syncthreads();
+            if (threadIdx.x == 0) s_last = atomicAdd(p.count + first_cta, 1u) == (unsigned)(last_cta - first_cta);
+            __syncthreads();
+            if (s_last) {
+                __threadfence();
+                if (threadIdx.x == 0) p.count[first_cta] = 0u;
+                // the first part lies in its CTA's slot 1 (it starts at the unit's beginning), the others in slot 0
+                auto part_of = [&](int64_t c) { return p.part + (c * 2 + (c == first_cta ? 1 : 0)) * kPart; };
+                for (int idx = threadIdx.x; idx < kRows * (D / 4); idx += kDecodeThreads) {
+                    const int r = idx / (D / 4), d = idx % (D / 4) * 4;
+                    if (r >= rows) break;
+                    float m = kNoMax;
+                    for (int64_t c = first_cta; c <= last_cta; ++c) m = fmaxf(m, __ldcg(part_of(c) + kRows * D + r));
+                    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                    float sum = 0.0f;
+                    for (int64_t c = first_cta; c <= last_cta; ++c) {
+                        const float *src = part_of(c);
+                        const float f = exp2_approx(__ldcg(src + kRows * D + r) - m);
+                        const float4 y = __ldcg(reinterpret_cast<const float4 *>(src + r * D + d));
+                        v.x = fmaf(y.x, f, v.x); v.y = fmaf(y.y, f, v.y); v.z = fmaf(y.z, f, v.z); v.w = fmaf(y.w, f, v.w);
+                        sum = fmaf(__ldcg(src + kRows * D + kRows + r), f, sum);
+                    }
+                    store_row(r, d, v, m, sum);
+                }
+            }
+        }
+
+        // ---- next unit ----
+        at = u.first_block + hi;
+        if (at >= end) break;
+        u.first_block += u.blocks;
+        if (++u.h == kv.kv_heads) {
+            u.h = 0;
+            do {
+                ++u.b;
+                bool cut;
+                u.s = seq_shape(kv, u.b, cut);
+                u.blocks = unit_blocks(u.s);
+            } while (u.blocks == 0);
+        }
+    }
+}
+
+template <int D, int NT>
+static fp8_status_t launch_decode(const fp8_ctx *ctx, const AttnParams &p, cudaStream_t st)
+{
+    const KvParams &kv = p.kv;
+    // an upper bound of the list's length; CTAs beyond the blocks that there are leave at once
+    const int64_t blocks = (int64_t)kv.seqs * kv.kv_heads * ((kv.max_kv_len + kBlockTokens - 1) / kBlockTokens);
+    int64_t grid = (int64_t)ctx->sm_count * (NT == 1 ? 3 : 2);
+    if ((blocks + kDecodeWarps - 1) / kDecodeWarps < grid) grid = (blocks + kDecodeWarps - 1) / kDecodeWarps;
+    if (grid > kAttnCounters) return FP8_ERR_UNSUPPORTED;
+    count_launch();
+    attn_decode_kernel<D, NT><<<(unsigned)grid, kDecodeThreads, 0, st>>>(p);
+    return cudaGetLastError() == cudaSuccess ? FP8_OK : FP8_ERR_CUDA;
+}
+
+fp8_status_t attn_decode(const fp8_ctx *ctx, const AttnParams &p, int head_dim, int rows, cudaStream_t st)
+{
+    if (head_dim == 128) return rows <= 8 ? launch_decode<128, 1>(ctx, p, st) : launch_decode<128, 2>(ctx, p, st);
+    return rows <= 8 ? launch_decode<64, 1>(ctx, p, st) : launch_decode<64, 2>(ctx, p, st);
+}
+
+}  // namespace fp8lin

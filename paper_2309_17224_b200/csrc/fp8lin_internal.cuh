@@ -16,6 +16,7 @@ namespace fp8lin {
 // ---------------------------------------------------------------------------
 
 constexpr int kReduceSlots = 64;   // independent grid-reduction slots, used round-robin
+constexpr int kAttnCounters = 4096;   // words of fp8_ctx::d_attn_count
 constexpr int kSlotWords = 4;      // {running max, arrival counter, scratch flag, redo flag of a predicted cast}
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
@@ -33,7 +34,8 @@ struct fp8_ctx {
     unsigned *d_slots;    // kReduceSlots * kSlotWords words, all zero between calls
     unsigned next_slot;
     unsigned *d_predict_stats;   // {guesses that held, guesses that did not} of fp8_cast_predicted
-    float *d_partial;     // FP32 workspace for split-K partial sums
+    float *d_partial;     // FP32 workspace for split-K partial sums and for attention over split contexts
+    unsigned *d_attn_count;   // arrival counters of attention over split contexts, all zero between calls
     size_t partial_bytes;
     fp8lin::EncodeTiledFn encode_tiled;
 };
