@@ -2,16 +2,14 @@
 //
 // The mathematics.  With b_j, d_j the scaling biases of token j's key and value row (delta added), K8, V8 the numbers
 // of their bytes and c = scale * log2(e), a row of queries q needs
-//     s_j = c 2^-b_j (q . K8_j),   out = sum_j 2^s_j 2^-d_j V8_j / sum_j 2^s_j.
-// The matrix instructions read K8 and V8, so the power of two of a value row is taken into the weight that multiplies
-// it: with w_j = s_j - d_j and any M,
-//     out = sum_j p_j V8_j / sum_j p_j 2^d_j,   p_j = 2^(w_j - M),
-// exactly.  M follows the running maximum of w (not of s): p_j, which is rounded to fp16 for the product with V8 (whose
-// bytes are fp16 numbers exactly), then keeps its 11 bits wherever its product matters, however different the rows'
-// biases are.  M is chosen 7 below the maximum and moved only when a w exceeds M + 15, so that moving it (and rescaling
-// what has been summed) is rare; p_j stays below 2^15 and is resolved down to 2^-31 of the largest weight.
-// The denominator is summed in FP32 from the same p_j.  (Rows of one sequence whose biases lie more than 120 apart, that
-// is values 2^120 times each other, are beyond what its range resolves.)
+//     s_j = c 2^-b_j (q . K8_j),   p_j = 2^(s_j - M),   out = sum_j p_j (2^-d_j V8_j) / sum_j p_j.
+// M is the row's maximum when it was last looked at: it moves only when a score exceeds it by more than kSlack, so that
+// rescaling what has been summed is rare (p_j stays below 2^kSlack, and FP32 has room below).
+// The second product runs on bf16: a value 2^-d V8 has four significant bits, so it is a bf16 number exactly, and a
+// weight is the sum of two, p = p1 + p2, p1 the leading eight bits and p2 the rest rounded to eight: sixteen bits at any
+// size.  One bf16 (2^-9 of every weight) would be coarser than the rounding of the output itself; fp16 would do for
+// weights near the maximum but has none left below 2^-39 of it, and those count in dimensions where the tokens above
+// them hold zeros.  The denominator is the FP32 sum of the unrounded p_j.
 #pragma once
 
 #include "kv_common.cuh"
@@ -27,12 +25,12 @@ struct AttnParams {
     unsigned *count;      // arrival counters (ctx->d_attn_count), zero between calls
     int64_t ld_q, ld_o;
     int32_t q_heads, group, causal;
+    int32_t row_tiles, splits;   // chunk kernel: tiles of 128 rows of the longest sequence, parts that a context is cut into
     float c;              // scale * log2(e)
 };
 
-constexpr float kNoMax = -3.0e38f;    // "no token yet": finite, so that 2^(-inf - M) is 0 and not NaN
-constexpr float kLift = 7.0f;         // M = maximum - kLift ...
-constexpr float kSlack = 15.0f;       // ... until a weight exceeds M + kSlack
+constexpr float kNoMax = -3.0e38f;    // M before the first token: finite, so that 2^(-inf - M) is 0 and not NaN
+constexpr float kSlack = 40.0f;       // M is moved when a score exceeds it by more
 constexpr float kLn2 = 0.693147180559945309f;
 
 #ifdef __CUDACC__
@@ -83,6 +81,27 @@ __device__ __forceinline__ uint2 ldg_stream2(const void *p)
 __device__ __forceinline__ float key_factor(int b, int delta)
 {
     return b == FP8_KV_BIAS_NONFINITE ? __int_as_float(0x7FFFFFFF) : pow2_normal(min(126, -(b + delta)));
+}
+
+// E4 bytes as bf16: the exponent and mantissa fields moved to where bf16 has them give the number times 2^-120 (also for
+// the subnormals of E4), which the multiplication by 2^(120 - d) mends and scales at once, exactly.
+//   spread: a word whose bytes 1 and 3 hold the two E4 bytes (bytes 0 and 2 are ignored)
+__device__ __forceinline__ uint32_t e4_fields_as_bf16(uint32_t spread) { return ((spread >> 4) & 0x07F007F0u) | (spread & 0x80008000u); }
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t x, uint32_t y)
+{
+    uint32_t r;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(y));
+    return r;
+}
+// 2^(120 - d) as a bf16 number; for d < -7 that is beyond bf16 and the rest, 2^(-7 - d), is a second factor.
+__device__ __forceinline__ uint32_t value_factor(int d) { return (uint32_t)(247 - max(d, -7)) << 7; }
+__device__ __forceinline__ uint32_t value_factor_rest(int d) { return (uint32_t)(127 + max(-7 - d, 0)) << 7; }
+
+// p = p1 + p2 for two weights: the upper halves as they are, the rest rounded.
+__device__ __forceinline__ void split_bf16(float a, float b, uint32_t &p1, uint32_t &p2)
+{
+    p1 = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
+    p2 = pack_bf16x2(a - __uint_as_float(__float_as_uint(a) & 0xFFFF0000u), b - __uint_as_float(__float_as_uint(b) & 0xFFFF0000u));
 }
 
 // A sequence's lengths, cut to the bounds of the launch.

@@ -4,13 +4,13 @@
 // Bound by the cache's bytes.  Every byte goes from global memory into the registers of the lane that feeds it to the
 // matrix instruction: no shared memory on the way, no barrier, no swizzle.  A warp takes blocks of 16 tokens (never
 // across a page); tokens are the rows of the first product and head dimensions the rows of the second, queries are the
-// columns of both (m16n8k16, fp16 operands, FP32 sums), so eight queries cost one instruction and none is padded to 16:
+// columns of both (m16n8k16, 16-bit operands, FP32 sums), so eight queries cost one instruction and none is padded to 16:
 //   S^T[16 tokens x 8 rows] = K[16 x D] Q^T:   lane (g = lane / 4, t = lane % 4) holds 16 contiguous bytes of tokens g and
 //       g + 8 per 64 dimensions; which dimension meets which contraction index is free as long as Q agrees, so the
-//       bytes are used in memory order
-//   O^T[D x 8 rows] += V^T P^T:   lane (g, t) holds 16 contiguous dimensions of tokens 2t, 2t+1, 2t+8, 2t+9; two byte
-//       permutes interleave two tokens, one conversion makes an fp16 pair of E4 bytes.  P^T comes out of S^T by two 8x8
-//       transposes (movmatrix).
+//       bytes are used in memory order (K as fp16, one conversion per two bytes; a query row as fp16 under a power of two)
+//   O^T[D x 8 rows] += V^T P^T:   lane (g, t) holds 16 contiguous dimensions of tokens 2t, 2t+1, 2t+8, 2t+9; a byte
+//       permute brings two tokens together, five instructions make a bf16 pair.  P^T, in its two terms, comes out of
+//       S^T by 8x8 transposes (movmatrix).
 // Two blocks are in flight per warp, each re-requested as soon as its registers are free: with 12 warps on an SM about
 // 80 KB.  The blocks of all (sequence, head) units form one list, cut evenly between the CTAs (a sequence's length
 // changes nothing in the balance); a unit that lies in several CTAs leaves partial sums in the workspace, joined in
@@ -26,6 +26,12 @@ constexpr int kBlockTokens = 16;
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
@@ -265,15 +271,14 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 3 : 2) attn_decode_k
             const bool marked1 = bk[1] == FP8_KV_BIAS_NONFINITE || bv[1] == FP8_KV_BIAS_NONFINITE;
             const float f0 = marked0 ? __int_as_float(0x7FFFFFFF) : pow2_normal(min(126, -(bk[0] + kv.delta)));
             const float f1 = marked1 ? __int_as_float(0x7FFFFFFF) : pow2_normal(min(126, -(bk[1] + kv.delta)));
-            const float d0 = (float)bv[0], d1 = (float)bv[1];
-            // w = s - d; beyond what a row sees -infinity
+            // scores; beyond what a row sees -infinity
             bool above = false;
 #pragma unroll
             for (int j = 0; j < NT; ++j)
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
-                    s[j][k] = fmaf(s[j][k] * f0, rc[j][k], -d0);
-                    s[j][2 + k] = fmaf(s[j][2 + k] * f1, rc[j][k], -d1);
+                    s[j][k] = s[j][k] * f0 * rc[j][k];
+                    s[j][2 + k] = s[j][2 + k] * f1 * rc[j][k];
                     if (j0 + kBlockTokens > all_see) {
                         if (j0 + g >= limit[j][k]) s[j][k] = -INFINITY;
                         if (j0 + g + 8 >= limit[j][k]) s[j][2 + k] = -INFINITY;
@@ -289,7 +294,7 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 3 : 2) attn_decode_k
                         m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 4));
                         m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 8));
                         m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 16));
-                        const float next = fmaxf(top[j][k], m - kLift);
+                        const float next = fmaxf(top[j][k], m);
                         const float shrink = exp2_approx(top[j][k] - next);
                         top[j][k] = next;
                         l[j][k] *= shrink;
@@ -300,22 +305,26 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 3 : 2) attn_decode_k
                         }
                     }
             }
-            // p, the denominator, and P^T as the second product's operand
-            const float e0 = pow2_normal(max(-126, bv[0] + kv.delta)), e1 = pow2_normal(max(-126, bv[1] + kv.delta));
-            uint32_t pt[NT][2];
+            // p, the denominator, and P^T's two terms as the second product's operands
+            uint32_t pt[NT][2][2];
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     s[j][k] = exp2_approx(s[j][k] - top[j][k]);
                     s[j][2 + k] = exp2_approx(s[j][2 + k] - top[j][k]);
-                    l[j][k] = fmaf(s[j][k], e0, fmaf(s[j][2 + k], e1, l[j][k]));
+                    l[j][k] += s[j][k] + s[j][2 + k];
                 }
-                pt[j][0] = transpose8x8(pack_f16(s[j][0], s[j][1]));
-                pt[j][1] = transpose8x8(pack_f16(s[j][2], s[j][3]));
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    uint32_t p1, p2;
+                    split_bf16(s[j][2 * r], s[j][2 * r + 1], p1, p2);
+                    pt[j][0][r] = transpose8x8(p1);
+                    pt[j][1][r] = transpose8x8(p2);
+                }
             }
             // values that no weight may meet, because 0 times a NaN is one: tokens behind the end, marked rows
-            const unsigned marks = __ballot_sync(0xFFFFFFFFu, marked0) | 0u, marks8 = __ballot_sync(0xFFFFFFFFu, marked1);
+            const unsigned marks = __ballot_sync(0xFFFFFFFFu, marked0), marks8 = __ballot_sync(0xFFFFFFFFu, marked1);
             if ((marks | marks8) != 0u || j0 + kBlockTokens > u.s.len) {
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
@@ -327,15 +336,38 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 3 : 2) attn_decode_k
                     }
                 }
             }
+            // 2^(120 - d) of tokens 2t, 2t + 1, and of 2t + 8, 2t + 9
+            const int dv0 = bv[0] + kv.delta, dv1 = bv[1] + kv.delta;
+            uint32_t f_lo, f_hi, rest_lo = 0, rest_hi = 0;
+            {
+                const uint32_t both = value_factor(dv0) | value_factor(dv1) << 16;
+                const uint32_t even = __shfl_sync(0xFFFFFFFFu, both, 8 * t), odd = __shfl_sync(0xFFFFFFFFu, both, 8 * t + 4);
+                f_lo = __byte_perm(even, odd, 0x5410);
+                f_hi = __byte_perm(even, odd, 0x7632);
+            }
+            const bool two_steps = __any_sync(0xFFFFFFFFu, min(dv0, dv1) < -7);   // values beyond 2^15
+            if (two_steps) {
+                const uint32_t both = value_factor_rest(dv0) | value_factor_rest(dv1) << 16;
+                const uint32_t even = __shfl_sync(0xFFFFFFFFu, both, 8 * t), odd = __shfl_sync(0xFFFFFFFFu, both, 8 * t + 4);
+                rest_lo = __byte_perm(even, odd, 0x5410);
+                rest_hi = __byte_perm(even, odd, 0x7632);
+            }
 #pragma unroll
             for (int m = 0; m < D / 16; ++m) {
-                // dimensions 2m and 2m + 1 of the lane's sixteen (or eight), four tokens
-                uint32_t a0, a1, a2, a3;
-                const uint32_t sel = (m & 1) ? 0x7362u : 0x5140u;
-                e4_to_f16(__byte_perm(cur.v[0][m >> 1], cur.v[1][m >> 1], sel), a0, a1);
-                e4_to_f16(__byte_perm(cur.v[2][m >> 1], cur.v[3][m >> 1], sel), a2, a3);
+                // dimensions 2m and 2m + 1 of the lane's sixteen (or eight): byte 2 (m & 1) and the next of word m / 2
+                uint32_t a[4];
 #pragma unroll
-                for (int j = 0; j < NT; ++j) mma_f16(o[j][m], a0, a1, a2, a3, pt[j][0], pt[j][1]);
+                for (int k = 0; k < 4; ++k) {
+                    const uint32_t from = 2u * (m & 1) + (k & 1);      // byte of both tokens' words, to bytes 1 and 3
+                    const uint32_t x = __byte_perm(cur.v[k & 2][m >> 1], cur.v[(k & 2) + 1][m >> 1], ((4u + from) << 12) | (from << 4));
+                    a[k] = mul_bf16x2(e4_fields_as_bf16(x), k < 2 ? f_lo : f_hi);
+                    if (two_steps) a[k] = mul_bf16x2(a[k], k < 2 ? rest_lo : rest_hi);
+                }
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                    mma_bf16(o[j][m], a[0], a[1], a[2], a[3], pt[j][0][0], pt[j][0][1]);
+                    mma_bf16(o[j][m], a[0], a[1], a[2], a[3], pt[j][1][0], pt[j][1][1]);
+                }
             }
             if (i + 2 < count) load_v<D>(cur, kv.v8 + v_off, g, t);
         };
@@ -372,7 +404,7 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 3 : 2) attn_decode_k
             *reinterpret_cast<uint2 *>(p.out + row * p.ld_o + (int64_t)head * D + d) =
                 make_uint2(pack_bf16x2(v.x * inv, v.y * inv), pack_bf16x2(v.z * inv, v.w * inv));
             if (p.lse && d == 0)
-                p.lse[row * p.q_heads + head] = sum == 0.0f ? -INFINITY : (m - (float)kv.delta + log2_approx(sum)) * kLn2;
+                p.lse[row * p.q_heads + head] = sum == 0.0f ? -INFINITY : (m + log2_approx(sum)) * kLn2;
         };
         for (int idx = threadIdx.x; idx < kRows * (D / 4); idx += kDecodeThreads) {
             const int r = idx / (D / 4), d = idx % (D / 4) * 4;

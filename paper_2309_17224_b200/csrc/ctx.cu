@@ -5,6 +5,7 @@
 
 namespace fp8lin {
 cudaError_t configure_gemm_kernels(int max_smem_optin);  // gemm.cu
+cudaError_t configure_attn_kernels();                    // attn_chunk.cu
 std::atomic<unsigned long long> g_kernel_launches{0};
 }
 
@@ -72,7 +73,7 @@ fp8_status_t fp8_create(fp8_ctx **out, int device)
         return FP8_ERR_CUDA;
     }
     ctx->encode_tiled = (fp8lin::EncodeTiledFn)fn;
-    if (fp8lin::configure_gemm_kernels(ctx->max_smem_optin) != cudaSuccess) {
+    if (fp8lin::configure_gemm_kernels(ctx->max_smem_optin) != cudaSuccess || fp8lin::configure_attn_kernels() != cudaSuccess) {
         cudaFree(ctx->d_partial);
         cudaFree(buf);
         delete ctx;
