@@ -25,12 +25,13 @@ struct AttnParams {
     unsigned *count;      // arrival counters (ctx->d_attn_count), zero between calls
     int64_t ld_q, ld_o;
     int32_t q_heads, group, causal;
-    int32_t row_tiles, splits;   // chunk kernel: tiles of 128 rows of the longest sequence, parts that a context is cut into
+    int32_t row_tiles, min_share;   // chunk kernel: units of the longest sequence per head; least steps of a CTA
     float c;              // scale * log2(e)
 };
 
 constexpr float kNoMax = -3.0e38f;    // M before the first token: finite, so that 2^(-inf - M) is 0 and not NaN
 constexpr float kSlack = 40.0f;       // M is moved when a score exceeds it by more
+constexpr float kSumLimit = 1.152921504606847e18f;   // 2^60: the same, seen in the sum of the weights
 constexpr float kLn2 = 0.693147180559945309f;
 
 #ifdef __CUDACC__

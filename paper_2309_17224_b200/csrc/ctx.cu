@@ -102,6 +102,10 @@ fp8_status_t fp8_device_flags(fp8_ctx *ctx, void *stream, unsigned *flags, int c
         return FP8_ERR_CUDA;
     if (clear && cudaMemsetAsync(ctx->d_status, 0, sizeof(unsigned), st) != cudaSuccess) return FP8_ERR_CUDA;
     if (cudaStreamSynchronize(st) != cudaSuccess) return FP8_ERR_CUDA;
+    // a kernel that gave up waiting may not have arrived everywhere
+    if (clear && (*flags & FP8_FLAG_TIMEOUT) &&
+        cudaMemsetAsync(ctx->d_attn_count, 0, fp8lin::kAttnCounters * sizeof(unsigned), st) != cudaSuccess)
+        return FP8_ERR_CUDA;
     return (*flags & FP8_FLAG_TIMEOUT) ? FP8_ERR_DEVICE_TIMEOUT : FP8_OK;
 }
 
