@@ -4,7 +4,7 @@
 namespace fp8lin {
 
 fp8_status_t attn_decode(const fp8_ctx *ctx, const AttnParams &p, int head_dim, int rows, cudaStream_t st);   // attn_decode.cu
-fp8_status_t attn_chunk(const fp8_ctx *ctx, const AttnParams &p, const fp8_kv_cache_t *c, int64_t rows, cudaStream_t st);   // attn_chunk.cu
+fp8_status_t attn_chunk(const fp8_ctx *ctx, const AttnParams &p, const fp8_kv_cache_t *c, cudaStream_t st);   // attn_chunk.cu
 
 }  // namespace fp8lin
 
@@ -40,7 +40,7 @@ fp8_status_t fp8_attn_paged(fp8_ctx *ctx, const fp8_kv_cache_t *c, const fp8_seq
     if (rows > (int64_t)1 << 30) return FP8_ERR_SHAPE;
     // at most 16 query rows per key/value head: the kernel whose instructions take 8 or 16 rows; more: tiles of 128
     if (rows <= 16) return attn_decode(ctx, p, c->head_dim, (int)rows, (cudaStream_t)stream);
-    return attn_chunk(ctx, p, c, rows, (cudaStream_t)stream);
+    return attn_chunk(ctx, p, c, (cudaStream_t)stream);
 }
 
 }  // extern "C"

@@ -1,28 +1,32 @@
 // Attention over the paged FP8 cache for many query rows: chunks of a prompt, drafted tokens.
 //
 // The query rows of one key/value head (token by token, the head's query heads side by side) are taken in tiles of 128,
-// NQ tiles to a CTA, and the cached tokens in tiles of 128; two products per pair of tiles on the 5th-generation tensor
-// cores:
+// two tiles to a unit, and the cached tokens in tiles of 128, a step each; two products per pair of tiles on the
+// 5th-generation tensor cores:
 //   S = Q K^T   e4m3 x e4m3: the cache's key bytes are the operand as they lie (TMA, no conversion).  A query row is the
 //               sum of two e4m3 numbers under one power of two, q 2^e = hi + lo (hi rounded to nearest, lo the rest):
 //               eight significant bits together, so bf16 queries are exact unless 2^17 below their row's largest.  Two
 //               e4m3 products cost what one bf16 product costs.
-//   O += P V    bf16: a value 2^-d V8 is a bf16 number; four warps make them on their way into shared memory (once for
-//               all query rows of the CTA).  P in its two bf16 terms is read from tensor memory, where it takes the place
-//               of the scores that it came from, 32 tokens' terms side by side.
-// So a pair of tiles costs the tensor cores three bf16 products where bf16 attention has two.
+//   O += P V    tf32: P is left in tensor memory as the FP32 numbers that the softmax computes, in place of the scores, and
+//               read from there; a value 2^-d V8 is a tf32 number exactly, four warps make them on their way into shared
+//               memory (token index innermost; once for both query tiles).  The tensor cores drop P's lower thirteen
+//               bits: a weight loses up to 2^-10 of itself, 2^-11.5 on average, which the denominator is scaled by.
+//               A tf32 product costs two bf16 products; one bf16 product would be coarser than the output's rounding, two
+//               (P in two bf16 terms) cost the same as tf32 and five more instructions per pair of weights (measured:
+//               2048 tokens on 16384, 64/8 heads, 1675 us), and fp16 has no weights below 2^-39 of the largest.
 //
-// NQ = 2 (more than 128 rows): one CTA per SM, all 512 tensor-memory columns; while one tile's softmax runs, the other's
-// products do, and the values are converted once for 256 rows.  NQ = 1 (up to 128 rows): two CTAs per SM do the same for
-// one another.  Within a tile the order is strict: S, softmax, O, next S; that also makes the rescaling of O safe without
-// a barrier of its own, as S of a step is complete only after O of the step before.
+// One CTA per SM holds all 512 tensor-memory columns as two slots of S / P and O.  While one slot's softmax runs, the
+// other's products do.  With more than 128 rows the slots are the unit's two query tiles, with up to 128 they are the even
+// and the odd steps of the one tile, added up at its end.  Within a slot the order is strict: S, softmax, O, next S; that
+// also makes the rescaling of O safe without a barrier of its own, as S of a step is complete only after O of the one
+// before.
 //
-// The steps (tiles of tokens) of all units (query tiles of a key/value head) form one list that is cut evenly between the
-// CTAs, whatever the sequences' lengths and the mask; a unit that lies in several CTAs leaves partial sums in the
-// workspace, joined in order by the CTA that arrives last.
+// The steps of all units (query tiles of a key/value head) form one list that is cut evenly between the CTAs, whatever the
+// sequences' lengths and the mask; a unit that lies in several CTAs leaves partial sums in the workspace, joined in order
+// by the CTA that arrives last.
 //
-// Warps: 0 .. 4 NQ - 1 softmax and output (one query row per thread), then four for values, key loads and scaling
-// biases, one for the products.
+// Warps: 0-3 and 4-7 softmax of the two slots (one query row per thread) and output, 8-11 values, key loads and scaling
+// biases, 12 the products (13-15 only complete a warpgroup, whose registers the softmax takes).
 #include "attn_common.cuh"
 #include "ptx.cuh"
 
@@ -31,25 +35,31 @@ namespace fp8lin {
 constexpr int kTile = 128;                 // query rows of a tile, and tokens of a step
 constexpr int kKStages = 2;
 
-template <int D, int NQ>
+constexpr int kVStages = 2;
+constexpr int kChunkThreads = 512;
+// Registers per thread of the four warpgroups (softmax, softmax, values, products): 152 + 152 + 112 + 96 = 4 x 128, what
+// the block is launched with.
+constexpr int kSoftmaxRegs = 152, kValueRegs = 112, kProductRegs = 96;
+constexpr int kUnitRows = 2 * kTile;
+
+template <int D>
 struct ChunkShape {
-    static constexpr int kThreads = 32 * (4 * NQ + 5);
-    static constexpr int kResident = NQ == 1 ? 2 : 1;        // CTAs per SM
-    static constexpr int kVStages = NQ == 1 ? 1 : 2;
     static constexpr int kQBytes = kTile * 2 * D;            // of one query tile
     static constexpr int kKBytes = kTile * D;
-    static constexpr int kVBytes = kTile * D * 2;
-    static constexpr int kQ = 0;
-    static constexpr int kK = kQ + NQ * kQBytes;
+    static constexpr int kVBytes = kTile * D * 4;            // four blocks of [D][32 tokens]
+    static constexpr int kQ = 0;                             // (the second tile's place holds the odd slot's statistics
+    static constexpr int kK = kQ + 2 * kQBytes;              // where the slots share one query tile)
     static constexpr int kV = kK + kKStages * kKBytes;
     static constexpr int kScale = kV + kVStages * kVBytes;   // [2][128] floats: 2^-b of a tile's keys
     static constexpr int kBar = kScale + 2 * kTile * 4;
-    static constexpr int kNumBars = 2 * kKStages + 2 * kVStages + 2 + 4 * NQ;
+    static constexpr int kNumBars = 2 * kKStages + 2 * kVStages + 4 + 4 * 2 + 3;
     static constexpr int kTotal = kBar + kNumBars * 8 + 16;
     static constexpr int kDynamic = kTotal + 1024;           // slack to align the base to 1024 bytes
-    static constexpr uint32_t kTmemCols = 256 * NQ;          // per query tile 128 columns of S, then P; 128 of O
     static constexpr int kPart = kTile * (D + 2);            // floats of a tile's partial result: sums, M, denominators
 };
+constexpr uint32_t kTmemCols = 512, kTmemSlot = 256;         // per slot 128 columns of S, then P; 128 of O
+// 1 - 2^-11 E[1/m], m a mantissa in [1, 2) with its logarithm evenly spread: what P keeps on average
+constexpr float kTf32Kept = 1.0f - 0.7213f / 2048.0f;
 constexpr uint32_t kTmemO = 128;
 
 __device__ __forceinline__ void chunk_mma_f8(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
@@ -58,9 +68,9 @@ __device__ __forceinline__ void chunk_mma_f8(uint32_t d, uint64_t a, uint64_t b,
                  "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
                  : "memory");
 }
-__device__ __forceinline__ void chunk_mma_bf16_tmem(uint32_t d, uint32_t a_tmem, uint64_t b, uint32_t idesc, uint32_t accumulate)
+__device__ __forceinline__ void chunk_mma_tf32_tmem(uint32_t d, uint32_t a_tmem, uint64_t b, uint32_t idesc, uint32_t accumulate)
 {
-    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d),
+    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::tf32 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d),
                  "r"(a_tmem), "l"(b), "r"(idesc), "r"(accumulate)
                  : "memory");
 }
@@ -150,19 +160,22 @@ __device__ __forceinline__ void lds_pairs(uint32_t addr, f32x2 &a, f32x2 &b)
 {
     asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(a), "=l"(b) : "r"(addr));
 }
+__device__ __forceinline__ void sts4(uint32_t addr, float v)
+{
+    asm volatile("st.shared.b32 [%0], %1;" ::"r"(addr), "r"(__float_as_uint(v)) : "memory");
+}
 __device__ __forceinline__ void sts16(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d)
 {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
 
-// Shared-memory matrix descriptors (start address, leading and stride offsets in 16-byte units, version 1, swizzle).
+// Shared-memory matrix descriptors (start address, leading and stride offsets in 16-byte units, version 1, swizzle);
+// all operands here have the contraction index innermost.
 //   128-byte swizzle, operand rows of 128 contiguous bytes along the contraction, groups of eight rows 1024 bytes apart
 //   64-byte swizzle, rows of 64 bytes, groups of eight rows 512 bytes apart
-//   128-byte swizzle, contraction rows of 128 bytes of the N index, eight of them 1024 bytes; N blocks `lbo` apart
-__device__ __forceinline__ uint64_t desc_sw128(uint32_t addr, uint32_t lbo)
+__device__ __forceinline__ uint64_t desc_sw128(uint32_t addr)
 {
-    return (uint64_t)((addr >> 4) & 0x3FFFu) | (uint64_t)((lbo >> 4) & 0x3FFFu) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 |
-           (uint64_t)2 << 61;
+    return (uint64_t)((addr >> 4) & 0x3FFFu) | (uint64_t)1 << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
 }
 __device__ __forceinline__ uint64_t desc_sw64(uint32_t addr)
 {
@@ -176,7 +189,7 @@ __device__ __forceinline__ void tma_load_page(uint32_t dst, const CUtensorMap *m
                  : "memory");
 }
 
-// A unit of the list: NQ query tiles of one key/value head.
+// A unit of the list: up to two query tiles of one key/value head.
 struct ChunkUnit {
     int e;            // entry: sequence * row_tiles + place of the tiles in the sequence
     int h;
@@ -186,13 +199,12 @@ struct ChunkUnit {
     int64_t first;    // place of the unit's first step in the list
 };
 
-template <int NQ>
 __device__ __forceinline__ int entry_of(const AttnParams &p, int e, SeqShape &s, int &row0, int &rows, bool &cut)
 {
     const int b = e / p.row_tiles;
     s = seq_shape(p.kv, b, cut);
-    row0 = (e - b * p.row_tiles) * (NQ * kTile);
-    rows = (int)min((int64_t)s.n * p.group - row0, (int64_t)(NQ * kTile));
+    row0 = (e - b * p.row_tiles) * kUnitRows;
+    rows = (int)min((int64_t)s.n * p.group - row0, (int64_t)kUnitRows);
     if (rows <= 0) return 0;
     int see = s.len;
     if (p.causal) see = min(s.len, max(0, s.len - s.n + (row0 + rows - 1) / p.group + 1));
@@ -200,7 +212,6 @@ __device__ __forceinline__ int entry_of(const AttnParams &p, int e, SeqShape &s,
 }
 
 // Length of the list, by a whole warp.
-template <int NQ>
 __device__ __forceinline__ int64_t list_length(const AttnParams &p, int lane, bool &cut)
 {
     const int entries = p.kv.seqs * p.row_tiles;
@@ -210,7 +221,7 @@ __device__ __forceinline__ int64_t list_length(const AttnParams &p, int lane, bo
         SeqShape s;
         int row0, rows;
         bool c;
-        mine += entry_of<NQ>(p, e, s, row0, rows, c);
+        mine += entry_of(p, e, s, row0, rows, c);
         cut |= c;
     }
 #pragma unroll
@@ -219,7 +230,6 @@ __device__ __forceinline__ int64_t list_length(const AttnParams &p, int lane, bo
 }
 
 // The unit that holds step `at` of the list (at < list_length), by a whole warp.
-template <int NQ>
 __device__ __forceinline__ ChunkUnit unit_at(const AttnParams &p, int64_t at, int lane)
 {
     const int entries = p.kv.seqs * p.row_tiles;
@@ -231,7 +241,7 @@ __device__ __forceinline__ ChunkUnit unit_at(const AttnParams &p, int64_t at, in
             SeqShape s;
             int row0, rows;
             bool c;
-            n = entry_of<NQ>(p, e0 + lane, s, row0, rows, c);
+            n = entry_of(p, e0 + lane, s, row0, rows, c);
         }
         int64_t upto = (int64_t)n * p.kv.kv_heads;
 #pragma unroll
@@ -244,7 +254,7 @@ __device__ __forceinline__ ChunkUnit unit_at(const AttnParams &p, int64_t at, in
             const int l = __ffs(hit) - 1;
             u.e = e0 + l;
             bool c;
-            u.steps = entry_of<NQ>(p, u.e, u.s, u.row0, u.rows, c);
+            u.steps = entry_of(p, u.e, u.s, u.row0, u.rows, c);
             const int64_t start = before + __shfl_sync(0xFFFFFFFFu, upto, l) - (int64_t)u.steps * p.kv.kv_heads;
             u.h = (int)((at - start) / u.steps);
             u.first = start + (int64_t)u.h * u.steps;
@@ -254,7 +264,6 @@ __device__ __forceinline__ ChunkUnit unit_at(const AttnParams &p, int64_t at, in
     }
 }
 
-template <int NQ>
 __device__ __forceinline__ void next_unit(const AttnParams &p, ChunkUnit &u)
 {
     u.first += u.steps;
@@ -262,11 +271,11 @@ __device__ __forceinline__ void next_unit(const AttnParams &p, ChunkUnit &u)
     u.h = 0;
     do {
         bool c;
-        u.steps = entry_of<NQ>(p, ++u.e, u.s, u.row0, u.rows, c);
+        u.steps = entry_of(p, ++u.e, u.s, u.row0, u.rows, c);
     } while (u.steps == 0);
 }
 
-// The weights of 32 tokens for one row: p = 2^(rc u - M) in two bf16 terms, and their sum.
+// The weights of 32 tokens for one row, p = 2^(rc u - M), and their sum.
 __device__ __forceinline__ f32x2 weights32(const f32x2 (&u)[16], f32x2 rc2, float top, uint32_t (&ph)[32])
 {
     const f32x2 minus = pack2(-top, -top);
@@ -277,32 +286,26 @@ __device__ __forceinline__ f32x2 weights32(const f32x2 (&u)[16], f32x2 rc2, floa
         unpack2(fma2(u[k], rc2, minus), lo, hi);
         lo = exp2_approx(lo);
         hi = exp2_approx(hi);
-        const f32x2 both = pack2(lo, hi);
-        if (k & 1) s1 = add2(s1, both);
-        else s0 = add2(s0, both);
-        const uint32_t a = __float_as_uint(lo), b = __float_as_uint(hi);
-        ph[k] = __byte_perm(a, b, 0x7632);                       // the leading eight bits ...
-        const f32x2 rest = add2(both, pack2(__uint_as_float((a & 0xFFFF0000u) ^ 0x80000000u), __uint_as_float((b & 0xFFFF0000u) ^ 0x80000000u)));
-        unpack2(rest, lo, hi);
-        ph[16 + k] = pack_bf16x2(lo, hi);                        // ... and what they leave
+        ph[2 * k] = __float_as_uint(lo);
+        ph[2 * k + 1] = __float_as_uint(hi);
+        if (k & 1) s1 = add2(s1, pack2(lo, hi));
+        else s0 = add2(s0, pack2(lo, hi));
     }
     return add2(s0, s1);
 }
 
-template <int D, int NQ>
-__global__ void __launch_bounds__((ChunkShape<D, NQ>::kThreads), (ChunkShape<D, NQ>::kResident))
-attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const AttnParams p)
+template <int D>
+__global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const AttnParams p)
 {
-    using L = ChunkShape<D, NQ>;
-    constexpr int kVS = L::kVStages;
-    constexpr int kFirstValueWarp = 4 * NQ, kProductWarp = 4 * NQ + 4;
+    using L = ChunkShape<D>;
+    constexpr int kFirstValueWarp = 8, kProductWarp = 12;
     extern __shared__ uint8_t smem_raw[];
     const KvParams &kv = p.kv;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     // ---- the CTA's share of the list ----
     bool cut;
-    const int64_t total = list_length<NQ>(p, lane, cut);
+    const int64_t total = list_length(p, lane, cut);
     if (blockIdx.x == 0 && warp == 0 && __any_sync(0xFFFFFFFFu, cut) && lane == 0) raise_flags(kv.d_status, FP8_FLAG_BAD_INDEX);
     const int64_t share = max((total + gridDim.x - 1) / (int64_t)gridDim.x, (int64_t)p.min_share);
     const int64_t begin = blockIdx.x * share, end = min(total, begin + share);
@@ -312,34 +315,41 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const AttnParams p)
     const uint32_t base = smem_u32(smem), bars = base + L::kBar;
     auto k_full = [&](uint32_t g) { return bars + 8u * (g % kKStages); };
     auto k_empty = [&](uint32_t g) { return bars + 8u * (kKStages + g % kKStages); };
-    auto v_full = [&](uint32_t g) { return bars + 8u * (2 * kKStages + g % kVS); };
-    auto v_empty = [&](uint32_t g) { return bars + 8u * (2 * kKStages + kVS + g % kVS); };
-    const uint32_t bars2 = bars + 8u * (2 * kKStages + 2 * kVS);
-    auto sc_full = [&](uint32_t g) { return bars2 + 8u * (g & 1u); };
-    auto q_full = [&](int q) { return bars2 + 16u + 8u * q; };
-    auto s_full = [&](int q) { return bars2 + 16u + 8u * (NQ + q); };
-    auto p_full = [&](int q) { return bars2 + 16u + 8u * (2 * NQ + q); };
-    auto o_full = [&](int q) { return bars2 + 16u + 8u * (3 * NQ + q); };
+    auto v_full = [&](uint32_t g) { return bars + 8u * (2 * kKStages + g % kVStages); };
+    auto v_empty = [&](uint32_t g) { return bars + 8u * (2 * kKStages + kVStages + g % kVStages); };
+    const uint32_t bars2 = bars + 8u * (2 * kKStages + 2 * kVStages);
+    // of a slot's n-th step (two places each: the values' warps may be a step ahead of a slot, and a slot that sits out a
+    // unit must not meet a phase that it has not waited for)
+    auto sc_full = [&](int q, uint32_t n) { return bars2 + 8u * (2 * q + (n & 1u)); };
+    auto q_full = [&](int q) { return bars2 + 32u + 8u * q; };
+    auto s_full = [&](int q) { return bars2 + 48u + 8u * q; };
+    auto p_full = [&](int q) { return bars2 + 64u + 8u * q; };
+    auto o_full = [&](int q) { return bars2 + 80u + 8u * q; };
+    auto slot_bar = [&](int q) { return bars2 + 96u + 8u * q; };     // the 128 threads of a slot; both slots' 256
+    const uint32_t both_bar = bars2 + 112u;
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + L::kBar + L::kNumBars * 8);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
-    volatile int *is_last = reinterpret_cast<volatile int *>(tmem_slot + 2);     // [NQ]
+    volatile int *is_last = reinterpret_cast<volatile int *>(tmem_slot + 2);     // [2]
 
     if (threadIdx.x == 0) {
         for (uint32_t i = 0; i < kKStages; ++i) { mbar_init(k_full(i), 1); mbar_init(k_empty(i), 1); }
-        for (uint32_t i = 0; i < kVS; ++i) { mbar_init(v_full(i), 128); mbar_init(v_empty(i), 1); }
-        for (uint32_t i = 0; i < 2; ++i) mbar_init(sc_full(i), 128);
-        for (int q = 0; q < NQ; ++q) {
+        for (uint32_t i = 0; i < kVStages; ++i) { mbar_init(v_full(i), 128); mbar_init(v_empty(i), 1); }
+        for (int q = 0; q < 2; ++q) {
+            mbar_init(sc_full(q, 0), 128);
+            mbar_init(sc_full(q, 1), 128);
             mbar_init(q_full(q), 128);
             mbar_init(s_full(q), 1);
             mbar_init(p_full(q), 4);
             mbar_init(o_full(q), 1);
+            mbar_init(slot_bar(q), 128);
         }
+        mbar_init(both_bar, 256);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     if (warp == kProductWarp) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(L::kTmemCols) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(kTmemCols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     chunk_fence_before();
@@ -347,120 +357,127 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const AttnParams p)
     chunk_fence_after();
     const uint32_t tmem = *tmem_slot;
 
-    ChunkUnit u = unit_at<NQ>(p, begin, lane);
+    ChunkUnit u = unit_at(p, begin, lane);
     int64_t at = begin;
     uint32_t g0 = 0;          // steps of this CTA before the current unit
     bool alive = true;
 
-    if (warp == kProductWarp) {
+    if (warp >= kProductWarp) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kProductRegs));
         // ------------------------------- products -------------------------------
-        const uint32_t idesc_s = (1u << 4) | ((uint32_t)(kTile >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);   // e4m3 x e4m3
-        const uint32_t idesc_o = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(D >> 3) << 17) |
-                                 ((uint32_t)(kTile >> 4) << 24);                                                 // bf16, B along N
-        uint32_t n_units[NQ] = {}, n_steps[NQ] = {};
-        auto scores = [&](int q, uint32_t g) {
-            const uint32_t k_addr = base + L::kK + (g % kKStages) * L::kKBytes, q_addr = base + L::kQ + q * L::kQBytes;
-            const uint64_t dk = D == 128 ? desc_sw128(k_addr, 16) : desc_sw64(k_addr);
+        const uint32_t idesc_s = (1u << 4) | ((uint32_t)(kTile >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);                       // e4m3
+        const uint32_t idesc_o = (1u << 4) | (2u << 7) | (2u << 10) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);   // tf32
+        uint32_t n_units[2] = {}, n_steps[2] = {};
+        // S of step g into slot q, from query tile qt
+        auto scores = [&](int q, int qt, uint32_t g) {
+            const uint32_t k_addr = base + L::kK + (g % kKStages) * L::kKBytes, q_addr = base + L::kQ + qt * L::kQBytes;
+            const uint64_t dk = D == 128 ? desc_sw128(k_addr) : desc_sw64(k_addr);
 #pragma unroll
             for (int term = 0; term < 2; ++term) {
-                const uint64_t dq = D == 128 ? desc_sw128(q_addr + term * kTile * 128, 16) : desc_sw128(q_addr, 16) + 4u * term;
+                const uint64_t dq = D == 128 ? desc_sw128(q_addr + term * kTile * 128) : desc_sw128(q_addr) + 4u * term;
 #pragma unroll
-                for (int k = 0; k < D / 32; ++k) chunk_mma_f8(tmem + 256u * q, dq + 2u * k, dk + 2u * k, idesc_s, (term | k) ? 1u : 0u);
+                for (int k = 0; k < D / 32; ++k) chunk_mma_f8(tmem + kTmemSlot * q, dq + 2u * k, dk + 2u * k, idesc_s, (term | k) ? 1u : 0u);
             }
+            chunk_commit(s_full(q));
         };
-        if (lane == 0) {
+        // O of slot q += P of the slot, V of step g
+        auto outputs = [&](int q, uint32_t g, bool first) {
+            const uint64_t dv = desc_sw128(base + L::kV + (g % kVStages) * L::kVBytes);
+            const uint32_t slot = tmem + kTmemSlot * q;
+#pragma unroll
+            for (int k = 0; k < kTile / 8; ++k)      // eight tokens: 32 bytes of a block's rows, D * 128 bytes from block to block
+                chunk_mma_tf32_tmem(slot + kTmemO, slot + 8u * k, dv + (uint32_t)(k >> 2) * (D * 128 / 16) + 2u * (k & 3), idesc_o, first && k == 0 ? 0u : 1u);
+        };
+        if (warp == kProductWarp && lane == 0) {
             while (true) {
                 const int lo = (int)(at - u.first), steps = (int)min((int64_t)u.steps, end - u.first) - lo;
-                const int nq = NQ == 1 || u.rows <= kTile ? 1 : 2;
-                for (int q = 0; q < nq && alive; ++q) alive = mbar_wait(q_full(q), n_units[q]++ & 1u, abort_flag, kv.d_status);
+                const bool two = u.rows > kTile;           // two query tiles; else even and odd steps
+                alive = mbar_wait(q_full(0), n_units[0]++ & 1u, abort_flag, kv.d_status);
+                if (two) alive = alive && mbar_wait(q_full(1), n_units[1]++ & 1u, abort_flag, kv.d_status);
                 alive = alive && mbar_wait(k_full(g0), (g0 / kKStages) & 1u, abort_flag, kv.d_status);
                 if (!alive) break;
                 chunk_fence_after();
-                for (int q = 0; q < nq; ++q) {
-                    scores(q, g0);
-                    chunk_commit(s_full(q));
+                scores(0, 0, g0);
+                if (two) {
+                    scores(1, 1, g0);
+                    chunk_commit(k_empty(g0));
+                } else {
+                    chunk_commit(k_empty(g0));
+                    if (steps > 1) {
+                        alive = mbar_wait(k_full(g0 + 1), ((g0 + 1) / kKStages) & 1u, abort_flag, kv.d_status);
+                        if (!alive) break;
+                        chunk_fence_after();
+                        scores(1, 0, g0 + 1);
+                        chunk_commit(k_empty(g0 + 1));
+                    }
                 }
-                chunk_commit(k_empty(g0));
+                const int ahead = two ? 1 : 2;             // steps from one of a slot to its next
                 for (int i = 0; i < steps && alive; ++i) {
-                    const uint32_t g = g0 + i;
-                    const uint64_t dv = desc_sw128(base + L::kV + (g % kVS) * L::kVBytes, kTile * 128);
-                    alive = mbar_wait(v_full(g), (g / kVS) & 1u, abort_flag, kv.d_status);
-                    for (int q = 0; q < nq && alive; ++q) {
+                    const uint32_t g = g0 + i, gn = g + ahead;
+                    alive = mbar_wait(v_full(g), (g / kVStages) & 1u, abort_flag, kv.d_status);
+                    const int q0 = two ? 0 : i & 1, q1 = two ? 1 : i & 1;
+                    for (int q = q0; q <= q1 && alive; ++q) {
                         alive = mbar_wait(p_full(q), n_steps[q]++ & 1u, abort_flag, kv.d_status);
                         if (!alive) break;
                         chunk_fence_after();
-                        const uint32_t acc = tmem + 256u * q + kTmemO;
-#pragma unroll
-                        for (int k = 0; k < kTile / 16; ++k) {      // 16 tokens: columns 8 (k % 2) of the 32 that hold 32 tokens
-                            const uint32_t p1 = tmem + 256u * q + 32u * (k >> 1) + 8u * (k & 1);
-                            chunk_mma_bf16_tmem(acc, p1, dv + 128u * k, idesc_o, (i | k) ? 1u : 0u);
-                            chunk_mma_bf16_tmem(acc, p1 + 16u, dv + 128u * k, idesc_o, 1u);
-                        }
-                        if (q == nq - 1) chunk_commit(v_empty(g));
-                        if (i + 1 == steps) {
+                        outputs(q, g, i < ahead);
+                        if (q == q1) chunk_commit(v_empty(g));
+                        if (i + ahead >= steps) {
                             chunk_commit(o_full(q));
                         } else {
-                            if (q == 0) {
-                                alive = mbar_wait(k_full(g + 1), ((g + 1) / kKStages) & 1u, abort_flag, kv.d_status);
+                            if (q == q0) {
+                                alive = mbar_wait(k_full(gn), (gn / kKStages) & 1u, abort_flag, kv.d_status);
                                 if (!alive) break;
                                 chunk_fence_after();
                             }
-                            scores(q, g + 1);
-                            chunk_commit(s_full(q));
-                            if (q == nq - 1) chunk_commit(k_empty(g + 1));
+                            scores(q, two ? q : 0, gn);
+                            if (q == q1) chunk_commit(k_empty(gn));
                         }
                     }
                 }
                 g0 += steps;
                 at += steps;
                 if (!alive || at >= end) break;
-                next_unit<NQ>(p, u);
+                next_unit(p, u);
             }
         }
     } else if (warp >= kFirstValueWarp) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kValueRegs));
         // ------------------------------- values, keys' loads, scaling biases -------------------------------
-        // A warp takes 32 tokens of each tile: lane (tok, c) = (lane / 4, lane % 4) of eight tokens at a time, 16 bytes.
-        // Two neighbouring tokens and four pieces of 16 dimensions meet all banks once in each store of eight lanes.
-        const int cw = warp - kFirstValueWarp, sub = lane >> 2, c = lane & 3;
-        constexpr int kHalves = D / 64, kLoads = 4 * kHalves;
+        // A warp takes 32 tokens of each tile, a lane one token's row: 32 lanes store one dimension of their tokens side
+        // by side (all banks once).  Shared memory: four blocks of 32 tokens, [D][32 tokens], 128-byte rows, swizzled.
+        const int cw = warp - kFirstValueWarp;
+        constexpr int kLoads = D / 16;
         const int per_tile = kTile >> kv.page_shift, in_page = (1 << kv.page_shift) - 1;
         unsigned bad_pages = 0;
+        uint32_t n_steps[2] = {}; // of the slots so far
+        uint32_t place[8];        // of the lane's token in the rows of dimensions = 0 .. 7 mod 8
+#pragma unroll
+        for (int k = 0; k < 8; ++k) place[k] = base + L::kV + cw * (D * 128) + (((lane >> 2) ^ k) << 4) + ((lane & 3) << 2);
         while (true) {
             const int lo = (int)(at - u.first), steps = (int)min((int64_t)u.steps, end - u.first) - lo;
+            const bool two = u.rows > kTile;
             const SeqShape s = u.s;
             const int32_t *table = kv.table + (int64_t)(u.e / p.row_tiles) * kv.table_stride;
             const int64_t row_h = (int64_t)u.h << kv.page_shift;
             const int last_page = s.len > 0 ? (s.len - 1) >> kv.page_shift : -1;
-            uint4 cur[kLoads], nxt[kLoads];
-            int bk = 0, bv = 0, bk_n = 0, bv_n = 0;
-            auto request = [&](int tile, uint4 (&v)[kLoads], int &b_k, int &b_v) {
-                // pages of the warp's tokens 0..15 and 16..31 (the same one unless pages hold 16 tokens)
-                const int t0 = tile * kTile + cw * 32;
-                int pg[2];
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    pg[i] = t0 + 16 * i < s.len ? __ldg(table + ((t0 + 16 * i) >> kv.page_shift)) : 0;
-                    if ((unsigned)pg[i] >= (unsigned)kv.pages) { pg[i] = -1; bad_pages = 1; }
-                }
-#pragma unroll
-                for (int i = 0; i < kLoads; ++i) {
-                    const int g8 = i / kHalves, half = i % kHalves;           // eight tokens g8 * 8 + sub
-                    const int tk = t0 + g8 * 8 + sub;
-                    v[i] = make_uint4(0, 0, 0, 0);
-                    if (tk < s.len && pg[g8 >> 1] >= 0)
-                        v[i] = ldg_stream(kv.v8 + pg[g8 >> 1] * kv.page_stride + (row_h + (tk & in_page)) * D + half * 64 + c * 16);
-                }
-                const int tk = t0 + lane, mine = lane < 16 ? pg[0] : pg[1];
-                b_k = b_v = 0;
-                if (tk < s.len) {
-                    b_k = b_v = FP8_KV_BIAS_NONFINITE;
-                    if (mine >= 0) {
-                        const int64_t where = mine * kv.bias_stride + row_h + (tk & in_page);
-                        b_k = kv.bk[where];
-                        b_v = kv.bv[where];
-                    }
-                }
+            // a token's page (-1: the token is behind the end, -2: the page number is out of range), its row and biases
+            auto page_of_token = [&](int tile) {
+                const int tk = tile * kTile + cw * 32 + lane;
+                const int page = tk < s.len ? __ldg(table + (tk >> kv.page_shift)) : -1;
+                return tk < s.len && (unsigned)page >= (unsigned)kv.pages ? -2 : page;
             };
+            auto row_of = [&](int tile, int page, int &b_k, int &b_v) {
+                const int64_t row = row_h + ((tile * kTile + cw * 32 + lane) & in_page);
+                b_k = b_v = page == -1 ? 0 : FP8_KV_BIAS_NONFINITE;
+                if (page == -2) bad_pages = 1;
+                if (page < 0) return (const uint4 *)nullptr;
+                b_k = kv.bk[page * kv.bias_stride + row];
+                b_v = kv.bv[page * kv.bias_stride + row];
+                return reinterpret_cast<const uint4 *>(kv.v8 + page * kv.page_stride + row * D);
+            };
+            uint4 cur[kLoads];
+            int bk = 0, bv = 0, bk_n = 0, bv_n = 0, page_n = -1;
             // keys: the first of these warps, one lane per page of the tile
             auto page_of = [&](int tile) {
                 const int j = tile * per_tile + lane;
@@ -485,7 +502,12 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const AttnParams p)
                 alive = request_keys(lo, g0, page_of(lo));
                 if (steps > 1) page = page_of(lo + 1);
             }
-            if (alive) request(lo, cur, bk, bv);
+            {
+                const uint4 *src = row_of(lo, page_of_token(lo), bk, bv);
+#pragma unroll
+                for (int k = 0; k < kLoads; ++k) cur[k] = src ? __ldg(src + k) : make_uint4(0, 0, 0, 0);
+                if (steps > 1) page_n = page_of_token(lo + 1);
+            }
             for (int i = 0; i < steps && alive; ++i) {
                 const int tile = lo + i;
                 const uint32_t g = g0 + i;
@@ -494,67 +516,76 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const AttnParams p)
                     if (!alive) break;
                     if (i + 2 < steps) page = page_of(tile + 2);
                 }
-                auto wait_free = [&](uint32_t gg) {        // the products of step gg have read their values
-                    const bool ok = mbar_wait(v_empty(gg), (gg / kVS) & 1u, abort_flag, kv.d_status);
-                    return (bool)__all_sync(0xFFFFFFFFu, ok);
-                };
-                if (kVS == 2 && g >= 2 && !(alive = wait_free(g - 2))) break;
-                // the tile's factors: 2^-b of the keys for the softmax (its reader two steps ago is done: the products
-                // of that step, waited for above or a step ago, followed it), 2^(120 - d) for the values
+                if (g >= 2) {         // the products of step g - 2 have read the values in this place, and its softmax the factors
+                    const bool ok = mbar_wait(v_empty(g), ((g / kVStages) & 1u) ^ 1u, abort_flag, kv.d_status);
+                    if (!(alive = __all_sync(0xFFFFFFFFu, ok))) break;
+                }
+                // 2^-b of the key for the softmax, 2^-d for the value
                 const bool marked = bk == FP8_KV_BIAS_NONFINITE || bv == FP8_KV_BIAS_NONFINITE;
-                const unsigned drop = __ballot_sync(0xFFFFFFFFu, marked);
                 reinterpret_cast<float *>(smem + L::kScale)[(g & 1u) * kTile + cw * 32 + lane] =
                     marked ? __int_as_float(0x7FFFFFFF) : pow2_normal(min(126, -(bk + kv.delta)));
-                const uint32_t factor = value_factor(bv + kv.delta), rest = value_factor_rest(bv + kv.delta);
-                const bool two_steps = __any_sync(0xFFFFFFFFu, bv + kv.delta < -7);     // values beyond 2^15
-                mbar_arrive(sc_full(g));
-                if (i + 1 < steps) request(tile + 1, nxt, bk_n, bv_n);
-                if (kVS == 1 && g >= 1 && !(alive = wait_free(g - 1))) break;
+                if (two || (i & 1) == 0) mbar_arrive(sc_full(0, n_steps[0]++));
+                if (two || (i & 1) == 1) mbar_arrive(sc_full(1, n_steps[1]++));
+                // the next tile's row takes the registers as they are converted
+                const uint4 *src_n = nullptr;
+                if (i + 1 < steps) src_n = row_of(tile + 1, page_n, bk_n, bv_n);
+                if (i + 2 < steps) page_n = page_of_token(tile + 2);
+                const float f = pow2_normal(min(126, -(applied_bias(bv) + kv.delta)));
+                const f32x2 f2 = pack2(f, f);
+                const uint32_t stage = (g % kVStages) * L::kVBytes;
 #pragma unroll
                 for (int k = 0; k < kLoads; ++k) {
-                    const int g8 = k / kHalves, half = k % kHalves, tk = cw * 32 + g8 * 8 + sub;
-                    uint4 v = cur[k];
-                    if ((drop >> (g8 * 8 + sub)) & 1u) v = make_uint4(0, 0, 0, 0);   // 0 times a NaN byte would be one
-                    const uint32_t f = __shfl_sync(0xFFFFFFFFu, factor, g8 * 8 + sub) * 0x10001u;
-                    const uint32_t x[4] = {v.x, v.y, v.z, v.w};
-                    uint32_t w[8];
+                    const uint32_t w[4] = {cur[k].x, cur[k].y, cur[k].z, cur[k].w};
+                    cur[k] = src_n ? __ldg(src_n + k) : make_uint4(0, 0, 0, 0);
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
-                        w[2 * q] = mul_bf16x2(e4_fields_as_bf16(__byte_perm(x[q], 0u, 0x1000)), f);
-                        w[2 * q + 1] = mul_bf16x2(e4_fields_as_bf16(__byte_perm(x[q], 0u, 0x3020)), f);
-                    }
-                    if (two_steps) {
-                        const uint32_t f2 = __shfl_sync(0xFFFFFFFFu, rest, g8 * 8 + sub) * 0x10001u;
+                        uint32_t h[2];
+                        e4_to_f16(marked ? 0u : w[q], h[0], h[1]);     // (0 times a NaN byte would be one)
+                        float v[4];
+                        unpack4<FP8_F16>(h, v);
+                        unpack2(mul2(pack2(v[0], v[1]), f2), v[0], v[1]);
+                        unpack2(mul2(pack2(v[2], v[3]), f2), v[2], v[3]);
 #pragma unroll
-                        for (int q = 0; q < 8; ++q) w[q] = mul_bf16x2(w[q], f2);
+                        for (int j = 0; j < 4; ++j) {
+                            const int dim = 16 * k + 4 * q + j;
+                            sts4(place[dim & 7] + stage + dim * 128, v[j]);
+                        }
                     }
-                    const uint32_t row = base + L::kV + (g % kVS) * L::kVBytes + half * (kTile * 128) + tk * 128;
-                    sts16(row + (((2 * c) ^ (tk & 7)) << 4), w[0], w[1], w[2], w[3]);
-                    sts16(row + (((2 * c + 1) ^ (tk & 7)) << 4), w[4], w[5], w[6], w[7]);
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 mbar_arrive(v_full(g));
-#pragma unroll
-                for (int k = 0; k < kLoads; ++k) cur[k] = nxt[k];
                 bk = bk_n;
                 bv = bv_n;
             }
             g0 += steps;
             at += steps;
             if (!alive || at >= end) break;
-            next_unit<NQ>(p, u);
+            next_unit(p, u);
         }
         if (bad_pages) raise_flags(kv.d_status, FP8_FLAG_BAD_INDEX);
     } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
         // ------------------------------- softmax and output -------------------------------
-        const int qt = NQ == 1 ? 0 : warp >> 2, r = threadIdx.x & 127;         // query tile, row in it
-        const uint32_t lanes = tmem + 256u * qt + ((uint32_t)((warp & 3) * 32) << 16);
-        uint32_t n_units = 0, n_steps = 0;
+        const int slot = warp >> 2, r = threadIdx.x & 127;                     // slot, row of the query tile
+        const uint32_t quarter = (uint32_t)((warp & 3) * 32) << 16, lanes = tmem + kTmemSlot * slot + quarter;
+        uint32_t n_units[2] = {}, n_steps = 0, n_slot = 0, n_both = 0;      // units, steps, barriers so far
+        // (barriers with a limit, like all waits: a warp that gave up does not leave the others waiting)
+        auto sync_slot = [&]() {
+            mbar_arrive(slot_bar(slot));
+            const bool ok = mbar_wait(slot_bar(slot), n_slot++ & 1u, abort_flag, kv.d_status);
+            return (bool)__all_sync(0xFFFFFFFFu, ok);
+        };
+        auto sync_both = [&]() {
+            mbar_arrive(both_bar);
+            const bool ok = mbar_wait(both_bar, n_both++ & 1u, abort_flag, kv.d_status);
+            return (bool)__all_sync(0xFFFFFFFFu, ok);
+        };
         while (true) {
             const int lo = (int)(at - u.first), hi = (int)min((int64_t)u.steps, end - u.first), steps = hi - lo;
             const SeqShape s = u.s;
-            const int row0 = u.row0 + qt * kTile, rows = u.rows - qt * kTile;  // of this query tile
-            if (rows > 0) {
+            const bool two = u.rows > kTile, joined = !two && steps > 1;       // joined: the slots hold parts of one tile
+            const int row0 = u.row0 + (two ? slot * kTile : 0), rows = u.rows - (two ? slot * kTile : 0);
+            if (two || slot == 0 || joined) {
                 const int tok = min((row0 + r) / p.group, s.n - 1), head = u.h * p.group + (row0 + r) % p.group;
                 // ---- queries as two e4m3 terms, one row per thread ----
                 float rc;               // |c| / the row's power of two
@@ -574,31 +605,33 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const AttnParams p)
                     const float f = copysignf(pow2_normal(e), p.c);     // a negative scale goes into the queries: rc >= 0
                     // (not 0: it multiplies the -infinity of masked tokens)
                     rc = m >= 0x7F800000u ? __int_as_float(0x7FFFFFFF) : fmaxf(fabsf(p.c) * pow2_normal(-e), 1e-37f);
+                    if (two || slot == 0) {
 #pragma unroll 2
-                    for (int i = 0; i < D / 16; ++i) {
-                        uint4 x = make_uint4(0, 0, 0, 0), y = x;
-                        if (r < rows) { x = src[2 * i]; y = src[2 * i + 1]; }
-                        const uint32_t w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-                        uint32_t hi4[4], lo4[4];
+                        for (int i = 0; i < D / 16; ++i) {
+                            uint4 x = make_uint4(0, 0, 0, 0), y = x;
+                            if (r < rows) { x = src[2 * i]; y = src[2 * i + 1]; }
+                            const uint32_t w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+                            uint32_t hi4[4], lo4[4];
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const float a0 = __uint_as_float(w[2 * j] << 16) * f, a1 = __uint_as_float(w[2 * j] & 0xFFFF0000u) * f;
-                            const float a2 = __uint_as_float(w[2 * j + 1] << 16) * f, a3 = __uint_as_float(w[2 * j + 1] & 0xFFFF0000u) * f;
-                            hi4[j] = cvt_pair<FP8_E4>(a1, a0) | (cvt_pair<FP8_E4>(a3, a2) << 16);
-                            uint32_t h2[2];
-                            e4_to_f16(hi4[j], h2[0], h2[1]);
-                            float back[4];
-                            unpack4<FP8_F16>(h2, back);
-                            lo4[j] = cvt_pair<FP8_E4>(a1 - back[1], a0 - back[0]) | (cvt_pair<FP8_E4>(a3 - back[3], a2 - back[2]) << 16);
+                            for (int j = 0; j < 4; ++j) {
+                                const float a0 = __uint_as_float(w[2 * j] << 16) * f, a1 = __uint_as_float(w[2 * j] & 0xFFFF0000u) * f;
+                                const float a2 = __uint_as_float(w[2 * j + 1] << 16) * f, a3 = __uint_as_float(w[2 * j + 1] & 0xFFFF0000u) * f;
+                                hi4[j] = cvt_pair<FP8_E4>(a1, a0) | (cvt_pair<FP8_E4>(a3, a2) << 16);
+                                uint32_t h2[2];
+                                e4_to_f16(hi4[j], h2[0], h2[1]);
+                                float back[4];
+                                unpack4<FP8_F16>(h2, back);
+                                lo4[j] = cvt_pair<FP8_E4>(a1 - back[1], a0 - back[0]) | (cvt_pair<FP8_E4>(a3 - back[3], a2 - back[2]) << 16);
+                            }
+                            // D = 128: a row of hi, and 16 KB on its row of lo; D = 64: hi and lo side by side in one 128-byte row
+                            const int c_hi = i, c_lo = D == 128 ? i : i + 4;
+                            const uint32_t row = base + L::kQ + slot * L::kQBytes + r * 128;
+                            sts16(row + ((c_hi ^ (r & 7)) << 4), hi4[0], hi4[1], hi4[2], hi4[3]);
+                            sts16(row + (D == 128 ? kTile * 128 : 0) + ((c_lo ^ (r & 7)) << 4), lo4[0], lo4[1], lo4[2], lo4[3]);
                         }
-                        // D = 128: a row of hi, and 16 KB on its row of lo; D = 64: hi and lo side by side in one 128-byte row
-                        const int c_hi = i, c_lo = D == 128 ? i : i + 4;
-                        const uint32_t row = base + L::kQ + qt * L::kQBytes + r * 128;
-                        sts16(row + ((c_hi ^ (r & 7)) << 4), hi4[0], hi4[1], hi4[2], hi4[3]);
-                        sts16(row + (D == 128 ? kTile * 128 : 0) + ((c_lo ^ (r & 7)) << 4), lo4[0], lo4[1], lo4[2], lo4[3]);
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        mbar_arrive(q_full(slot));
                     }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    mbar_arrive(q_full(qt));
                 }
                 int limit = s.len;       // tokens that the row sees
                 if (p.causal) limit = min(s.len, max(0, s.len - s.n + (row0 + r) / p.group + 1));
@@ -607,11 +640,13 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const AttnParams p)
                 float top = kNoMax;
                 f32x2 sum = pack2(0.0f, 0.0f);
                 const f32x2 rc2 = pack2(rc, rc);
-                for (int i = 0; i < steps; ++i) {
+                const int start = two ? 0 : slot, ahead = two ? 1 : 2;
+                for (int i = start; i < steps; i += ahead) {
                     const uint32_t g = g0 + i;
                     const int t0 = (lo + i) * kTile;
-                    bool ok = mbar_wait(s_full(qt), n_steps++ & 1u, abort_flag, kv.d_status);
-                    ok = ok && mbar_wait(sc_full(g), (g >> 1) & 1u, abort_flag, kv.d_status);
+                    bool ok = mbar_wait(sc_full(slot, n_steps), (n_steps >> 1) & 1u, abort_flag, kv.d_status);
+                    ok = ok && mbar_wait(s_full(slot), n_steps & 1u, abort_flag, kv.d_status);
+                    ++n_steps;
                     if (!(alive = __all_sync(0xFFFFFFFFu, ok))) break;
                     chunk_fence_after();
                     if (active) {
@@ -631,7 +666,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const AttnParams p)
                                 v[k] = mul2(pack2(__uint_as_float(x[2 * k]), __uint_as_float(x[2 * k + 1])), f0);
                                 v[k + 1] = mul2(pack2(__uint_as_float(x[2 * k + 2]), __uint_as_float(x[2 * k + 3])), f1);
                             }
-                            if (mask) {
+                            if (__builtin_expect(mask, 0)) {
 #pragma unroll
                                 for (int k = 0; k < 16; ++k) {
                                     float a, b;
@@ -648,7 +683,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const AttnParams p)
                             f32x2 add = weights32(v, rc2, top, ph);
                             float a, b;
                             unpack2(add2(sum, add), a, b);
-                            if (__any_sync(0xFFFFFFFFu, a + b > kSumLimit)) {
+                            if (__builtin_expect(__any_sync(0xFFFFFFFFu, a + b > kSumLimit), 0)) {
                                 float m = -INFINITY;
 #pragma unroll
                                 for (int k = 0; k < 16; ++k) {
@@ -656,29 +691,21 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const AttnParams p)
                                     m = fmaxf(m, fmaxf(a, b));
                                 }
                                 m *= rc;
-                                // by a whole number of powers of two: exact for the bf16 weights already written
-                                const float next = m > top ? (top == kNoMax ? m : top + ceilf(m - top)) : top, shrink = exp2_approx(top - next);
+                                const float next = fmaxf(top, m), shrink = exp2_approx(top - next);
                                 top = next;
                                 sum = mul2(sum, pack2(shrink, shrink));
                                 tmem_wait_st();
-                                const uint32_t shrink_h = pack_bf16x2(shrink, shrink);
-                                for (int k = 0; k < 2 * ch; ++k) {
+                                // this tile's weights so far, and what has been summed before it
+#pragma unroll 1
+                                for (int k = 0; k < 8 + D / 16; ++k) {
+                                    if (k < 8 ? k >= 2 * ch : i == start) continue;
                                     uint32_t y[16];
-                                    tmem_load16(lanes + 16u * k, y);
+                                    const uint32_t where = lanes + 16u * k;    // columns of P, then of O
+                                    tmem_load16(where, y);
                                     tmem_wait_ld();
 #pragma unroll
-                                    for (int q = 0; q < 16; ++q) y[q] = mul_bf16x2(y[q], shrink_h);
-                                    tmem_store16(lanes + 16u * k, y);
-                                }
-                                if (i > 0) {
-                                    for (int k = 0; k < D / 16; ++k) {
-                                        uint32_t y[16];
-                                        tmem_load16(lanes + kTmemO + 16u * k, y);
-                                        tmem_wait_ld();
-#pragma unroll
-                                        for (int q = 0; q < 16; ++q) y[q] = __float_as_uint(__uint_as_float(y[q]) * shrink);
-                                        tmem_store16(lanes + kTmemO + 16u * k, y);
-                                    }
+                                    for (int q = 0; q < 16; ++q) y[q] = __float_as_uint(__uint_as_float(y[q]) * shrink);
+                                    tmem_store16(where, y);
                                 }
                                 add = weights32(v, rc2, top, ph);
                             }
@@ -689,97 +716,131 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const AttnParams p)
                     }
                     chunk_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(p_full(qt));
+                    if (lane == 0) mbar_arrive(p_full(slot));
                 }
                 if (!alive) break;
-                // ---- output ----
-                float l;
+                // ---- output: O of the slot, or of both slots under the larger M ----
+                float l, scale0 = 1.0f, scale1 = 0.0f;
                 {
                     float a, b;
                     unpack2(sum, a, b);
-                    l = a + b;
+                    l = (a + b) * kTf32Kept;
                 }
-                const bool ok = mbar_wait(o_full(qt), n_units++ & 1u, abort_flag, kv.d_status);
-                if (!(alive = __all_sync(0xFFFFFFFFu, ok))) break;
+                bool ok = mbar_wait(o_full(slot), n_units[slot] & 1u, abort_flag, kv.d_status);
+                float *stats = reinterpret_cast<float *>(smem + L::kQ + L::kQBytes);
+                if (joined) {
+                    if (slot == 0) ok = ok && mbar_wait(o_full(1), n_units[1] & 1u, abort_flag, kv.d_status);
+                    else { stats[r] = top; stats[kTile + r] = l; }
+                    if (!(alive = __all_sync(0xFFFFFFFFu, ok) && sync_both())) break;
+                    if (slot == 0) {
+                        const float top1 = stats[r], l1 = stats[kTile + r], both = fmaxf(top, top1);
+                        scale0 = exp2_approx(top - both);
+                        scale1 = exp2_approx(top1 - both);
+                        l = l * scale0 + l1 * scale1;
+                        top = both;
+                    }
+                } else if (!(alive = __all_sync(0xFFFFFFFFu, ok))) {
+                    break;
+                }
                 chunk_fence_after();
+                // 16 dimensions of the row's sum, from d on
+                auto load_o = [&](int d, uint32_t (&y)[16]) {
+                    tmem_load16(lanes + kTmemO + d, y);
+                    if (joined) {
+                        uint32_t z[16];
+                        tmem_load16(lanes + kTmemSlot + kTmemO + d, z);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int q = 0; q < 16; ++q) y[q] = __float_as_uint(fmaf(__uint_as_float(z[q]), scale1, __uint_as_float(y[q]) * scale0));
+                    } else {
+                        tmem_wait_ld();
+                    }
+                };
                 const bool mine = r < rows;
                 const int64_t out_row = s.first + tok;
-                if (lo == 0 && hi == u.steps) {
-                    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-                    uint16_t *dst = p.out + out_row * p.ld_o + (int64_t)head * D;
-                    if (active) {
-#pragma unroll 1
-                        for (int ch = 0; ch < D / 32; ++ch) {
-                            uint32_t x[32];
-                            tmem_load32(lanes + kTmemO + 32u * ch, x);
-                            tmem_wait_ld();
+                if (two || slot == 0) {
+                    if (lo == 0 && hi == u.steps) {
+                        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+                        uint16_t *dst = p.out + out_row * p.ld_o + (int64_t)head * D;
+                        if (active) {
+#pragma unroll 2
+                            for (int d = 0; d < D; d += 16) {
+                                uint32_t x[16];
+                                load_o(d, x);
+                                uint32_t y[8];
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                uint32_t y[4];
-#pragma unroll
-                                for (int q = 0; q < 4; ++q)
-                                    y[q] = pack_bf16x2(__uint_as_float(x[8 * k + 2 * q]) * inv, __uint_as_float(x[8 * k + 2 * q + 1]) * inv);
-                                if (mine) *reinterpret_cast<uint4 *>(dst + ch * 32 + k * 8) = make_uint4(y[0], y[1], y[2], y[3]);
+                                for (int q = 0; q < 8; ++q) y[q] = pack_bf16x2(__uint_as_float(x[2 * q]) * inv, __uint_as_float(x[2 * q + 1]) * inv);
+                                if (mine) {
+                                    *reinterpret_cast<uint4 *>(dst + d) = make_uint4(y[0], y[1], y[2], y[3]);
+                                    *reinterpret_cast<uint4 *>(dst + d + 8) = make_uint4(y[4], y[5], y[6], y[7]);
+                                }
+                                __syncwarp();
                             }
-                            __syncwarp();
+                            if (mine && p.lse) p.lse[out_row * p.q_heads + head] = l == 0.0f ? -INFINITY : (top + log2_approx(l * (1.0f / kTf32Kept))) * kLn2;
                         }
-                        if (mine && p.lse) p.lse[out_row * p.q_heads + head] = l == 0.0f ? -INFINITY : (top + log2_approx(l)) * kLn2;
-                    }
-                } else {
-                    // some of the unit's steps: sums and statistics to the workspace, joined in order by the last CTA
-                    const int64_t first_cta = u.first / share, last_cta = (u.first + u.steps - 1) / share;
-                    float *slot = p.part + (((int64_t)blockIdx.x * 2 + (lo == 0 ? 1 : 0)) * NQ + qt) * L::kPart;
-                    if (active) {
-#pragma unroll 1
-                        for (int ch = 0; ch < D / 32; ++ch) {
-                            uint32_t x[32];
-                            tmem_load32(lanes + kTmemO + 32u * ch, x);
-                            tmem_wait_ld();
+                    } else {
+                        // some of the unit's steps: sums and statistics to the workspace, joined in order by the last CTA
+                        const int qt = two ? slot : 0;
+                        const int64_t first_cta = u.first / share, last_cta = (u.first + u.steps - 1) / share;
+                        float *part = p.part + (((int64_t)blockIdx.x * 2 + (lo == 0 ? 1 : 0)) * 2 + qt) * L::kPart;
+                        if (active) {
+#pragma unroll 2
+                            for (int d = 0; d < D; d += 16) {
+                                uint32_t x[16];
+                                load_o(d, x);
 #pragma unroll
-                            for (int k = 0; k < 8; ++k)
-                                if (mine) *reinterpret_cast<uint4 *>(slot + r * D + ch * 32 + 4 * k) = make_uint4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
-                            __syncwarp();
+                                for (int k = 0; k < 4; ++k)
+                                    if (mine) *reinterpret_cast<uint4 *>(part + r * D + d + 4 * k) = make_uint4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
+                                __syncwarp();
+                            }
+                            if (mine) { part[kTile * D + r] = top; part[kTile * D + kTile + r] = l; }
                         }
-                        if (mine) { slot[kTile * D + r] = top; slot[kTile * D + kTile + r] = l; }
-                    }
-                    __threadfence();
-                    asm volatile("bar.sync %0, 128;" ::"r"(1 + qt) : "memory");
-                    if (r == 0) is_last[qt] = atomicAdd(p.count + first_cta * NQ + qt, 1u) == (unsigned)(last_cta - first_cta);
-                    asm volatile("bar.sync %0, 128;" ::"r"(1 + qt) : "memory");
-                    if (is_last[qt]) {
                         __threadfence();
-                        if (r == 0) p.count[first_cta * NQ + qt] = 0u;
-                        // the first part lies in its CTA's slot 1 (it starts at the unit's beginning), the others in slot 0
-                        auto part_of = [&](int64_t cta) { return p.part + ((cta * 2 + (cta == first_cta ? 1 : 0)) * NQ + qt) * L::kPart; };
-                        constexpr int kPerRow = D / 4;           // lanes side by side along a row
-                        for (int rr = r / kPerRow; rr < min(rows, kTile); rr += 128 / kPerRow) {
-                            const int d = r % kPerRow * 4;
-                            float m = kNoMax;
-                            for (int64_t k = first_cta; k <= last_cta; ++k) m = fmaxf(m, __ldcg(part_of(k) + kTile * D + rr));
-                            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                            float sum_l = 0.0f;
-                            for (int64_t k = first_cta; k <= last_cta; ++k) {
-                                const float *src = part_of(k);
-                                const float f = exp2_approx(__ldcg(src + kTile * D + rr) - m);
-                                const float4 y = __ldcg(reinterpret_cast<const float4 *>(src + rr * D + d));
-                                v.x = fmaf(y.x, f, v.x); v.y = fmaf(y.y, f, v.y); v.z = fmaf(y.z, f, v.z); v.w = fmaf(y.w, f, v.w);
-                                sum_l = fmaf(__ldcg(src + kTile * D + kTile + rr), f, sum_l);
+                        if (!(alive = sync_slot())) break;
+                        if (r == 0) is_last[slot] = atomicAdd(p.count + first_cta * 2 + qt, 1u) == (unsigned)(last_cta - first_cta);
+                        if (!(alive = sync_slot())) break;
+                        if (is_last[slot]) {
+                            __threadfence();
+                            if (r == 0) p.count[first_cta * 2 + qt] = 0u;
+                            // the first part lies in its CTA's place 1 (it starts at the unit's beginning), the others in place 0
+                            auto part_of = [&](int64_t cta) { return p.part + ((cta * 2 + (cta == first_cta ? 1 : 0)) * 2 + qt) * L::kPart; };
+                            constexpr int kPerRow = D / 4;           // lanes side by side along a row
+                            for (int rr = r / kPerRow; rr < min(rows, kTile); rr += 128 / kPerRow) {
+                                const int d = r % kPerRow * 4;
+                                float m = kNoMax;
+                                for (int64_t k = first_cta; k <= last_cta; ++k) m = fmaxf(m, __ldcg(part_of(k) + kTile * D + rr));
+                                float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                                float sum_l = 0.0f;
+                                for (int64_t k = first_cta; k <= last_cta; ++k) {
+                                    const float *src = part_of(k);
+                                    const float f = exp2_approx(__ldcg(src + kTile * D + rr) - m);
+                                    const float4 y = __ldcg(reinterpret_cast<const float4 *>(src + rr * D + d));
+                                    v.x = fmaf(y.x, f, v.x); v.y = fmaf(y.y, f, v.y); v.z = fmaf(y.z, f, v.z); v.w = fmaf(y.w, f, v.w);
+                                    sum_l = fmaf(__ldcg(src + kTile * D + kTile + rr), f, sum_l);
+                                }
+                                const float inv = sum_l == 0.0f ? 0.0f : 1.0f / sum_l;
+                                const int64_t orow = s.first + (row0 + rr) / p.group;
+                                const int hd = u.h * p.group + (row0 + rr) % p.group;
+                                *reinterpret_cast<uint2 *>(p.out + orow * p.ld_o + (int64_t)hd * D + d) =
+                                    make_uint2(pack_bf16x2(v.x * inv, v.y * inv), pack_bf16x2(v.z * inv, v.w * inv));
+                                if (p.lse && d == 0)
+                                    p.lse[orow * p.q_heads + hd] = sum_l == 0.0f ? -INFINITY : (m + log2_approx(sum_l * (1.0f / kTf32Kept))) * kLn2;
                             }
-                            const float inv = sum_l == 0.0f ? 0.0f : 1.0f / sum_l;
-                            const int64_t orow = s.first + (row0 + rr) / p.group;
-                            const int hd = u.h * p.group + (row0 + rr) % p.group;
-                            *reinterpret_cast<uint2 *>(p.out + orow * p.ld_o + (int64_t)hd * D + d) =
-                                make_uint2(pack_bf16x2(v.x * inv, v.y * inv), pack_bf16x2(v.z * inv, v.w * inv));
-                            if (p.lse && d == 0)
-                                p.lse[orow * p.q_heads + hd] = sum_l == 0.0f ? -INFINITY : (m + log2_approx(sum_l)) * kLn2;
                         }
                     }
                 }
+                if (joined) {         // the odd slot's sums have been read
+                    chunk_fence_before();
+                    if (!(alive = sync_both())) break;
+                    chunk_fence_after();
+                }
             }
+            ++n_units[0];
+            if (two || joined) ++n_units[1];
             g0 += steps;
             at += steps;
             if (at >= end) break;
-            next_unit<NQ>(p, u);
+            next_unit(p, u);
         }
     }
 
@@ -790,7 +851,7 @@ attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const AttnParams p)
     __syncthreads();
     chunk_fence_after();
     if (warp == kProductWarp)
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(L::kTmemCols) : "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
 }
 
 // Map over the keys: [pages][kv_heads * page_size][D] bytes, one box = one head's tokens of one page.
@@ -805,46 +866,37 @@ static bool encode_keys(const fp8_ctx *ctx, CUtensorMap *map, const fp8_kv_cache
                              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D, int NQ>
-static cudaError_t configure_chunk()
-{
-    return cudaFuncSetAttribute(attn_chunk_kernel<D, NQ>, cudaFuncAttributeMaxDynamicSharedMemorySize, ChunkShape<D, NQ>::kDynamic);
-}
 cudaError_t configure_attn_kernels()
 {
-    cudaError_t e = configure_chunk<128, 1>();
-    if (e == cudaSuccess) e = configure_chunk<128, 2>();
-    if (e == cudaSuccess) e = configure_chunk<64, 1>();
-    if (e == cudaSuccess) e = configure_chunk<64, 2>();
-    return e;
+    const cudaError_t e = cudaFuncSetAttribute(attn_chunk_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, ChunkShape<128>::kDynamic);
+    if (e != cudaSuccess) return e;
+    return cudaFuncSetAttribute(attn_chunk_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, ChunkShape<64>::kDynamic);
 }
 
-template <int D, int NQ>
+template <int D>
 static fp8_status_t launch_chunk(const fp8_ctx *ctx, AttnParams p, const fp8_kv_cache_t *c, cudaStream_t st)
 {
-    using L = ChunkShape<D, NQ>;
+    using L = ChunkShape<D>;
     const KvParams &kv = p.kv;
-    const int64_t row_tiles = ((int64_t)kv.max_q_len * p.group + NQ * kTile - 1) / (NQ * kTile);
+    const int64_t row_tiles = ((int64_t)kv.max_q_len * p.group + kUnitRows - 1) / kUnitRows;
     const int64_t units = row_tiles * kv.seqs * kv.kv_heads, longest = ((int64_t)kv.max_kv_len + kTile - 1) / kTile;
     if (row_tiles * kv.seqs > INT32_MAX) return FP8_ERR_SHAPE;
     p.row_tiles = (int)row_tiles;
-    // a CTA's share is at least four steps (see attn_chunk_kernel: shares below that spend more on joining than they save)
-    p.min_share = 4;
-    int64_t grid = (int64_t)ctx->sm_count * L::kResident;
+    p.min_share = 4;      // steps: shorter shares spend more on starting and joining than they save
+    int64_t grid = ctx->sm_count;
     const int64_t most = (units * longest + p.min_share - 1) / p.min_share;
     if (most < grid) grid = most;
-    if (grid * NQ > kAttnCounters || grid * 2 * NQ * L::kPart * 4 > (int64_t)ctx->partial_bytes) return FP8_ERR_UNSUPPORTED;
+    if (grid * 2 > kAttnCounters || grid * 4 * L::kPart * 4 > (int64_t)ctx->partial_bytes) return FP8_ERR_UNSUPPORTED;
     CUtensorMap map;
     if (!encode_keys(ctx, &map, c)) return FP8_ERR_CUDA;
     count_launch();
-    attn_chunk_kernel<D, NQ><<<(unsigned)grid, L::kThreads, L::kDynamic, st>>>(map, p);
+    attn_chunk_kernel<D><<<(unsigned)grid, kChunkThreads, L::kDynamic, st>>>(map, p);
     return cudaGetLastError() == cudaSuccess ? FP8_OK : FP8_ERR_CUDA;
 }
 
-fp8_status_t attn_chunk(const fp8_ctx *ctx, const AttnParams &p, const fp8_kv_cache_t *c, int64_t rows, cudaStream_t st)
+fp8_status_t attn_chunk(const fp8_ctx *ctx, const AttnParams &p, const fp8_kv_cache_t *c, cudaStream_t st)
 {
-    if (c->head_dim == 128) return rows <= kTile ? launch_chunk<128, 1>(ctx, p, c, st) : launch_chunk<128, 2>(ctx, p, c, st);
-    return rows <= kTile ? launch_chunk<64, 1>(ctx, p, c, st) : launch_chunk<64, 2>(ctx, p, c, st);
+    return c->head_dim == 128 ? launch_chunk<128>(ctx, p, c, st) : launch_chunk<64>(ctx, p, c, st);
 }
 
 }  // namespace fp8lin
