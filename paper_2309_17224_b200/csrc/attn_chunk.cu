@@ -26,7 +26,7 @@
 // by the CTA that arrives last.
 //
 // Warps: 0-3 and 4-7 softmax of the two slots (one query row per thread) and output, 8-11 values, key loads and scaling
-// biases, 12 the products (13-15 only complete a warpgroup, whose registers the softmax takes).
+// biases, 12 the products.
 #include "attn_common.cuh"
 #include "ptx.cuh"
 
@@ -36,10 +36,7 @@ constexpr int kTile = 128;                 // query rows of a tile, and tokens o
 constexpr int kKStages = 2;
 
 constexpr int kVStages = 2;
-constexpr int kChunkThreads = 512;
-// Registers per thread of the four warpgroups (softmax, softmax, values, products): 152 + 152 + 112 + 96 = 4 x 128, what
-// the block is launched with.
-constexpr int kSoftmaxRegs = 152, kValueRegs = 112, kProductRegs = 96;
+constexpr int kChunkThreads = 32 * 13;
 constexpr int kUnitRows = 2 * kTile;
 
 template <int D>
@@ -154,11 +151,6 @@ __device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b)
     f32x2 r;
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
-}
-// Two pairs of floats from shared memory (the same address in all lanes: one wavefront).
-__device__ __forceinline__ void lds_pairs(uint32_t addr, f32x2 &a, f32x2 &b)
-{
-    asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(a), "=l"(b) : "r"(addr));
 }
 __device__ __forceinline__ void sts4(uint32_t addr, float v)
 {
@@ -275,23 +267,43 @@ __device__ __forceinline__ void next_unit(const AttnParams &p, ChunkUnit &u)
     } while (u.steps == 0);
 }
 
-// The weights of 32 tokens for one row, p = 2^(rc u - M), and their sum.
-__device__ __forceinline__ f32x2 weights32(const f32x2 (&u)[16], f32x2 rc2, float top, uint32_t (&ph)[32])
+// One row's scores for kSpan tokens of a step as they came from tensor memory, times the keys' factors: u = 2^-b (q . K8),
+// s = rc u; -infinity for tokens j0 .. that the row does not see (limit).
+constexpr int kSpan = 32;
+__device__ __forceinline__ void scores_of_row(const uint32_t (&x)[kSpan], const float *factors, bool mask, int j0, int limit, f32x2 (&u)[kSpan / 2])
+{
+    const ulonglong2 *f = reinterpret_cast<const ulonglong2 *>(factors);     // the same address in all lanes
+#pragma unroll
+    for (int k = 0; k < kSpan / 2; k += 2) {
+        const ulonglong2 f4 = f[k / 2];
+        u[k] = mul2(pack2(__uint_as_float(x[2 * k]), __uint_as_float(x[2 * k + 1])), f4.x);
+        u[k + 1] = mul2(pack2(__uint_as_float(x[2 * k + 2]), __uint_as_float(x[2 * k + 3])), f4.y);
+    }
+    if (__builtin_expect(mask, 0)) {
+#pragma unroll
+        for (int k = 0; k < kSpan / 2; ++k) {
+            float lo, hi;
+            unpack2(u[k], lo, hi);
+            if (j0 + 2 * k >= limit) lo = -INFINITY;
+            if (j0 + 2 * k + 1 >= limit) hi = -INFINITY;
+            u[k] = pack2(lo, hi);
+        }
+    }
+}
+
+// u becomes the weights p = 2^(rc u - M); their sum.
+__device__ __forceinline__ f32x2 weights_of_row(f32x2 (&u)[kSpan / 2], f32x2 rc2, float top)
 {
     const f32x2 minus = pack2(-top, -top);
-    f32x2 s0 = pack2(0.0f, 0.0f), s1 = s0;
+    f32x2 s[4];
 #pragma unroll
-    for (int k = 0; k < 16; ++k) {
+    for (int k = 0; k < kSpan / 2; ++k) {
         float lo, hi;
         unpack2(fma2(u[k], rc2, minus), lo, hi);
-        lo = exp2_approx(lo);
-        hi = exp2_approx(hi);
-        ph[2 * k] = __float_as_uint(lo);
-        ph[2 * k + 1] = __float_as_uint(hi);
-        if (k & 1) s1 = add2(s1, pack2(lo, hi));
-        else s0 = add2(s0, pack2(lo, hi));
+        u[k] = pack2(exp2_approx(lo), exp2_approx(hi));
+        s[k & 3] = k < 4 ? u[k] : add2(s[k & 3], u[k]);
     }
-    return add2(s0, s1);
+    return add2(add2(s[0], s[1]), add2(s[2], s[3]));
 }
 
 template <int D>
@@ -362,8 +374,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
     uint32_t g0 = 0;          // steps of this CTA before the current unit
     bool alive = true;
 
-    if (warp >= kProductWarp) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kProductRegs));
+    if (warp == kProductWarp) {
         // ------------------------------- products -------------------------------
         const uint32_t idesc_s = (1u << 4) | ((uint32_t)(kTile >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);                       // e4m3
         const uint32_t idesc_o = (1u << 4) | (2u << 7) | (2u << 10) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);   // tf32
@@ -388,7 +399,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
             for (int k = 0; k < kTile / 8; ++k)      // eight tokens: 32 bytes of a block's rows, D * 128 bytes from block to block
                 chunk_mma_tf32_tmem(slot + kTmemO, slot + 8u * k, dv + (uint32_t)(k >> 2) * (D * 128 / 16) + 2u * (k & 3), idesc_o, first && k == 0 ? 0u : 1u);
         };
-        if (warp == kProductWarp && lane == 0) {
+        if (lane == 0) {
             while (true) {
                 const int lo = (int)(at - u.first), steps = (int)min((int64_t)u.steps, end - u.first) - lo;
                 const bool two = u.rows > kTile;           // two query tiles; else even and odd steps
@@ -442,7 +453,6 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
             }
         }
     } else if (warp >= kFirstValueWarp) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kValueRegs));
         // ------------------------------- values, keys' loads, scaling biases -------------------------------
         // A warp takes 32 tokens of each tile, a lane one token's row: 32 lanes store one dimension of their tokens side
         // by side (all banks once).  Shared memory: four blocks of 32 tokens, [D][32 tokens], 128-byte rows, swizzled.
@@ -564,7 +574,6 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
         }
         if (bad_pages) raise_flags(kv.d_status, FP8_FLAG_BAD_INDEX);
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
         // ------------------------------- softmax and output -------------------------------
         const int slot = warp >> 2, r = threadIdx.x & 127;                     // slot, row of the query tile
         const uint32_t quarter = (uint32_t)((warp & 3) * 32) << 16, lanes = tmem + kTmemSlot * slot + quarter;
@@ -650,44 +659,26 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
                     if (!(alive = __all_sync(0xFFFFFFFFu, ok))) break;
                     chunk_fence_after();
                     if (active) {
-                        const uint32_t sc = base + L::kScale + (g & 1u) * (kTile * 4);
+                        const float *factors = reinterpret_cast<const float *>(smem + L::kScale) + (g & 1u) * kTile;
                         const bool mask = t0 + kTile > least;
-#pragma unroll 1
-                        for (int ch = 0; ch < 4; ++ch) {
-                            uint32_t x[32];
-                            tmem_load32(lanes + 32u * ch, x);
+                        auto span = [&](uint32_t (&x)[kSpan], int c0) {
+                            f32x2 w[kSpan / 2];
                             tmem_wait_ld();
-                            // v = 2^-b (q . K8), s = rc v
-                            f32x2 v[16];
-#pragma unroll
-                            for (int k = 0; k < 16; k += 2) {
-                                f32x2 f0, f1;
-                                lds_pairs(sc + (ch * 32 + 2 * k) * 4, f0, f1);
-                                v[k] = mul2(pack2(__uint_as_float(x[2 * k]), __uint_as_float(x[2 * k + 1])), f0);
-                                v[k + 1] = mul2(pack2(__uint_as_float(x[2 * k + 2]), __uint_as_float(x[2 * k + 3])), f1);
-                            }
-                            if (__builtin_expect(mask, 0)) {
-#pragma unroll
-                                for (int k = 0; k < 16; ++k) {
-                                    float a, b;
-                                    unpack2(v[k], a, b);
-                                    const int j = t0 + ch * 32 + 2 * k;
-                                    if (j >= limit) a = -INFINITY;
-                                    if (j + 1 >= limit) b = -INFINITY;
-                                    v[k] = pack2(a, b);
-                                }
-                            }
+                            scores_of_row(x, factors + c0, mask, t0 + c0, limit, w);
                             // weights under M as it stands; only where their sum shows that a score lies far above M (or
                             // at the first token) is the maximum looked at, M moved and the weights taken again
-                            uint32_t ph[32];
-                            f32x2 add = weights32(v, rc2, top, ph);
+                            f32x2 add = weights_of_row(w, rc2, top);
                             float a, b;
                             unpack2(add2(sum, add), a, b);
                             if (__builtin_expect(__any_sync(0xFFFFFFFFu, a + b > kSumLimit), 0)) {
+                                uint32_t z[kSpan];
+                                tmem_load32(lanes + c0, z);
+                                tmem_wait_ld();
+                                scores_of_row(z, factors + c0, mask, t0 + c0, limit, w);
                                 float m = -INFINITY;
 #pragma unroll
-                                for (int k = 0; k < 16; ++k) {
-                                    unpack2(v[k], a, b);
+                                for (int k = 0; k < kSpan / 2; ++k) {
+                                    unpack2(w[k], a, b);
                                     m = fmaxf(m, fmaxf(a, b));
                                 }
                                 m *= rc;
@@ -695,10 +686,10 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
                                 top = next;
                                 sum = mul2(sum, pack2(shrink, shrink));
                                 tmem_wait_st();
-                                // this tile's weights so far, and what has been summed before it
+                                // this step's weights so far, and what has been summed before it
 #pragma unroll 1
                                 for (int k = 0; k < 8 + D / 16; ++k) {
-                                    if (k < 8 ? k >= 2 * ch : i == start) continue;
+                                    if (k < 8 ? 16 * k >= c0 : i == start) continue;
                                     uint32_t y[16];
                                     const uint32_t where = lanes + 16u * k;    // columns of P, then of O
                                     tmem_load16(where, y);
@@ -707,10 +698,23 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
                                     for (int q = 0; q < 16; ++q) y[q] = __float_as_uint(__uint_as_float(y[q]) * shrink);
                                     tmem_store16(where, y);
                                 }
-                                add = weights32(v, rc2, top, ph);
+                                add = weights_of_row(w, rc2, top);
                             }
                             sum = add2(sum, add);
-                            tmem_store32(lanes + 32u * ch, ph);
+                            uint32_t y[kSpan];
+#pragma unroll
+                            for (int k = 0; k < kSpan / 2; ++k) {
+                                unpack2(w[k], a, b);
+                                y[2 * k] = __float_as_uint(a);
+                                y[2 * k + 1] = __float_as_uint(b);
+                            }
+                            tmem_store32(lanes + c0, y);
+                        };
+#pragma unroll 1
+                        for (int c0 = 0; c0 < kTile; c0 += kSpan) {
+                            uint32_t x[kSpan];
+                            tmem_load32(lanes + c0, x);
+                            span(x, c0);
                         }
                         tmem_wait_st();
                     }
