@@ -809,26 +809,40 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
                             // the first part lies in its CTA's place 1 (it starts at the unit's beginning), the others in place 0
                             auto part_of = [&](int64_t cta) { return p.part + ((cta * 2 + (cta == first_cta ? 1 : 0)) * 2 + qt) * L::kPart; };
                             constexpr int kPerRow = D / 4;           // lanes side by side along a row
-                            for (int rr = r / kPerRow; rr < min(rows, kTile); rr += 128 / kPerRow) {
-                                const int d = r % kPerRow * 4;
-                                float m = kNoMax;
-                                for (int64_t k = first_cta; k <= last_cta; ++k) m = fmaxf(m, __ldcg(part_of(k) + kTile * D + rr));
-                                float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                                float sum_l = 0.0f;
-                                for (int64_t k = first_cta; k <= last_cta; ++k) {
-                                    const float *src = part_of(k);
-                                    const float f = exp2_approx(__ldcg(src + kTile * D + rr) - m);
-                                    const float4 y = __ldcg(reinterpret_cast<const float4 *>(src + rr * D + d));
-                                    v.x = fmaf(y.x, f, v.x); v.y = fmaf(y.y, f, v.y); v.z = fmaf(y.z, f, v.z); v.w = fmaf(y.w, f, v.w);
-                                    sum_l = fmaf(__ldcg(src + kTile * D + kTile + rr), f, sum_l);
+                            // eight rows' loads at a time: their latency is what this costs
+                            constexpr int kStep = 128 / kPerRow, kBatch = 8;
+                            const int d = r % kPerRow * 4, most = min(rows, kTile);
+                            for (int r0 = r / kPerRow; r0 < most; r0 += kBatch * kStep) {
+                                JoinedRow joint[kBatch];
+#pragma unroll
+                                for (int k = 0; k < kBatch; ++k) join_start(joint[k]);
+                                for (int64_t cta = first_cta; cta <= last_cta; ++cta) {
+                                    const float *src = part_of(cta);
+                                    float m[kBatch], l_part[kBatch];
+                                    float4 y[kBatch];
+#pragma unroll
+                                    for (int k = 0; k < kBatch; ++k) {
+                                        const int rr = min(r0 + k * kStep, most - 1);
+                                        m[k] = __ldcg(src + kTile * D + rr);
+                                        l_part[k] = __ldcg(src + kTile * D + kTile + rr);
+                                        y[k] = __ldcg(reinterpret_cast<const float4 *>(src + rr * D + d));
+                                    }
+#pragma unroll
+                                    for (int k = 0; k < kBatch; ++k) join_part(joint[k], m[k], l_part[k], y[k]);
                                 }
-                                const float inv = sum_l == 0.0f ? 0.0f : 1.0f / sum_l;
-                                const int64_t orow = s.first + (row0 + rr) / p.group;
-                                const int hd = u.h * p.group + (row0 + rr) % p.group;
-                                *reinterpret_cast<uint2 *>(p.out + orow * p.ld_o + (int64_t)hd * D + d) =
-                                    make_uint2(pack_bf16x2(v.x * inv, v.y * inv), pack_bf16x2(v.z * inv, v.w * inv));
-                                if (p.lse && d == 0)
-                                    p.lse[orow * p.q_heads + hd] = sum_l == 0.0f ? -INFINITY : (m + log2_approx(sum_l * (1.0f / kTf32Kept))) * kLn2;
+#pragma unroll
+                                for (int k = 0; k < kBatch; ++k) {
+                                    const int rr = r0 + k * kStep;
+                                    if (rr >= most) break;
+                                    const JoinedRow &a = joint[k];
+                                    const float inv = a.l == 0.0f ? 0.0f : 1.0f / a.l;
+                                    const int64_t orow = s.first + (row0 + rr) / p.group;
+                                    const int hd = u.h * p.group + (row0 + rr) % p.group;
+                                    *reinterpret_cast<uint2 *>(p.out + orow * p.ld_o + (int64_t)hd * D + d) =
+                                        make_uint2(pack_bf16x2(a.v.x * inv, a.v.y * inv), pack_bf16x2(a.v.z * inv, a.v.w * inv));
+                                    if (p.lse && d == 0)
+                                        p.lse[orow * p.q_heads + hd] = a.l == 0.0f ? -INFINITY : (a.m + log2_approx(a.l * (1.0f / kTf32Kept))) * kLn2;
+                                }
                             }
                         }
                     }

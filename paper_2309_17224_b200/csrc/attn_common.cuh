@@ -105,6 +105,28 @@ __device__ __forceinline__ void split_bf16(float a, float b, uint32_t &p1, uint3
     p2 = pack_bf16x2(a - __uint_as_float(__float_as_uint(a) & 0xFFFF0000u), b - __uint_as_float(__float_as_uint(b) & 0xFFFF0000u));
 }
 
+// Four dimensions of a row's sum under the running M of the parts joined so far.
+struct JoinedRow {
+    float4 v;
+    float m, l;
+};
+__device__ __forceinline__ void join_start(JoinedRow &a)
+{
+    a.v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    a.m = kNoMax;
+    a.l = 0.0f;
+}
+__device__ __forceinline__ void join_part(JoinedRow &a, float m, float l, float4 y)
+{
+    const float top = fmaxf(a.m, m), f = exp2_approx(a.m - top), g = exp2_approx(m - top);
+    a.v.x = fmaf(y.x, g, a.v.x * f);
+    a.v.y = fmaf(y.y, g, a.v.y * f);
+    a.v.z = fmaf(y.z, g, a.v.z * f);
+    a.v.w = fmaf(y.w, g, a.v.w * f);
+    a.l = fmaf(l, g, a.l * f);
+    a.m = top;
+}
+
 // A sequence's lengths, cut to the bounds of the launch.
 struct SeqShape {
     int first, n, len;

@@ -94,7 +94,7 @@ struct Unit {
 __device__ __forceinline__ int unit_blocks(const SeqShape &s) { return s.n > 0 ? max(1, (s.len + kBlockTokens - 1) / kBlockTokens) : 0; }
 
 template <int D, int NT>
-__global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 3 : 2) attn_decode_kernel(const AttnParams p)
+__global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 4 : 2) attn_decode_kernel(const AttnParams p)
 {
     constexpr int kRows = 8 * NT;
     constexpr int kPart = kRows * (D + 2);       // floats of a partial result
@@ -228,7 +228,7 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 3 : 2) attn_decode_k
             const int blk = lo + warp + (i0 + lane) * kDecodeWarps;
             pages = i0 + lane < count ? __ldg(table + (blk >> blocks_per_page_shift)) : 0;
         };
-        int64_t v_at[2];
+        int64_t v_at;
         auto request_k = [&](KvBlock<D> &x, int i, int64_t &v_off) {
             if ((i & 31) == 0) fetch_pages(i);
             const int page = __shfl_sync(0xFFFFFFFFu, pages, i & 31);
@@ -240,11 +240,10 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 3 : 2) attn_decode_k
             const int64_t b_off = pg * kv.bias_stride + row;
             load_k<D>(x, kv.k8 + v_off, kv.bk + b_off, kv.bv + b_off, g, t);
         };
-        KvBlock<D> x[2];
-        if (count > 0) { request_k(x[0], 0, v_at[0]); load_v<D>(x[0], kv.v8 + v_at[0], g, t); }
-        if (count > 1) { request_k(x[1], 1, v_at[1]); load_v<D>(x[1], kv.v8 + v_at[1], g, t); }
+        KvBlock<D> cur;
+        if (count > 0) { request_k(cur, 0, v_at); load_v<D>(cur, kv.v8 + v_at, g, t); }
 
-        auto step = [&](KvBlock<D> &cur, int64_t &v_off, int i) {
+        for (int i = 0; i < count; ++i) {
             const int j0 = (lo + warp + i * kDecodeWarps) * kBlockTokens;
             // S^T
             float s[NT][4];
@@ -264,8 +263,8 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 3 : 2) attn_decode_k
             int bk[2] = {cur.bk[0], cur.bk[1]}, bv[2] = {cur.bv[0], cur.bv[1]};
             if (cur.bad) bk[0] = bk[1] = bv[0] = bv[1] = FP8_KV_BIAS_NONFINITE;
             const int bad = cur.bad;
-            // the registers of K are free: the block after next
-            if (i + 2 < count) request_k(cur, i + 2, v_off);
+            // the registers of K are free: the next block's
+            if (i + 1 < count) request_k(cur, i + 1, v_at);
             if (bad && lane == 0) raise_flags(kv.d_status, FP8_FLAG_BAD_INDEX);
             const bool marked0 = bk[0] == FP8_KV_BIAS_NONFINITE || bv[0] == FP8_KV_BIAS_NONFINITE;
             const bool marked1 = bk[1] == FP8_KV_BIAS_NONFINITE || bv[1] == FP8_KV_BIAS_NONFINITE;
@@ -369,13 +368,8 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 3 : 2) attn_decode_k
                     mma_bf16(o[j][m], a[0], a[1], a[2], a[3], pt[j][1][0], pt[j][1][1]);
                 }
             }
-            if (i + 2 < count) load_v<D>(cur, kv.v8 + v_off, g, t);
-        };
-        for (int i = 0; i < count; i += 2) {
-            step(x[0], v_at[0], i);
-            if (i + 1 < count) step(x[1], v_at[1], i + 1);
+            if (i + 1 < count) load_v<D>(cur, kv.v8 + v_at, g, t);
         }
-
         // ---- join the warps ----
         __syncthreads();   // the previous unit's sums have been read
 #pragma unroll
@@ -438,22 +432,37 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 3 : 2) attn_decode_k
                 if (threadIdx.x == 0) p.count[first_cta] = 0u;
                 // the first part lies in its CTA's slot 1 (it starts at the unit's beginning), the others in slot 0
                 auto part_of = [&](int64_t c) { return p.part + (c * 2 + (c == first_cta ? 1 : 0)) * kPart; };
-                for (int idx = threadIdx.x; idx < kRows * (D / 4); idx += kDecodeThreads) {
-                    const int r = idx / (D / 4), d = idx % (D / 4) * 4;
-                    if (r >= rows) break;
-                    float m = kNoMax;
-                    for (int64_t c = first_cta; c <= last_cta; ++c) m = fmaxf(m, __ldcg(part_of(c) + kRows * D + r));
-                    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                    float sum = 0.0f;
-                    for (int64_t c = first_cta; c <= last_cta; ++c) {
-                        const float *src = part_of(c);
-                        const float f = exp2_approx(__ldcg(src + kRows * D + r) - m);
-                        const float4 y = __ldcg(reinterpret_cast<const float4 *>(src + r * D + d));
-                        v.x = fmaf(y.x, f, v.x); v.y = fmaf(y.y, f, v.y); v.z = fmaf(y.z, f, v.z); v.w = fmaf(y.w, f, v.w);
-                        sum = fmaf(__ldcg(src + kRows * D + kRows + r), f, sum);
+                // all of a thread's rows at once and four parts' loads at a time: the loads' latency is what this costs
+                constexpr int kItems = kRows * (D / 4) / kDecodeThreads;
+                const int d = threadIdx.x % (D / 4) * 4, r0 = threadIdx.x / (D / 4);
+                constexpr int kStep = kDecodeThreads / (D / 4);
+                JoinedRow sum[kItems];
+#pragma unroll
+                for (int k = 0; k < kItems; ++k) join_start(sum[k]);
+                for (int64_t c0 = first_cta; c0 <= last_cta; c0 += 4) {
+                    float m[4][kItems], l_part[4][kItems];
+                    float4 y[4][kItems];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const float *src = part_of(min(c0 + c, last_cta));
+#pragma unroll
+                        for (int k = 0; k < kItems; ++k) {
+                            const int r = min(r0 + k * kStep, rows - 1);
+                            m[c][k] = __ldcg(src + kRows * D + r);
+                            l_part[c][k] = __ldcg(src + kRows * D + kRows + r);
+                            y[c][k] = __ldcg(reinterpret_cast<const float4 *>(src + r * D + d));
+                        }
                     }
-                    store_row(r, d, v, m, sum);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        if (c0 + c <= last_cta) {
+#pragma unroll
+                            for (int k = 0; k < kItems; ++k) join_part(sum[k], m[c][k], l_part[c][k], y[c][k]);
+                        }
                 }
+#pragma unroll
+                for (int k = 0; k < kItems; ++k)
+                    if (r0 + k * kStep < rows) store_row(r0 + k * kStep, d, sum[k].v, sum[k].m, sum[k].l);
             }
         }
 
@@ -479,7 +488,7 @@ static fp8_status_t launch_decode(const fp8_ctx *ctx, const AttnParams &p, cudaS
     const KvParams &kv = p.kv;
     // an upper bound of the list's length; CTAs beyond the blocks that there are leave at once
     const int64_t blocks = (int64_t)kv.seqs * kv.kv_heads * ((kv.max_kv_len + kBlockTokens - 1) / kBlockTokens);
-    int64_t grid = (int64_t)ctx->sm_count * (NT == 1 ? 3 : 2);
+    int64_t grid = (int64_t)ctx->sm_count * (NT == 1 ? 4 : 2);
     if ((blocks + kDecodeWarps - 1) / kDecodeWarps < grid) grid = (blocks + kDecodeWarps - 1) / kDecodeWarps;
     if (grid > kAttnCounters) return FP8_ERR_UNSUPPORTED;
     count_launch();
