@@ -151,6 +151,11 @@ def _stream():
     return c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
+def _raw_stream(device):
+    """The current stream's handle without the stream object (calls of a few microseconds notice the difference)."""
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
 _DT = {torch.bfloat16: BF16, torch.float16: F16, torch.float32: F32}
 
 
@@ -210,6 +215,7 @@ class KvCache:
         if _page_stride(k8) != _page_stride(v8) or _page_stride(bk) != _page_stride(bv):
             raise ValueError("k8 and v8, bk and bv have their pages equally far apart")
         self.k8, self.v8, self.bk, self.bv, self.conv = k8, v8, bk, bv, conv
+        self.kv_heads, self.head_dim = heads, dim
         self._desc = KvCacheDesc(k8.data_ptr(), v8.data_ptr(), bk.data_ptr(), bv.data_ptr(), _page_stride(k8),
                                  _page_stride(bk), pages, heads, size, dim)
         self._ref = byref(self._desc)
@@ -239,10 +245,11 @@ class SeqBatch:
 
 def _rows3(t, heads, dim, what):
     """Check a [tokens, heads, head_dim] tensor whose heads are contiguous; its row distance in elements."""
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim or t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim):
-        raise ValueError(f"{what}: [tokens, {heads}, {dim}] with contiguous heads expected, got {tuple(t.shape)} "
-                         f"strides {t.stride()}")
-    return t.stride(0) if t.shape[0] > 1 else heads * dim
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[1] != heads or shape[2] != dim or stride[2] != 1 or (heads > 1 and stride[1] != dim):
+        raise ValueError(f"{what}: [tokens, {heads}, {dim}] with contiguous heads expected, got {tuple(shape)} "
+                         f"strides {stride}")
+    return stride[0] if shape[0] > 1 else heads * dim
 
 
 MATMUL_FWD, MATMUL_DGRAD, MATMUL_WGRAD = 0, 1, 2
@@ -496,16 +503,19 @@ class Context:
 
     # -- paged FP8 cache ----------------------------------------------------------
     def _kv(self, fn, name, cache, batch, k, v):
-        d = cache._desc
         some = k if k is not None else v
         if some is None:
             raise ValueError("keys, values or both")
-        ld_k = _rows3(k, d.kv_heads, d.head_dim, "keys") if k is not None else 0
-        ld_v = _rows3(v, d.kv_heads, d.head_dim, "values") if v is not None else 0
-        if k is not None and v is not None and (k.dtype != v.dtype or k.shape != v.shape):
+        heads, dim = cache.kv_heads, cache.head_dim
+        ld_k = _rows3(k, heads, dim, "keys") if k is not None else 0
+        ld_v = _rows3(v, heads, dim, "values") if v is not None else 0
+        if k is not None and v is not None and (k.dtype != v.dtype or k.shape[0] != v.shape[0]):
             raise ValueError("keys and values of one shape and type")
         batch._desc.tokens = some.shape[0]
-        _check(fn(self._h, cache._ref, batch._ref, _ptr(k), _ptr(v), _DT[some.dtype], ld_k, ld_v, cache.conv, _stream()), name)
+        status = fn(self._h, cache._ref, batch._ref, None if k is None else k.data_ptr(), None if v is None else v.data_ptr(),
+                    _DT[some.dtype], ld_k, ld_v, cache.conv, _raw_stream(self.device))
+        if status:
+            _check(status, name)
 
     def kv_append(self, cache, batch, k, v):
         """``fp8_kv_append``: quantise the new tokens' keys and values, [tokens, kv_heads, head_dim], into the cache."""
@@ -518,17 +528,22 @@ class Context:
     def attn_paged(self, cache, batch, q, out, scale=None, causal=True, lse=None):
         """``fp8_attn_paged``: q, out [tokens, q_heads, head_dim] bf16, lse float32 [tokens, q_heads] or None; scale
         1 / sqrt(head_dim) by default."""
-        d = cache._desc
-        heads, dim = q.shape[1], d.head_dim
+        shape, dim = q.shape, cache.head_dim
+        heads = shape[1]
         ld_q, ld_o = _rows3(q, heads, dim, "q"), _rows3(out, heads, dim, "out")
-        if q.dtype != torch.bfloat16 or out.dtype != torch.bfloat16 or out.shape != q.shape:
+        if q.dtype != torch.bfloat16 or out.dtype != torch.bfloat16 or out.shape[0] != shape[0]:
             raise ValueError("q and out: bf16 tensors of one shape")
-        if lse is not None and (lse.dtype != torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous()):
-            raise ValueError("lse: contiguous float32 [tokens, q_heads]")
-        batch._desc.tokens = q.shape[0]
-        _check(_lib.fp8_attn_paged(self._h, cache._ref, batch._ref, q.data_ptr(), ld_q, heads, out.data_ptr(), ld_o,
-                                   _ptr(lse), dim ** -0.5 if scale is None else scale, 1 if causal else 0, cache.conv,
-                                   _stream()), "fp8_attn_paged")
+        lse_ptr = None
+        if lse is not None:
+            if lse.dtype != torch.float32 or lse.shape != shape[:2] or not lse.is_contiguous():
+                raise ValueError("lse: contiguous float32 [tokens, q_heads]")
+            lse_ptr = lse.data_ptr()
+        batch._desc.tokens = shape[0]
+        status = _lib.fp8_attn_paged(self._h, cache._ref, batch._ref, q.data_ptr(), ld_q, heads, out.data_ptr(), ld_o, lse_ptr,
+                                     dim ** -0.5 if scale is None else scale, 1 if causal else 0, cache.conv,
+                                     _raw_stream(self.device))
+        if status:
+            _check(status, "fp8_attn_paged")
 
 
 def raw():
