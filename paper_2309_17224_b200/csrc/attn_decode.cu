@@ -163,6 +163,30 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 4 : 2) attn_decode_k
         const int lo = (int)(at - u.first_block), hi = (int)min((int64_t)u.blocks, end - u.first_block);
         const int rows = u.s.n * p.group;
 
+        // ---- this warp's blocks: lo + warp, every fourth; the first is requested before the queries are looked at ----
+        const int32_t *table = kv.table + (int64_t)u.b * kv.table_stride;
+        const int mine = max(0, (hi - lo - warp + kDecodeWarps - 1) / kDecodeWarps);
+        const int count = u.s.len > 0 ? mine : 0;
+        int pages = 0;            // lane i: page of the warp's block (32 * round + i)
+        auto fetch_pages = [&](int i0) {
+            const int blk = lo + warp + (i0 + lane) * kDecodeWarps;
+            pages = i0 + lane < count ? __ldg(table + (blk >> blocks_per_page_shift)) : 0;
+        };
+        int64_t v_at;
+        auto request_k = [&](KvBlock<D> &x, int i, int64_t &v_off) {
+            if ((i & 31) == 0) fetch_pages(i);
+            const int page = __shfl_sync(0xFFFFFFFFu, pages, i & 31);
+            const int blk = lo + warp + i * kDecodeWarps;
+            x.bad = (unsigned)page >= (unsigned)kv.pages;
+            const int64_t row = ((int64_t)u.h << kv.page_shift) + ((blk * kBlockTokens) & (size - 1));
+            const int64_t pg = x.bad ? 0 : page;
+            v_off = pg * kv.page_stride + row * D;
+            const int64_t b_off = pg * kv.bias_stride + row;
+            load_k<D>(x, kv.k8 + v_off, kv.bk + b_off, kv.bv + b_off, g, t);
+        };
+        KvBlock<D> cur;
+        if (count > 0) { request_k(cur, 0, v_at); load_v<D>(cur, kv.v8 + v_at, g, t); }
+
         // ---- queries: fp16 under a power of two per row (exact for bf16 unless 2^28 below the row's largest) ----
         uint32_t q[NT][D / 16][2];
         float rc[NT][2];          // c / that power, for the rows of S^T's columns
@@ -218,30 +242,6 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 4 : 2) attn_decode_k
             top[j][0] = top[j][1] = kNoMax;
             l[j][0] = l[j][1] = 0.0f;
         }
-
-        // ---- this warp's blocks: lo + warp, every fourth ----
-        const int32_t *table = kv.table + (int64_t)u.b * kv.table_stride;
-        const int mine = max(0, (hi - lo - warp + kDecodeWarps - 1) / kDecodeWarps);
-        const int count = u.s.len > 0 ? mine : 0;
-        int pages = 0;            // lane i: page of the warp's block (32 * round + i)
-        auto fetch_pages = [&](int i0) {
-            const int blk = lo + warp + (i0 + lane) * kDecodeWarps;
-            pages = i0 + lane < count ? __ldg(table + (blk >> blocks_per_page_shift)) : 0;
-        };
-        int64_t v_at;
-        auto request_k = [&](KvBlock<D> &x, int i, int64_t &v_off) {
-            if ((i & 31) == 0) fetch_pages(i);
-            const int page = __shfl_sync(0xFFFFFFFFu, pages, i & 31);
-            const int blk = lo + warp + i * kDecodeWarps;
-            x.bad = (unsigned)page >= (unsigned)kv.pages;
-            const int64_t row = ((int64_t)u.h << kv.page_shift) + ((blk * kBlockTokens) & (size - 1));
-            const int64_t pg = x.bad ? 0 : page;
-            v_off = pg * kv.page_stride + row * D;
-            const int64_t b_off = pg * kv.bias_stride + row;
-            load_k<D>(x, kv.k8 + v_off, kv.bk + b_off, kv.bv + b_off, g, t);
-        };
-        KvBlock<D> cur;
-        if (count > 0) { request_k(cur, 0, v_at); load_v<D>(cur, kv.v8 + v_at, g, t); }
 
         for (int i = 0; i < count; ++i) {
             const int j0 = (lo + warp + i * kDecodeWarps) * kBlockTokens;
