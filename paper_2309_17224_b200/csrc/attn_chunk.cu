@@ -59,16 +59,32 @@ constexpr uint32_t kTmemCols = 512, kTmemSlot = 256;         // per slot 128 col
 constexpr float kTf32Kept = 1.0f - 0.7213f / 2048.0f;
 constexpr uint32_t kTmemO = 128;
 
-__device__ __forceinline__ void chunk_mma_f8(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+// The tensor cores' instructions take their operands from uniform registers.  So the whole warp walks the steps with
+// values that the compiler can see to be uniform, and one elected lane issues: with a single lane in the loop every operand
+// of every instruction was first moved over (2048 tokens on 16384: 1474 us, and the more the longer the code per
+// instruction).
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __shfl_sync(0xFFFFFFFFu, v, 0); }
+__device__ __forceinline__ bool elect_one()
 {
-    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
-                 "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+    uint32_t r;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xFFFFFFFF;\nselp.u32 %0, 1, 0, p;\n}\n" : "=r"(r));
+    return r != 0;
+}
+// d, the descriptors' low words (HI their high ones), a's tensor-memory address, instruction descriptor
+template <uint32_t A_HI, uint32_t B_HI>
+__device__ __forceinline__ void chunk_mma_f8(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n.reg .pred p;\n.reg .b64 da, db;\nsetp.ne.b32 p, %4, 0;\nmov.b64 da, {%1, %5};\nmov.b64 db, {%2, %6};\n"
+                 "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], da, db, %3, p;\n}\n" ::"r"(d),
+                 "r"(a), "r"(b), "r"(idesc), "r"(accumulate), "n"(A_HI), "n"(B_HI)
                  : "memory");
 }
-__device__ __forceinline__ void chunk_mma_tf32_tmem(uint32_t d, uint32_t a_tmem, uint64_t b, uint32_t idesc, uint32_t accumulate)
+template <uint32_t B_HI>
+__device__ __forceinline__ void chunk_mma_tf32_tmem(uint32_t d, uint32_t a_tmem, uint32_t b, uint32_t idesc, uint32_t accumulate)
 {
-    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::tf32 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d),
-                 "r"(a_tmem), "l"(b), "r"(idesc), "r"(accumulate)
+    asm volatile("{\n.reg .pred p;\n.reg .b64 db;\nsetp.ne.b32 p, %4, 0;\nmov.b64 db, {%2, %5};\n"
+                 "tcgen05.mma.cta_group::1.kind::tf32 [%0], [%1], db, %3, p;\n}\n" ::"r"(d),
+                 "r"(a_tmem), "r"(b), "r"(idesc), "r"(accumulate), "n"(B_HI)
                  : "memory");
 }
 __device__ __forceinline__ void chunk_commit(uint32_t bar)
@@ -165,14 +181,8 @@ __device__ __forceinline__ void sts16(uint32_t addr, uint32_t a, uint32_t b, uin
 // all operands here have the contraction index innermost.
 //   128-byte swizzle, operand rows of 128 contiguous bytes along the contraction, groups of eight rows 1024 bytes apart
 //   64-byte swizzle, rows of 64 bytes, groups of eight rows 512 bytes apart
-__device__ __forceinline__ uint64_t desc_sw128(uint32_t addr)
-{
-    return (uint64_t)((addr >> 4) & 0x3FFFu) | (uint64_t)1 << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
-}
-__device__ __forceinline__ uint64_t desc_sw64(uint32_t addr)
-{
-    return (uint64_t)((addr >> 4) & 0x3FFFu) | (uint64_t)1 << 16 | (uint64_t)(512 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)4 << 61;
-}
+__device__ __forceinline__ uint32_t desc_lo(uint32_t addr) { return ((addr >> 4) & 0x3FFFu) | 1u << 16; }
+constexpr uint32_t kSw128 = (1024 >> 4) | 1u << 14 | 2u << 29, kSw64 = (512 >> 4) | 1u << 14 | 4u << 29;
 
 __device__ __forceinline__ void tma_load_page(uint32_t dst, const CUtensorMap *map, uint32_t bar, int y, int z)
 {
@@ -379,78 +389,88 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
         const uint32_t idesc_s = (1u << 4) | ((uint32_t)(kTile >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);                       // e4m3
         const uint32_t idesc_o = (1u << 4) | (2u << 7) | (2u << 10) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);   // tf32
         uint32_t n_units[2] = {}, n_steps[2] = {};
+        const uint32_t tm = uniform(tmem), base_lo = uniform(desc_lo(base));
         // S of step g into slot q, from query tile qt
-        auto scores = [&](int q, int qt, uint32_t g) {
-            const uint32_t k_addr = base + L::kK + (g % kKStages) * L::kKBytes, q_addr = base + L::kQ + qt * L::kQBytes;
-            const uint64_t dk = D == 128 ? desc_sw128(k_addr) : desc_sw64(k_addr);
+        auto scores = [&](uint32_t q, uint32_t qt, uint32_t g) {
+            const uint32_t dk = base_lo + (L::kK + (g % kKStages) * L::kKBytes) / 16, dq = base_lo + (L::kQ + qt * L::kQBytes) / 16;
+            if (elect_one()) {
 #pragma unroll
-            for (int term = 0; term < 2; ++term) {
-                const uint64_t dq = D == 128 ? desc_sw128(q_addr + term * kTile * 128) : desc_sw128(q_addr) + 4u * term;
+                for (uint32_t term = 0; term < 2; ++term)
 #pragma unroll
-                for (int k = 0; k < D / 32; ++k) chunk_mma_f8(tmem + kTmemSlot * q, dq + 2u * k, dk + 2u * k, idesc_s, (term | k) ? 1u : 0u);
+                    for (uint32_t k = 0; k < D / 32; ++k)
+                        chunk_mma_f8<kSw128, D == 128 ? kSw128 : kSw64>(tm + kTmemSlot * q, dq + term * (D == 128 ? kTile * 128 / 16 : 4) + 2u * k,
+                                                                        dk + 2u * k, idesc_s, (term | k) ? 1u : 0u);
+                chunk_commit(s_full(q));
             }
-            chunk_commit(s_full(q));
+            __syncwarp();
         };
         // O of slot q += P of the slot, V of step g
-        auto outputs = [&](int q, uint32_t g, bool first) {
-            const uint64_t dv = desc_sw128(base + L::kV + (g % kVStages) * L::kVBytes);
-            const uint32_t slot = tmem + kTmemSlot * q;
+        auto outputs = [&](uint32_t q, uint32_t g, uint32_t accumulate) {
+            const uint32_t dv = base_lo + (L::kV + (g % kVStages) * L::kVBytes) / 16, slot = tm + kTmemSlot * q;
+            if (elect_one()) {
 #pragma unroll
-            for (int k = 0; k < kTile / 8; ++k)      // eight tokens: 32 bytes of a block's rows, D * 128 bytes from block to block
-                chunk_mma_tf32_tmem(slot + kTmemO, slot + 8u * k, dv + (uint32_t)(k >> 2) * (D * 128 / 16) + 2u * (k & 3), idesc_o, first && k == 0 ? 0u : 1u);
+                for (uint32_t k = 0; k < kTile / 8; ++k)      // eight tokens: 32 bytes of a block's rows, D * 128 bytes from block to block
+                    chunk_mma_tf32_tmem<kSw128>(slot + kTmemO, slot + 8u * k, dv + (k >> 2) * (D * 128 / 16) + 2u * (k & 3), idesc_o,
+                                                k == 0 ? accumulate : 1u);
+            }
+            __syncwarp();
         };
-        if (lane == 0) {
-            while (true) {
-                const int lo = (int)(at - u.first), steps = (int)min((int64_t)u.steps, end - u.first) - lo;
-                const bool two = u.rows > kTile;           // two query tiles; else even and odd steps
-                alive = mbar_wait(q_full(0), n_units[0]++ & 1u, abort_flag, kv.d_status);
-                if (two) alive = alive && mbar_wait(q_full(1), n_units[1]++ & 1u, abort_flag, kv.d_status);
-                alive = alive && mbar_wait(k_full(g0), (g0 / kKStages) & 1u, abort_flag, kv.d_status);
+        auto commit = [&](uint32_t bar) {
+            if (elect_one()) chunk_commit(bar);
+            __syncwarp();
+        };
+        auto wait = [&](uint32_t bar, uint32_t parity) {
+            const bool ok = mbar_wait(bar, parity, abort_flag, kv.d_status);
+            return (bool)__all_sync(0xFFFFFFFFu, ok);
+        };
+        while (true) {
+            const int lo = (int)(at - u.first);
+            const int steps = (int)uniform((uint32_t)((int)min((int64_t)u.steps, end - u.first) - lo));
+            const uint32_t two = uniform(u.rows > kTile);      // two query tiles; else even and odd steps
+            g0 = uniform(g0);
+            alive = wait(q_full(0), n_units[0]++ & 1u);
+            if (two) alive = alive && wait(q_full(1), n_units[1]++ & 1u);
+            alive = alive && wait(k_full(g0), (g0 / kKStages) & 1u);
+            if (!alive) break;
+            chunk_fence_after();
+            scores(0, 0, g0);
+            if (two) scores(1, 1, g0);
+            commit(k_empty(g0));
+            if (!two && steps > 1) {
+                alive = wait(k_full(g0 + 1), ((g0 + 1) / kKStages) & 1u);
                 if (!alive) break;
                 chunk_fence_after();
-                scores(0, 0, g0);
-                if (two) {
-                    scores(1, 1, g0);
-                    chunk_commit(k_empty(g0));
-                } else {
-                    chunk_commit(k_empty(g0));
-                    if (steps > 1) {
-                        alive = mbar_wait(k_full(g0 + 1), ((g0 + 1) / kKStages) & 1u, abort_flag, kv.d_status);
-                        if (!alive) break;
-                        chunk_fence_after();
-                        scores(1, 0, g0 + 1);
-                        chunk_commit(k_empty(g0 + 1));
-                    }
-                }
-                const int ahead = two ? 1 : 2;             // steps from one of a slot to its next
-                for (int i = 0; i < steps && alive; ++i) {
-                    const uint32_t g = g0 + i, gn = g + ahead;
-                    alive = mbar_wait(v_full(g), (g / kVStages) & 1u, abort_flag, kv.d_status);
-                    const int q0 = two ? 0 : i & 1, q1 = two ? 1 : i & 1;
-                    for (int q = q0; q <= q1 && alive; ++q) {
-                        alive = mbar_wait(p_full(q), n_steps[q]++ & 1u, abort_flag, kv.d_status);
-                        if (!alive) break;
-                        chunk_fence_after();
-                        outputs(q, g, i < ahead);
-                        if (q == q1) chunk_commit(v_empty(g));
-                        if (i + ahead >= steps) {
-                            chunk_commit(o_full(q));
-                        } else {
-                            if (q == q0) {
-                                alive = mbar_wait(k_full(gn), (gn / kKStages) & 1u, abort_flag, kv.d_status);
-                                if (!alive) break;
-                                chunk_fence_after();
-                            }
-                            scores(q, two ? q : 0, gn);
-                            if (q == q1) chunk_commit(k_empty(gn));
-                        }
-                    }
-                }
-                g0 += steps;
-                at += steps;
-                if (!alive || at >= end) break;
-                next_unit(p, u);
+                scores(1, 0, g0 + 1);
+                commit(k_empty(g0 + 1));
             }
+            const int ahead = two ? 1 : 2;             // steps from one of a slot to its next
+            for (int i = 0; i < steps; ++i) {
+                const uint32_t g = g0 + i, gn = g + ahead;
+                const bool last = i + ahead >= steps;
+                if (!(alive = wait(v_full(g), (g / kVStages) & 1u))) break;
+                const uint32_t q0 = two ? 0 : i & 1, q1 = two ? 1 : i & 1;
+                for (uint32_t q = q0; q <= q1; ++q) {
+                    if (!(alive = wait(p_full(q), (q ? n_steps[1]++ : n_steps[0]++) & 1u))) break;
+                    chunk_fence_after();
+                    outputs(q, g, i < ahead ? 0u : 1u);
+                    if (q == q1) commit(v_empty(g));
+                    if (last) {
+                        commit(o_full(q));
+                    } else {
+                        if (q == q0) {
+                            if (!(alive = wait(k_full(gn), (gn / kKStages) & 1u))) break;
+                            chunk_fence_after();
+                        }
+                        scores(q, two ? q : 0, gn);
+                        if (q == q1) commit(k_empty(gn));
+                    }
+                }
+                if (!alive) break;
+            }
+            g0 += steps;
+            at += steps;
+            if (!alive || at >= end) break;
+            next_unit(p, u);
         }
     } else if (warp >= kFirstValueWarp) {
         // ------------------------------- values, keys' loads, scaling biases -------------------------------
