@@ -47,9 +47,9 @@ struct ChunkShape {
     static constexpr int kQ = 0;                             // (the second tile's place holds the odd slot's statistics
     static constexpr int kK = kQ + 2 * kQBytes;              // where the slots share one query tile)
     static constexpr int kV = kK + kKStages * kKBytes;
-    static constexpr int kScale = kV + kVStages * kVBytes;   // [2][128] floats: 2^-b of a tile's keys
-    static constexpr int kBar = kScale + 2 * kTile * 4;
-    static constexpr int kNumBars = 2 * kKStages + 2 * kVStages + 4 + 4 * 2 + 3;
+    static constexpr int kScale = kV + kVStages * kVBytes;   // [3][128] floats: 2^-b of a tile's keys
+    static constexpr int kBar = kScale + 3 * kTile * 4;
+    static constexpr int kNumBars = 2 * kKStages + 2 * kVStages + 8 + 4 * 2 + 3;
     static constexpr int kTotal = kBar + kNumBars * 8 + 16;
     static constexpr int kDynamic = kTotal + 1024;           // slack to align the base to 1024 bytes
     static constexpr int kPart = kTile * (D + 2);            // floats of a tile's partial result: sums, M, denominators
@@ -280,9 +280,14 @@ __device__ __forceinline__ void next_unit(const AttnParams &p, ChunkUnit &u)
 // One row's scores for kSpan tokens of a step as they came from tensor memory, times the keys' factors: u = 2^-b (q . K8),
 // s = rc u; -infinity for tokens j0 .. that the row does not see (limit).
 constexpr int kSpan = 32;
-__device__ __forceinline__ void scores_of_row(const uint32_t (&x)[kSpan], const float *factors, bool mask, int j0, int limit, f32x2 (&u)[kSpan / 2])
+__device__ __forceinline__ void scores_of_row(uint32_t taddr, const float *factors, bool mask, int j0, int limit, f32x2 (&u)[kSpan / 2])
 {
-    const ulonglong2 *f = reinterpret_cast<const ulonglong2 *>(factors);     // the same address in all lanes
+    uint32_t x[kSpan];
+    tmem_load32(taddr, x);
+    ulonglong2 f[kSpan / 4];                         // (the same address in all lanes; loaded while the scores are on their way)
+#pragma unroll
+    for (int k = 0; k < kSpan / 4; ++k) f[k] = reinterpret_cast<const ulonglong2 *>(factors)[k];
+    tmem_wait_ld();
 #pragma unroll
     for (int k = 0; k < kSpan / 2; k += 2) {
         const ulonglong2 f4 = f[k / 2];
@@ -340,15 +345,15 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
     auto v_full = [&](uint32_t g) { return bars + 8u * (2 * kKStages + g % kVStages); };
     auto v_empty = [&](uint32_t g) { return bars + 8u * (2 * kKStages + kVStages + g % kVStages); };
     const uint32_t bars2 = bars + 8u * (2 * kKStages + 2 * kVStages);
-    // of a slot's n-th step (two places each: the values' warps may be a step ahead of a slot, and a slot that sits out a
-    // unit must not meet a phase that it has not waited for)
-    auto sc_full = [&](int q, uint32_t n) { return bars2 + 8u * (2 * q + (n & 1u)); };
-    auto q_full = [&](int q) { return bars2 + 32u + 8u * q; };
-    auto s_full = [&](int q) { return bars2 + 48u + 8u * q; };
-    auto p_full = [&](int q) { return bars2 + 64u + 8u * q; };
-    auto o_full = [&](int q) { return bars2 + 80u + 8u * q; };
-    auto slot_bar = [&](int q) { return bars2 + 96u + 8u * q; };     // the 128 threads of a slot; both slots' 256
-    const uint32_t both_bar = bars2 + 112u;
+    // of a slot's n-th step (four places each: the values' warps may be three steps ahead of a slot, and a slot that sits
+    // out a unit must not meet a phase that it has not waited for)
+    auto sc_full = [&](int q, uint32_t n) { return bars2 + 8u * (4 * q + (n & 3u)); };
+    auto q_full = [&](int q) { return bars2 + 64u + 8u * q; };
+    auto s_full = [&](int q) { return bars2 + 80u + 8u * q; };
+    auto p_full = [&](int q) { return bars2 + 96u + 8u * q; };
+    auto o_full = [&](int q) { return bars2 + 112u + 8u * q; };
+    auto slot_bar = [&](int q) { return bars2 + 128u + 8u * q; };     // the 128 threads of a slot; both slots' 256
+    const uint32_t both_bar = bars2 + 144u;
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + L::kBar + L::kNumBars * 8);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
     volatile int *is_last = reinterpret_cast<volatile int *>(tmem_slot + 2);     // [2]
@@ -357,8 +362,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
         for (uint32_t i = 0; i < kKStages; ++i) { mbar_init(k_full(i), 1); mbar_init(k_empty(i), 1); }
         for (uint32_t i = 0; i < kVStages; ++i) { mbar_init(v_full(i), 128); mbar_init(v_empty(i), 1); }
         for (int q = 0; q < 2; ++q) {
-            mbar_init(sc_full(q, 0), 128);
-            mbar_init(sc_full(q, 1), 128);
+            for (uint32_t i = 0; i < 4; ++i) mbar_init(sc_full(q, i), 128);
             mbar_init(q_full(q), 128);
             mbar_init(s_full(q), 1);
             mbar_init(p_full(q), 4);
@@ -541,21 +545,21 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
             for (int i = 0; i < steps && alive; ++i) {
                 const int tile = lo + i;
                 const uint32_t g = g0 + i;
+                // 2^-b of the key for the softmax (step g - 3 has used this place: its products, waited for a step ago, are done)
+                const bool marked = bk == FP8_KV_BIAS_NONFINITE || bv == FP8_KV_BIAS_NONFINITE;
+                reinterpret_cast<float *>(smem + L::kScale)[(g % 3u) * kTile + cw * 32 + lane] =
+                    marked ? __int_as_float(0x7FFFFFFF) : pow2_normal(min(126, -(bk + kv.delta)));
+                if (two || (i & 1) == 0) mbar_arrive(sc_full(0, n_steps[0]++));
+                if (two || (i & 1) == 1) mbar_arrive(sc_full(1, n_steps[1]++));
                 if (cw == 0 && i + 1 < steps) {
                     alive = request_keys(tile + 1, g + 1, page);
                     if (!alive) break;
                     if (i + 2 < steps) page = page_of(tile + 2);
                 }
-                if (g >= 2) {         // the products of step g - 2 have read the values in this place, and its softmax the factors
+                if (g >= 2) {         // the products of step g - 2 have read the values in this place
                     const bool ok = mbar_wait(v_empty(g), ((g / kVStages) & 1u) ^ 1u, abort_flag, kv.d_status);
                     if (!(alive = __all_sync(0xFFFFFFFFu, ok))) break;
                 }
-                // 2^-b of the key for the softmax, 2^-d for the value
-                const bool marked = bk == FP8_KV_BIAS_NONFINITE || bv == FP8_KV_BIAS_NONFINITE;
-                reinterpret_cast<float *>(smem + L::kScale)[(g & 1u) * kTile + cw * 32 + lane] =
-                    marked ? __int_as_float(0x7FFFFFFF) : pow2_normal(min(126, -(bk + kv.delta)));
-                if (two || (i & 1) == 0) mbar_arrive(sc_full(0, n_steps[0]++));
-                if (two || (i & 1) == 1) mbar_arrive(sc_full(1, n_steps[1]++));
                 // the next tile's row takes the registers as they are converted
                 const uint4 *src_n = nullptr;
                 if (i + 1 < steps) src_n = row_of(tile + 1, page_n, bk_n, bv_n);
@@ -673,28 +677,25 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
                 for (int i = start; i < steps; i += ahead) {
                     const uint32_t g = g0 + i;
                     const int t0 = (lo + i) * kTile;
-                    bool ok = mbar_wait(sc_full(slot, n_steps), (n_steps >> 1) & 1u, abort_flag, kv.d_status);
+                    bool ok = mbar_wait(sc_full(slot, n_steps), (n_steps >> 2) & 1u, abort_flag, kv.d_status);
                     ok = ok && mbar_wait(s_full(slot), n_steps & 1u, abort_flag, kv.d_status);
                     ++n_steps;
                     if (!(alive = __all_sync(0xFFFFFFFFu, ok))) break;
                     chunk_fence_after();
                     if (active) {
-                        const float *factors = reinterpret_cast<const float *>(smem + L::kScale) + (g & 1u) * kTile;
+                        const float *factors = reinterpret_cast<const float *>(smem + L::kScale) + (g % 3u) * kTile;
                         const bool mask = t0 + kTile > least;
-                        auto span = [&](uint32_t (&x)[kSpan], int c0) {
+#pragma unroll 1
+                        for (int c0 = 0; c0 < kTile; c0 += kSpan) {
                             f32x2 w[kSpan / 2];
-                            tmem_wait_ld();
-                            scores_of_row(x, factors + c0, mask, t0 + c0, limit, w);
+                            scores_of_row(lanes + c0, factors + c0, mask, t0 + c0, limit, w);
                             // weights under M as it stands; only where their sum shows that a score lies far above M (or
                             // at the first token) is the maximum looked at, M moved and the weights taken again
                             f32x2 add = weights_of_row(w, rc2, top);
                             float a, b;
                             unpack2(add2(sum, add), a, b);
                             if (__builtin_expect(__any_sync(0xFFFFFFFFu, a + b > kSumLimit), 0)) {
-                                uint32_t z[kSpan];
-                                tmem_load32(lanes + c0, z);
-                                tmem_wait_ld();
-                                scores_of_row(z, factors + c0, mask, t0 + c0, limit, w);
+                                scores_of_row(lanes + c0, factors + c0, mask, t0 + c0, limit, w);
                                 float m = -INFINITY;
 #pragma unroll
                                 for (int k = 0; k < kSpan / 2; ++k) {
@@ -729,12 +730,6 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
                                 y[2 * k + 1] = __float_as_uint(b);
                             }
                             tmem_store32(lanes + c0, y);
-                        };
-#pragma unroll 1
-                        for (int c0 = 0; c0 < kTile; c0 += kSpan) {
-                            uint32_t x[kSpan];
-                            tmem_load32(lanes + c0, x);
-                            span(x, c0);
                         }
                         tmem_wait_st();
                     }
