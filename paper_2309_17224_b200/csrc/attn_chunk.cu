@@ -510,12 +510,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
                 b_v = kv.bv[page * kv.bias_stride + row];
                 return reinterpret_cast<const uint4 *>(kv.v8 + page * kv.page_stride + row * D);
             };
-            // 16 bytes of the lane's row, two loads ahead of their use (the loop below is rolled: it takes as long as
-            // unrolled, with a seventh of the code in the instruction cache that the softmax runs from)
-            auto piece = [&](const uint4 *src, int k) { return src ? __ldg(src + k) : make_uint4(0, 0, 0, 0); };
-            uint4 one, two_on;
+            uint4 cur[kLoads];
             int bk = 0, bv = 0, bk_n = 0, bv_n = 0, page_n = -1;
-            const uint4 *src, *src_n = nullptr;
             // keys: the first of these warps, one lane per page of the tile
             auto page_of = [&](int tile) {
                 const int j = tile * per_tile + lane;
@@ -541,9 +537,9 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
                 if (steps > 1) page = page_of(lo + 1);
             }
             {
-                src = row_of(lo, page_of_token(lo), bk, bv);
-                one = piece(src, 0);
-                two_on = piece(src, 1);
+                const uint4 *src = row_of(lo, page_of_token(lo), bk, bv);
+#pragma unroll
+                for (int k = 0; k < kLoads; ++k) cur[k] = src ? __ldg(src + k) : make_uint4(0, 0, 0, 0);
                 if (steps > 1) page_n = page_of_token(lo + 1);
             }
             for (int i = 0; i < steps && alive; ++i) {
@@ -564,18 +560,17 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
                     const bool ok = mbar_wait(v_empty(g), ((g / kVStages) & 1u) ^ 1u, abort_flag, kv.d_status);
                     if (!(alive = __all_sync(0xFFFFFFFFu, ok))) break;
                 }
-                src_n = nullptr;
+                // the next tile's row takes the registers as they are converted
+                const uint4 *src_n = nullptr;
                 if (i + 1 < steps) src_n = row_of(tile + 1, page_n, bk_n, bv_n);
                 if (i + 2 < steps) page_n = page_of_token(tile + 2);
                 const float f = pow2_normal(min(126, -(applied_bias(bv) + kv.delta)));
                 const f32x2 f2 = pack2(f, f);
                 const uint32_t stage = (g % kVStages) * L::kVBytes;
-#pragma unroll 1
+#pragma unroll
                 for (int k = 0; k < kLoads; ++k) {
-                    const uint32_t w[4] = {one.x, one.y, one.z, one.w};
-                    one = two_on;
-                    two_on = k + 2 < kLoads ? piece(src, k + 2) : piece(src_n, k + 2 - kLoads);
-                    const uint32_t row = stage + 16 * k * 128;
+                    const uint32_t w[4] = {cur[k].x, cur[k].y, cur[k].z, cur[k].w};
+                    cur[k] = src_n ? __ldg(src_n + k) : make_uint4(0, 0, 0, 0);
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         uint32_t h[2];
@@ -586,7 +581,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
                         unpack2(mul2(pack2(v[2], v[3]), f2), v[2], v[3]);
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
-                            sts4(place[(4 * q + j) & 7] + row + (4 * q + j) * 128, v[j]);
+                            const int dim = 16 * k + 4 * q + j;
+                            sts4(place[dim & 7] + stage + dim * 128, v[j]);
                         }
                     }
                 }
@@ -594,7 +590,6 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
                 mbar_arrive(v_full(g));
                 bk = bk_n;
                 bv = bv_n;
-                src = src_n;
             }
             g0 += steps;
             at += steps;
