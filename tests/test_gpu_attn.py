@@ -187,6 +187,39 @@ def test_repeated_calls_give_the_same_bits_on_a_busy_gpu_and_on_another_stream(l
             assert torch.equal(o.view(torch.int16), first.view(torch.int16))
 
 
+@pytest.mark.parametrize("q_heads,kv_heads,dim", [(32, 32, 64), (8, 8, 128), (16, 2, 128)])
+def test_units_of_one_step_and_of_several_follow_one_another(lib, ctx, q_heads, kv_heads, dim):
+    """Contexts whose lengths leave one step of a (sequence, head) to a multiprocessor before or behind several of the
+    next, in calls that nothing waits between: what one unit leaves behind must not reach the next."""
+    lens, news = [701, 543, 595, 492, 461, 90, 128, 300], [37, 23, 23, 19, 30, 33, 17, 30]
+    case = R.make_case(34, lens, news, kv_heads, dim, 16, O.CONV_NATIVE, fill=0x7F)
+    dev, cache, batch = gpu_state(lib, case, O.CONV_NATIVE, 37, 701)
+    q = torch.randn((sum(news), q_heads, dim), generator=case["g"]).to(torch.bfloat16)
+    qd = q.cuda()
+    outs = [(torch.empty_like(qd), torch.empty(qd.shape[:2], device="cuda")) for _ in range(30)]
+    for o, l in outs:
+        ctx.attn_paged(cache, batch, qd, o, lse=l)
+    torch.cuda.synchronize()
+    cpu = [case[n].numpy() for n in ("k8", "v8", "bk", "bv")]
+    want = R.attention(cpu, case["table"].numpy(), case["q_start"].numpy(), lens, q.double().numpy(), dim ** -0.5, True, O.CONV_NATIVE)
+    check(*outs[0], want)
+    for o, l in outs[1:]:
+        assert torch.equal(o.view(torch.int16), outs[0][0].view(torch.int16)) and torch.equal(l, outs[0][1])
+
+
+def test_launches_are_counted(lib, ctx):
+    for news in (1, 40):
+        case = R.make_case(35, [200, 90], [news] * 2, 2, 64, 16, O.CONV_PAPER)
+        dev, cache, batch = gpu_state(lib, case, O.CONV_PAPER, news, 200)
+        q = torch.zeros((2 * news, 4, 64), dtype=torch.bfloat16, device="cuda")
+        k = torch.zeros((2 * news, 2, 64), dtype=torch.bfloat16, device="cuda")
+        before = lib.launch_count()
+        ctx.kv_append(cache, batch, k, k)
+        ctx.attn_paged(cache, batch, q, torch.empty_like(q))
+        ctx.kv_read(cache, batch, k, None)
+        assert lib.launch_count() == before + 3
+
+
 def test_graph_replay_follows_the_lengths_on_the_device(lib, ctx):
     """Captured once; the lengths, the tokens and the pages of later replays come from device memory."""
     conv, heads, dim = O.CONV_PAPER, 2, 128
