@@ -11,10 +11,15 @@
 //   O^T[D x 8 rows] += V^T P^T:   lane (g, t) holds 16 contiguous dimensions of tokens 2t, 2t+1, 2t+8, 2t+9; a byte
 //       permute brings two tokens together, five instructions make a bf16 pair.  P^T, in its two terms, comes out of
 //       S^T by 8x8 transposes (movmatrix).
-// Two blocks are in flight per warp, each re-requested as soon as its registers are free: with 12 warps on an SM about
-// 80 KB.  The blocks of all (sequence, head) units form one list, cut evenly between the CTAs (a sequence's length
-// changes nothing in the balance); a unit that lies in several CTAs leaves partial sums in the workspace, joined in
-// order by the CTA that arrives last, so results do not depend on the order of arrival.
+// A warp holds one block: its keys' registers are requested again (the next block's) as soon as the first product is done,
+// its values' after the second; four CTAs per SM for up to 8 rows, two above.  (Together with the join's many loads in
+// flight this took 16 sequences on 4096 from 40.2 us, with two blocks per warp, to 35.8.)  The blocks of all (sequence,
+// head) units form one list, cut evenly between the CTAs (a sequence's length changes nothing in the balance); a unit that
+// lies in several CTAs leaves partial sums in the workspace, joined in order by the CTA that arrives last, so results do
+// not depend on the order of arrival.
+// Measured from a graph (64/8 heads of 128): 16 ragged sequences on up to 4096 tokens 36 us for 109 MB (17 us at the
+// measured copy rate).  Longer contexts add 5.1 to 5.75 TB/s; about 14 us are fixed: launch, lookup, first loads, changes
+// of unit, and 2.6 us for the join.
 #include "attn_common.cuh"
 
 namespace fp8lin {
@@ -22,6 +27,45 @@ namespace fp8lin {
 constexpr int kDecodeWarps = 4;
 constexpr int kDecodeThreads = 32 * kDecodeWarps;
 constexpr int kBlockTokens = 16;
+
+constexpr float kSlack = 40.0f;       // M is moved when a score exceeds it by more
+
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
+{
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ uint2 load_stream2(const void *p)
+{
+    uint2 v;
+    asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
+    return v;
+}
+
+// E4 bytes as bf16: the exponent and mantissa fields moved to where bf16 has them give the number times 2^-120 (also for
+// the subnormals of E4), which the multiplication by 2^(120 - d) mends and scales at once, exactly.
+//   spread: a word whose bytes 1 and 3 hold the two E4 bytes (bytes 0 and 2 are ignored)
+__device__ __forceinline__ uint32_t e4_fields_as_bf16(uint32_t spread) { return ((spread >> 4) & 0x07F007F0u) | (spread & 0x80008000u); }
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t x, uint32_t y)
+{
+    uint32_t r;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(y));
+    return r;
+}
+// 2^(120 - d) as a bf16 number; for d < -7 that is beyond bf16 and the rest, 2^(-7 - d), is a second factor.
+__device__ __forceinline__ uint32_t value_factor(int d) { return (uint32_t)(247 - max(d, -7)) << 7; }
+__device__ __forceinline__ uint32_t value_factor_rest(int d) { return (uint32_t)(127 + max(-7 - d, 0)) << 7; }
+
+// A weight as the sum of two bf16 numbers, p = p1 + p2 (two weights at a time): p1 the leading eight bits as they are, p2 the
+// rest rounded to eight, sixteen bits at any size.  One bf16 (2^-9 of every weight) would be coarser than the rounding of
+// the output itself; fp16 would do for weights near the maximum but has none left below 2^-39 of it, and those count in
+// dimensions where the tokens above them hold zeros.
+__device__ __forceinline__ void split_bf16(float a, float b, uint32_t &p1, uint32_t &p2)
+{
+    p1 = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
+    p2 = pack_bf16x2(a - __uint_as_float(__float_as_uint(a) & 0xFFFF0000u), b - __uint_as_float(__float_as_uint(b) & 0xFFFF0000u));
+}
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
@@ -60,7 +104,7 @@ __device__ __forceinline__ void load_k(KvBlock<D> &x, const uint8_t *k, const in
     for (int r = 0; r < 2; ++r) {
 #pragma unroll
         for (int i = 0; i < KvBlock<D>::kKChunks; ++i) {
-            const uint4 w = ldg_stream(k + (g + 8 * r) * D + (t + 4 * i) * 16);
+            const uint4 w = load_stream(k + (g + 8 * r) * D + (t + 4 * i) * 16);
             x.k[r][i][0] = w.x; x.k[r][i][1] = w.y; x.k[r][i][2] = w.z; x.k[r][i][3] = w.w;
         }
         x.bk[r] = bk[g + 8 * r];
@@ -74,10 +118,10 @@ __device__ __forceinline__ void load_v(KvBlock<D> &x, const uint8_t *v, int g, i
     for (int r = 0; r < 4; ++r) {
         const uint8_t *src = v + (2 * t + (r & 1) + 8 * (r >> 1)) * D + g * (D / 8);
         if constexpr (D == 128) {
-            const uint4 w = ldg_stream(src);
+            const uint4 w = load_stream(src);
             x.v[r][0] = w.x; x.v[r][1] = w.y; x.v[r][2] = w.z; x.v[r][3] = w.w;
         } else {
-            const uint2 w = ldg_stream2(src);
+            const uint2 w = load_stream2(src);
             x.v[r][0] = w.x; x.v[r][1] = w.y;
         }
     }

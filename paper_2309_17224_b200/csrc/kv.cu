@@ -21,13 +21,6 @@ struct RowShape {
     static constexpr int kHeads = kRowsPerWarp * kUnroll;        // heads of a warp's task
 };
 
-__device__ __forceinline__ uint4 load_stream(const void *p)
-{
-    uint4 v;
-    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-    return v;
-}
-
 // Largest magnitude (as FP32 bits: NaN above infinity above every number) of one lane's 16 bytes.  Magnitudes of one type
 // are in the order of their bits, so 16-bit types are compared two at a time and only the largest is converted.
 template <int DT>

@@ -95,6 +95,14 @@ __device__ __forceinline__ RowPlace place_of_row(const KvParams &p, int t, int l
     return (unsigned)page < (unsigned)p.pages ? kWritten : kBad;
 }
 
+// 16 bytes that are used once.
+__device__ __forceinline__ uint4 load_stream(const void *p)
+{
+    uint4 v;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+
 // The bias that a cached row's bytes were cast under.
 __device__ __forceinline__ int applied_bias(int b) { return b == FP8_KV_BIAS_NONFINITE ? 0 : b; }
 
