@@ -19,10 +19,10 @@
 // other's products do.  With more than 128 rows the slots are the unit's two query tiles, with up to 128 they are the even
 // and the odd steps of the one tile, added up at its end.  Within a slot the order is strict: S, softmax, O, next S; that
 // also makes the rescaling of O safe without a barrier of its own, as S of a step is complete only after O of the one
-// before.  The first product of the next step overwrites weights that the second product of this one reads: both are
-// issued by one thread and rely on the tensor core taking one thread's instructions in their order.  (Halves of 64 tokens
-// in turn within a slot were slower, 1736 against 1517 us in separate runs: scores of 64 columns cost the tensor cores 1.5
-// times their share.)
+// before.  The first product of the next step overwrites the weights that the second product of this one reads.  Products of
+// different kinds and accumulators are not ordered by being issued one after the other, so the second product is committed
+// to a barrier of the slot, and the next scores of the slot are issued only behind it.  (Halves of 64 tokens in turn within a
+// slot were slower, 1736 against 1517 us in separate runs: scores of 64 columns cost the tensor cores 1.5 times their share.)
 // Measured from a graph: 2048 tokens on 16384, 64/8 heads of 128, 1391 us, 741 TFLOP/s.  A step takes about 6200 cycles,
 // its products 3072 of them; the softmax's chain of latencies and the wait for scores take the rest.
 //
@@ -54,7 +54,7 @@ struct ChunkShape {
     static constexpr int kV = kK + kKStages * kKBytes;
     static constexpr int kScale = kV + kVStages * kVBytes;   // [3][128] floats: 2^-b of a tile's keys
     static constexpr int kBar = kScale + 3 * kTile * 4;
-    static constexpr int kNumBars = 2 * kKStages + 2 * kVStages + 8 + 4 * 2 + 3;
+    static constexpr int kNumBars = 2 * kKStages + 2 * kVStages + 8 + 5 * 2 + 3;
     static constexpr int kTotal = kBar + kNumBars * 8 + 16;
     static constexpr int kDynamic = kTotal + 1024;           // slack to align the base to 1024 bytes
     static constexpr int kPart = kTile * (D + 2);            // floats of a tile's partial result: sums, M, denominators
@@ -360,6 +360,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
     auto o_full = [&](int q) { return bars2 + 112u + 8u * q; };
     auto slot_bar = [&](int q) { return bars2 + 128u + 8u * q; };     // the 128 threads of a slot; both slots' 256
     const uint32_t both_bar = bars2 + 144u;
+    auto pv_done = [&](int q) { return bars2 + 152u + 8u * q; };      // the slot's second product has read its weights
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + L::kBar + L::kNumBars * 8);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
     volatile int *is_last = reinterpret_cast<volatile int *>(tmem_slot + 2);     // [2]
@@ -374,6 +375,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
             mbar_init(p_full(q), 4);
             mbar_init(o_full(q), 1);
             mbar_init(slot_bar(q), 128);
+            mbar_init(pv_done(q), 1);
         }
         mbar_init(both_bar, 256);
         *abort_flag = 0;
@@ -398,8 +400,18 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
         // ------------------------------- products -------------------------------
         const uint32_t idesc_s = (1u << 4) | ((uint32_t)(kTile >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);                       // e4m3
         const uint32_t idesc_o = (1u << 4) | (2u << 7) | (2u << 10) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);   // tf32
-        uint32_t n_units[2] = {}, n_steps[2] = {};
+        uint32_t n_units[2] = {}, n_steps[2] = {}, n_scores[2] = {};
         const uint32_t tm = uniform(tmem), base_lo = uniform(desc_lo(base));
+        auto wait = [&](uint32_t bar, uint32_t parity) {
+            const bool ok = mbar_wait(bar, parity, abort_flag, kv.d_status);
+            return (bool)__all_sync(0xFFFFFFFFu, ok);
+        };
+        // the weights in slot q's columns have been read (nothing to wait for before the slot's first scores: each of its
+        // scores has one second product behind it)
+        auto columns_free = [&](uint32_t q) {
+            const uint32_t n = q ? n_scores[1]++ : n_scores[0]++;
+            return n == 0 || wait(pv_done(q), (n - 1) & 1u);
+        };
         // S of step g into slot q, from query tile qt
         auto scores = [&](uint32_t q, uint32_t qt, uint32_t g) {
             const uint32_t dk = base_lo + (L::kK + (g % kKStages) * L::kKBytes) / 16, dq = base_lo + (L::kQ + qt * L::kQBytes) / 16;
@@ -422,16 +434,13 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
                 for (uint32_t k = 0; k < kTile / 8; ++k)      // eight tokens: 32 bytes of a block's rows, D * 128 bytes from block to block
                     chunk_mma_tf32_tmem<kSw128>(slot + kTmemO, slot + 8u * k, dv + (k >> 2) * (D * 128 / 16) + 2u * (k & 3), idesc_o,
                                                 k == 0 ? accumulate : 1u);
+                chunk_commit(pv_done(q));
             }
             __syncwarp();
         };
         auto commit = [&](uint32_t bar) {
             if (elect_one()) chunk_commit(bar);
             __syncwarp();
-        };
-        auto wait = [&](uint32_t bar, uint32_t parity) {
-            const bool ok = mbar_wait(bar, parity, abort_flag, kv.d_status);
-            return (bool)__all_sync(0xFFFFFFFFu, ok);
         };
         while (true) {
             const int lo = (int)(at - u.first);
@@ -440,14 +449,15 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
             g0 = uniform(g0);
             alive = wait(q_full(0), n_units[0]++ & 1u);
             if (two) alive = alive && wait(q_full(1), n_units[1]++ & 1u);
-            alive = alive && wait(k_full(g0), (g0 / kKStages) & 1u);
+            alive = alive && wait(k_full(g0), (g0 / kKStages) & 1u) && columns_free(0);
+            if (two) alive = alive && columns_free(1);
             if (!alive) break;
             chunk_fence_after();
             scores(0, 0, g0);
             if (two) scores(1, 1, g0);
             commit(k_empty(g0));
             if (!two && steps > 1) {
-                alive = wait(k_full(g0 + 1), ((g0 + 1) / kKStages) & 1u);
+                alive = wait(k_full(g0 + 1), ((g0 + 1) / kKStages) & 1u) && columns_free(1);
                 if (!alive) break;
                 chunk_fence_after();
                 scores(1, 0, g0 + 1);
@@ -469,8 +479,9 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
                     } else {
                         if (q == q0) {
                             if (!(alive = wait(k_full(gn), (gn / kKStages) & 1u))) break;
-                            chunk_fence_after();
                         }
+                        if (!(alive = columns_free(q))) break;
+                        chunk_fence_after();
                         scores(q, two ? q : 0, gn);
                         if (q == q1) commit(k_empty(gn));
                     }
