@@ -215,7 +215,7 @@ class KvCache:
         if _page_stride(k8) != _page_stride(v8) or _page_stride(bk) != _page_stride(bv):
             raise ValueError("k8 and v8, bk and bv have their pages equally far apart")
         self.k8, self.v8, self.bk, self.bv, self.conv = k8, v8, bk, bv, conv
-        self.kv_heads, self.head_dim = heads, dim
+        self.kv_heads, self.page_size, self.head_dim = heads, size, dim
         self._desc = KvCacheDesc(k8.data_ptr(), v8.data_ptr(), bk.data_ptr(), bv.data_ptr(), _page_stride(k8),
                                  _page_stride(bk), pages, heads, size, dim)
         self._ref = byref(self._desc)
@@ -227,20 +227,27 @@ def _page_stride(t):
 
 class SeqBatch:
     """The sequences of one call (``fp8_seq_batch_t``): q_start int32 [seqs + 1], kv_len int32 [seqs], page_table int32
-    [seqs, table width], all on the GPU; the bounds of rows and tokens per sequence are host numbers."""
+    [seqs, table width], all on the GPU; the bounds of rows and tokens per sequence are host numbers.  Every row of the table
+    has a column for each page of max_kv_len tokens (checked by the calls, which know the page size)."""
 
     def __init__(self, q_start, kv_len, page_table, max_q_len, max_kv_len):
         seqs = kv_len.shape[0]
         for t in (q_start, kv_len, page_table):
             if t.dtype != torch.int32 or (t.shape[-1] > 1 and t.stride(-1) != 1) or not t.is_cuda:
                 raise ValueError("q_start, kv_len and page_table are int32 tensors on the GPU")
-        if q_start.shape != (seqs + 1,) or page_table.dim() != 2 or page_table.shape[0] != seqs:
+        if q_start.shape != (seqs + 1,) or kv_len.dim() != 1 or page_table.dim() != 2 or page_table.shape[0] != seqs:
             raise ValueError("q_start [seqs + 1], kv_len [seqs], page_table [seqs, width]")
         self.q_start, self.kv_len, self.page_table = q_start, kv_len, page_table
-        self._width = page_table.shape[1]
+        self._width, self._max_kv_len = page_table.shape[1], max_kv_len
         self._desc = SeqBatchDesc(q_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(),
                                   page_table.stride(0) if seqs > 1 else self._width, seqs, 0, max_q_len, max_kv_len)
         self._ref = byref(self._desc)
+
+
+def _check_table(cache, batch):
+    # the library sees the distance between the table's rows only: in a slice of a wider table that is more than a row has
+    if batch._width * cache.page_size < batch._max_kv_len:
+        raise ValueError(f"page_table has {batch._width} columns of {cache.page_size} tokens, max_kv_len is {batch._max_kv_len}")
 
 
 def _rows3(t, heads, dim, what):
@@ -507,6 +514,7 @@ class Context:
         if some is None:
             raise ValueError("keys, values or both")
         heads, dim = cache.kv_heads, cache.head_dim
+        _check_table(cache, batch)
         ld_k = _rows3(k, heads, dim, "keys") if k is not None else 0
         ld_v = _rows3(v, heads, dim, "values") if v is not None else 0
         if k is not None and v is not None and (k.dtype != v.dtype or k.shape[0] != v.shape[0]):
@@ -530,6 +538,7 @@ class Context:
         1 / sqrt(head_dim) by default."""
         shape, dim = q.shape, cache.head_dim
         heads = shape[1]
+        _check_table(cache, batch)
         ld_q, ld_o = _rows3(q, heads, dim, "q"), _rows3(out, heads, dim, "out")
         if q.dtype != torch.bfloat16 or out.dtype != torch.bfloat16 or out.shape[0] != shape[0]:
             raise ValueError("q and out: bf16 tensors of one shape")

@@ -1,0 +1,64 @@
+"""Arguments of the cache calls that are refused before a pointer reaches the library (no GPU: the tensors only claim to be
+on one, and the context has no handle)."""
+import pytest
+import torch
+
+from paper_2309_17224_b200 import build as B
+
+B.build()
+from paper_2309_17224_b200 import fp8lin
+
+
+class OnGpu(torch.Tensor):
+    is_cuda = property(lambda self: True)
+
+    def get_device(self):
+        return 0
+
+
+def on_gpu(t):
+    return t.as_subclass(OnGpu)
+
+
+def zeros(*shape, dtype=torch.bfloat16):
+    return on_gpu(torch.zeros(shape, dtype=dtype))
+
+
+@pytest.fixture
+def ctx():
+    c = object.__new__(fp8lin.Context)
+    c._h, c.device = None, 0
+    return c
+
+
+def cache_of(pages=8, heads=2, size=16, dim=64):
+    k8, v8 = (zeros(pages, heads, size, dim, dtype=torch.uint8) for _ in range(2))
+    bk, bv = (zeros(pages, heads, size, dtype=torch.int8) for _ in range(2))
+    return fp8lin.KvCache(k8, v8, bk, bv)
+
+
+def batch_of(table, max_kv_len, seqs=2):
+    return fp8lin.SeqBatch(zeros(seqs + 1, dtype=torch.int32), zeros(seqs, dtype=torch.int32), table, max_q_len=4,
+                           max_kv_len=max_kv_len)
+
+
+def calls(ctx, cache, batch):
+    rows, q = zeros(4, 2, 64), zeros(4, 4, 64)
+    return [lambda: ctx.kv_append(cache, batch, rows, rows), lambda: ctx.kv_read(cache, batch, rows, None),
+            lambda: ctx.attn_paged(cache, batch, q, q)]
+
+
+def test_a_table_slice_with_too_few_columns_is_refused(ctx):
+    """Two columns of a table that is eight wide: the rows lie far enough apart for 64 tokens, but hold 32."""
+    wide = zeros(2, 8, dtype=torch.int32)
+    for call in calls(ctx, cache_of(), batch_of(wide[:, 6:], 33)):
+        with pytest.raises(ValueError, match="columns"):
+            call()
+    for call in calls(ctx, cache_of(), batch_of(wide[:1, :2], 33, seqs=1)):
+        with pytest.raises(ValueError, match="columns"):
+            call()
+
+
+def test_lengths_are_one_per_sequence():
+    with pytest.raises(ValueError):
+        fp8lin.SeqBatch(zeros(3, dtype=torch.int32), zeros(2, 2, dtype=torch.int32), zeros(2, 8, dtype=torch.int32), 4, 33)
