@@ -212,6 +212,9 @@ class KvCache:
             if t.shape != shape or t.dtype != dt or not t[0].is_contiguous() or not t.is_cuda:
                 raise ValueError("k8, v8: uint8 [pages, kv_heads, page_size, head_dim]; bk, bv: int8 [pages, kv_heads, "
                                  "page_size]; on the GPU, each page contiguous")
+        self.device = k8.get_device()
+        if any(t.get_device() != self.device for t in (v8, bk, bv)):
+            raise ValueError("k8, v8, bk and bv on one GPU")
         if _page_stride(k8) != _page_stride(v8) or _page_stride(bk) != _page_stride(bv):
             raise ValueError("k8 and v8, bk and bv have their pages equally far apart")
         self.k8, self.v8, self.bk, self.bv, self.conv = k8, v8, bk, bv, conv
@@ -237,6 +240,9 @@ class SeqBatch:
                 raise ValueError("q_start, kv_len and page_table are int32 tensors on the GPU")
         if q_start.shape != (seqs + 1,) or kv_len.dim() != 1 or page_table.dim() != 2 or page_table.shape[0] != seqs:
             raise ValueError("q_start [seqs + 1], kv_len [seqs], page_table [seqs, width]")
+        self.device = q_start.get_device()
+        if kv_len.get_device() != self.device or page_table.get_device() != self.device:
+            raise ValueError("q_start, kv_len and page_table on one GPU")
         self.q_start, self.kv_len, self.page_table = q_start, kv_len, page_table
         self._width, self._max_kv_len = page_table.shape[1], max_kv_len
         self._desc = SeqBatchDesc(q_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(),
@@ -244,15 +250,20 @@ class SeqBatch:
         self._ref = byref(self._desc)
 
 
-def _check_table(cache, batch):
+def _check_handles(cache, batch, device):
+    if cache.device != device or batch.device != device:
+        raise ValueError(f"cache and batch on the context's GPU {device} expected")
     # the library sees the distance between the table's rows only: in a slice of a wider table that is more than a row has
     if batch._width * cache.page_size < batch._max_kv_len:
         raise ValueError(f"page_table has {batch._width} columns of {cache.page_size} tokens, max_kv_len is {batch._max_kv_len}")
 
 
-def _rows3(t, heads, dim, what):
-    """Check a [tokens, heads, head_dim] tensor whose heads are contiguous; its row distance in elements."""
+def _rows3(t, heads, dim, what, device):
+    """Check a [tokens, heads, head_dim] tensor on the context's GPU whose heads are contiguous; its row distance in
+    elements."""
     shape, stride = t.shape, t.stride()
+    if t.get_device() != device:
+        raise ValueError(f"{what}: a tensor on GPU {device} expected, got one on {t.device}")
     if len(shape) != 3 or shape[1] != heads or shape[2] != dim or stride[2] != 1 or (heads > 1 and stride[1] != dim):
         raise ValueError(f"{what}: [tokens, {heads}, {dim}] with contiguous heads expected, got {tuple(shape)} "
                          f"strides {stride}")
@@ -514,14 +525,17 @@ class Context:
         if some is None:
             raise ValueError("keys, values or both")
         heads, dim = cache.kv_heads, cache.head_dim
-        _check_table(cache, batch)
-        ld_k = _rows3(k, heads, dim, "keys") if k is not None else 0
-        ld_v = _rows3(v, heads, dim, "values") if v is not None else 0
+        _check_handles(cache, batch, self.device)
+        ld_k = _rows3(k, heads, dim, "keys", self.device) if k is not None else 0
+        ld_v = _rows3(v, heads, dim, "values", self.device) if v is not None else 0
         if k is not None and v is not None and (k.dtype != v.dtype or k.shape[0] != v.shape[0]):
             raise ValueError("keys and values of one shape and type")
+        dt = _DT.get(some.dtype)
+        if dt is None:
+            raise ValueError(f"keys and values: bf16, fp16 or fp32, got {some.dtype}")
         batch._desc.tokens = some.shape[0]
         status = fn(self._h, cache._ref, batch._ref, None if k is None else k.data_ptr(), None if v is None else v.data_ptr(),
-                    _DT[some.dtype], ld_k, ld_v, cache.conv, _raw_stream(self.device))
+                    dt, ld_k, ld_v, cache.conv, _raw_stream(self.device))
         if status:
             _check(status, name)
 
@@ -537,15 +551,17 @@ class Context:
         """``fp8_attn_paged``: q, out [tokens, q_heads, head_dim] bf16, lse float32 [tokens, q_heads] or None; scale
         1 / sqrt(head_dim) by default."""
         shape, dim = q.shape, cache.head_dim
+        if len(shape) != 3:
+            raise ValueError(f"q: [tokens, q_heads, {dim}] expected, got {tuple(shape)}")
         heads = shape[1]
-        _check_table(cache, batch)
-        ld_q, ld_o = _rows3(q, heads, dim, "q"), _rows3(out, heads, dim, "out")
+        _check_handles(cache, batch, self.device)
+        ld_q, ld_o = _rows3(q, heads, dim, "q", self.device), _rows3(out, heads, dim, "out", self.device)
         if q.dtype != torch.bfloat16 or out.dtype != torch.bfloat16 or out.shape[0] != shape[0]:
             raise ValueError("q and out: bf16 tensors of one shape")
         lse_ptr = None
         if lse is not None:
-            if lse.dtype != torch.float32 or lse.shape != shape[:2] or not lse.is_contiguous():
-                raise ValueError("lse: contiguous float32 [tokens, q_heads]")
+            if lse.dtype != torch.float32 or lse.shape != shape[:2] or not lse.is_contiguous() or lse.get_device() != self.device:
+                raise ValueError("lse: contiguous float32 [tokens, q_heads] on the context's GPU")
             lse_ptr = lse.data_ptr()
         batch._desc.tokens = shape[0]
         status = _lib.fp8_attn_paged(self._h, cache._ref, batch._ref, q.data_ptr(), ld_q, heads, out.data_ptr(), ld_o, lse_ptr,

@@ -62,3 +62,31 @@ def test_a_table_slice_with_too_few_columns_is_refused(ctx):
 def test_lengths_are_one_per_sequence():
     with pytest.raises(ValueError):
         fp8lin.SeqBatch(zeros(3, dtype=torch.int32), zeros(2, 2, dtype=torch.int32), zeros(2, 8, dtype=torch.int32), 4, 33)
+
+
+def test_tensors_in_host_memory_are_refused(ctx):
+    cache, batch = cache_of(), batch_of(zeros(2, 8, dtype=torch.int32), 33)
+    rows, q = zeros(4, 2, 64), zeros(4, 4, 64)
+    host, host_q = torch.zeros((4, 2, 64), dtype=torch.bfloat16), torch.zeros((4, 4, 64), dtype=torch.bfloat16)
+    lse = torch.zeros((4, 4))
+    for call in (lambda: ctx.kv_append(cache, batch, host, rows), lambda: ctx.kv_append(cache, batch, rows, host),
+                 lambda: ctx.kv_read(cache, batch, None, host), lambda: ctx.attn_paged(cache, batch, host_q, q),
+                 lambda: ctx.attn_paged(cache, batch, q, host_q), lambda: ctx.attn_paged(cache, batch, q, q, lse=lse)):
+        with pytest.raises(ValueError, match="GPU"):
+            call()
+
+
+def test_other_types_and_shapes_are_refused(ctx):
+    cache, batch = cache_of(), batch_of(zeros(2, 8, dtype=torch.int32), 33)
+    rows = zeros(4, 2, 64, dtype=torch.float64)
+    with pytest.raises(ValueError, match="bf16, fp16 or fp32"):
+        ctx.kv_append(cache, batch, rows, rows)
+    with pytest.raises(ValueError):
+        ctx.attn_paged(cache, batch, zeros(256), zeros(256))
+
+
+def test_handles_of_another_gpu_are_refused(ctx):
+    ctx.device = 1
+    for call in calls(ctx, cache_of(), batch_of(zeros(2, 8, dtype=torch.int32), 33)):
+        with pytest.raises(ValueError, match="GPU 1"):
+            call()
