@@ -248,6 +248,16 @@ class SeqBatch:
         self._desc = SeqBatchDesc(q_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(),
                                   page_table.stride(0) if seqs > 1 else self._width, seqs, 0, max_q_len, max_kv_len)
         self._ref = byref(self._desc)
+        self._by_tokens = {}
+
+    def _of(self, tokens):
+        """The descriptor for a call on that many rows.  Calls change no descriptor, so threads can share a batch."""
+        ref = self._by_tokens.get(tokens)
+        if ref is None:
+            desc = SeqBatchDesc.from_buffer_copy(self._desc)
+            desc.tokens = tokens
+            ref = self._by_tokens.setdefault(tokens, byref(desc))
+        return ref
 
 
 def _check_handles(cache, batch, device):
@@ -533,8 +543,7 @@ class Context:
         dt = _DT.get(some.dtype)
         if dt is None:
             raise ValueError(f"keys and values: bf16, fp16 or fp32, got {some.dtype}")
-        batch._desc.tokens = some.shape[0]
-        status = fn(self._h, cache._ref, batch._ref, None if k is None else k.data_ptr(), None if v is None else v.data_ptr(),
+        status = fn(self._h, cache._ref, batch._of(some.shape[0]), None if k is None else k.data_ptr(), None if v is None else v.data_ptr(),
                     dt, ld_k, ld_v, cache.conv, _raw_stream(self.device))
         if status:
             _check(status, name)
@@ -563,8 +572,7 @@ class Context:
             if lse.dtype != torch.float32 or lse.shape != shape[:2] or not lse.is_contiguous() or lse.get_device() != self.device:
                 raise ValueError("lse: contiguous float32 [tokens, q_heads] on the context's GPU")
             lse_ptr = lse.data_ptr()
-        batch._desc.tokens = shape[0]
-        status = _lib.fp8_attn_paged(self._h, cache._ref, batch._ref, q.data_ptr(), ld_q, heads, out.data_ptr(), ld_o, lse_ptr,
+        status = _lib.fp8_attn_paged(self._h, cache._ref, batch._of(shape[0]), q.data_ptr(), ld_q, heads, out.data_ptr(), ld_o, lse_ptr,
                                      dim ** -0.5 if scale is None else scale, 1 if causal else 0, cache.conv,
                                      _raw_stream(self.device))
         if status:

@@ -90,3 +90,22 @@ def test_handles_of_another_gpu_are_refused(ctx):
     for call in calls(ctx, cache_of(), batch_of(zeros(2, 8, dtype=torch.int32), 33)):
         with pytest.raises(ValueError, match="GPU 1"):
             call()
+
+
+def test_calls_leave_a_shared_batch_as_it_is(ctx, monkeypatch):
+    """Two threads on one batch: a call sees its own number of rows, whatever another call sets in between."""
+    cache, batch = cache_of(), batch_of(zeros(2, 8, dtype=torch.int32), 33)
+    before, seen = bytes(batch._desc), []
+
+    def library(h, cache_ref, batch_ref, *rest):
+        seen.append((batch_ref._obj.tokens, batch_ref._obj.seqs, batch_ref._obj.max_kv_len))
+        if len(seen) == 1:                                        # a call of another thread, before this one reads
+            ctx.kv_append(cache, batch, zeros(7, 2, 64), zeros(7, 2, 64))
+            seen.append((batch_ref._obj.tokens, batch_ref._obj.seqs, batch_ref._obj.max_kv_len))
+        return fp8lin.OK
+
+    monkeypatch.setattr(fp8lin._lib, "fp8_kv_append", library)
+    monkeypatch.setattr(fp8lin, "_raw_stream", lambda device: None)
+    ctx.kv_append(cache, batch, zeros(4, 2, 64), zeros(4, 2, 64))
+    assert seen == [(4, 2, 33), (7, 2, 33), (4, 2, 33)]
+    assert bytes(batch._desc) == before
