@@ -51,7 +51,7 @@ typedef struct {
  *                 the last of them: row d_q_start[b] + i is token d_kv_len[b] - (rows of b) + i
  *   d_page_table  device int32, rows table_stride apart: page of tokens page_size * p .. page_size * (p + 1) - 1 at index p;
  *                 every row, the last one too, has ceil(max_kv_len / page_size) entries
- *   tokens        rows of q, k, v and out
+ *   tokens        rows of q, k, v and out, at least one
  *   max_q_len     bound of the rows of one sequence;  max_kv_len  bound of d_kv_len.  Both bound the launch, so tight
  *                 values cost least; sequences beyond them are cut and FP8_FLAG_BAD_INDEX is raised. */
 typedef struct {

@@ -529,7 +529,7 @@ class Context:
         _check(_lib.fp8_linear_wgrad(self._h, _ptr(dy8), _ptr(dy8_t), _ptr(d_bg), _ptr(x8), _ptr(x8_t), _ptr(d_bx),
                                      _ptr(dw), _DT[dw.dtype], T, K, N, conv, _stream()), "fp8_linear_wgrad")
 
-    # -- paged FP8 cache ----------------------------------------------------------
+    # -- paged FP8 cache (calls without rows check their arguments and launch nothing) -------------
     def _kv(self, fn, name, cache, batch, k, v):
         some = k if k is not None else v
         if some is None:
@@ -543,6 +543,8 @@ class Context:
         dt = _DT.get(some.dtype)
         if dt is None:
             raise ValueError(f"keys and values: bf16, fp16 or fp32, got {some.dtype}")
+        if some.shape[0] == 0:
+            return
         status = fn(self._h, cache._ref, batch._of(some.shape[0]), None if k is None else k.data_ptr(), None if v is None else v.data_ptr(),
                     dt, ld_k, ld_v, cache.conv, _raw_stream(self.device))
         if status:
@@ -572,6 +574,8 @@ class Context:
             if lse.dtype != torch.float32 or lse.shape != shape[:2] or not lse.is_contiguous() or lse.get_device() != self.device:
                 raise ValueError("lse: contiguous float32 [tokens, q_heads] on the context's GPU")
             lse_ptr = lse.data_ptr()
+        if shape[0] == 0:
+            return
         status = _lib.fp8_attn_paged(self._h, cache._ref, batch._of(shape[0]), q.data_ptr(), ld_q, heads, out.data_ptr(), ld_o, lse_ptr,
                                      dim ** -0.5 if scale is None else scale, 1 if causal else 0, cache.conv,
                                      _raw_stream(self.device))

@@ -63,15 +63,16 @@ class PagePool:
         for n in new_tokens:
             start.append(start[-1] + n)
         lens = [self.length(s) for s in seqs]
-        width = max(1, max(-(-n // self.page_size) for n in lens))
+        width = max([1] + [-(-n // self.page_size) for n in lens])
         rows = [(self._pages.get(s, []) + [0] * width)[:width] for s in seqs]
         return start, lens, rows
 
     def batch(self, seqs: Sequence, new_tokens: Sequence[int], device="cuda") -> "fp8lin.SeqBatch":
         start, lens, rows = self.indices(seqs, new_tokens)
         i32 = dict(dtype=torch.int32, device=device)
-        return fp8lin.SeqBatch(torch.tensor(start, **i32), torch.tensor(lens, **i32), torch.tensor(rows, **i32),
-                               max_q_len=max(1, max(new_tokens)), max_kv_len=max(1, max(lens)))
+        return fp8lin.SeqBatch(torch.tensor(start, **i32), torch.tensor(lens, **i32),
+                               torch.tensor(rows, **i32).view(len(lens), -1 if lens else 1),
+                               max_q_len=max([1, *new_tokens]), max_kv_len=max([1, *lens]))
 
 
 def empty_cache(pages: int, kv_heads: int, page_size: int, head_dim: int, conv: int = fp8lin.CONV_PAPER, device="cuda"):
@@ -101,6 +102,8 @@ class Fp8SelfAttention(torch.nn.Module):
 
     @torch.no_grad()
     def forward(self, x: torch.Tensor, batch: "fp8lin.SeqBatch") -> torch.Tensor:
+        if x.shape[0] == 0:                  # no sequence has new tokens
+            return torch.empty_like(x)
         hq, hk = self.q_heads, self.kv_heads
         qkv = self.qkv(x).unflatten(1, (hq + 2 * hk, self.head_dim))
         q, k, v = qkv[:, :hq], qkv[:, hq:hq + hk], qkv[:, hq + hk:]

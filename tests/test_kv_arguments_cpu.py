@@ -109,3 +109,28 @@ def test_calls_leave_a_shared_batch_as_it_is(ctx, monkeypatch):
     ctx.kv_append(cache, batch, zeros(4, 2, 64), zeros(4, 2, 64))
     assert seen == [(4, 2, 33), (7, 2, 33), (4, 2, 33)]
     assert bytes(batch._desc) == before
+
+
+def test_calls_without_rows_launch_nothing(ctx, monkeypatch):
+    def library(*args):
+        raise AssertionError("called")
+    for name in ("fp8_kv_append", "fp8_kv_read", "fp8_attn_paged"):
+        monkeypatch.setattr(fp8lin._lib, name, library)
+    cache, batch = cache_of(), batch_of(zeros(2, 8, dtype=torch.int32), 33)
+    rows, q = zeros(0, 2, 64), zeros(0, 4, 64)
+    ctx.kv_append(cache, batch, rows, rows)
+    ctx.kv_read(cache, batch, rows, None)
+    ctx.attn_paged(cache, batch, q, q)
+    with pytest.raises(ValueError):
+        ctx.attn_paged(cache, batch, q, zeros(1, 4, 64))
+
+
+def test_a_pool_makes_batches_without_rows(monkeypatch):
+    from paper_2309_17224_b200 import serving
+    make = torch.tensor
+    monkeypatch.setattr(serving.torch, "tensor", lambda data, dtype, device: on_gpu(make(data, dtype=dtype)))
+    pool = serving.PagePool(4, 16)
+    pool.extend(["a", "b"], [20, 0])
+    for seqs in (["a"], ["a", "b"], []):
+        batch = pool.batch(seqs, [0] * len(seqs))
+        assert batch.q_start.tolist() == [0] * (len(seqs) + 1) and batch.page_table.shape[0] == len(seqs)
