@@ -83,21 +83,24 @@ def empty_cache(pages: int, kv_heads: int, page_size: int, head_dim: int, conv: 
 
 
 class Fp8SelfAttention(torch.nn.Module):
-    """Self-attention of a decoder layer for inference: x [tokens, hidden] bf16 -> [tokens, hidden] bf16.
+    """Self-attention of a decoder layer for inference: x [tokens, hidden] -> [tokens, hidden] bf16.
 
     The tokens are those of ``batch`` (``PagePool.batch``), sequence after sequence; their keys and values enter ``cache``
-    and each attends causally to its sequence's cached tokens."""
+    and each attends causally to its sequence's cached tokens.  Calls that share ``ctx`` (by default the device's
+    ``default_context``) must not overlap on the GPU: a program that runs prefill and decoding on two streams gives the layers
+    of each a context of its own."""
 
     def __init__(self, hidden: int, q_heads: int, kv_heads: int, head_dim: int, cache: "fp8lin.KvCache", device="cuda",
-                 rotate: Optional[Callable[[torch.Tensor, torch.Tensor, "fp8lin.SeqBatch"], None]] = None):
+                 rotate: Optional[Callable[[torch.Tensor, torch.Tensor, "fp8lin.SeqBatch"], None]] = None,
+                 ctx: Optional["fp8lin.Context"] = None):
         super().__init__()
         if q_heads % kv_heads or (cache.kv_heads, cache.head_dim) != (kv_heads, head_dim):
             raise ValueError("q_heads a multiple of kv_heads; the cache has this layer's kv_heads and head_dim")
         self.q_heads, self.kv_heads, self.head_dim = q_heads, kv_heads, head_dim
         self.cache, self.rotate = cache, rotate
-        self.qkv = Fp8Linear(hidden, (q_heads + 2 * kv_heads) * head_dim, device=device)
-        self.out = Fp8Linear(q_heads * head_dim, hidden, device=device)
-        self.ctx = default_context(torch.device(device).index or 0)
+        self.ctx = ctx if ctx is not None else default_context(torch.device(device).index or 0)
+        self.qkv = Fp8Linear(hidden, (q_heads + 2 * kv_heads) * head_dim, device=device, ctx=self.ctx)
+        self.out = Fp8Linear(q_heads * head_dim, hidden, device=device, ctx=self.ctx)
         self.eval()
 
     @torch.no_grad()
