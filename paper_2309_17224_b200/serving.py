@@ -83,7 +83,7 @@ def empty_cache(pages: int, kv_heads: int, page_size: int, head_dim: int, conv: 
 
 
 class Fp8SelfAttention(torch.nn.Module):
-    """Self-attention of a decoder layer for inference: x [tokens, hidden] -> [tokens, hidden] bf16.
+    """Self-attention of a decoder layer for inference: x [tokens, hidden] bf16, fp16 or fp32 -> [tokens, hidden] bf16.
 
     The tokens are those of ``batch`` (``PagePool.batch``), sequence after sequence; their keys and values enter ``cache``
     and each attends causally to its sequence's cached tokens.  Calls that share ``ctx`` (by default the device's
@@ -99,14 +99,15 @@ class Fp8SelfAttention(torch.nn.Module):
         self.q_heads, self.kv_heads, self.head_dim = q_heads, kv_heads, head_dim
         self.cache, self.rotate = cache, rotate
         self.ctx = ctx if ctx is not None else default_context(torch.device(device).index or 0)
-        self.qkv = Fp8Linear(hidden, (q_heads + 2 * kv_heads) * head_dim, device=device, ctx=self.ctx)
+        # (attention reads bf16 queries whatever x is)
+        self.qkv = Fp8Linear(hidden, (q_heads + 2 * kv_heads) * head_dim, device=device, out_dtype=torch.bfloat16, ctx=self.ctx)
         self.out = Fp8Linear(q_heads * head_dim, hidden, device=device, ctx=self.ctx)
         self.eval()
 
     @torch.no_grad()
     def forward(self, x: torch.Tensor, batch: "fp8lin.SeqBatch") -> torch.Tensor:
         if x.shape[0] == 0:                  # no sequence has new tokens
-            return torch.empty_like(x)
+            return torch.empty(x.shape, dtype=torch.bfloat16, device=x.device)
         hq, hk = self.q_heads, self.kv_heads
         qkv = self.qkv(x).unflatten(1, (hq + 2 * hk, self.head_dim))
         q, k, v = qkv[:, :hq], qkv[:, hq:hq + hk], qkv[:, hq + hk:]

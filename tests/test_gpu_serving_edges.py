@@ -42,3 +42,21 @@ def test_layers_of_two_streams_have_contexts_of_their_own():
     torch.cuda.synchronize()
     for w, many in zip(want, got):
         assert all(torch.equal(w, y) for y in many)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
+@pytest.mark.parametrize("tokens", [1, 200])
+def test_inputs_of_other_types_give_the_same_bits(dtype, tokens):
+    """Numbers that all three types hold: the same bytes after quantisation, so the same output and the same cache."""
+    from paper_2309_17224_b200 import serving
+    layer = serving.Fp8SelfAttention(256, 8, 2, 64, serving.empty_cache(16, 2, 16, 64))
+    g = torch.Generator(device="cuda").manual_seed(10)
+    x = torch.randint(-64, 65, (tokens, 256), generator=g, device="cuda").to(torch.bfloat16)
+    pool = serving.PagePool(16, 16)
+    pool.extend(["a"], [tokens])
+    batch = pool.batch(["a"], [tokens])
+    want, cache = layer(x, batch), layer.cache.k8.clone()
+    got = layer(x.to(dtype), batch)
+    assert got.dtype == torch.bfloat16 and torch.equal(got, want)
+    pages = batch.page_table.flatten().long()
+    assert torch.equal(layer.cache.k8[pages[:-1]], cache[pages[:-1]])
