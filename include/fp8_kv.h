@@ -85,6 +85,7 @@ FP8_API fp8_status_t fp8_kv_read(fp8_ctx *ctx, const fp8_kv_cache_t *cache, cons
  *   out    [tokens][q_heads][head_dim] bf16, rows ld_o elements apart
  *   d_lse  NULL, or out float [tokens][q_heads]: ln sum_j p_j (what joining with attention over other keys needs)
  * A row that sees no token gives zeros and -infinity.  A query row with an infinity or a NaN gives NaN.
+ * Sequences have at most 2^30 tokens, also where max_kv_len is larger.
  * q_heads a multiple of kv_heads; q and out 16-byte aligned, ld_q and ld_o multiples of 8.  Calls that share one
  * fp8_ctx must not overlap on the device, like decode-size matmuls (long contexts are split across SMs and joined in
  * the context's workspace); they follow each other on one stream like any calls. */

@@ -25,6 +25,8 @@ fp8_status_t fp8_attn_paged(fp8_ctx *ctx, const fp8_kv_cache_t *c, const fp8_seq
         return FP8_ERR_ALIGN;
     AttnParams p;
     p.kv = make_kv_params(ctx, c, batch, (int)conv);
+    // sums of a length and a row's place then stay within 32 bits (2^30 tokens of one head are 128 GB of cache)
+    if (p.kv.max_kv_len > 1 << 30) p.kv.max_kv_len = 1 << 30;
     p.q = static_cast<const uint16_t *>(q);
     p.out = static_cast<uint16_t *>(out);
     p.lse = d_lse;

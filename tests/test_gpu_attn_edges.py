@@ -51,3 +51,22 @@ def test_units_of_two_tiles_and_of_one_share_the_columns_in_turn(lib, ctx, dim, 
     check(*outs[0], want)
     for o, l in outs[1:]:
         assert torch.equal(o.view(torch.int16), outs[0][0].view(torch.int16)) and torch.equal(l, outs[0][1])
+
+
+@pytest.mark.parametrize("news", [1, 40])
+@pytest.mark.parametrize("bound", [2 ** 31 - 1, 2 ** 31 - 100, 2 ** 30])
+def test_the_largest_length_bounds(lib, ctx, news, bound):
+    """A bound that says nothing (one sequence, so its table needs no second row) gives what a tight one gives."""
+    case = R.make_case(42, [90], [news], 2, 64, 16, O.CONV_PAPER)
+    dev, cache, batch = gpu_state(lib, case, O.CONV_PAPER, news, 90)
+    q = torch.randn((news, 8, 64), generator=case["g"]).to(torch.bfloat16).cuda()
+    want, out = torch.empty_like(q), torch.zeros_like(q)
+    ctx.attn_paged(cache, batch, q, want)
+    desc = type(batch._desc).from_buffer_copy(batch._desc)
+    desc.tokens, desc.max_kv_len, desc.table_stride = news, bound, 1 << 27
+    ctx.device_flags()
+    status = lib.raw().fp8_attn_paged(ctx._h, cache._ref, lib.byref(desc), q.data_ptr(), 512, 8, out.data_ptr(), 512, None,
+                                      64 ** -0.5, 1, cache.conv, None)
+    torch.cuda.synchronize()
+    assert status == lib.OK and ctx.device_flags() == 0
+    assert torch.allclose(out.float(), want.float(), rtol=2.0 ** -7, atol=2.0 ** -10)
