@@ -28,8 +28,10 @@ extern "C" {
 #define FP8_KV_BIAS_MAX 64
 
 /* Sticky device status bit, beside those of fp8lin.h: a page number outside the cache, or a length that contradicts
- * the bounds given on the host, was met.  No access out of range was made: nothing is written to such a page, its
- * tokens read back as zeros, queries that see them give NaN; lengths are cut to the bounds. */
+ * the bounds given on the host, was met, or a row that belongs to no sequence.  No access out of range was made: nothing is
+ * written to such a page, its tokens read back as zeros, queries that see them give NaN.  Of a sequence beyond its bounds
+ * the rows from max_q_len and the tokens from max_kv_len on are left out; the others keep their places.  Rows that are left
+ * out, and rows of no sequence, are not cached, read back as zeros, and attend to nothing (zeros, lse -infinity). */
 #define FP8_FLAG_BAD_INDEX 16u
 
 /* The cache of one layer: `pages` pages, each holding page_size tokens of every key/value head.
@@ -53,7 +55,7 @@ typedef struct {
  *                 every row, the last one too, has ceil(max_kv_len / page_size) entries
  *   tokens        rows of q, k, v and out, at least one
  *   max_q_len     bound of the rows of one sequence;  max_kv_len  bound of d_kv_len.  Both bound the launch, so tight
- *                 values cost least; sequences beyond them are cut and FP8_FLAG_BAD_INDEX is raised. */
+ *                 values cost least; of sequences beyond them the rest is left out (FP8_FLAG_BAD_INDEX). */
 typedef struct {
     const int32_t *d_q_start, *d_kv_len, *d_page_table;
     int64_t table_stride;

@@ -214,8 +214,7 @@ __device__ __forceinline__ int entry_of(const AttnParams &p, int e, SeqShape &s,
     row0 = (e - b * p.row_tiles) * kUnitRows;
     rows = (int)min((int64_t)s.n * p.group - row0, (int64_t)kUnitRows);
     if (rows <= 0) return 0;
-    int see = s.len;
-    if (p.causal) see = min(s.len, max(0, s.len - s.n + (row0 + rows - 1) / p.group + 1));
+    const int see = tokens_seen(s, p.causal, (row0 + rows - 1) / p.group);
     return max(1, (see + kTile - 1) / kTile);
 }
 
@@ -328,7 +327,7 @@ __device__ __forceinline__ f32x2 weights_of_row(f32x2 (&u)[kSpan / 2], f32x2 rc2
 }
 
 template <int D>
-__global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const AttnParams p)
+__global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ AttnParams p)
 {
     using L = ChunkShape<D>;
     constexpr int kFirstValueWarp = 8, kProductWarp = 12;
@@ -339,7 +338,10 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
     // ---- the CTA's share of the list ----
     bool cut;
     const int64_t total = list_length(p, lane, cut);
-    if (blockIdx.x == 0 && warp == 0 && __any_sync(0xFFFFFFFFu, cut) && lane == 0) raise_flags(kv.d_status, FP8_FLAG_BAD_INDEX);
+    if (__builtin_expect(__any_sync(0xFFFFFFFFu, cut), 0)) {
+        if (blockIdx.x == 0 && warp == 0 && lane == 0) raise_flags(kv.d_status, FP8_FLAG_BAD_INDEX);
+        write_left_out_rows(kv, p.out, p.ld_o, p.lse, p.q_heads, D);
+    }
     const int64_t share = max((total + gridDim.x - 1) / (int64_t)gridDim.x, (int64_t)p.min_share);
     const int64_t begin = blockIdx.x * share, end = min(total, begin + share);
     if (begin >= end) return;
@@ -683,8 +685,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
                         mbar_arrive(q_full(slot));
                     }
                 }
-                int limit = s.len;       // tokens that the row sees
-                if (p.causal) limit = min(s.len, max(0, s.len - s.n + (row0 + r) / p.group + 1));
+                const int limit = tokens_seen(s, p.causal, (row0 + r) / p.group);
                 const int least = __shfl_sync(0xFFFFFFFFu, limit, 0);   // the warp's first row sees least
                 const bool active = (warp & 3) * 32 < rows;
                 float top = kNoMax;

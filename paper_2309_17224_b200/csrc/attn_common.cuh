@@ -76,25 +76,53 @@ __device__ __forceinline__ void join_part(JoinedRow &a, float m, float l, float4
     a.m = top;
 }
 
-// A sequence's lengths, cut to the bounds of the launch.
+// A sequence's lengths, cut to the bounds of the launch, and the place of its first row: token pos of the sequence, from the
+// lengths as they were, so that a row of a sequence that was cut still sees what the cache has up to the row's own token.
 struct SeqShape {
-    int first, n, len;
+    int first, n, len, pos;
 };
+// tokens that the sequence's row i sees
+__device__ __forceinline__ int tokens_seen(const SeqShape &s, int causal, int i)
+{
+    return causal ? min(s.len, max(0, s.pos + i + 1)) : s.len;
+}
+// cut: something was cut, or rows before the first sequence or behind the last belong to none
 __device__ __forceinline__ SeqShape seq_shape(const KvParams &kv, int b, bool &cut)
 {
     SeqShape s;
     s.first = __ldg(kv.q_start + b);
     s.n = __ldg(kv.q_start + b + 1) - s.first;
     s.len = __ldg(kv.kv_len + b);
+    s.pos = s.len - s.n;
     cut = s.len < 0 || s.len > kv.max_kv_len || s.n < 0 || s.n > kv.max_q_len || s.first < 0 || s.first > kv.tokens ||
-          s.n > kv.tokens - s.first;
+          s.n > kv.tokens - s.first || (b == 0 && s.first != 0) || (b == kv.seqs - 1 && s.n != kv.tokens - s.first);
     if (cut) {
+        // (sums of a place and a row stay within 32 bits: lengths and rows are at most 2^30)
+        s.pos = (int)max(-(1ll << 30), min((long long)s.len - s.n, 1ll << 30));
         s.len = min(max(s.len, 0), kv.max_kv_len);
         s.n = min(max(s.n, 0), kv.max_q_len);
         if (s.first < 0 || s.first > kv.tokens) s.n = 0;
         else s.n = min(s.n, kv.tokens - s.first);
     }
     return s;
+}
+
+// Rows that no sequence has within its bounds: zeros, and -infinity as their lse.  By all warps of the grid; only called
+// where something was cut.
+static __device__ __noinline__ void write_left_out_rows(const KvParams &kv, uint16_t *out, int64_t ld_o, float *lse, int q_heads, int d)
+{
+    const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    for (int64_t t = (int64_t)blockIdx.x * warps + (threadIdx.x >> 5); t < kv.tokens; t += (int64_t)gridDim.x * warps) {
+        const int b = find_sequence(kv.q_start, kv.seqs, (int)t, lane);
+        bool cut;
+        if (b >= 0) {
+            const SeqShape s = seq_shape(kv, b, cut);
+            if (t - s.first < s.n) continue;
+        }
+        for (int64_t i = lane * 8; i < (int64_t)q_heads * d; i += 32 * 8) *reinterpret_cast<uint4 *>(out + t * ld_o + i) = make_uint4(0, 0, 0, 0);
+        if (lse)
+            for (int h = lane; h < q_heads; h += 32) lse[t * q_heads + h] = -INFINITY;
+    }
 }
 
 #endif

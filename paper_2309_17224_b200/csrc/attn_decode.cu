@@ -138,7 +138,7 @@ struct Unit {
 __device__ __forceinline__ int unit_blocks(const SeqShape &s) { return s.n > 0 ? max(1, (s.len + kBlockTokens - 1) / kBlockTokens) : 0; }
 
 template <int D, int NT>
-__global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 4 : 2) attn_decode_kernel(const AttnParams p)
+__global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 4 : 2) attn_decode_kernel(const __grid_constant__ AttnParams p)
 {
     constexpr int kRows = 8 * NT;
     constexpr int kPart = kRows * (D + 2);       // floats of a partial result
@@ -160,7 +160,10 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 4 : 2) attn_decode_k
         }
         total += __reduce_add_sync(0xFFFFFFFFu, n);
     }
-    if (blockIdx.x == 0 && warp == 0 && __any_sync(0xFFFFFFFFu, any_cut) && lane == 0) raise_flags(kv.d_status, FP8_FLAG_BAD_INDEX);
+    if (__builtin_expect(__any_sync(0xFFFFFFFFu, any_cut), 0)) {
+        if (blockIdx.x == 0 && warp == 0 && lane == 0) raise_flags(kv.d_status, FP8_FLAG_BAD_INDEX);
+        write_left_out_rows(kv, p.out, p.ld_o, p.lse, p.q_heads, D);
+    }
     total *= kv.kv_heads;
     // at least one block per warp, so that short lists are not spread over CTAs that then wait for one another's sums
     const int64_t share = max((total + gridDim.x - 1) / (int64_t)gridDim.x, (int64_t)kDecodeWarps);
@@ -172,7 +175,7 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 4 : 2) attn_decode_k
     {
         int64_t before = 0;
         for (int b0 = 0;; b0 += 32) {
-            SeqShape s = {0, 0, 0};
+            SeqShape s = {0, 0, 0, 0};
             int n = 0;
             if (b0 + lane < kv.seqs) {
                 bool cut;
@@ -192,6 +195,7 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 4 : 2) attn_decode_k
                 u.s.first = __shfl_sync(0xFFFFFFFFu, s.first, l);
                 u.s.n = __shfl_sync(0xFFFFFFFFu, s.n, l);
                 u.s.len = __shfl_sync(0xFFFFFFFFu, s.len, l);
+                u.s.pos = __shfl_sync(0xFFFFFFFFu, s.pos, l);
                 u.blocks = __shfl_sync(0xFFFFFFFFu, n, l);
                 const int64_t start = before + __shfl_sync(0xFFFFFFFFu, upto, l) - (int64_t)u.blocks * kv.kv_heads;
                 u.h = (int)((at - start) / u.blocks);
@@ -235,7 +239,7 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 4 : 2) attn_decode_k
         uint32_t q[NT][D / 16][2];
         float rc[NT][2];          // c / that power, for the rows of S^T's columns
         int limit[NT][2];         // tokens those rows see
-        int all_see = u.s.len;    // tokens that every row sees
+        const int all_see = tokens_seen(u.s, p.causal, 0);    // tokens that every row sees
         {
             float mine[NT];
 #pragma unroll
@@ -271,11 +275,9 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 4 : 2) attn_decode_k
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     rc[j][k] = __shfl_sync(0xFFFFFFFFu, mine[j], (2 * t + k) * 4);
-                    limit[j][k] = u.s.len;
-                    if (p.causal) limit[j][k] = min(u.s.len, max(0, u.s.len - u.s.n + (8 * j + 2 * t + k) / p.group + 1));
+                    limit[j][k] = tokens_seen(u.s, p.causal, (8 * j + 2 * t + k) / p.group);
                 }
             }
-            if (p.causal) all_see = max(0, u.s.len - u.s.n + 1);
         }
 
         float o[NT][D / 16][4], top[NT][2], l[NT][2];

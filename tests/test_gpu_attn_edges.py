@@ -70,3 +70,70 @@ def test_the_largest_length_bounds(lib, ctx, news, bound):
     torch.cuda.synchronize()
     assert status == lib.OK and ctx.device_flags() == 0
     assert torch.allclose(out.float(), want.float(), rtol=2.0 ** -7, atol=2.0 ** -10)
+
+
+@pytest.mark.parametrize("q_heads,kv_heads,dim", [(2, 2, 128), (4, 2, 64), (16, 2, 128), (64, 1, 64)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_rows_of_a_cut_sequence_keep_their_places(lib, ctx, q_heads, kv_heads, dim, causal):
+    """Sequence 1 has more rows than the bound says, sequence 2 more tokens, three rows come before the first sequence and five
+    behind the last: what is left out gives zeros and -infinity, every other row what the 64-bit rows give at its place."""
+    lens, news, most_q, most_kv = [50, 70, 100, 33], [5, 10, 7, 8], 8, 96
+    case = R.make_case(43, lens, news, kv_heads, dim, 16, O.CONV_PAPER, fill=0x7F)
+    dev, cache, batch = gpu_state(lib, case, O.CONV_PAPER, most_q, most_kv)
+    dev["q_start"] += 3
+    rows = 3 + sum(news) + 5
+    q = torch.randn((rows, q_heads, dim), generator=case["g"]).to(torch.bfloat16)
+    out = torch.full((rows, q_heads, dim), 7.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((rows, q_heads), 7.0, device="cuda")
+    ctx.device_flags()
+    ctx.attn_paged(cache, batch, q.cuda(), out, causal=causal, lse=lse)
+    assert ctx.device_flags() == lib.FLAG_BAD_INDEX
+    # one row at a time: a sequence of one new token whose length is what the row sees
+    cpu = [case[n].numpy() for n in ("k8", "v8", "bk", "bv")]
+    kept, sees, table = [], [], []
+    for b, (length, n) in enumerate(zip(lens, news)):
+        for i in range(min(n, most_q)):
+            kept.append(3 + sum(news[:b]) + i)
+            sees.append(min(length, most_kv, length - n + i + 1 if causal else length))
+            table.append(case["table"].numpy()[b])
+    want = R.attention(cpu, np.array(table), list(range(len(kept) + 1)), sees, q[kept].double().numpy(), dim ** -0.5, True, O.CONV_PAPER)
+    check(out[kept], lse[kept], want)
+    left = sorted(set(range(rows)) - set(kept))
+    assert (out[left] == 0).all() and torch.isneginf(lse[left]).all()
+
+
+@pytest.mark.parametrize("news", [1, 30])
+def test_more_rows_than_the_sequences_have(lib, ctx, news):
+    """A batch padded to a fixed number of rows, with empty sequences at its end: the padding is zeros, nothing else changes."""
+    case = R.make_case(44, [40, 300, 0, 0], [news, news, 0, 0], 2, 128, 32, O.CONV_NATIVE)
+    dev, cache, batch = gpu_state(lib, case, O.CONV_NATIVE, news, 300)
+    q = torch.randn((2 * news + 700, 8, 128), generator=case["g"]).to(torch.bfloat16).cuda()
+    want, want_lse = torch.empty_like(q[:2 * news]), torch.empty((2 * news, 8), device="cuda")
+    ctx.device_flags()
+    ctx.attn_paged(cache, batch, q[:2 * news], want, lse=want_lse)
+    assert ctx.device_flags() == 0
+    wide = torch.full((q.shape[0], 9, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full(q.shape[:2], 7.0, device="cuda")
+    ctx.attn_paged(cache, batch, q, wide[:, :8], lse=lse)
+    assert ctx.device_flags() == lib.FLAG_BAD_INDEX
+    assert torch.equal(wide[:2 * news, :8].contiguous().view(torch.int16), want.view(torch.int16)) and torch.equal(lse[:2 * news], want_lse)
+    assert (wide[2 * news:, :8] == 0).all() and torch.isneginf(lse[2 * news:]).all() and (wide[:, 8] == 7.0).all()
+
+
+def test_append_and_attention_agree_on_a_cut_sequence(lib, ctx):
+    """Ten rows under a bound of eight: the rows that enter the cache are the ones that the kept queries see as their own."""
+    conv, dim = O.CONV_NATIVE, 64
+    for heads in ((2, 2), (16, 2)):
+        case = R.make_case(45, [100], [10], heads[1], dim, 16, conv)
+        dev, cache, batch = gpu_state(lib, case, conv, 8, 100)
+        k, v = (torch.randn((10, heads[1], dim), generator=case["g"]).to(torch.bfloat16).cuda() for _ in range(2))
+        q = torch.randn((10, heads[0], dim), generator=case["g"]).to(torch.bfloat16)
+        ctx.kv_append(cache, batch, k, v)
+        out, lse = torch.empty((10, heads[0], dim), dtype=torch.bfloat16, device="cuda"), torch.empty((10, heads[0]), device="cuda")
+        ctx.attn_paged(cache, batch, q.cuda(), out, lse=lse)
+        cpu = [dev[n].cpu().numpy() for n in ("k8", "v8", "bk", "bv")]
+        own, _ = R.quantise_row(k[7, 0].double().cpu().numpy(), conv)
+        assert np.array_equal(R.cached_rows(cpu, case["table"].numpy(), 0, np.array([97]))[0][0, 0], own)
+        want = R.attention(cpu, case["table"].numpy(), [0, 10], [100], q.double().numpy(), dim ** -0.5, True, conv)
+        check(out[:8], lse[:8], tuple(x[:8] for x in want))
+        ctx.device_flags()
