@@ -33,13 +33,19 @@ fp8_status_t fp8_attn_paged(fp8_ctx *ctx, const fp8_kv_cache_t *c, const fp8_seq
     p.ld_q = ld_q;
     p.ld_o = ld_o;
     p.part = ctx->d_partial;
-    p.count = ctx->d_attn_count;
     p.q_heads = q_heads;
     p.group = q_heads / c->kv_heads;
     p.causal = causal != 0;
     p.c = scale * 1.44269504088896341f;
     const int64_t rows = (int64_t)batch->max_q_len * p.group;
     if (rows > (int64_t)1 << 30) return FP8_ERR_SHAPE;
+    // Every call counts arrivals under a number of its own.  A captured call has the same number in every replay, so captured
+    // calls have sets of counters of their own too, which no other call leaves anything in.
+    cudaStreamCaptureStatus capture;
+    if (cudaStreamIsCapturing((cudaStream_t)stream, &capture) != cudaSuccess) return FP8_ERR_CUDA;
+    const unsigned set = capture == cudaStreamCaptureStatusNone ? 0u : 1u + ctx->attn_captured++ % (kAttnSets - 1);
+    p.count = ctx->d_attn_count + (size_t)set * kAttnCounters;
+    p.call = ++ctx->attn_calls;
     // at most 16 query rows per key/value head: the kernel whose instructions take 8 or 16 rows; more: tiles of 128
     if (rows <= 16) return attn_decode(ctx, p, c->head_dim, (int)rows, (cudaStream_t)stream);
     return attn_chunk(ctx, p, c, (cudaStream_t)stream);

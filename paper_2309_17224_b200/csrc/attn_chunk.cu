@@ -834,11 +834,11 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
                         }
                         __threadfence();
                         if (!(alive = sync_slot())) break;
-                        if (r == 0) is_last[slot] = atomicAdd(p.count + first_cta * 2 + qt, 1u) == (unsigned)(last_cta - first_cta);
+                        if (r == 0) is_last[slot] = arrive(p.count + first_cta * 2 + qt, p.call) == (unsigned)(last_cta - first_cta);
                         if (!(alive = sync_slot())) break;
                         if (is_last[slot]) {
                             __threadfence();
-                            if (r == 0) p.count[first_cta * 2 + qt] = 0u;
+                            if (r == 0) p.count[first_cta * 2 + qt] = 0ull;   // a captured call comes again under its number
                             // the first part lies in its CTA's place 1 (it starts at the unit's beginning), the others in place 0
                             auto part_of = [&](int64_t cta) { return p.part + ((cta * 2 + (cta == first_cta ? 1 : 0)) * 2 + qt) * L::kPart; };
                             constexpr int kPerRow = D / 4;           // lanes side by side along a row

@@ -471,11 +471,11 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 4 : 2) attn_decode_k
         if (!whole) {
             __threadfence();
             __syncthreads();
-            if (threadIdx.x == 0) s_last = atomicAdd(p.count + first_cta, 1u) == (unsigned)(last_cta - first_cta);
+            if (threadIdx.x == 0) s_last = arrive(p.count + first_cta, p.call) == (unsigned)(last_cta - first_cta);
             __syncthreads();
             if (s_last) {
                 __threadfence();
-                if (threadIdx.x == 0) p.count[first_cta] = 0u;
+                if (threadIdx.x == 0) p.count[first_cta] = 0ull;   // a captured call comes again under its number
                 // the first part lies in its CTA's slot 1 (it starts at the unit's beginning), the others in slot 0
                 auto part_of = [&](int64_t c) { return p.part + (c * 2 + (c == first_cta ? 1 : 0)) * kPart; };
                 // all of a thread's rows at once and four parts' loads at a time: the loads' latency is what this costs

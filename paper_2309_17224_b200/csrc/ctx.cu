@@ -42,7 +42,7 @@ fp8_status_t fp8_create(fp8_ctx **out, int device)
     fp8_ctx *ctx = new (std::nothrow) fp8_ctx();
     if (!ctx) return FP8_ERR_CUDA;
     ctx->device = device;
-    ctx->next_slot = 0;
+    ctx->next_slot = ctx->attn_calls = ctx->attn_captured = 0;
     bool ok = cudaDeviceGetAttribute(&ctx->sm_count, cudaDevAttrMultiProcessorCount, device) == cudaSuccess &&
               cudaDeviceGetAttribute(&ctx->max_smem_optin, cudaDevAttrMaxSharedMemoryPerBlockOptin, device) ==
                   cudaSuccess;
@@ -51,14 +51,16 @@ fp8_status_t fp8_create(fp8_ctx **out, int device)
     if (!ok) { delete ctx; return FP8_ERR_CUDA; }
     if (major != 10) { delete ctx; return FP8_ERR_UNSUPPORTED; }  // sm_100a code only
 
-    size_t words = 1 + (size_t)fp8lin::kReduceSlots * fp8lin::kSlotWords + 2 + fp8lin::kAttnCounters;
+    // (the counters come first: they are 64 bits wide)
+    const size_t counters = (size_t)fp8lin::kAttnSets * fp8lin::kAttnCounters * 2;
+    size_t words = counters + 1 + (size_t)fp8lin::kReduceSlots * fp8lin::kSlotWords + 2;
     unsigned *buf = nullptr;
     if (cudaMalloc(&buf, words * sizeof(unsigned)) != cudaSuccess) { delete ctx; return FP8_ERR_CUDA; }
     if (cudaMemset(buf, 0, words * sizeof(unsigned)) != cudaSuccess) { cudaFree(buf); delete ctx; return FP8_ERR_CUDA; }
-    ctx->d_status = buf;
-    ctx->d_slots = buf + 1;
-    ctx->d_predict_stats = buf + 1 + fp8lin::kReduceSlots * fp8lin::kSlotWords;
-    ctx->d_attn_count = ctx->d_predict_stats + 2;
+    ctx->d_attn_count = reinterpret_cast<unsigned long long *>(buf);
+    ctx->d_status = buf + counters;
+    ctx->d_slots = ctx->d_status + 1;
+    ctx->d_predict_stats = ctx->d_slots + fp8lin::kReduceSlots * fp8lin::kSlotWords;
     ctx->partial_bytes = (size_t)64 << 20;
     ctx->d_partial = nullptr;
     if (cudaMalloc(&ctx->d_partial, ctx->partial_bytes) != cudaSuccess) { cudaFree(buf); delete ctx; return FP8_ERR_CUDA; }
@@ -87,7 +89,7 @@ fp8_status_t fp8_destroy(fp8_ctx *ctx)
 {
     if (!ctx) return FP8_ERR_NULL;
     cudaSetDevice(ctx->device);
-    cudaError_t e = cudaFree(ctx->d_status);
+    cudaError_t e = cudaFree(ctx->d_attn_count);   // (the status word and the slots lie behind the counters)
     cudaError_t e2 = cudaFree(ctx->d_partial);
     if (e == cudaSuccess) e = e2;
     delete ctx;
@@ -102,9 +104,10 @@ fp8_status_t fp8_device_flags(fp8_ctx *ctx, void *stream, unsigned *flags, int c
         return FP8_ERR_CUDA;
     if (clear && cudaMemsetAsync(ctx->d_status, 0, sizeof(unsigned), st) != cudaSuccess) return FP8_ERR_CUDA;
     if (cudaStreamSynchronize(st) != cudaSuccess) return FP8_ERR_CUDA;
-    // a kernel that gave up waiting may not have arrived everywhere
+    // a kernel that gave up waiting may not have arrived everywhere; captured calls come again under their numbers
     if (clear && (*flags & FP8_FLAG_TIMEOUT) &&
-        cudaMemsetAsync(ctx->d_attn_count, 0, fp8lin::kAttnCounters * sizeof(unsigned), st) != cudaSuccess)
+        (cudaMemsetAsync(ctx->d_attn_count, 0, sizeof(*ctx->d_attn_count) * fp8lin::kAttnSets * fp8lin::kAttnCounters, st) != cudaSuccess ||
+         cudaStreamSynchronize(st) != cudaSuccess))
         return FP8_ERR_CUDA;
     return (*flags & FP8_FLAG_TIMEOUT) ? FP8_ERR_DEVICE_TIMEOUT : FP8_OK;
 }

@@ -16,7 +16,8 @@ namespace fp8lin {
 // ---------------------------------------------------------------------------
 
 constexpr int kReduceSlots = 64;   // independent grid-reduction slots, used round-robin
-constexpr int kAttnCounters = 4096;   // words of fp8_ctx::d_attn_count
+constexpr int kAttnCounters = 1024;   // words of a set of fp8_ctx::d_attn_count
+constexpr int kAttnSets = 65;         // set 0 for launches, the others for launches captured into graphs, round-robin
 constexpr int kSlotWords = 4;      // {running max, arrival counter, scratch flag, redo flag of a predicted cast}
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
@@ -35,7 +36,8 @@ struct fp8_ctx {
     unsigned next_slot;
     unsigned *d_predict_stats;   // {guesses that held, guesses that did not} of fp8_cast_predicted
     float *d_partial;     // FP32 workspace for split-K partial sums and for attention over split contexts
-    unsigned *d_attn_count;   // arrival counters of attention over split contexts, all zero between calls
+    unsigned long long *d_attn_count;   // arrival counters of attention over split contexts: call number and arrivals
+    unsigned attn_calls, attn_captured;  // attention calls so far, and those of them that were captured
     size_t partial_bytes;
     fp8lin::EncodeTiledFn encode_tiled;
 };

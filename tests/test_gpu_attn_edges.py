@@ -137,3 +137,73 @@ def test_append_and_attention_agree_on_a_cut_sequence(lib, ctx):
         want = R.attention(cpu, case["table"].numpy(), [0, 10], [100], q.double().numpy(), dim ** -0.5, True, conv)
         check(out[:8], lse[:8], tuple(x[:8] for x in want))
         ctx.device_flags()
+
+
+def test_calls_that_overlapped_spoil_no_later_call(lib, ctx):
+    """Calls of several shapes at the same time on one context are against its contract, and their own outputs are lost.  The
+    calls after them, launched or replayed from a graph, give the bits that they gave before."""
+    conv, calls = O.CONV_PAPER, []
+    for news, heads, lens in ((1, (8, 1), [3000, 1500, 77]), (1, (16, 2), [5000]), (64, (8, 2), [3000, 1500, 77]), (300, (4, 1), [4000])):
+        case = R.make_case(46, lens, [news] * len(lens), heads[1], 128, 32, conv)
+        dev, cache, batch = gpu_state(lib, case, conv, news, max(lens))
+        q = torch.randn((news * len(lens), heads[0], 128), generator=case["g"]).to(torch.bfloat16).cuda()
+        calls.append((cache, batch, q))
+    own = lib.Context(0)
+
+    def run(i, out=None):
+        out = torch.full_like(calls[i][2], float("nan")) if out is None else out
+        own.attn_paged(*calls[i], out)
+        return out
+
+    want = [run(i) for i in range(len(calls))]
+    torch.cuda.synchronize()
+    replayed, graphs = [torch.empty_like(w) for w in want], []
+    for i in range(len(calls)):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            run(i, replayed[i])
+        graphs.append(g)
+    streams = [torch.cuda.Stream() for _ in range(4)]
+    for _ in range(5):
+        for n in range(40):
+            for j, s in enumerate(streams):
+                with torch.cuda.stream(s):
+                    if j == 0:
+                        graphs[n % 4].replay()
+                    else:
+                        run((n + j) % 4)
+        torch.cuda.synchronize()
+        for i in range(len(calls)):
+            replayed[i].fill_(float("nan"))
+            graphs[i].replay()
+            assert torch.equal(run(i).view(torch.int16), want[i].view(torch.int16))
+            assert torch.equal(replayed[i].view(torch.int16), want[i].view(torch.int16))
+    assert own.device_flags() & lib.FLAG_TIMEOUT == 0
+    own.close()
+
+
+def test_attention_goes_on_after_a_wait_ran_out(lib):
+    """A wait that runs out (on a barrier that nothing completes, with a limit of 2 ms) and the clearing of its flag, which
+    also clears the arrival counters, leave split calls right, launched and replayed."""
+    own = lib.Context(0)
+    for news, heads in ((1, (8, 1)), (64, (8, 2))):
+        case = R.make_case(47, [3000, 1500], [news] * 2, heads[1], 128, 32, O.CONV_PAPER)
+        dev, cache, batch = gpu_state(lib, case, O.CONV_PAPER, news, 3000)
+        q = torch.randn((2 * news, heads[0], 128), generator=case["g"]).to(torch.bfloat16).cuda()
+        want, out = torch.empty_like(q), torch.empty_like(q)
+        own.attn_paged(cache, batch, q, want)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            own.attn_paged(cache, batch, q, out)
+        own.selftest_wait_expiry(2_000_000)
+        assert own.device_flags(clear=True) & lib.FLAG_TIMEOUT
+        for _ in range(3):
+            out.fill_(float("nan"))
+            graph.replay()
+            assert torch.equal(out.view(torch.int16), want.view(torch.int16))
+            again = torch.empty_like(q)
+            own.attn_paged(cache, batch, q, again)
+            assert torch.equal(again.view(torch.int16), want.view(torch.int16))
+        assert own.device_flags() == 0
+    own.close()
