@@ -3,10 +3,12 @@
 // The query rows of one key/value head (token by token, the head's query heads side by side) are taken in tiles of 128,
 // two tiles to a unit, and the cached tokens in tiles of 128, a step each; two products per pair of tiles on the
 // 5th-generation tensor cores:
-//   S = Q K^T   e4m3 x e4m3: the cache's key bytes are the operand as they lie (TMA, no conversion).  A query row is the
-//               sum of two e4m3 numbers under one power of two, q 2^e = hi + lo (hi rounded to nearest, lo the rest):
-//               eight significant bits together, so bf16 queries are exact unless 2^17 below their row's largest.  Two
-//               e4m3 products cost what one bf16 product costs.
+//   S = Q K^T   8-bit floats: the cache's key bytes are the operand as they lie (TMA, no conversion).  A query row is the sum
+//               of two such numbers under one power of two, q 2^e = hi + lo: hi is e4m3, rounded to nearest, with the row's
+//               largest in (224, 448]; lo is the rest.  What hi leaves of a bf16 number is at most eight units of its last
+//               bit, and those have three significant bits: lo is e5m2 (an e4m3 lo ends 2^7 higher).  Together they are exact
+//               down to 2^-6, 2^13 below the row's largest, and within 2^-14 below that, 2^-21 of the largest.  Two such
+//               products cost what one bf16 product costs.
 //   O += P V    tf32: P is left in tensor memory as the FP32 numbers that the softmax computes, in place of the scores, and
 //               read from there; a value 2^-d V8 is a tf32 number exactly, four warps make them on their way into shared
 //               memory (token index innermost; once for both query tiles).  The tensor cores drop P's lower thirteen
@@ -400,7 +402,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
 
     if (warp == kProductWarp) {
         // ------------------------------- products -------------------------------
-        const uint32_t idesc_s = (1u << 4) | ((uint32_t)(kTile >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);                       // e4m3
+        const uint32_t idesc_s = (1u << 4) | ((uint32_t)(kTile >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);       // e4m3; a lo: e5m2
         const uint32_t idesc_o = (1u << 4) | (2u << 7) | (2u << 10) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);   // tf32
         uint32_t n_units[2] = {}, n_steps[2] = {}, n_scores[2] = {};
         const uint32_t tm = uniform(tmem), base_lo = uniform(desc_lo(base));
@@ -423,7 +425,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
 #pragma unroll
                     for (uint32_t k = 0; k < D / 32; ++k)
                         chunk_mma_f8<kSw128, D == 128 ? kSw128 : kSw64>(tm + kTmemSlot * q, dq + term * (D == 128 ? kTile * 128 / 16 : 4) + 2u * k,
-                                                                        dk + 2u * k, idesc_s, (term | k) ? 1u : 0u);
+                                                                        dk + 2u * k, idesc_s | term << 7, (term | k) ? 1u : 0u);
                 chunk_commit(s_full(q));
             }
             __syncwarp();
@@ -639,7 +641,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
             const int row0 = u.row0 + (two ? slot * kTile : 0), rows = u.rows - (two ? slot * kTile : 0);
             if (two || slot == 0 || joined) {
                 const int tok = min((row0 + r) / p.group, s.n - 1), head = u.h * p.group + (row0 + r) % p.group;
-                // ---- queries as two e4m3 terms, one row per thread ----
+                // ---- queries as two 8-bit terms, one row per thread ----
                 float rc;               // |c| / the row's power of two
                 {
                     const uint4 *src = reinterpret_cast<const uint4 *>(p.q + (int64_t)(s.first + tok) * p.ld_q + (int64_t)head * D);
@@ -673,7 +675,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
                                 e4_to_f16(hi4[j], h2[0], h2[1]);
                                 float back[4];
                                 unpack4<FP8_F16>(h2, back);
-                                lo4[j] = cvt_pair<FP8_E4>(a1 - back[1], a0 - back[0]) | (cvt_pair<FP8_E4>(a3 - back[3], a2 - back[2]) << 16);
+                                lo4[j] = cvt_pair<FP8_E5>(a1 - back[1], a0 - back[0]) | (cvt_pair<FP8_E5>(a3 - back[3], a2 - back[2]) << 16);
                             }
                             // D = 128: a row of hi, and 16 KB on its row of lo; D = 64: hi and lo side by side in one 128-byte row
                             const int c_hi = i, c_lo = D == 128 ? i : i + 4;

@@ -207,3 +207,42 @@ def test_attention_goes_on_after_a_wait_ran_out(lib):
             assert torch.equal(again.view(torch.int16), want.view(torch.int16))
         assert own.device_flags() == 0
     own.close()
+
+
+@pytest.mark.parametrize("news", [1, 2, 40, 150])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("gain", [12, 14, 16, 19])
+def test_one_query_channel_far_above_the_others(lib, ctx, news, dim, gain):
+    """Channel 0 of the queries is 2^gain times the others, and the keys are zero there: the scores come from query numbers far
+    below their row's largest.  A query number is held within 2^-21 of the row's largest (exactly, if it is not 2^13 below),
+    so to the FP32 sum's 2^-15 of scale * sum |q k| comes 2^-21 of scale * max |q| * sum |k|."""
+    lens, heads, kv_heads = [200, 333], 4, 2
+    case = R.make_case(48, lens, [news] * 2, kv_heads, dim, 32, O.CONV_PAPER, fill=0x7F)
+    case["k8"][..., 0] = 0
+    q = torch.randn((2 * news, heads, dim), generator=case["g"])
+    q[..., 0] = q[..., 0].sign() * 2.0 ** gain
+    q = q.to(torch.bfloat16)
+    dev, cache, batch = gpu_state(lib, case, O.CONV_PAPER, news, 333)
+    out, lse = torch.empty_like(q, device="cuda"), torch.empty(q.shape[:2], device="cuda")
+    ctx.attn_paged(cache, batch, q.cuda(), out, lse=lse)
+    cpu = [case[n].numpy() for n in ("k8", "v8", "bk", "bv")]
+    o, l, spread, score = R.attention(cpu, case["table"].numpy(), case["q_start"].numpy(), lens, q.double().numpy(), dim ** -0.5, True, O.CONV_PAPER)
+    for b, n in enumerate(lens):
+        kc, kb, _, _ = R.cached_rows(cpu, case["table"].numpy(), b, np.arange(n))
+        most = np.abs(R.numbers(kc, kb, O.CONV_PAPER)).sum(-1).max(0).repeat(heads // kv_heads)          # per query head
+        rows = slice(b * news, (b + 1) * news)
+        score[rows] += 2.0 ** -6 * dim ** -0.5 * np.abs(q[rows].double().numpy()).max(-1) * most
+    check(out, lse, (o, l, spread, score))
+
+
+@pytest.mark.parametrize("news", [1, 40, 150])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("gain", [10, 12, 13])
+def test_query_numbers_down_to_2_13_below_the_largest_are_exact(lib, ctx, news, dim, gain):
+    """Channel 0 is 2^gain, the others lie between 1 and 2 (every mantissa of bf16), the keys are zero in channel 0: nothing is
+    lost of the queries, so the scores keep the ordinary bound, 2^-15 of scale * sum |q k| over the channels that count."""
+    def edit(case, q):
+        case["k8"][..., 0] = 0
+        q.copy_(((1 + torch.randint(0, 128, q.shape, generator=case["g"]) / 128.0) * q.float().sign()).to(torch.bfloat16))
+        q[..., 0] = 2.0 ** gain
+    run_case(lib, ctx, 49, [200, 333], [news] * 2, 4, 2, dim, 32, O.CONV_PAPER, True, edit=edit)
