@@ -641,6 +641,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
             const int row0 = u.row0 + (two ? slot * kTile : 0), rows = u.rows - (two ? slot * kTile : 0);
             if (two || slot == 0 || joined) {
                 const int tok = min((row0 + r) / p.group, s.n - 1), head = u.h * p.group + (row0 + r) % p.group;
+                const int limit = tokens_seen(s, p.causal, (row0 + r) / p.group);   // tokens that the row sees
                 // ---- queries as two 8-bit terms, one row per thread ----
                 float rc;               // |c| / the row's power of two
                 {
@@ -657,8 +658,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
                     unsigned ignored = 0;
                     const int e = min(126, bias_from_amax_bits(m, FP8_E4, FP8_CONV_NATIVE, 0, &ignored));   // the largest in (224, 448]
                     const float f = copysignf(pow2_normal(e), p.c);     // a negative scale goes into the queries: rc >= 0
-                    // (not 0: it multiplies the -infinity of masked tokens)
-                    rc = m >= 0x7F800000u ? __int_as_float(0x7FFFFFFF) : fmaxf(fabsf(p.c) * pow2_normal(-e), 1e-37f);
+                    // (not 0, and no NaN in a row that sees nothing: it multiplies the -infinity of masked tokens)
+                    rc = m >= 0x7F800000u && limit > 0 ? __int_as_float(0x7FFFFFFF) : fmaxf(fabsf(p.c) * pow2_normal(-e), 1e-37f);
                     if (two || slot == 0) {
 #pragma unroll 2
                         for (int i = 0; i < D / 16; ++i) {
@@ -687,7 +688,6 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
                         mbar_arrive(q_full(slot));
                     }
                 }
-                const int limit = tokens_seen(s, p.causal, (row0 + r) / p.group);
                 const int least = __shfl_sync(0xFFFFFFFFu, limit, 0);   // the warp's first row sees least
                 const bool active = (warp & 3) * 32 < rows;
                 float top = kNoMax;

@@ -246,3 +246,15 @@ def test_query_numbers_down_to_2_13_below_the_largest_are_exact(lib, ctx, news, 
         q.copy_(((1 + torch.randint(0, 128, q.shape, generator=case["g"]) / 128.0) * q.float().sign()).to(torch.bfloat16))
         q[..., 0] = 2.0 ** gain
     run_case(lib, ctx, 49, [200, 333], [news] * 2, 4, 2, dim, 32, O.CONV_PAPER, True, edit=edit)
+
+
+@pytest.mark.parametrize("news", [3, 40, 150])
+@pytest.mark.parametrize("causal", [True, False])
+def test_queries_that_are_not_finite_and_see_nothing_give_zeros(lib, ctx, news, causal):
+    """Rows of empty sequences, and under the causal mask rows before the first cached token, whatever the query holds."""
+    def edit(case, q):
+        q[0, 1, 3], q[0, 2, 0], q[0, 3, :] = float("inf"), float("nan"), float("-inf")
+        q[news, 2, 5] = float("nan")
+        q[2 * news:] = float("inf")
+    out, lse = run_case(lib, ctx, 50, [0, 2, 0], [news] * 3, 4, 2, 64, 16, O.CONV_PAPER, causal, edit=edit)
+    assert (out[:news, :4] == 0).all() and (out[2 * news:, :4] == 0).all() and torch.isneginf(lse[:news]).all()
