@@ -569,7 +569,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
                 // 2^-b of the key for the softmax (step g - 3 has used this place: its products, waited for a step ago, are done)
                 const bool marked = bk == FP8_KV_BIAS_NONFINITE || bv == FP8_KV_BIAS_NONFINITE;
                 reinterpret_cast<float *>(smem + L::kScale)[(g % 3u) * kTile + cw * 32 + lane] =
-                    marked ? __int_as_float(0x7FFFFFFF) : pow2_normal(min(126, -(bk + kv.delta)));
+                    marked ? __int_as_float(0x7FFFFFFF) : key_factor(bk + kv.delta);
                 if (two || (i & 1) == 0) mbar_arrive(sc_full(0, n_steps[0]++));
                 if (two || (i & 1) == 1) mbar_arrive(sc_full(1, n_steps[1]++));
                 if (cw == 0 && i + 1 < steps) {
@@ -643,7 +643,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
                 const int tok = min((row0 + r) / p.group, s.n - 1), head = u.h * p.group + (row0 + r) % p.group;
                 const int limit = tokens_seen(s, p.causal, (row0 + r) / p.group);   // tokens that the row sees
                 // ---- queries as two 8-bit terms, one row per thread ----
-                float rc;               // |c| / the row's power of two
+                float rc;               // |c| / the row's power of two, and the keys' share
                 {
                     const uint4 *src = reinterpret_cast<const uint4 *>(p.q + (int64_t)(s.first + tok) * p.ld_q + (int64_t)head * D);
                     uint32_t m = 0;
@@ -659,7 +659,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
                     const int e = min(126, bias_from_amax_bits(m, FP8_E4, FP8_CONV_NATIVE, 0, &ignored));   // the largest in (224, 448]
                     const float f = copysignf(pow2_normal(e), p.c);     // a negative scale goes into the queries: rc >= 0
                     // (not 0, and no NaN in a row that sees nothing: it multiplies the -infinity of masked tokens)
-                    rc = m >= 0x7F800000u && limit > 0 ? __int_as_float(0x7FFFFFFF) : fmaxf(fabsf(p.c) * pow2_normal(-e), 1e-37f);
+                    rc = m >= 0x7F800000u && limit > 0 ? __int_as_float(0x7FFFFFFF) : fmaxf(query_factor(fabsf(p.c), e), 1e-45f);
                     if (two || slot == 0) {
 #pragma unroll 2
                         for (int i = 0; i < D / 16; ++i) {

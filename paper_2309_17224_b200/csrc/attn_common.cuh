@@ -26,6 +26,11 @@ struct AttnParams {
     float c;              // scale * log2(e)
 };
 
+// A score is (q 2^e . K8) (2^-b) (|c| 2^-e), each factor a power of two but for c.  The first product is below 2^32; a key factor is
+// up to 2^126 and would take it out of FP32 where keys are large and queries small, so kKeyLift powers of two of the key
+// factor (2^-65 and more) go to the query's.
+constexpr int kKeyLift = 36;
+
 constexpr float kNoMax = -3.0e38f;    // M before the first token: finite, so that 2^(-inf - M) is 0 and not NaN
 constexpr float kLn2 = 0.693147180559945309f;
 
@@ -36,6 +41,15 @@ __device__ __forceinline__ float exp2_approx(float x)
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+// 2^-b for the keys cast under bias b (delta added), 2^-kKeyLift of it
+__device__ __forceinline__ float key_factor(int b) { return pow2_normal(min(126, -b) - kKeyLift); }
+// c 2^-e with the keys' powers of two, -113 <= -e <= 126 or so; finite, so that a score of 0 stays 0
+__device__ __forceinline__ float query_factor(float c, int e)
+{
+    const int n = kKeyLift - e;
+    const float x = c * pow2_normal(min(n, 100)) * pow2_normal(max(n - 100, 0));
+    return fminf(fmaxf(x, -3.402823466e38f), 3.402823466e38f);
 }
 __device__ __forceinline__ float log2_approx(float x)
 {

@@ -237,7 +237,7 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 4 : 2) attn_decode_k
 
         // ---- queries: fp16 under a power of two per row (exact for bf16 unless 2^28 below the row's largest) ----
         uint32_t q[NT][D / 16][2];
-        float rc[NT][2];          // c / that power, for the rows of S^T's columns
+        float rc[NT][2];          // c / that power and the keys' share, for the rows of S^T's columns
         int limit[NT][2];         // tokens those rows see
         const int all_see = tokens_seen(u.s, p.causal, 0);    // tokens that every row sees
         {
@@ -266,7 +266,7 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 4 : 2) attn_decode_k
                 // the row's largest lands in [2^14, 2^15)
                 const int e = m == 0 ? 0 : max(-113, min(126, 14 + 127 - (int)(m >> 23)));
                 const float f = pow2_normal(e);
-                mine[j] = m >= 0x7F800000u ? __int_as_float(0x7FFFFFFF) : p.c * pow2_normal(-e);
+                mine[j] = m >= 0x7F800000u ? __int_as_float(0x7FFFFFFF) : query_factor(p.c, e);
 #pragma unroll
                 for (int i = 0; i < D / 64; ++i)
 #pragma unroll
@@ -314,8 +314,8 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 4 : 2) attn_decode_k
             if (bad && lane == 0) raise_flags(kv.d_status, FP8_FLAG_BAD_INDEX);
             const bool marked0 = bk[0] == FP8_KV_BIAS_NONFINITE || bv[0] == FP8_KV_BIAS_NONFINITE;
             const bool marked1 = bk[1] == FP8_KV_BIAS_NONFINITE || bv[1] == FP8_KV_BIAS_NONFINITE;
-            const float f0 = marked0 ? __int_as_float(0x7FFFFFFF) : pow2_normal(min(126, -(bk[0] + kv.delta)));
-            const float f1 = marked1 ? __int_as_float(0x7FFFFFFF) : pow2_normal(min(126, -(bk[1] + kv.delta)));
+            const float f0 = marked0 ? __int_as_float(0x7FFFFFFF) : key_factor(bk[0] + kv.delta);
+            const float f1 = marked1 ? __int_as_float(0x7FFFFFFF) : key_factor(bk[1] + kv.delta);
             // scores; beyond what a row sees -infinity
             bool above = false;
 #pragma unroll

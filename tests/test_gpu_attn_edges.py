@@ -258,3 +258,34 @@ def test_queries_that_are_not_finite_and_see_nothing_give_zeros(lib, ctx, news, 
         q[2 * news:] = float("inf")
     out, lse = run_case(lib, ctx, 50, [0, 2, 0], [news] * 3, 4, 2, 64, 16, O.CONV_PAPER, causal, edit=edit)
     assert (out[:news, :4] == 0).all() and (out[2 * news:, :4] == 0).all() and torch.isneginf(lse[:news]).all()
+
+
+@pytest.mark.parametrize("news", [1, 2, 40, 150])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("powers", [118, 110, 90, -60, -70])
+def test_large_keys_meet_small_queries(lib, ctx, news, dim, powers):
+    """Keys of about 2^powers under queries of about 2^-powers: scores of ordinary size, from numbers whose product with the
+    other side's normalised row is not an FP32 number."""
+    def edit(case, q):
+        case["bk"].copy_((case["bk"].int() - powers).clamp(-127, 64).to(torch.int8))
+        q.copy_((q.float() * 2.0 ** -powers).to(torch.bfloat16))
+    run_case(lib, ctx, 51, [200, 333], [news] * 2, 4, 2, dim, 32, O.CONV_NATIVE, True, edit=edit, fill=0x30)
+
+
+@pytest.mark.parametrize("news", [1, 40])
+def test_a_scale_of_zero_weighs_all_tokens_alike(lib, ctx, news):
+    """Also where keys and queries are near the ends of their range."""
+    def edit(case, q):
+        case["bk"].fill_(-119)
+        q.copy_((q.float() * 2.0 ** 120).to(torch.bfloat16))
+    run_case(lib, ctx, 52, [200, 333], [news] * 2, 4, 2, 64, 32, O.CONV_NATIVE, True, edit=edit, scale=0.0, fill=0x30)
+
+
+@pytest.mark.parametrize("news", [1, 40])
+@pytest.mark.parametrize("scale", [0.125, -0.125])
+def test_keys_of_zeros_under_the_largest_queries(lib, ctx, news, scale):
+    def edit(case, q):
+        case["k8"][:, :, ::2] = 0
+        case["k8"][:, :, 1::2] = 0x80
+        q.copy_((q.float().sign() * 3e38).to(torch.bfloat16))
+    run_case(lib, ctx, 53, [200, 333], [news] * 2, 4, 2, 64, 32, O.CONV_PAPER, False, edit=edit, scale=scale, fill=0x30)
