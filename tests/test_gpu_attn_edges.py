@@ -289,3 +289,42 @@ def test_keys_of_zeros_under_the_largest_queries(lib, ctx, news, scale):
         case["k8"][:, :, 1::2] = 0x80
         q.copy_((q.float().sign() * 3e38).to(torch.bfloat16))
     run_case(lib, ctx, 53, [200, 333], [news] * 2, 4, 2, 64, 32, O.CONV_PAPER, False, edit=edit, scale=scale, fill=0x30)
+
+
+@pytest.mark.parametrize("news,lens", [(1, [300, 64]), (30, [300, 64]), (150, [300, 200]), (30, [5000, 4000])])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_equal_weights_are_exact(lib, ctx, news, lens, dim):
+    """Queries of zeros: every weight is 1, an output is the mean of its tokens' values.  Nothing but the FP32 sum (2^-20 of the
+    mean of |v|, at most 5000 numbers of 4 bits within 2^6 of each other) and the rounding to bf16 is between them."""
+    case = R.make_case(54, lens, [news] * 2, 2, dim, 32, O.CONV_NATIVE, fill=0x7F)
+    case["bv"].fill_(8)
+    case["v8"].copy_(torch.randint(0x28, 0x58, case["v8"].shape, generator=case["g"], dtype=torch.uint8))       # 2^-2 .. 2^4
+    dev, cache, batch = gpu_state(lib, case, O.CONV_NATIVE, news, max(lens))
+    q = torch.zeros((2 * news, 4, dim), dtype=torch.bfloat16)
+    out, lse = torch.empty_like(q, device="cuda"), torch.empty(q.shape[:2], device="cuda")
+    ctx.attn_paged(cache, batch, q.cuda(), out, lse=lse)
+    cpu = [case[n].numpy() for n in ("k8", "v8", "bk", "bv")]
+    o, l, spread, _ = R.attention(cpu, case["table"].numpy(), case["q_start"].numpy(), lens, q.double().numpy(), 1.0, True, O.CONV_NATIVE)
+    step = np.exp2(np.floor(np.log2(np.abs(o) * (1 + 2.0 ** -20))) - 7)
+    assert (np.abs(out.double().cpu().numpy() - o) <= step / 2 + 2.0 ** -20 * spread).all()
+    assert (np.abs(lse.double().cpu().numpy() - l) <= 2.0 ** -19 * (1 + np.abs(l))).all()
+
+
+@pytest.mark.parametrize("news", [1, 30, 150])
+@pytest.mark.parametrize("gain", [0.5, 2.0])
+def test_outputs_are_too_large_as_often_as_too_small(lib, ctx, news, gain):
+    """Positive values, random scores: the roundings of weights and outputs leave no drift.  An output's rounding to bf16 is
+    within 2^-8 of it and evenly spread, 2^-8 / sqrt(12) on average; the mean of n has 1 / sqrt(n) of that, and five times
+    as much is allowed, beside 2^-16 for the weights' roundings, which are 2^-11 at most and have either sign."""
+    dim, lens = 128, [900, 700, 800, 600]
+    case = R.make_case(55, lens, [news] * 4, 4, dim, 32, O.CONV_NATIVE, fill=0x7F)
+    case["bv"].fill_(8)
+    case["v8"].copy_(torch.randint(0x38, 0x40, case["v8"].shape, generator=case["g"], dtype=torch.uint8))
+    q = (torch.randn((4 * news, 16, dim), generator=case["g"]) * gain).to(torch.bfloat16)
+    dev, cache, batch = gpu_state(lib, case, O.CONV_NATIVE, news, 900)
+    out = torch.empty_like(q, device="cuda")
+    ctx.attn_paged(cache, batch, q.cuda(), out)
+    cpu = [case[n].numpy() for n in ("k8", "v8", "bk", "bv")]
+    o = R.attention(cpu, case["table"].numpy(), case["q_start"].numpy(), lens, q.double().numpy(), dim ** -0.5, True, O.CONV_NATIVE)[0]
+    drift = (out.double().cpu().numpy() / o - 1).mean()
+    assert abs(drift) <= 5 * 2.0 ** -8 / np.sqrt(12 * o.size) + 2.0 ** -16
