@@ -57,7 +57,8 @@ struct ChunkShape {
     static constexpr int kK = kQ + 2 * kQBytes;              // where the slots share one query tile)
     static constexpr int kV = kK + kKStages * kKBytes;
     static constexpr int kScale = kV + kVStages * kVBytes;   // [3][128] floats: 2^-b of a tile's keys
-    static constexpr int kBar = kScale + 3 * kTile * 4;
+    static constexpr int kLarge = kScale + 3 * kTile * 4;    // [3][4] words: whether a step's values are large, a word per warp
+    static constexpr int kBar = kLarge + 3 * 16;
     static constexpr int kNumBars = 2 * kKStages + 2 * kVStages + 8 + 5 * 2 + 3;
     static constexpr int kTotal = kBar + kNumBars * 8 + 16;
     static constexpr int kDynamic = kTotal + 1024;           // slack to align the base to 1024 bytes
@@ -68,7 +69,9 @@ constexpr uint32_t kTmemCols = 512, kTmemSlot = 256;         // per slot 128 col
 // M lies log2 of 1 + this below the maximum, which makes the weights that much larger; their sum is scaled back.
 constexpr float kTf32Cut = 0.7213f / 2048.0f, kTf32Kept = 1.0f / (1.0f + kTf32Cut), kTf32Lift = kTf32Cut * 1.442695f;
 constexpr uint32_t kTmemO = 128;
-constexpr float kSumLimit = 1.152921504606847e18f;   // 2^60: M is moved when the weights' sum exceeds it
+// M is moved when the weights' sum exceeds a limit: 2^60, and once values are large 2^-10 (a unit has up to 148 parts), where M
+// is put kLargeLift above the maximum and above the sum's logarithm.
+constexpr float kSumLimit = 1.152921504606847e18f, kLargeSumLimit = 1.0f / 1024.0f, kLargeLift = 18.0f;
 
 // The tensor cores' instructions take their operands from uniform registers.  So the whole warp walks the steps with
 // values that the compiler can see to be uniform, and one elected lane issues: with a single lane in the loop every operand
@@ -573,6 +576,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
                 const bool marked = bk == FP8_KV_BIAS_NONFINITE || bv == FP8_KV_BIAS_NONFINITE;
                 reinterpret_cast<float *>(smem + L::kScale)[(g % 3u) * kTile + cw * 32 + lane] =
                     marked ? __int_as_float(0x7FFFFFFF) : key_factor(bk + kv.delta);
+                const unsigned large = __ballot_sync(0xFFFFFFFFu, !marked && bv + kv.delta < kLargeValue);
+                if (lane == 0) reinterpret_cast<unsigned *>(smem + L::kLarge)[(g % 3u) * 4 + cw] = large;
                 if (two || (i & 1) == 0) mbar_arrive(sc_full(0, n_steps[0]++));
                 if (two || (i & 1) == 1) mbar_arrive(sc_full(1, n_steps[1]++));
                 if (cw == 0 && i + 1 < steps) {
@@ -693,7 +698,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
                 }
                 const int least = __shfl_sync(0xFFFFFFFFu, limit, 0);   // the warp's first row sees least
                 const bool active = (warp & 3) * 32 < rows;
-                float top = kNoMax;
+                float top = kNoMax, sum_limit = kSumLimit;
                 f32x2 sum = pack2(0.0f, 0.0f);
                 const f32x2 rc2 = pack2(rc, rc);
                 const int start = two ? 0 : slot, ahead = two ? 1 : 2;
@@ -708,6 +713,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
                     if (active) {
                         const float *factors = reinterpret_cast<const float *>(smem + L::kScale) + (g % 3u) * kTile;
                         const bool mask = t0 + kTile > least;
+                        const uint4 large = *reinterpret_cast<const uint4 *>(smem + L::kLarge + (g % 3u) * 16);
+                        if (large.x | large.y | large.z | large.w) sum_limit = kLargeSumLimit;
 #pragma unroll 1
                         for (int c0 = 0; c0 < kTile; c0 += kSpan) {
                             f32x2 w[kSpan / 2];
@@ -717,7 +724,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
                             f32x2 add = weights_of_row(w, rc2, top);
                             float a, b;
                             unpack2(add2(sum, add), a, b);
-                            if (__builtin_expect(__any_sync(0xFFFFFFFFu, a + b > kSumLimit), 0)) {
+                            if (__builtin_expect(__any_sync(0xFFFFFFFFu, a + b > sum_limit), 0)) {
                                 scores_of_row(lanes + c0, factors + c0, mask, t0 + c0, limit, w);
                                 float m = -INFINITY;
 #pragma unroll
@@ -726,6 +733,10 @@ __global__ void __launch_bounds__(kChunkThreads, 1) attn_chunk_kernel(const __gr
                                     m = fmaxf(m, fmaxf(a, b));
                                 }
                                 m = fmaf(m, rc, -kTf32Lift);
+                                if (sum_limit != kSumLimit) {     // also above what the weights so far sum up to
+                                    unpack2(sum, a, b);
+                                    m = fmaxf(m, top + log2_approx(a + b)) + kLargeLift;
+                                }
                                 const float next = fmaxf(top, m), shrink = exp2_approx(top - next);
                                 top = next;
                                 sum = mul2(sum, pack2(shrink, shrink));

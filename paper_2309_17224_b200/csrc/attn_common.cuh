@@ -4,7 +4,10 @@
 // of their bytes and c = scale * log2(e), a row of queries q needs
 //     s_j = c 2^-b_j (q . K8_j),   p_j = 2^(s_j - M),   out = sum_j p_j (2^-d_j V8_j) / sum_j p_j.
 // M is the row's maximum when it was last looked at: it moves only when a score lies far above it, so that rescaling what
-// has been summed is rare (FP32 has the room).  Statistics and sums are FP32.  A value 2^-d V8 has four significant bits, so
+// has been summed is rare.  FP32 has the room for weights up to 2^60 as long as values stay below 2^49.  From the first tokens
+// on that hold larger ones (kLargeValue) M is kept above the maximum by so much that the weights' sum stays below 1, and sums
+// of weights and values are finite wherever the result is; of such a sequence's weights those below about 2^-77 (2^30
+// tokens) to 2^-100 (a few hundred) of the largest are lost.  Statistics and sums are FP32.  A value 2^-d V8 has four significant bits, so
 // it is a bf16 or tf32 number exactly; how a weight p is held for the second product each kernel says.
 #pragma once
 
@@ -31,6 +34,7 @@ struct AttnParams {
 // factor (2^-65 and more) go to the query's.
 constexpr int kKeyLift = 36;
 
+constexpr int kLargeValue = -40;      // values cast under a bias (delta added) below this may reach 2^49
 constexpr float kNoMax = -3.0e38f;    // M before the first token: finite, so that 2^(-inf - M) is 0 and not NaN
 constexpr float kLn2 = 0.693147180559945309f;
 

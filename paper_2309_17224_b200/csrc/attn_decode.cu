@@ -20,6 +20,8 @@
 // Measured from a graph (64/8 heads of 128): 16 ragged sequences on up to 4096 tokens 36 us for 109 MB (17 us at the
 // measured copy rate).  Longer contexts add 5.1 to 5.75 TB/s; about 14 us are fixed: launch, lookup, first loads, changes
 // of unit, and 2.6 us for the join.
+#include <type_traits>
+
 #include "attn_common.cuh"
 
 namespace fp8lin {
@@ -28,7 +30,9 @@ constexpr int kDecodeWarps = 4;
 constexpr int kDecodeThreads = 32 * kDecodeWarps;
 constexpr int kBlockTokens = 16;
 
-constexpr float kSlack = 40.0f;       // M is moved when a score exceeds it by more
+// M is moved when a score exceeds it by more than kSlack, to that score.  Once values are large no weight may be above a
+// quarter divided by the number of tokens: M is moved when a score comes closer to it than that, to kLargeLift further away.
+constexpr float kSlack = 40.0f, kLargeLift = 8.0f;
 
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
 {
@@ -289,132 +293,171 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 4 : 2) attn_decode_k
             l[j][0] = l[j][1] = 0.0f;
         }
 
-        for (int i = 0; i < count; ++i) {
-            const int j0 = (lo + warp + i * kDecodeWarps) * kBlockTokens;
-            // S^T
-            float s[NT][4];
-#pragma unroll
-            for (int j = 0; j < NT; ++j) s[j][0] = s[j][1] = s[j][2] = s[j][3] = 0.0f;
-#pragma unroll
-            for (int c = 0; c < D / 64; ++c)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    uint32_t a0, a1, a2, a3;
-                    e4_to_f16(cur.k[0][c][k], a0, a2);
-                    e4_to_f16(cur.k[1][c][k], a1, a3);
-#pragma unroll
-                    for (int j = 0; j < NT; ++j) mma_f16(s[j], a0, a1, a2, a3, q[j][4 * c + k][0], q[j][4 * c + k][1]);
+        // The blocks from i on; without LARGE up to the first that holds large values, whose index is returned.  (Two loops: one
+        // for both costs the few registers that it has too many, 16 sequences on 4096 tokens 37.4 against 36.5 us.)
+        auto walk = [&](auto large_mode, int i) {
+            constexpr bool kLarge = decltype(large_mode)::value;
+            const float margin = (float)(34 - __clz(u.s.len));        // log2 of four times the tokens, and up to one more
+            for (; i < count; ++i) {
+                const int j0 = (lo + warp + i * kDecodeWarps) * kBlockTokens;
+                if constexpr (!kLarge) {
+                    // (marked rows and what lies behind the end are no values)
+                    auto large = [&](int r) {
+                        return cur.bv[r] != FP8_KV_BIAS_NONFINITE && cur.bv[r] + kv.delta < kLargeValue && j0 + g + 8 * r < u.s.len;
+                    };
+                    if (__builtin_expect(__any_sync(0xFFFFFFFFu, min(cur.bv[0], cur.bv[1]) < kLargeValue), 0) &&
+                        __any_sync(0xFFFFFFFFu, !cur.bad && (large(0) || large(1))))
+                        break;
                 }
-            // a page out of range is read as page 0 and then taken as non-finite
-            int bk[2] = {cur.bk[0], cur.bk[1]}, bv[2] = {cur.bv[0], cur.bv[1]};
-            if (cur.bad) bk[0] = bk[1] = bv[0] = bv[1] = FP8_KV_BIAS_NONFINITE;
-            const int bad = cur.bad;
-            // the registers of K are free: the next block's
-            if (i + 1 < count) request_k(cur, i + 1, v_at);
-            if (bad && lane == 0) raise_flags(kv.d_status, FP8_FLAG_BAD_INDEX);
-            const bool marked0 = bk[0] == FP8_KV_BIAS_NONFINITE || bv[0] == FP8_KV_BIAS_NONFINITE;
-            const bool marked1 = bk[1] == FP8_KV_BIAS_NONFINITE || bv[1] == FP8_KV_BIAS_NONFINITE;
-            const float f0 = marked0 ? __int_as_float(0x7FFFFFFF) : key_factor(bk[0] + kv.delta);
-            const float f1 = marked1 ? __int_as_float(0x7FFFFFFF) : key_factor(bk[1] + kv.delta);
-            // scores; beyond what a row sees -infinity
-            bool above = false;
+                // S^T
+                float s[NT][4];
 #pragma unroll
-            for (int j = 0; j < NT; ++j)
+                for (int j = 0; j < NT; ++j) s[j][0] = s[j][1] = s[j][2] = s[j][3] = 0.0f;
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    s[j][k] = s[j][k] * f0 * rc[j][k];
-                    s[j][2 + k] = s[j][2 + k] * f1 * rc[j][k];
-                    if (j0 + kBlockTokens > all_see) {
-                        if (j0 + g >= limit[j][k]) s[j][k] = -INFINITY;
-                        if (j0 + g + 8 >= limit[j][k]) s[j][2 + k] = -INFINITY;
+                for (int c = 0; c < D / 64; ++c)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        uint32_t a0, a1, a2, a3;
+                        e4_to_f16(cur.k[0][c][k], a0, a2);
+                        e4_to_f16(cur.k[1][c][k], a1, a3);
+#pragma unroll
+                        for (int j = 0; j < NT; ++j) mma_f16(s[j], a0, a1, a2, a3, q[j][4 * c + k][0], q[j][4 * c + k][1]);
                     }
-                    above |= fmaxf(s[j][k], s[j][2 + k]) > top[j][k] + kSlack;
-                }
-            if (__any_sync(0xFFFFFFFFu, above)) {
+                // a page out of range is read as page 0 and then taken as non-finite
+                int bk[2] = {cur.bk[0], cur.bk[1]}, bv[2] = {cur.bv[0], cur.bv[1]};
+                if (cur.bad) bk[0] = bk[1] = bv[0] = bv[1] = FP8_KV_BIAS_NONFINITE;
+                const int bad = cur.bad;
+                // the registers of K are free: the next block's
+                if (i + 1 < count) request_k(cur, i + 1, v_at);
+                if (bad && lane == 0) raise_flags(kv.d_status, FP8_FLAG_BAD_INDEX);
+                const bool marked0 = bk[0] == FP8_KV_BIAS_NONFINITE || bv[0] == FP8_KV_BIAS_NONFINITE;
+                const bool marked1 = bk[1] == FP8_KV_BIAS_NONFINITE || bv[1] == FP8_KV_BIAS_NONFINITE;
+                const float f0 = marked0 ? __int_as_float(0x7FFFFFFF) : key_factor(bk[0] + kv.delta);
+                const float f1 = marked1 ? __int_as_float(0x7FFFFFFF) : key_factor(bk[1] + kv.delta);
+                // scores; beyond what a row sees -infinity
+                bool above = false;
 #pragma unroll
                 for (int j = 0; j < NT; ++j)
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
-                        float m = fmaxf(s[j][k], s[j][2 + k]);
-                        m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 4));
-                        m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 8));
-                        m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 16));
-                        const float next = fmaxf(top[j][k], m);
-                        const float shrink = exp2_approx(top[j][k] - next);
-                        top[j][k] = next;
-                        l[j][k] *= shrink;
-#pragma unroll
-                        for (int m2 = 0; m2 < D / 16; ++m2) {
-                            o[j][m2][k] *= shrink;
-                            o[j][m2][2 + k] *= shrink;
+                        s[j][k] = s[j][k] * f0 * rc[j][k];
+                        s[j][2 + k] = s[j][2 + k] * f1 * rc[j][k];
+                        if (j0 + kBlockTokens > all_see) {
+                            if (j0 + g >= limit[j][k]) s[j][k] = -INFINITY;
+                            if (j0 + g + 8 >= limit[j][k]) s[j][2 + k] = -INFINITY;
                         }
+                        above |= fmaxf(s[j][k], s[j][2 + k]) > (kLarge ? top[j][k] - margin : top[j][k] + kSlack);
                     }
-            }
-            // p, the denominator, and P^T's two terms as the second product's operands
-            uint32_t pt[NT][2][2];
+                if (__any_sync(0xFFFFFFFFu, above)) {
 #pragma unroll
-            for (int j = 0; j < NT; ++j) {
+                    for (int j = 0; j < NT; ++j)
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    s[j][k] = exp2_approx(s[j][k] - top[j][k]);
-                    s[j][2 + k] = exp2_approx(s[j][2 + k] - top[j][k]);
-                    l[j][k] += s[j][k] + s[j][2 + k];
+                        for (int k = 0; k < 2; ++k) {
+                            float m = fmaxf(s[j][k], s[j][2 + k]);
+                            m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 4));
+                            m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 8));
+                            m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 16));
+                            const float next = fmaxf(top[j][k], kLarge ? m + margin + kLargeLift : m);
+                            const float shrink = exp2_approx(top[j][k] - next);
+                            top[j][k] = next;
+                            l[j][k] *= shrink;
+#pragma unroll
+                            for (int m2 = 0; m2 < D / 16; ++m2) {
+                                o[j][m2][k] *= shrink;
+                                o[j][m2][2 + k] *= shrink;
+                            }
+                        }
                 }
-#pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    uint32_t p1, p2;
-                    split_bf16(s[j][2 * r], s[j][2 * r + 1], p1, p2);
-                    pt[j][0][r] = transpose8x8(p1);
-                    pt[j][1][r] = transpose8x8(p2);
-                }
-            }
-            // values that no weight may meet, because 0 times a NaN is one: tokens behind the end, marked rows
-            const unsigned marks = __ballot_sync(0xFFFFFFFFu, marked0), marks8 = __ballot_sync(0xFFFFFFFFu, marked1);
-            if ((marks | marks8) != 0u || j0 + kBlockTokens > u.s.len) {
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int row = 2 * t + (r & 1);
-                    const bool drop = ((((r >> 1) ? marks8 : marks) >> (4 * row)) & 1u) || j0 + row + 8 * (r >> 1) >= u.s.len;
-                    if (drop) {
-#pragma unroll
-                        for (int k = 0; k < KvBlock<D>::kVWords; ++k) cur.v[r][k] = 0u;
-                    }
-                }
-            }
-            // 2^(120 - d) of tokens 2t, 2t + 1, and of 2t + 8, 2t + 9
-            const int dv0 = bv[0] + kv.delta, dv1 = bv[1] + kv.delta;
-            uint32_t f_lo, f_hi, rest_lo = 0, rest_hi = 0;
-            {
-                const uint32_t both = value_factor(dv0) | value_factor(dv1) << 16;
-                const uint32_t even = __shfl_sync(0xFFFFFFFFu, both, 8 * t), odd = __shfl_sync(0xFFFFFFFFu, both, 8 * t + 4);
-                f_lo = __byte_perm(even, odd, 0x5410);
-                f_hi = __byte_perm(even, odd, 0x7632);
-            }
-            const bool two_steps = __any_sync(0xFFFFFFFFu, min(dv0, dv1) < -7);   // values beyond 2^15
-            if (two_steps) {
-                const uint32_t both = value_factor_rest(dv0) | value_factor_rest(dv1) << 16;
-                const uint32_t even = __shfl_sync(0xFFFFFFFFu, both, 8 * t), odd = __shfl_sync(0xFFFFFFFFu, both, 8 * t + 4);
-                rest_lo = __byte_perm(even, odd, 0x5410);
-                rest_hi = __byte_perm(even, odd, 0x7632);
-            }
-#pragma unroll
-            for (int m = 0; m < D / 16; ++m) {
-                // dimensions 2m and 2m + 1 of the lane's sixteen (or eight): byte 2 (m & 1) and the next of word m / 2
-                uint32_t a[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const uint32_t from = 2u * (m & 1) + (k & 1);      // byte of both tokens' words, to bytes 1 and 3
-                    const uint32_t x = __byte_perm(cur.v[k & 2][m >> 1], cur.v[(k & 2) + 1][m >> 1], ((4u + from) << 12) | (from << 4));
-                    a[k] = mul_bf16x2(e4_fields_as_bf16(x), k < 2 ? f_lo : f_hi);
-                    if (two_steps) a[k] = mul_bf16x2(a[k], k < 2 ? rest_lo : rest_hi);
-                }
+                // p, the denominator, and P^T's two terms as the second product's operands
+                uint32_t pt[NT][2][2];
 #pragma unroll
                 for (int j = 0; j < NT; ++j) {
-                    mma_bf16(o[j][m], a[0], a[1], a[2], a[3], pt[j][0][0], pt[j][0][1]);
-                    mma_bf16(o[j][m], a[0], a[1], a[2], a[3], pt[j][1][0], pt[j][1][1]);
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        s[j][k] = exp2_approx(s[j][k] - top[j][k]);
+                        s[j][2 + k] = exp2_approx(s[j][2 + k] - top[j][k]);
+                        l[j][k] += s[j][k] + s[j][2 + k];
+                    }
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        uint32_t p1, p2;
+                        split_bf16(s[j][2 * r], s[j][2 * r + 1], p1, p2);
+                        pt[j][0][r] = transpose8x8(p1);
+                        pt[j][1][r] = transpose8x8(p2);
+                    }
                 }
+                // values that no weight may meet, because 0 times a NaN is one: tokens behind the end, marked rows
+                const unsigned marks = __ballot_sync(0xFFFFFFFFu, marked0), marks8 = __ballot_sync(0xFFFFFFFFu, marked1);
+                if ((marks | marks8) != 0u || j0 + kBlockTokens > u.s.len) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int row = 2 * t + (r & 1);
+                        const bool drop = ((((r >> 1) ? marks8 : marks) >> (4 * row)) & 1u) || j0 + row + 8 * (r >> 1) >= u.s.len;
+                        if (drop) {
+#pragma unroll
+                            for (int k = 0; k < KvBlock<D>::kVWords; ++k) cur.v[r][k] = 0u;
+                        }
+                    }
+                }
+                // 2^(120 - d) of tokens 2t, 2t + 1, and of 2t + 8, 2t + 9
+                const int dv0 = bv[0] + kv.delta, dv1 = bv[1] + kv.delta;
+                uint32_t f_lo, f_hi, rest_lo = 0, rest_hi = 0;
+                {
+                    const uint32_t both = value_factor(dv0) | value_factor(dv1) << 16;
+                    const uint32_t even = __shfl_sync(0xFFFFFFFFu, both, 8 * t), odd = __shfl_sync(0xFFFFFFFFu, both, 8 * t + 4);
+                    f_lo = __byte_perm(even, odd, 0x5410);
+                    f_hi = __byte_perm(even, odd, 0x7632);
+                }
+                const bool two_steps = __any_sync(0xFFFFFFFFu, min(dv0, dv1) < -7);   // values beyond 2^15
+                if (two_steps) {
+                    const uint32_t both = value_factor_rest(dv0) | value_factor_rest(dv1) << 16;
+                    const uint32_t even = __shfl_sync(0xFFFFFFFFu, both, 8 * t), odd = __shfl_sync(0xFFFFFFFFu, both, 8 * t + 4);
+                    rest_lo = __byte_perm(even, odd, 0x5410);
+                    rest_hi = __byte_perm(even, odd, 0x7632);
+                }
+#pragma unroll
+                for (int m = 0; m < D / 16; ++m) {
+                    // dimensions 2m and 2m + 1 of the lane's sixteen (or eight): byte 2 (m & 1) and the next of word m / 2
+                    uint32_t a[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const uint32_t from = 2u * (m & 1) + (k & 1);      // byte of both tokens' words, to bytes 1 and 3
+                        const uint32_t x = __byte_perm(cur.v[k & 2][m >> 1], cur.v[(k & 2) + 1][m >> 1], ((4u + from) << 12) | (from << 4));
+                        a[k] = mul_bf16x2(e4_fields_as_bf16(x), k < 2 ? f_lo : f_hi);
+                        if (two_steps) a[k] = mul_bf16x2(a[k], k < 2 ? rest_lo : rest_hi);
+                    }
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) {
+                        mma_bf16(o[j][m], a[0], a[1], a[2], a[3], pt[j][0][0], pt[j][0][1]);
+                        mma_bf16(o[j][m], a[0], a[1], a[2], a[3], pt[j][1][0], pt[j][1][1]);
+                    }
+                }
+                if (i + 1 < count) load_v<D>(cur, kv.v8 + v_at, g, t);
             }
-            if (i + 1 < count) load_v<D>(cur, kv.v8 + v_at, g, t);
+            return i;
+        };
+        int done = walk(std::false_type(), 0);
+        if (done < count) {
+            // what was summed so far goes under an M that is as far above it
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    float v = l[j][k];
+                    v += __shfl_xor_sync(0xFFFFFFFFu, v, 4);
+                    v += __shfl_xor_sync(0xFFFFFFFFu, v, 8);
+                    v += __shfl_xor_sync(0xFFFFFFFFu, v, 16);
+                    const float next = fmaxf(top[j][k], top[j][k] + log2_approx(v) + (34 - __clz(u.s.len)) + kLargeLift);
+                    const float shrink = exp2_approx(top[j][k] - next);
+                    top[j][k] = next;
+                    l[j][k] *= shrink;
+#pragma unroll
+                    for (int m = 0; m < D / 16; ++m) {
+                        o[j][m][k] *= shrink;
+                        o[j][m][2 + k] *= shrink;
+                    }
+                }
+            walk(std::true_type(), done);
         }
         // ---- join the warps ----
         __syncthreads();   // the previous unit's sums have been read

@@ -328,3 +328,61 @@ def test_outputs_are_too_large_as_often_as_too_small(lib, ctx, news, gain):
     o = R.attention(cpu, case["table"].numpy(), case["q_start"].numpy(), lens, q.double().numpy(), dim ** -0.5, True, O.CONV_NATIVE)[0]
     drift = (out.double().cpu().numpy() / o - 1).mean()
     assert abs(drift) <= 5 * 2.0 ** -8 / np.sqrt(12 * o.size) + 2.0 ** -16
+
+
+def large_values(dim, powers, bias, late, everywhere, page=32):
+    """Scores of 0 and of about `powers` powers of two, the higher ones on the later tokens (late) or on the earlier; values of the
+    tokens with the higher scores, or everywhere, cast under `bias`.  The higher ones hold zeros in the last quarter of
+    their dimensions, where the others' weights decide."""
+    def edit(case, q):
+        q.zero_()
+        q[..., 0] = 1.0
+        case["k8"].zero_()
+        case["bk"].zero_()
+        case["bv"].fill_(bias if everywhere else 8)
+        for b, n in enumerate(case["kv_len"].tolist()):
+            for j in range(n):
+                if (j >= n // 2) == late:
+                    pg, off = int(case["table"][b, j // page]), j % page
+                    case["k8"][pg, :, off, 0] = 0x38 - j % 2
+                    case["bv"][pg, :, off] = bias
+                    if powers <= 55:
+                        case["v8"][pg, :, off, 3 * dim // 4:] = 0
+    return edit
+
+
+@pytest.mark.parametrize("news,heads", [(1, (8, 1)), (2, (8, 1)), (40, (4, 2)), (150, (4, 2))])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("powers", [0, 30, 39.5, 50, 59, 90])
+@pytest.mark.parametrize("bias", [-42, -72, -119])
+def test_large_values_stay_finite(lib, ctx, news, heads, dim, powers, bias):
+    """Values up to 3e38 under weights that differ by up to 2^90: where the result is a finite number, so is the output."""
+    lens = [200, 333]
+    for late in (True, False):
+        for everywhere in (False, True):
+            run_case(lib, ctx, 56, lens, [news] * 2, heads[0], heads[1], dim, 32, O.CONV_NATIVE, True, scale=powers * float(np.log(2)),
+                     edit=large_values(dim, powers, bias, late, everywhere))
+
+
+@pytest.mark.parametrize("news,heads", [(1, (8, 1)), (40, (4, 1))])
+def test_large_values_in_long_contexts(lib, ctx, news, heads):
+    """... also where a context is split: some parts hold large values, others none."""
+    for powers, late in ((0, True), (39.5, True), (50, False)):
+        run_case(lib, ctx, 57, [6000], [news], heads[0], heads[1], 128, 64, O.CONV_NATIVE, True, scale=powers * float(np.log(2)),
+                 edit=large_values(128, powers, -119, late, powers == 0, page=64))
+
+
+@pytest.mark.parametrize("news", [1, 40])
+def test_stale_biases_change_nothing(lib, ctx, news):
+    """Biases of large values behind a sequence's end, in its own pages: the same bits as with other bytes there."""
+    outs = []
+    for stale in (8, -119):
+        case = R.make_case(58, [201, 333], [news] * 2, 2, 128, 128, O.CONV_NATIVE, fill=0x30)
+        held = case["bv"] != -128
+        case["bv"][~held] = stale
+        dev, cache, batch = gpu_state(lib, case, O.CONV_NATIVE, news, 333)
+        q = torch.randn((2 * news, 8, 128), generator=torch.Generator().manual_seed(1)).to(torch.bfloat16).cuda()
+        out, lse = torch.empty_like(q), torch.empty(q.shape[:2], device="cuda")
+        ctx.attn_paged(cache, batch, q, out, lse=lse)
+        outs.append((out, lse))
+    assert torch.equal(outs[0][0].view(torch.int16), outs[1][0].view(torch.int16)) and torch.equal(outs[0][1], outs[1][1])
