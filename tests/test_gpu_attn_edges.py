@@ -386,3 +386,34 @@ def test_stale_biases_change_nothing(lib, ctx, news):
         ctx.attn_paged(cache, batch, q, out, lse=lse)
         outs.append((out, lse))
     assert torch.equal(outs[0][0].view(torch.int16), outs[1][0].view(torch.int16)) and torch.equal(outs[0][1], outs[1][1])
+
+
+@pytest.mark.parametrize("news", [1, 40])
+def test_a_cache_beyond_32_bits(lib, ctx, news):
+    """A cache of 4.6 GB whose keys and values of a page share one buffer; the tokens lie in its first and its last pages."""
+    pages, heads, size, dim, conv = 70000, 2, 128, 128, O.CONV_NATIVE
+    lens = [300, 170]
+    case = R.make_case(59, lens, [news] * 2, heads, dim, size, conv)
+    both = torch.zeros((pages, 2, heads, size, dim), dtype=torch.uint8, device="cuda")
+    biases = torch.zeros((pages, 2, heads, size), dtype=torch.int8, device="cuda")
+    assert both.numel() > 1 << 32
+    far = torch.tensor([0, pages - 1, 35001, pages - 2, 1, pages - 3, 2, pages - 4])[:case["k8"].shape[0]]
+    for n, part, t in (("k8", 0, both), ("v8", 1, both), ("bk", 0, biases), ("bv", 1, biases)):
+        t[far.cuda(), part] = case[n].cuda()
+    cache = lib.KvCache(both[:, 0], both[:, 1], biases[:, 0], biases[:, 1], conv=conv)
+    batch = lib.SeqBatch(case["q_start"].cuda(), case["kv_len"].cuda(), far[case["table"].long()].to(torch.int32).cuda(), news, 300)
+    q = torch.randn((2 * news, 8, dim), generator=case["g"]).to(torch.bfloat16)
+    out, lse = torch.empty_like(q, device="cuda"), torch.empty(q.shape[:2], device="cuda")
+    ctx.attn_paged(cache, batch, q.cuda(), out, lse=lse)
+    cpu = [case[n].numpy() for n in ("k8", "v8", "bk", "bv")]
+    check(out, lse, R.attention(cpu, case["table"].numpy(), case["q_start"].numpy(), lens, q.double().numpy(), dim ** -0.5, True, conv))
+
+
+@pytest.mark.parametrize("q_heads,kv_heads,dim", [(8, 1, 128), (4, 4, 64), (32, 2, 64)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_a_chunk_beside_many_single_tokens(lib, ctx, q_heads, kv_heads, dim, causal):
+    """What a step of a server that takes in a prompt while others go on looks like: units of one row and of 256 alternate."""
+    lens = [3, 700, 64, 129, 1, 300, 515] * 5 + [600]
+    news = [1] * 35 + [290]
+    lens[17], news[17], lens[3], news[3] = 400, 130, 0, 0
+    run_case(lib, ctx, 60, lens, news, q_heads, kv_heads, dim, 32, O.CONV_PAPER, causal)
