@@ -46,7 +46,9 @@ fp8_status_t fp8_attn_paged(fp8_ctx *ctx, const fp8_kv_cache_t *c, const fp8_seq
     const unsigned set = capture == cudaStreamCaptureStatusNone ? 0u : 1u + ctx->attn_captured++ % (kAttnSets - 1);
     p.count = ctx->d_attn_count + (size_t)set * kAttnCounters;
     p.call = ++ctx->attn_calls;
-    // at most 16 query rows per key/value head: the kernel whose instructions take 8 or 16 rows; more: tiles of 128
+    // At most 16 query rows per key/value head: the kernel whose instructions take 8 or 16 rows; more: tiles of 128.  Few rows
+    // / chunks, us from a graph, 16 sequences on up to 4096 tokens: 1 row (8/8 heads) 35 / 73, 8 rows (64/8) 36 / 75, 16 rows
+    // (64/4) 30 / 46 and (64/8, two tokens) 51 / 81; 24 rows (three tokens) 83 by chunks.
     if (rows <= 16) return attn_decode(ctx, p, c->head_dim, (int)rows, (cudaStream_t)stream);
     return attn_chunk(ctx, p, c, (cudaStream_t)stream);
 }

@@ -12,8 +12,11 @@
 //       permute brings two tokens together, five instructions make a bf16 pair.  P^T, in its two terms, comes out of
 //       S^T by 8x8 transposes (movmatrix).
 // A warp holds one block: its keys' registers are requested again (the next block's) as soon as the first product is done,
-// its values' after the second; four CTAs per SM for up to 8 rows, two above.  (Together with the join's many loads in
-// flight this took 16 sequences on 4096 from 40.2 us, with two blocks per warp, to 35.8.)  The blocks of all (sequence,
+// its values' after the second.  (Together with the join's many loads in flight this took 16 sequences on 4096 from 40.2 us,
+// with two blocks per warp, to 35.8.)  CTAs per SM (decode_ctas) are as many as the registers allow without a spill: up to 8
+// rows three of 168 registers for 128 dimensions (four of 128 spill 84 bytes: 16 sequences on 4096 36.9 against 35.7 us, 64 on
+// 512 28.1 against 26.2) and four of 128 for 64 dimensions (three: 32/32 heads, 16 on 4096, 72 against 64 us); up to 16 rows
+// two of 254 and 189.  The blocks of all (sequence,
 // head) units form one list, cut evenly between the CTAs (a sequence's length changes nothing in the balance); a unit that
 // lies in several CTAs leaves partial sums in the workspace, joined in order by the CTA that arrives last, so results do
 // not depend on the order of arrival.
@@ -29,6 +32,7 @@ namespace fp8lin {
 constexpr int kDecodeWarps = 4;
 constexpr int kDecodeThreads = 32 * kDecodeWarps;
 constexpr int kBlockTokens = 16;
+constexpr int decode_ctas(int d, int nt) { return nt > 1 ? 2 : d == 128 ? 3 : 4; }
 
 // M is moved when a score exceeds it by more than kSlack, to that score.  Once values are large no weight may be above a
 // quarter divided by the number of tokens: M is moved when a score comes closer to it than that, to kLargeLift further away.
@@ -142,7 +146,7 @@ struct Unit {
 __device__ __forceinline__ int unit_blocks(const SeqShape &s) { return s.n > 0 ? max(1, (s.len + kBlockTokens - 1) / kBlockTokens) : 0; }
 
 template <int D, int NT>
-__global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 4 : 2) attn_decode_kernel(const __grid_constant__ AttnParams p)
+__global__ void __launch_bounds__(kDecodeThreads, decode_ctas(D, NT)) attn_decode_kernel(const __grid_constant__ AttnParams p)
 {
     constexpr int kRows = 8 * NT;
     constexpr int kPart = kRows * (D + 2);       // floats of a partial result
@@ -293,8 +297,8 @@ __global__ void __launch_bounds__(kDecodeThreads, NT == 1 ? 4 : 2) attn_decode_k
             l[j][0] = l[j][1] = 0.0f;
         }
 
-        // The blocks from i on; without LARGE up to the first that holds large values, whose index is returned.  (Two loops: one
-        // for both costs the few registers that it has too many, 16 sequences on 4096 tokens 37.4 against 36.5 us.)
+        // The blocks from i on; without LARGE up to the first that holds large values, whose index is returned.  (One loop
+        // for both, with the margin in a register: 16 sequences on 4096 tokens 37.4 against 36.5 us at four CTAs per SM.)
         auto walk = [&](auto large_mode, int i) {
             constexpr bool kLarge = decltype(large_mode)::value;
             const float margin = (float)(34 - __clz(u.s.len));        // log2 of four times the tokens, and up to one more
@@ -577,7 +581,7 @@ static fp8_status_t launch_decode(const fp8_ctx *ctx, const AttnParams &p, cudaS
     const KvParams &kv = p.kv;
     // an upper bound of the list's length; CTAs beyond the blocks that there are leave at once
     const int64_t blocks = (int64_t)kv.seqs * kv.kv_heads * ((kv.max_kv_len + kBlockTokens - 1) / kBlockTokens);
-    int64_t grid = (int64_t)ctx->sm_count * (NT == 1 ? 4 : 2);
+    int64_t grid = (int64_t)ctx->sm_count * decode_ctas(D, NT);
     if ((blocks + kDecodeWarps - 1) / kDecodeWarps < grid) grid = (blocks + kDecodeWarps - 1) / kDecodeWarps;
     if (grid > kAttnCounters) return FP8_ERR_UNSUPPORTED;
     count_launch();
