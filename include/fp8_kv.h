@@ -11,6 +11,9 @@
  *             under 64); 0 for a row of zeros
  *     byte  = RNE_E4(x * 2^(bias + delta)), saturating, exactly as fp8_cast_e4 with that bias
  *     number read back = native(byte) * 2^-(bias + delta),   delta = 1 under FP8_CONV_PAPER, else 0.
+ * Under FP8_CONV_PAPER the largest byte is 448 for the paper's 480: rows whose amax lies in (232, 240] times a power of two
+ * clip and raise FP8_FLAG_SATURATED, about one row in twenty of ordinary data, so the flag says little for such a cache.
+ * Under FP8_CONV_NATIVE no finite row clips.
  * A row that holds an infinity or a NaN is cast under bias 0 and marked with the bias FP8_KV_BIAS_NONFINITE
  * (FP8_FLAG_NONFINITE_AMAX is raised): it reads back as cast, and the attention of every query that sees the row, and
  * of no other, gives NaN.
@@ -82,7 +85,14 @@ FP8_API fp8_status_t fp8_kv_read(fp8_ctx *ctx, const fp8_kv_cache_t *cache, cons
 /* Attention of the new tokens over the cached ones, query head h reading key/value head h / (q_heads / kv_heads):
  *     out[r, h] = sum_j p_j v_j / sum_j p_j,   p_j = exp(scale * q[r, h] . k_j),
  * j over the d_kv_len[b] cached tokens of the row's sequence, with causal != 0 only over those up to the row's own.
- * K and V are the numbers of fp8_kv_read; products, sums and softmax statistics are FP32.
+ * K and V are the numbers of fp8_kv_read.  Sums and softmax statistics are FP32.  What enters the products:
+ *   up to 16 query rows per key/value head (max_q_len * q_heads / kv_heads): a query row as fp16 under a power of two (exact
+ *     for numbers down to 2^-28 of the row's largest); a weight p_j with 16 bits
+ *   more rows: a query row as two 8-bit floats under a power of two (exact down to 2^-13 of the row's largest, within 2^-21
+ *     of the largest below that); a weight with 11 bits, off by 2^-10 of itself at most, by nothing on average and
+ *     where its bits suffice (one token, equal scores)
+ * Results are finite wherever the formula's are within bf16's range; in sequences with values of 2^49 and more, weights below
+ * 2^-77 of the largest may be lost.
  *   q      [tokens][q_heads][head_dim] bf16, rows ld_q elements apart, heads contiguous
  *   out    [tokens][q_heads][head_dim] bf16, rows ld_o elements apart
  *   d_lse  NULL, or out float [tokens][q_heads]: ln sum_j p_j (what joining with attention over other keys needs)

@@ -27,8 +27,9 @@
 // different kinds and accumulators are not ordered by being issued one after the other, so the second product is committed
 // to a barrier of the slot, and the next scores of the slot are issued only behind it.  (Halves of 64 tokens in turn within a
 // slot were slower, 1736 against 1517 us in separate runs: scores of 64 columns cost the tensor cores 1.5 times their share.)
-// Measured from a graph: 2048 tokens on 16384, 64/8 heads of 128, 1391 us, 741 TFLOP/s.  A step takes about 6200 cycles,
-// its products 3072 of them; the softmax's chain of latencies and the wait for scores take the rest.
+// Measured from a graph: 2048 tokens on 16384, 64/8 heads of 128, 1453 us, 709 TFLOP/s.  A step takes about 6800 cycles, its
+// products 3072 of them; the softmax's chain of latencies and the waits for products and scores take the rest (before
+// the wait between the second product and the next scores, and the care for large values: 1391 us).
 //
 // The steps of all units (query tiles of a key/value head) form one list that is cut evenly between the CTAs, whatever the
 // sequences' lengths and the mask; a unit that lies in several CTAs leaves partial sums in the workspace, joined in order

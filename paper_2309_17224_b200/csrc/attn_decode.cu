@@ -20,9 +20,9 @@
 // head) units form one list, cut evenly between the CTAs (a sequence's length changes nothing in the balance); a unit that
 // lies in several CTAs leaves partial sums in the workspace, joined in order by the CTA that arrives last, so results do
 // not depend on the order of arrival.
-// Measured from a graph (64/8 heads of 128): 16 ragged sequences on up to 4096 tokens 36 us for 109 MB (17 us at the
-// measured copy rate).  Longer contexts add 5.1 to 5.75 TB/s; about 14 us are fixed: launch, lookup, first loads, changes
-// of unit, and 2.6 us for the join.
+// Measured from a graph (64/8 heads of 128): 16 ragged sequences on up to 4096 tokens 35.4 us for 109 MB (17 us at the
+// measured copy rate), on up to 16384 95 us for 435 MB.  Longer contexts add 5.45 TB/s; about 15 us are fixed: launch, lookup,
+// first loads, changes of unit, and the join (2.6 us, taken at four CTAs per SM).
 #include <type_traits>
 
 #include "attn_common.cuh"

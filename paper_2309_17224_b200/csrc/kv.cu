@@ -5,7 +5,9 @@
 // A warp takes one token and a few of its heads, keys and values together (the walk row -> sequence -> page is done once,
 // and its three dependent loads overlap the loads of the numbers), and ends: blocks that come and go fill the SMs evenly,
 // where a resident grid that walks the tokens loses the last, partly filled round (8192 tokens of 32 heads of 128: 41.8
-// against 43.9 us; 65536 tokens read: 53.9 against 57.3).  Memory-bound: 201 MB in 41.8 us, 320 MB in 53.9 us.
+// against 43.9 us; 65536 tokens of 8 heads read: 53.9 against 57.3, both when this was chosen).  Measured from a graph: the
+// first 41.7 us for 202 MB (FP16 41.5, FP32 65.3 for 336 MB), bound by instruction issue; the second 52.8 us for 320 MB (FP32
+// 86.1 for 533 MB), bound by memory.
 // Four heads one after the other per lane group, 128 bytes in flight per lane; two where that would leave the SMs half
 // empty (16 tokens of 8 heads: 3.1 against 4.2 us; 8192 tokens of 32 heads: 44.2 against 41.8).
 #include "kv_common.cuh"

@@ -68,6 +68,9 @@ class PagePool:
         return start, lens, rows
 
     def batch(self, seqs: Sequence, new_tokens: Sequence[int], device="cuda") -> "fp8lin.SeqBatch":
+        """The index tensors of a step, for all layers of it: new storage and three copies from host memory that the caller
+        waits for (48 us for one sequence of 64 pages, 104 for 16, 274 for 64).  A captured graph keeps reading the tensors that
+        it was captured with: a program that replays one keeps a batch and copies new starts, lengths and pages into it."""
         start, lens, rows = self.indices(seqs, new_tokens)
         i32 = dict(dtype=torch.int32, device=device)
         return fp8lin.SeqBatch(torch.tensor(start, **i32), torch.tensor(lens, **i32),
@@ -76,7 +79,9 @@ class PagePool:
 
 
 def empty_cache(pages: int, kv_heads: int, page_size: int, head_dim: int, conv: int = fp8lin.CONV_PAPER, device="cuda"):
-    """The pages of one layer, uninitialised (what no token was written to is never read)."""
+    """The pages of one layer, uninitialised (what no token was written to is never read).  With CONV_PAPER, the convention of
+    the linears, about one row in twenty clips its largest numbers by up to a fifteenth and raises FLAG_SATURATED; with
+    CONV_NATIVE none does."""
     k8, v8 = (torch.empty((pages, kv_heads, page_size, head_dim), dtype=torch.uint8, device=device) for _ in range(2))
     bk, bv = (torch.empty((pages, kv_heads, page_size), dtype=torch.int8, device=device) for _ in range(2))
     return fp8lin.KvCache(k8, v8, bk, bv, conv=conv)
