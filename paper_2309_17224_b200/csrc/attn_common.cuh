@@ -48,7 +48,7 @@ __device__ __forceinline__ float exp2_approx(float x)
 }
 // 2^-b for the keys cast under bias b (delta added), 2^-kKeyLift of it
 __device__ __forceinline__ float key_factor(int b) { return pow2_normal(min(126, -b) - kKeyLift); }
-// c 2^-e with the keys' powers of two, -113 <= -e <= 126 or so; finite, so that a score of 0 stays 0
+// c 2^-e with the keys' powers of two, for e from -120 to 126; finite, so that a score of 0 stays 0
 __device__ __forceinline__ float query_factor(float c, int e)
 {
     const int n = kKeyLift - e;
