@@ -1,0 +1,126 @@
+// What the row-wise kernels (norm.cu, loss.cu) share: elements of three types, reductions, the amax of an output.
+#pragma once
+
+#include <float.h>
+
+#include "cast_common.cuh"
+
+namespace fp8lin {
+
+inline bool row_aligned(const void *p, int64_t ld, int dt, unsigned bytes)
+{
+    return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * (dt == FP8_F32 ? 4 : 2))) & (bytes - 1)) == 0;
+}
+inline bool element_aligned(const void *p, int dt) { return (reinterpret_cast<uintptr_t>(p) & (dt == FP8_F32 ? 3u : 1u)) == 0; }
+
+// Launches go to the context's device, whichever is the caller's current one (the default streams of all devices share a
+// handle).
+struct OnDevice {
+    int before = -1;
+    explicit OnDevice(int device)
+    {
+        int now = device;
+        if (cudaGetDevice(&now) == cudaSuccess && now != device && cudaSetDevice(device) == cudaSuccess) before = now;
+    }
+    ~OnDevice()
+    {
+        if (before >= 0) cudaSetDevice(before);
+    }
+    OnDevice(const OnDevice &) = delete;
+    OnDevice &operator=(const OnDevice &) = delete;
+};
+
+// Where a call's amax goes (nowhere where slot is NULL): blocks fold their maxima into a slot of the context, the last
+// one publishes the amax and, where asked, its scaling bias, and leaves the slot zeroed for the next call.
+struct AmaxSink {
+    unsigned *slot;
+    float *d_amax;
+    int32_t *d_bias;
+    unsigned *d_status;
+    int fmt, conv, margin;
+};
+
+#ifdef __CUDACC__
+
+// v rounded to the tensors' type, as a float; the element's bits
+template <int DT>
+__device__ __forceinline__ uint32_t element_bits(float v)
+{
+    if (DT == FP8_F32) return __float_as_uint(v);
+    uint32_t w;
+    if (DT == FP8_BF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(0.0f), "f"(v));
+    else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(0.0f), "f"(v));
+    return w & 0xFFFFu;
+}
+template <int DT>
+__device__ __forceinline__ float element_value(uint32_t bits)
+{
+    if (DT == FP8_F32) return __uint_as_float(bits);
+    if (DT == FP8_BF16) return __uint_as_float(bits << 16);
+    float f;
+    asm("cvt.f32.f16 %0, %1;" : "=f"(f) : "h"((uint16_t)bits));
+    return f;
+}
+template <int DT>
+__device__ __forceinline__ void store_bits(void *y, int64_t i, uint32_t bits)
+{
+    if (DT == FP8_F32) reinterpret_cast<uint32_t *>(y)[i] = bits;
+    else reinterpret_cast<uint16_t *>(y)[i] = (uint16_t)bits;
+}
+__device__ __forceinline__ float load_any(const void *x, int dt, int64_t i)
+{
+    if (dt == FP8_F32) return load1<FP8_F32>(x, i);
+    return dt == FP8_BF16 ? load1<FP8_BF16>(x, i) : load1<FP8_F16>(x, i);
+}
+
+// Magnitudes as unsigned numbers: NaN above infinity above what is finite.
+__device__ __forceinline__ uint32_t magnitude_key(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+
+__device__ __forceinline__ float warp_sum(float v)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    return v;
+}
+
+// Sum over the block, to all threads.  `part`: one word a warp; two calls in a row use different words, and there is a
+// barrier between a call and the one after the next.
+template <int THREADS>
+__device__ __forceinline__ float block_sum(float v, float *part)
+{
+    v = warp_sum(v);
+    if (THREADS == 32) return v;
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = part[0];
+#pragma unroll
+    for (int i = 1; i < THREADS / 32; ++i) v += part[i];
+    return v;
+}
+
+// Fold a thread's magnitude key into the sink; every thread of every block calls it once, at the end.
+__device__ __forceinline__ void sink_amax(uint32_t key, const AmaxSink &o)
+{
+    __shared__ uint32_t warp_max[32];
+    if (!o.slot) return;
+    key = __reduce_max_sync(0xFFFFFFFFu, key);
+    if ((threadIdx.x & 31) == 0) warp_max[threadIdx.x >> 5] = key;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    for (unsigned i = 1; i < blockDim.x / 32; ++i) key = max(key, warp_max[i]);
+    atomicMax(&o.slot[0], key);
+    __threadfence();
+    if (atomicAdd(&o.slot[1], 1u) + 1u != gridDim.x) return;
+    __threadfence();
+    key = atomicExch(&o.slot[0], 0u);
+    o.slot[1] = 0u;
+    if (o.d_amax) *o.d_amax = __uint_as_float(key);
+    if (o.d_bias) {
+        unsigned flags = 0;
+        *o.d_bias = bias_from_amax_bits(key, o.fmt, o.conv, o.margin, &flags);
+        if (flags) atomicOr(o.d_status, flags);
+    }
+}
+
+#endif
+}  // namespace fp8lin

@@ -29,6 +29,10 @@ ACT_GELU = 1
 ACT_SWIGLU = 2
 FLAG_NONFINITE_AMAX, FLAG_ZERO_AMAX, FLAG_SATURATED, FLAG_TIMEOUT, FLAG_BAD_INDEX = 1, 2, 4, 8, 16
 KV_BIAS_NONFINITE, KV_BIAS_MAX = -128, 64
+NORM_LAYER, NORM_RMS = 0, 1
+I32, I64 = 0, 1
+DISTILL_TOP, DISTILL_REST = 0, 1
+LOSS_SAVED, LOSS_TOP_MAX, LOSS_LISTED_MAX, LOSS_VOCAB_MAX = 4, 128, 256, 1 << 20
 
 SYMBOLS = (
     "fp8_create", "fp8_destroy", "fp8_status_string", "fp8_device_flags", "fp8_amax", "fp8_scaling_bias",
@@ -36,6 +40,7 @@ SYMBOLS = (
     "fp8_linear_wgrad", "fp8_amax_noalloc", "fp8_linear_fwd_act", "fp8_cast_predicted", "fp8_prediction_stats",
     "fp8_linear_dgrad_act", "fp8_selftest_wait_expiry", "fp8_range_stats", "fp8_linear_fwd_q", "fp8_linear_dgrad_q", "fp8_amax_history_bias", "fp8_launch_count", "fp8_cast_group", "fp8_selftest_mma_ceiling", "fp8_bias_log_append", "fp8_bias_mode", "fp8_linear_f16acc", "fp8_linear_infer", "fp8_linear_infer_cast", "fp8_linear_group",
     "fp8_kv_append", "fp8_kv_read", "fp8_attn_paged",
+    "fp8_norm_fwd", "fp8_norm_bwd", "fp8_token_logprobs", "fp8_token_logprobs_bwd", "fp8_distill_fwd", "fp8_distill_bwd",
     "fp8h_gelu", "fp8h_gelu_backward", "fp8h_mse_grad", "fp8h_sgd",
 )
 
@@ -119,6 +124,31 @@ _lib.fp8_kv_append.argtypes = [_P, POINTER(KvCacheDesc), POINTER(SeqBatchDesc), 
 _lib.fp8_kv_read.argtypes = _lib.fp8_kv_append.argtypes
 _lib.fp8_attn_paged.argtypes = [_P, POINTER(KvCacheDesc), POINTER(SeqBatchDesc), _P, c_int64, c_int32, _P, c_int64, _P,
                                 c_float, c_int32, c_int, _P]
+
+
+class NormFwdDesc(ctypes.Structure):
+    """``fp8_norm_fwd_t``."""
+    _fields_ = [(n, c_void_p) for n in ("x", "residual", "weight", "bias_vec", "h", "y", "d_mean", "d_rstd", "y8", "d_bias_in",
+                                        "d_amax", "d_bias_out")] + \
+               [(n, c_int64) for n in ("rows", "cols", "ld_x", "ld_residual", "ld_h", "ld_y")] + \
+               [(n, c_int32) for n in ("kind", "dt", "w_dt", "conv", "margin")] + [("eps", c_float)]
+
+
+class NormBwdDesc(ctypes.Structure):
+    """``fp8_norm_bwd_t``."""
+    _fields_ = [(n, c_void_p) for n in ("dy", "h", "dh", "weight", "d_mean", "d_rstd", "dx", "dw", "db", "d_amax")] + \
+               [(n, c_int64) for n in ("rows", "cols", "ld_dy", "ld_h", "ld_dh", "ld_dx")] + \
+               [(n, c_int32) for n in ("kind", "dt", "w_dt", "reserved")]
+
+
+_lib.fp8_norm_fwd.argtypes = [_P, POINTER(NormFwdDesc), _P]
+_lib.fp8_norm_bwd.argtypes = [_P, POINTER(NormBwdDesc), _P]
+_logits_args = [_P, _P, c_int, c_int64, c_int64, c_int64, c_float]
+_list_args = [_P, c_int, c_int64, _P, c_int64, c_int32, c_int]
+_lib.fp8_token_logprobs.argtypes = _logits_args + [_P, c_int, _P, _P, _P, _P, c_int32, _P, _P, _P]
+_lib.fp8_token_logprobs_bwd.argtypes = _logits_args + [_P, c_int, _P, _P, c_int64, _P, c_int64, _P, c_int64, _P, _P]
+_lib.fp8_distill_fwd.argtypes = _logits_args + _list_args + [_P, _P, _P]
+_lib.fp8_distill_bwd.argtypes = _logits_args + _list_args + [_P, _P, c_int64, _P, c_int64, _P, _P]
 _lib.fp8h_gelu.argtypes = [_P, _P, c_int64, _P]
 _lib.fp8h_gelu_backward.argtypes = [_P, _P, _P, c_int64, _P]
 _lib.fp8h_mse_grad.argtypes = [_P, _P, ctypes.c_float, _P, c_int64, _P]
@@ -279,6 +309,42 @@ def _rows3(t, heads, dim, what, device):
                          f"strides {stride}")
     return stride[0] if shape[0] > 1 else heads * dim
 
+
+_IT = {torch.int32: I32, torch.int64: I64}
+
+
+def _matrix(t, shape, dtypes, what, device):
+    """Check a 2-D tensor (shape, one of the types, contiguous rows, the context's GPU); its row distance in elements."""
+    if t.get_device() != device:
+        raise ValueError(f"{what}: a tensor on GPU {device} expected, got one on {t.device}")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{what}: {' or '.join(str(d) for d in dtypes)} expected, got {t.dtype}")
+    if t.dim() != 2 or (shape is not None and t.shape != shape) or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what}: {'two dimensions' if shape is None else tuple(shape)} with contiguous rows expected, got "
+                         f"{tuple(t.shape)} strides {t.stride()}")
+    rows, cols = t.shape
+    ld = t.stride(0) if rows > 1 else cols
+    if ld < cols:
+        raise ValueError(f"{what}: rows overlap (strides {t.stride()})")
+    return ld
+
+
+def _vector(t, n, dtypes, what, device, strided=False):
+    """Check a 1-D tensor of n elements (contiguous, or any distance with ``strided``); the distance of its elements."""
+    if t.get_device() != device:
+        raise ValueError(f"{what}: a tensor on GPU {device} expected, got one on {t.device}")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{what}: {' or '.join(str(d) for d in dtypes)} expected, got {t.dtype}")
+    if t.dim() != 1 or t.shape[0] != n or (not strided and n > 1 and t.stride(0) != 1):
+        raise ValueError(f"{what}: {n} {'' if strided else 'contiguous '}elements expected, got {tuple(t.shape)} strides {t.stride()}")
+    return t.stride(0) if n > 1 else 1
+
+
+def _address(t):
+    return None if t is None else t.data_ptr()
+
+
+_F32 = (torch.float32,)
 
 MATMUL_FWD, MATMUL_DGRAD, MATMUL_WGRAD = 0, 1, 2
 
@@ -581,6 +647,166 @@ class Context:
                                      _raw_stream(self.device))
         if status:
             _check(status, "fp8_attn_paged")
+
+    # -- norm between two linears (include/fp8_norm.h); calls without rows check their arguments and launch nothing -------
+    def norm_fwd(self, x, weight=None, bias_vec=None, residual=None, eps=1e-5, kind=NORM_LAYER, h=None, y=None, d_mean=None,
+                 d_rstd=None, y8=None, d_bias=None, d_amax_out=None, d_bias_out=None, conv=CONV_PAPER, margin=0):
+        """``fp8_norm_fwd``: x, residual, h, y [rows, cols] of one type; weight, bias_vec [cols] of that type or float32;
+        y8 uint8 [rows, cols]; d_bias: the bias to cast under, None for that of Eq. 3 (d_bias_out)."""
+        dev = self.device
+        ld_x = _matrix(x, None, _DT, "x", dev)
+        shape, dt = x.shape, (x.dtype,)
+        rows, cols = shape
+        lds = [0 if t is None else _matrix(t, shape, dt, what, dev) for t, what in ((residual, "residual"), (h, "h"), (y, "y"))]
+        w_dt = self._vectors(((weight, "weight"), (bias_vec, "bias_vec")), cols, x.dtype)
+        for t, n, want, what in ((d_mean, rows, _F32, "d_mean"), (d_rstd, rows, _F32, "d_rstd"), (d_amax_out, 1, _F32, "d_amax_out"),
+                                 (d_bias, 1, (torch.int32,), "d_bias"), (d_bias_out, 1, (torch.int32,), "d_bias_out")):
+            if t is not None:
+                _vector(t, n, want, what, dev)
+        if y8 is not None and _matrix(y8, shape, (torch.uint8,), "y8", dev) != cols:
+            raise ValueError("y8: contiguous bytes expected")
+        if rows == 0:
+            return
+        desc = NormFwdDesc(x.data_ptr(), _address(residual), _address(weight), _address(bias_vec), _address(h), _address(y),
+                           _address(d_mean), _address(d_rstd), _address(y8), _address(d_bias), _address(d_amax_out),
+                           _address(d_bias_out), rows, cols, ld_x, *lds, kind, _DT[x.dtype], w_dt, conv, margin, eps)
+        status = _lib.fp8_norm_fwd(self._h, byref(desc), _raw_stream(dev))
+        if status:
+            _check(status, "fp8_norm_fwd")
+
+    def norm_bwd(self, dy, h, weight, d_mean, d_rstd, dx, dh=None, dw=None, db=None, d_amax=None, kind=NORM_LAYER):
+        """``fp8_norm_bwd``: dy, h, dh, dx [rows, cols] of one type; weight, dw, db [cols] of that type or float32; d_mean
+        (None for NORM_RMS), d_rstd float32 [rows]."""
+        dev = self.device
+        ld_dy = _matrix(dy, None, _DT, "dy", dev)
+        shape, dt = dy.shape, (dy.dtype,)
+        rows, cols = shape
+        ld_h = _matrix(h, shape, dt, "h", dev)
+        ld_dh, ld_dx = [0 if t is None else _matrix(t, shape, dt, what, dev) for t, what in ((dh, "dh"), (dx, "dx"))]
+        w_dt = self._vectors(((weight, "weight"), (dw, "dw"), (db, "db")), cols, dy.dtype)
+        for t, n, what in ((d_mean, rows, "d_mean"), (d_rstd, rows, "d_rstd"), (d_amax, 1, "d_amax")):
+            if t is not None:
+                _vector(t, n, _F32, what, dev)
+        if rows == 0:
+            for t in (dw, db):
+                if t is not None:
+                    t.zero_()
+            return
+        desc = NormBwdDesc(dy.data_ptr(), h.data_ptr(), _address(dh), _address(weight), _address(d_mean), _address(d_rstd),
+                           _address(dx), _address(dw), _address(db), _address(d_amax), rows, cols, ld_dy, ld_h, ld_dh, ld_dx, kind,
+                           _DT[dy.dtype], w_dt, 0)
+        status = _lib.fp8_norm_bwd(self._h, byref(desc), _raw_stream(dev))
+        if status:
+            _check(status, "fp8_norm_bwd")
+
+    def _vectors(self, named, cols, dtype):
+        """Check vectors of ``cols`` elements, all of one type: ``dtype`` or float32; that type."""
+        w_dt = None
+        for t, what in named:
+            if t is not None:
+                _vector(t, cols, (dtype,) if dtype == torch.float32 else (dtype, torch.float32), what, self.device)
+                if w_dt not in (None, t.dtype):
+                    raise ValueError(f"{what}: the type of the other vectors ({w_dt}) expected, got {t.dtype}")
+                w_dt = t.dtype
+        return _DT[w_dt or dtype]
+
+    # -- a head's losses (include/fp8_loss.h); calls without rows check their arguments and launch nothing -----------------
+    def _logits(self, logits, scale):
+        ld = _matrix(logits, None, _DT, "logits", self.device)
+        rows, vocab = logits.shape
+        return rows, (self._h, logits.data_ptr(), _DT[logits.dtype], ld, rows, vocab, scale)
+
+    def _saved(self, saved, rows):
+        if saved is not None and _matrix(saved, (rows, LOSS_SAVED), _F32, "saved", self.device) != LOSS_SAVED:
+            raise ValueError("saved: contiguous float32 [rows, 4] expected")
+        return _address(saved)
+
+    def _row_numbers(self, t, rows, what):
+        """Pointer and stride of one float32 a row (None: no pointer)."""
+        if t is None:
+            return None, 0
+        return t.data_ptr(), _vector(t, rows, _F32, what, self.device, strided=True)
+
+    def token_logprobs(self, logits, targets=None, scale=1.0, logprob=None, entropy=None, lse=None, saved=None, top_logprob=None,
+                       top_index=None):
+        """``fp8_token_logprobs``: logits [rows, vocab] bf16, fp16 or fp32; targets int32 or int64 [rows] (negative: none);
+        logprob, entropy, lse float32 [rows]; saved float32 [rows, 4]; top_logprob float32 and top_index (the type of
+        targets) [rows, k]."""
+        rows, args = self._logits(logits, scale)
+        for t, what in ((logprob, "logprob"), (entropy, "entropy"), (lse, "lse")):
+            if t is not None:
+                _vector(t, rows, _F32, what, self.device)
+        it = targets.dtype if targets is not None else top_index.dtype if top_index is not None else torch.int32
+        if targets is not None:
+            _vector(targets, rows, _IT, "targets", self.device)
+        k = 0
+        if (top_logprob is None) != (top_index is None):
+            raise ValueError("top_logprob and top_index go together")
+        if top_index is not None:
+            k = top_index.shape[-1]
+            for t, want, what in ((top_index, (it,) if targets is not None else _IT, "top_index"), (top_logprob, _F32, "top_logprob")):
+                if _matrix(t, (rows, k), want, what, self.device) != k:
+                    raise ValueError(f"{what}: contiguous [rows, k] expected")
+        keep = self._saved(saved, rows)
+        if rows == 0:
+            return
+        status = _lib.fp8_token_logprobs(*args, _address(targets), _IT[it], _address(logprob), _address(entropy), _address(lse), keep, k,
+                                         _address(top_logprob), _address(top_index), _raw_stream(self.device))
+        if status:
+            _check(status, "fp8_token_logprobs")
+
+    def token_logprobs_bwd(self, logits, targets, saved, dlogits, g_logprob=None, g_entropy=None, scale=1.0, d_amax=None):
+        """``fp8_token_logprobs_bwd``: saved as the forward call left it; g_logprob, g_entropy float32 [rows], any stride;
+        dlogits like logits (or logits itself)."""
+        rows, args = self._logits(logits, scale)
+        ld_d = _matrix(dlogits, logits.shape, (logits.dtype,), "dlogits", self.device)
+        if targets is not None:
+            _vector(targets, rows, _IT, "targets", self.device)
+        if d_amax is not None:
+            _vector(d_amax, 1, _F32, "d_amax", self.device)
+        keep = self._saved(saved, rows)
+        g_lp, g_h = self._row_numbers(g_logprob, rows, "g_logprob"), self._row_numbers(g_entropy, rows, "g_entropy")
+        if rows == 0:
+            return
+        status = _lib.fp8_token_logprobs_bwd(*args, _address(targets), I32 if targets is None else _IT[targets.dtype], keep, *g_lp, *g_h,
+                                             dlogits.data_ptr(), ld_d, _address(d_amax), _raw_stream(self.device))
+        if status:
+            _check(status, "fp8_token_logprobs_bwd")
+
+    def _teacher(self, index, value, rows, rest):
+        if index.dim() != 2 or index.shape[0] != rows:
+            raise ValueError(f"index: [{rows}, listed] expected, got {tuple(index.shape)}")
+        ld_i = _matrix(index, index.shape, _IT, "index", self.device)
+        ld_v = _matrix(value, index.shape, _F32, "value", self.device)
+        return index.data_ptr(), _IT[index.dtype], ld_i, value.data_ptr(), ld_v, index.shape[1], DISTILL_REST if rest else DISTILL_TOP
+
+    def distill_fwd(self, logits, index, value, loss, rest=True, scale=1.0, saved=None):
+        """``fp8_distill_fwd``: index int32 or int64, value float32 [rows, listed] (what ``token_logprobs`` writes as
+        top_index and top_logprob); loss float32 [rows]; saved float32 [rows, 4]."""
+        rows, args = self._logits(logits, scale)
+        teacher = self._teacher(index, value, rows, rest)
+        _vector(loss, rows, _F32, "loss", self.device)
+        keep = self._saved(saved, rows)
+        if rows == 0:
+            return
+        status = _lib.fp8_distill_fwd(*args, *teacher, loss.data_ptr(), keep, _raw_stream(self.device))
+        if status:
+            _check(status, "fp8_distill_fwd")
+
+    def distill_bwd(self, logits, index, value, saved, g_loss, dlogits, rest=True, scale=1.0, d_amax=None):
+        """``fp8_distill_bwd``: saved as the forward call left it; g_loss float32 [rows], any stride; dlogits like logits (or
+        logits itself)."""
+        rows, args = self._logits(logits, scale)
+        teacher = self._teacher(index, value, rows, rest)
+        ld_d = _matrix(dlogits, logits.shape, (logits.dtype,), "dlogits", self.device)
+        if d_amax is not None:
+            _vector(d_amax, 1, _F32, "d_amax", self.device)
+        keep, g = self._saved(saved, rows), self._row_numbers(g_loss, rows, "g_loss")
+        if rows == 0:
+            return
+        status = _lib.fp8_distill_bwd(*args, *teacher, keep, *g, dlogits.data_ptr(), ld_d, _address(d_amax), _raw_stream(self.device))
+        if status:
+            _check(status, "fp8_distill_bwd")
 
 
 def raw():
