@@ -7,6 +7,7 @@ namespace fp8lin {
 cudaError_t configure_gemm_kernels(int max_smem_optin);  // gemm.cu
 cudaError_t configure_attn_kernels();                    // attn_chunk.cu
 cudaError_t configure_loss_kernels();                    // loss.cu
+cudaError_t configure_norm_kernels();                    // norm.cu
 std::atomic<unsigned long long> g_kernel_launches{0};
 }
 
@@ -77,7 +78,7 @@ fp8_status_t fp8_create(fp8_ctx **out, int device)
     }
     ctx->encode_tiled = (fp8lin::EncodeTiledFn)fn;
     if (fp8lin::configure_gemm_kernels(ctx->max_smem_optin) != cudaSuccess || fp8lin::configure_attn_kernels() != cudaSuccess ||
-        fp8lin::configure_loss_kernels() != cudaSuccess) {
+        fp8lin::configure_loss_kernels() != cudaSuccess || fp8lin::configure_norm_kernels() != cudaSuccess) {
         cudaFree(ctx->d_partial);
         cudaFree(buf);
         delete ctx;

@@ -48,21 +48,6 @@ struct Row {
     __device__ __forceinline__ int edge(int t) const { return t < head ? t : tail + t - head < n ? tail + t - head : -1; }
 };
 
-template <int DT>
-__device__ __forceinline__ void unpack(const uint4 &v, float (&f)[Row<DT>::kVec])
-{
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-    float g[4];
-    unpack4<DT>(w, g);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) f[i] = g[i];
-    if (DT != FP8_F32) {
-        unpack4<DT>(w + 2, g);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) f[Row<DT>::kVec - 4 + i] = g[i];
-    }
-}
-
 // A vector whose elements are all -infinity.
 template <int DT>
 __device__ __forceinline__ uint4 no_vector()
@@ -197,7 +182,7 @@ __device__ __forceinline__ void find_top(const Row<DT> &row, float m, int k, Top
         flagged &= flagged - 1;
         for (int v = owner + lane * kLossThreads; v < row.vecs; v += 32 * kLossThreads) {
             float f[Row<DT>::kVec];
-            unpack<DT>(__ldg(row.vectors() + v), f);
+            unpack_vector<DT>(__ldg(row.vectors() + v), f);
 #pragma unroll
             for (int i = 0; i < Row<DT>::kVec; ++i) offer(f[i], row.head + v * Row<DT>::kVec + i);
         }
@@ -278,7 +263,7 @@ __device__ __forceinline__ void stream_row(const Row<DT> &row, float c, Sums &su
         for (int u = 0; u < kUnroll; ++u) {
             float f[kVec];
             hide(v0 + u * kLossThreads, raw[u]);
-            unpack<DT>(raw[u], f);
+            unpack_vector<DT>(raw[u], f);
             float top = f[0];
 #pragma unroll
             for (int i = 1; i < kVec; ++i) top = fmaxf(top, f[i]);
@@ -534,7 +519,7 @@ __device__ __forceinline__ void write_row(const Row<DT> &row, void *out, int64_t
                 float f[kVec];
                 uint32_t w[4];
                 hide(v0 + u * kLossThreads, raw[u]);
-                unpack<DT>(raw[u], f);
+                unpack_vector<DT>(raw[u], f);
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     w[i] = DT == FP8_F32 ? value(f[i]) : value(f[2 * i % kVec]) | (value(f[(2 * i + 1) % kVec]) << 16);

@@ -21,6 +21,16 @@ struct NormFwd {
     AmaxSink sink;
 };
 
+// Mean and sum of squared deviations of a row from its first estimate of the mean and the sums {d, d^2} of the deviations
+// from that.  The estimate carries the rounding of a sum of whole numbers; where the mean is far above the spread (eight times,
+// say), the mean of the small deviations corrects it, which is what keeps the spread's digits.
+__device__ __forceinline__ float2 corrected(float estimate, float2 sums, int cols, float inv_cols)
+{
+    if (estimate * estimate <= 64.0f * sums.y * inv_cols) return make_float2(estimate, sums.y);
+    const float mean = __fmaf_rn(sums.x, inv_cols, estimate), e = mean - estimate;
+    return make_float2(mean, fmaxf(0.0f, __fmaf_rn(-e, __fmaf_rn(-(float)cols, e, 2.0f * sums.x), sums.y)));
+}
+
 template <int DT>
 __device__ __forceinline__ float normalised(const NormFwd &p, float h, float mean, float rstd, int j)
 {
@@ -33,7 +43,8 @@ __device__ __forceinline__ float normalised(const NormFwd &p, float h, float mea
 template <int DT, bool CAST_ONLY>
 __global__ void __launch_bounds__(kNormThreads) norm_fwd_any_kernel(const NormFwd p)
 {
-    __shared__ float part[2][kNormThreads / 32];
+    __shared__ float part[kNormThreads / 32];
+    __shared__ float2 part2[kNormThreads / 32];
     uint32_t key = 0;
     bool sat = false;
     const bool bytes = p.y8 && p.bias;
@@ -57,15 +68,19 @@ __global__ void __launch_bounds__(kNormThreads) norm_fwd_any_kernel(const NormFw
                 if (p.h) store_bits<DT>(p.h, r * p.ld_h + j, element_bits<DT>(v));
                 s += v;
             }
-            s = block_sum<kNormThreads>(s, part[0]);
+            s = block_sum<kNormThreads>(s, part);
             if (p.layer) mean = s * p.inv_cols;
-            float q = 0.0f;
+            float2 q = make_float2(0.0f, 0.0f);
             for (int j = threadIdx.x; j < p.cols; j += kNormThreads) {
                 const float d = h_at(j) - mean;
-                q = __fmaf_rn(d, d, q);
+                q = make_float2(q.x + d, __fmaf_rn(d, d, q.y));
             }
-            q = block_sum<kNormThreads>(q, part[1]);
-            rstd = 1.0f / sqrtf(__fmaf_rn(q, p.inv_cols, p.eps));
+            q = block_sum2<kNormThreads>(q, part2);
+            if (p.layer) {
+                q = corrected(mean, q, p.cols, p.inv_cols);
+                mean = q.x;
+            }
+            rstd = 1.0f / sqrtf(__fmaf_rn(q.y, p.inv_cols, p.eps));
             if (threadIdx.x == 0) {
                 if (p.mean) p.mean[r] = mean;
                 if (p.rstd) p.rstd[r] = rstd;
@@ -86,6 +101,248 @@ __global__ void __launch_bounds__(kNormThreads) norm_fwd_any_kernel(const NormFw
     }
     if (sat) raise_flags(p.sink.d_status, FP8_FLAG_SATURATED);
     if (!CAST_ONLY) sink_amax(key, p.sink);
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// rows of whole 16-byte vectors
+// ---------------------------------------------------------------------------------------------------------------------
+// TPR threads hold a row in registers, EPT elements each (TPR * EPT >= cols): the statistics, the output and its bytes come
+// from one reading.
+template <int DT>
+constexpr int kPerVec = DT == FP8_F32 ? 4 : 8;
+template <int TPR>
+constexpr int kRowBlock = TPR < 128 ? 128 : TPR;   // threads of a block: four rows at a time where a warp holds one
+
+// `n` elements of a coefficient vector from col on (16-byte loads), `fill` where there is none.
+template <int DT, bool WF32>
+__device__ __forceinline__ void load_coefficients(const void *w, int col, float fill, float (&f)[kPerVec<DT>])
+{
+    constexpr int kN = kPerVec<DT>;
+    if (!w) {
+#pragma unroll
+        for (int i = 0; i < kN; ++i) f[i] = fill;
+    } else if (WF32) {
+#pragma unroll
+        for (int i = 0; i < kN; i += 4) {
+            const float4 v = __ldg(reinterpret_cast<const float4 *>(static_cast<const float *>(w) + col + i));
+            f[i] = v.x; f[i + 1] = v.y; f[i + 2] = v.z; f[i + 3] = v.w;
+        }
+    } else {
+        unpack_vector<DT>(__ldg(reinterpret_cast<const uint4 *>(static_cast<const uint8_t *>(w) + (int64_t)col * InType<DT>::kBytes)), f);
+    }
+}
+
+// y of a vector, rounded to the tensors' type (the operations of `normalised`, in their order)
+template <int DT, bool WF32>
+__device__ __forceinline__ uint4 normalise_vector(const NormFwd &p, const float (&h)[kPerVec<DT>], float mean, float rstd, int col)
+{
+    float w[kPerVec<DT>], b[kPerVec<DT>], v[kPerVec<DT>];
+    load_coefficients<DT, WF32>(p.w, col, 1.0f, w);
+    load_coefficients<DT, WF32>(p.b, col, 0.0f, b);
+#pragma unroll
+    for (int i = 0; i < kPerVec<DT>; ++i) v[i] = __fmaf_rn(__fmul_rn(__fsub_rn(h[i], mean), rstd), w[i], b[i]);
+    return pack_vector<DT>(v);
+}
+
+// Largest magnitude of packed elements (as fp8_amax folds them), and its key.
+template <int DT>
+__device__ __forceinline__ uint32_t fold_vector(uint32_t acc, const uint4 &v)
+{
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc = DT == FP8_F32 ? max(acc, w[i] & 0x7FFFFFFFu) : __vmaxu2(acc, w[i] & 0x7FFF7FFFu);
+    return acc;
+}
+template <int DT>
+__device__ __forceinline__ uint32_t folded_key(uint32_t acc)
+{
+    if (DT == FP8_F32) return acc;
+    return magnitude_key(element_value<DT>(max(acc & 0xFFFFu, acc >> 16)));
+}
+
+// The E4 bytes of a vector of y, to y8 + at (8 or 4 bytes, aligned).
+template <int DT>
+__device__ __forceinline__ void store_bytes(uint8_t *y8, int64_t at, const uint4 &y, Pow2Pair scale, bool &sat)
+{
+    const uint32_t w[4] = {y.x, y.y, y.z, y.w};
+    const uint32_t lo = cast4w<FP8_E4, DT, true>(w, scale, sat);
+    if (DT == FP8_F32) __stcs(reinterpret_cast<uint32_t *>(y8 + at), lo);
+    else __stcs(reinterpret_cast<uint2 *>(y8 + at), make_uint2(lo, cast4w<FP8_E4, DT, true>(w + 2, scale, sat)));
+}
+
+// CLUSTER: the blocks are one cluster that knows the amax when its rows are done, and casts them from shared memory in the
+// same launch.
+template <int DT, bool WF32, int TPR, int EPT, bool CLUSTER>
+__global__ void __launch_bounds__(kRowBlock<TPR>) norm_fwd_rows_kernel(const NormFwd p)
+{
+    constexpr int kN = kPerVec<DT>, kVecs = EPT / kN, kSize = InType<DT>::kBytes, kGroups = kRowBlock<TPR> / TPR;
+    extern __shared__ __align__(16) uint4 stage[];   // CLUSTER: y of this block's rows
+    __shared__ float part[TPR / 32];
+    __shared__ float2 part2[2][TPR / 32];
+    int turn = 0;
+    const int t = threadIdx.x % TPR, group = threadIdx.x / TPR;
+    const int64_t first = (int64_t)blockIdx.x * kGroups + group, step = (int64_t)gridDim.x * kGroups;
+    const int row_vecs = p.cols / kN;
+    uint32_t acc = 0;
+    bool sat = false;
+    const bool bytes = !CLUSTER && p.y8 && p.bias, want_y = CLUSTER || p.y || bytes || p.sink.slot;
+    Pow2Pair scale = {1.0f, 1.0f};
+    if (bytes) scale = make_pow2_pair(*p.bias + p.delta);
+    uint4 x[kVecs], res[kVecs];
+    auto load = [&](int64_t r) {
+        const uint4 *px = reinterpret_cast<const uint4 *>(static_cast<const uint8_t *>(p.x) + r * p.ld_x * kSize);
+        const uint4 *pr = reinterpret_cast<const uint4 *>(static_cast<const uint8_t *>(p.res) + r * p.ld_res * kSize);
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) {
+            if (t + i * TPR >= row_vecs) continue;
+            x[i] = __ldcs(px + t + i * TPR);
+            if (p.res) res[i] = __ldcs(pr + t + i * TPR);
+        }
+    };
+    if (first < p.rows) load(first);
+    for (int64_t r = first; r < p.rows; r += step, turn ^= 1) {
+        float h[kVecs][kN], s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) {
+            if (t + i * TPR >= row_vecs) continue;
+            unpack_vector<DT>(x[i], h[i]);
+            if (p.res) {
+                float f[kN];
+                unpack_vector<DT>(res[i], f);
+#pragma unroll
+                for (int k = 0; k < kN; ++k) f[k] += h[i][k];
+                const uint4 sum = pack_vector<DT>(f);
+                unpack_vector<DT>(sum, h[i]);
+                if (p.h) reinterpret_cast<uint4 *>(static_cast<uint8_t *>(p.h) + r * p.ld_h * kSize)[t + i * TPR] = sum;
+            } else if (p.h) {
+                reinterpret_cast<uint4 *>(static_cast<uint8_t *>(p.h) + r * p.ld_h * kSize)[t + i * TPR] = x[i];
+            }
+#pragma unroll
+            for (int k = 0; k < kN; ++k) s += h[i][k];
+        }
+        if (r + step < p.rows) load(r + step);   // (while this row is reduced)
+        float mean = p.layer ? block_sum<TPR>(s, part) * p.inv_cols : 0.0f;
+        float2 q = make_float2(0.0f, 0.0f);
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) {
+            if (t + i * TPR >= row_vecs) continue;
+#pragma unroll
+            for (int k = 0; k < kN; ++k) {
+                const float d = h[i][k] - mean;
+                q = make_float2(q.x + d, __fmaf_rn(d, d, q.y));
+            }
+        }
+        q = block_sum2<TPR>(q, part2[turn]);
+        if (p.layer) {
+            q = corrected(mean, q, p.cols, p.inv_cols);
+            mean = q.x;
+        }
+        const float rstd = 1.0f / sqrtf(__fmaf_rn(q.y, p.inv_cols, p.eps));
+        if (t == 0) {
+            if (p.mean) p.mean[r] = mean;
+            if (p.rstd) p.rstd[r] = rstd;
+        }
+        if (want_y) {
+#pragma unroll
+            for (int i = 0; i < kVecs; ++i) {
+                const int v = t + i * TPR;
+                if (v >= row_vecs) continue;
+                const uint4 y = normalise_vector<DT, WF32>(p, h[i], mean, rstd, v * kN);
+                acc = fold_vector<DT>(acc, y);
+                if (p.y) reinterpret_cast<uint4 *>(static_cast<uint8_t *>(p.y) + r * p.ld_y * kSize)[v] = y;
+                if (CLUSTER) stage[((r - first) / gridDim.x + group) * row_vecs + v] = y;
+                if (bytes) store_bytes<DT>(p.y8, r * p.cols + v * kN, y, scale, sat);
+            }
+        }
+    }
+    if (CLUSTER) {
+        const unsigned blocks = gridDim.x;
+        __shared__ uint32_t block_key;
+        uint32_t key = __reduce_max_sync(0xFFFFFFFFu, folded_key<DT>(acc));
+        if (threadIdx.x == 0) block_key = 0u;
+        __syncthreads();
+        if ((threadIdx.x & 31) == 0) atomicMax(&block_key, key);
+        __syncthreads();
+        key = block_key;
+        if (blocks > 1) {
+            asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+            asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+            for (unsigned b = 0; b < blocks; ++b) {
+                uint32_t remote, other;
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(smem_u32(&block_key)), "r"(b));
+                asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(other) : "r"(remote) : "memory");
+                key = max(key, other);
+            }
+            // (no block leaves while another reads its word)
+            asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        }
+        unsigned flags = 0;
+        const int bias = bias_from_amax_bits(key, FP8_E4, p.sink.conv, p.sink.margin, &flags);
+        if (blockIdx.x == 0 && threadIdx.x == 0) {
+            if (p.sink.d_amax) *p.sink.d_amax = __uint_as_float(key);
+            *p.sink.d_bias = bias;
+            if (flags) raise_flags(p.sink.d_status, flags);
+        }
+        scale = make_pow2_pair(bias + p.delta);
+        for (int64_t r = first; r < p.rows; r += step)
+            for (int v = t; v < row_vecs; v += TPR)
+                store_bytes<DT>(p.y8, r * p.cols + v * kN, stage[((r - first) / gridDim.x + group) * row_vecs + v], scale, sat);
+        __syncwarp();
+        if (blocks > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    }
+    if (sat) raise_flags(p.sink.d_status, FP8_FLAG_SATURATED);
+    if (!CLUSTER) sink_amax(folded_key<DT>(acc), p.sink);
+}
+
+// The bytes of y from the sums and the statistics of the launch before, under the bias that it left: four rows of one vector a
+// thread, last rows first (what the launch before wrote last is what L2 holds).
+template <int DT, bool WF32>
+__global__ void __launch_bounds__(kNormThreads) norm_cast_rows_kernel(const NormFwd p)
+{
+    constexpr int kN = kPerVec<DT>, kSize = InType<DT>::kBytes, kRows = 4;
+    const unsigned row_vecs = p.cols / kN;
+    const uint64_t at = (uint64_t)(gridDim.x - 1 - blockIdx.x) * kNormThreads + threadIdx.x;
+    int64_t r0;
+    int v;
+    if (gridDim.x < (1u << 24)) {   // (divisions of 32 bits where they do)
+        r0 = (int64_t)((unsigned)at / row_vecs) * kRows;
+        v = (int)((unsigned)at % row_vecs);
+    } else {
+        r0 = (int64_t)(at / row_vecs) * kRows;
+        v = (int)(at % row_vecs);
+    }
+    if (r0 >= p.rows) return;
+    uint4 x[kRows], res[kRows];
+    float mean[kRows], rstd[kRows];
+    const bool sum = p.res && !p.h;
+    const uint8_t *src = static_cast<const uint8_t *>(p.h ? p.h : p.x);
+    const int64_t ld = p.h ? p.ld_h : p.ld_x;
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        const int64_t r = r0 + i;
+        if (r >= p.rows) continue;
+        x[i] = __ldcs(reinterpret_cast<const uint4 *>(src + r * ld * kSize) + v);
+        if (sum) res[i] = __ldcs(reinterpret_cast<const uint4 *>(static_cast<const uint8_t *>(p.res) + r * p.ld_res * kSize) + v);
+        mean[i] = p.layer ? p.mean[r] : 0.0f;
+        rstd[i] = p.rstd[r];
+    }
+    const Pow2Pair scale = make_pow2_pair(*p.bias + p.delta);
+    bool sat = false;
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        if (r0 + i >= p.rows) continue;
+        float h[kN];
+        unpack_vector<DT>(x[i], h);
+        if (sum) {
+            float f[kN];
+            unpack_vector<DT>(res[i], f);
+#pragma unroll
+            for (int k = 0; k < kN; ++k) f[k] += h[k];
+            unpack_vector<DT>(pack_vector<DT>(f), h);
+        }
+        store_bytes<DT>(p.y8, (r0 + i) * p.cols + v * kN, normalise_vector<DT, WF32>(p, h, mean[i], rstd[i], v * kN), scale, sat);
+    }
+    if (sat) raise_flags(p.sink.d_status, FP8_FLAG_SATURATED);
 }
 
 struct NormBwd {
@@ -136,6 +393,147 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_any_kernel(const NormBw
     sink_amax(key, p.sink);
 }
 
+// The same for rows of whole vectors: TPR threads hold a row, and for all rows of a block the sums of their own columns; the
+// next row is on its way while this one is reduced, where the registers allow.
+template <int DT, bool WF32, int TPR, int EPT>
+__global__ void __launch_bounds__(kRowBlock<TPR>) norm_bwd_rows_kernel(const NormBwd p)
+{
+    constexpr int kN = kPerVec<DT>, kVecs = EPT / kN, kSize = InType<DT>::kBytes, kGroups = kRowBlock<TPR> / TPR;
+    constexpr bool kAhead = TPR * (DT == FP8_F32 ? 2 : 1) <= 512;
+    __shared__ float2 part[2][TPR / 32];
+    const int t = threadIdx.x % TPR, group = threadIdx.x / TPR;
+    const int64_t step = (int64_t)gridDim.x * kGroups;
+    const int row_vecs = p.cols / kN;
+    uint32_t acc = 0;
+    int turn = 0;
+    float sum_w[kVecs][kN] = {}, sum_b[kVecs][kN] = {};
+    uint4 dy[kVecs], h[kVecs], dh[kVecs];
+    float mean = 0.0f, rstd = 0.0f;
+    auto vectors = [&](const void *q, int64_t r, int64_t ld) {
+        return reinterpret_cast<const uint4 *>(static_cast<const uint8_t *>(q) + r * ld * kSize);
+    };
+    auto load = [&](int64_t r, uint4 (&dy)[kVecs], uint4 (&h)[kVecs], uint4 (&dh)[kVecs], float &mean, float &rstd) {
+        const uint4 *py = vectors(p.dy, r, p.ld_dy), *ph = vectors(p.h, r, p.ld_h), *pd = vectors(p.dh, r, p.ld_dh);
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) {
+            if (t + i * TPR >= row_vecs) continue;
+            dy[i] = __ldcs(py + t + i * TPR);
+            h[i] = __ldcs(ph + t + i * TPR);
+            if (p.dh && kAhead) dh[i] = __ldcs(pd + t + i * TPR);
+        }
+        mean = p.layer ? p.mean[r] : 0.0f;
+        rstd = p.rstd[r];
+    };
+    int64_t r = (int64_t)blockIdx.x * kGroups + group;
+    if (kAhead && r < p.rows) load(r, dy, h, dh, mean, rstd);
+    for (; r < p.rows; r += step, turn ^= 1) {
+        uint4 dy2[kVecs], h2[kVecs], dh2[kVecs];
+        float mean2 = 0.0f, rstd2 = 0.0f;
+        if (!kAhead) load(r, dy, h, dh, mean, rstd);
+        else if (r + step < p.rows) load(r + step, dy2, h2, dh2, mean2, rstd2);
+        float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) {
+            const int v = t + i * TPR;
+            if (v >= row_vecs) continue;
+            float y[kN], x[kN], w[kN];
+            unpack_vector<DT>(dy[i], y);
+            unpack_vector<DT>(h[i], x);
+            load_coefficients<DT, WF32>(p.w, v * kN, 1.0f, w);
+#pragma unroll
+            for (int k = 0; k < kN; ++k) {
+                const float xh = (x[k] - mean) * rstd, g = y[k] * w[k];
+                s1 += g;
+                s2 = __fmaf_rn(g, xh, s2);
+                sum_w[i][k] = __fmaf_rn(y[k], xh, sum_w[i][k]);
+                sum_b[i][k] += y[k];
+            }
+        }
+        if (p.dx) {
+            s1 = warp_sum(s1);
+            s2 = warp_sum(s2);
+            if (TPR > 32) {
+                if ((threadIdx.x & 31) == 0) part[turn][threadIdx.x >> 5] = make_float2(s1, s2);
+                __syncthreads();
+                s1 = s2 = 0.0f;
+#pragma unroll
+                for (int i = 0; i < TPR / 32; ++i) {
+                    s1 += part[turn][i].x;
+                    s2 += part[turn][i].y;
+                }
+            }
+            const float c1 = p.layer ? s1 * p.inv_cols : 0.0f, c2 = s2 * p.inv_cols;
+            uint4 *px = reinterpret_cast<uint4 *>(static_cast<uint8_t *>(p.dx) + r * p.ld_dx * kSize);
+#pragma unroll
+            for (int i = 0; i < kVecs; ++i) {
+                const int v = t + i * TPR;
+                if (v >= row_vecs) continue;
+                float y[kN], x[kN], w[kN];
+                unpack_vector<DT>(dy[i], y);
+                unpack_vector<DT>(h[i], x);
+                load_coefficients<DT, WF32>(p.w, v * kN, 1.0f, w);
+#pragma unroll
+                for (int k = 0; k < kN; ++k) {
+                    const float xh = (x[k] - mean) * rstd;
+                    y[k] = rstd * (y[k] * w[k] - c1 - xh * c2);
+                }
+                if (p.dh) {
+                    unpack_vector<DT>(kAhead ? dh[i] : __ldcs(vectors(p.dh, r, p.ld_dh) + v), x);
+#pragma unroll
+                    for (int k = 0; k < kN; ++k) y[k] += x[k];
+                }
+                const uint4 out = pack_vector<DT>(y);
+                acc = fold_vector<DT>(acc, out);
+                px[v] = out;
+            }
+        }
+        if (kAhead) {
+#pragma unroll
+            for (int i = 0; i < kVecs; ++i) {
+                dy[i] = dy2[i];
+                h[i] = h2[i];
+                dh[i] = dh2[i];
+            }
+            mean = mean2;
+            rstd = rstd2;
+        }
+    }
+    if (p.part_w || p.part_b) {
+        __shared__ float4 lines[kGroups > 1 ? kGroups : 1][kGroups > 1 ? TPR * EPT / 4 : 1];
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            float *out = which ? p.part_b : p.part_w;
+            if (!out) continue;
+            out += (int64_t)blockIdx.x * p.cols;
+            if (kGroups > 1) __syncthreads();
+#pragma unroll
+            for (int i = 0; i < kVecs; ++i) {
+                const int v = t + i * TPR;
+                if (v >= row_vecs) continue;
+#pragma unroll
+                for (int k = 0; k < kN; k += 4) {
+                    const float(&s)[kN] = which ? sum_b[i] : sum_w[i];
+                    const float4 f = make_float4(s[k], s[k + 1], s[k + 2], s[k + 3]);
+                    if (kGroups > 1) lines[group][(v * kN + k) / 4] = f;
+                    else reinterpret_cast<float4 *>(out)[(v * kN + k) / 4] = f;
+                }
+            }
+            if (kGroups > 1) {
+                __syncthreads();
+                for (int j = threadIdx.x; j < p.cols / 4; j += kRowBlock<TPR>) {
+                    float4 f = lines[0][j];
+#pragma unroll
+                    for (int g = 1; g < kGroups; ++g) {
+                        f.x += lines[g][j].x; f.y += lines[g][j].y; f.z += lines[g][j].z; f.w += lines[g][j].w;
+                    }
+                    reinterpret_cast<float4 *>(out)[j] = f;
+                }
+            }
+        }
+    }
+    sink_amax(folded_key<DT>(acc), p.sink);
+}
+
 // Sums of the blocks' lines, in their order: 32 columns a block, eight lines at a time.
 __global__ void __launch_bounds__(256) norm_bwd_sum_kernel(const float *part_w, const float *part_b, int lines, int cols, int w_dt,
                                                            void *dw, void *db)
@@ -164,9 +562,110 @@ static unsigned blocks_for_rows(const fp8_ctx *ctx, int64_t rows, int per_sm)
     return (unsigned)(rows < most ? rows : most);
 }
 
-template <int DT>
-static void launch_fwd(const fp8_ctx *ctx, NormFwd p, bool two, cudaStream_t st)
+// Threads that hold a row, and elements that each of them holds.
+template <int TPR, int EPT>
+struct RowHold {
+    static constexpr int kThreads = TPR, kElements = EPT;
+};
+constexpr int kMostHeld = 16384;
+// A warp per row as long as 32 elements a lane hold it (SUMS: the backward pass, which holds two sums beside each element;
+// 16), then as few threads as 16 elements a thread allow.
+template <bool SUMS, typename F>
+static void by_row_shape(int cols, F f)
 {
+    if (cols <= 256) f(RowHold<32, 8>{});
+    else if (cols <= 512) f(RowHold<32, 16>{});
+    else if (cols <= 1024) f(RowHold<SUMS ? 128 : 32, SUMS ? 8 : 32>{});
+    else if (cols <= 2048) f(RowHold<256, 8>{});
+    else if (cols <= 4096) f(RowHold<256, 16>{});
+    else if (cols <= 8192) f(RowHold<512, 16>{});
+    else f(RowHold<1024, 16>{});
+}
+
+// Two passes as one launch of one cluster: up to eight blocks, whose rows of y fit their shared memory.
+constexpr int kClusterBlocks = 8, kClusterStage = 96 << 10;
+
+template <int DT, bool WF32, int TPR, int EPT>
+static cudaError_t launch_fwd_rows(const fp8_ctx *ctx, NormFwd p, bool two, cudaStream_t st)
+{
+    constexpr int kBlock = kRowBlock<TPR>, kGroups = kBlock / TPR;
+    const int64_t blocks = (p.rows + kGroups - 1) / kGroups;
+    if (two) {
+        int cluster = 1;
+        while (cluster < kClusterBlocks && cluster < blocks) cluster *= 2;
+        const int64_t stage = (blocks + cluster - 1) / cluster * kGroups * p.cols * InType<DT>::kBytes;
+        if (stage <= kClusterStage) {
+            cudaLaunchAttribute attr[1];
+            attr[0].id = cudaLaunchAttributeClusterDimension;
+            attr[0].val.clusterDim.x = (unsigned)cluster;
+            attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3((unsigned)cluster);
+            cfg.blockDim = dim3(kBlock);
+            cfg.dynamicSmemBytes = (size_t)stage;
+            cfg.stream = st;
+            cfg.attrs = attr;
+            cfg.numAttrs = 1;
+            count_launch();
+            return cudaLaunchKernelEx(&cfg, norm_fwd_rows_kernel<DT, WF32, TPR, EPT, true>, p);
+        }
+    }
+    const int32_t *bias = p.bias;
+    if (two) p.bias = nullptr;
+    const int64_t most = (int64_t)ctx->sm_count * (1024 / kBlock);
+    count_launch();
+    norm_fwd_rows_kernel<DT, WF32, TPR, EPT, false><<<(unsigned)(blocks < most ? blocks : most), kBlock, 0, st>>>(p);
+    if (two) {
+        p.bias = bias;
+        const int64_t work = (p.rows + 3) / 4 * (p.cols / kPerVec<DT>);
+        count_launch();
+        norm_cast_rows_kernel<DT, WF32><<<(unsigned)((work + kNormThreads - 1) / kNormThreads), kNormThreads, 0, st>>>(p);
+    }
+    return cudaGetLastError();
+}
+
+template <int DT, bool WF32>
+static cudaError_t allow_stage()
+{
+    cudaError_t e = cudaSuccess;
+    for (int cols : {256, 512, 1024, 2048, 4096, 8192, kMostHeld})
+        by_row_shape<false>(cols, [&](auto s) {
+            if (e == cudaSuccess)
+                e = cudaFuncSetAttribute(norm_fwd_rows_kernel<DT, WF32, decltype(s)::kThreads, decltype(s)::kElements, true>,
+                                         cudaFuncAttributeMaxDynamicSharedMemorySize, kClusterStage);
+        });
+    return e;
+}
+cudaError_t configure_norm_kernels()
+{
+    cudaError_t e = allow_stage<FP8_BF16, false>();
+    if (e == cudaSuccess) e = allow_stage<FP8_BF16, true>();
+    if (e == cudaSuccess) e = allow_stage<FP8_F16, false>();
+    if (e == cudaSuccess) e = allow_stage<FP8_F16, true>();
+    return e == cudaSuccess ? allow_stage<FP8_F32, false>() : e;
+}
+
+// Whether every row, and every coefficient vector, consists of whole aligned vectors.
+static bool whole_vectors(int dt, int64_t cols)
+{
+    return cols % (dt == FP8_F32 ? 4 : 8) == 0;
+}
+static bool fast_rows(const NormFwd &p, int dt)
+{
+    auto row = [&](const void *q, int64_t ld) { return !q || row_aligned(q, ld, dt, 16); };
+    return whole_vectors(dt, p.cols) && p.cols <= kMostHeld && row(p.x, p.ld_x) && row(p.res, p.ld_res) && row(p.h, p.ld_h) && row(p.y, p.ld_y) &&
+           row(p.w, 0) && row(p.b, 0) && (reinterpret_cast<uintptr_t>(p.y8) & 7u) == 0 &&
+           (p.rows + 3) / 4 * (int64_t)p.cols / (dt == FP8_F32 ? 4 : 8) / kNormThreads < 0x7FFFFFFF;
+}
+
+template <int DT, bool WF32>
+static cudaError_t launch_fwd(const fp8_ctx *ctx, NormFwd p, bool two, cudaStream_t st)
+{
+    if (fast_rows(p, DT)) {
+        cudaError_t e = cudaSuccess;
+        by_row_shape<false>(p.cols, [&](auto s) { e = launch_fwd_rows<DT, WF32, decltype(s)::kThreads, decltype(s)::kElements>(ctx, p, two, st); });
+        return e;
+    }
     const unsigned grid = blocks_for_rows(ctx, p.rows, 8);
     const int32_t *bias = p.bias;
     if (two) p.bias = nullptr;
@@ -177,13 +676,47 @@ static void launch_fwd(const fp8_ctx *ctx, NormFwd p, bool two, cudaStream_t st)
         count_launch();
         norm_fwd_any_kernel<DT, true><<<grid, kNormThreads, 0, st>>>(p);
     }
+    return cudaGetLastError();
 }
 
-template <int DT>
-static void launch_bwd(const fp8_ctx *ctx, const NormBwd &p, unsigned grid, cudaStream_t st)
+// Lines of the workspace that a call's row sums take (as many blocks as its kernel has), within the workspace.
+static unsigned bwd_blocks(const fp8_ctx *ctx, int64_t blocks, int per_sm, int sums, int64_t cols)
 {
+    int64_t n = (int64_t)ctx->sm_count * per_sm;
+    if (n > blocks) n = blocks;
+    if (sums) {
+        const int64_t lines = (int64_t)(ctx->partial_bytes / sizeof(float)) / (sums * cols);   // at least two (cols up to 2^22)
+        if (n > lines) n = lines;
+    }
+    return (unsigned)n;
+}
+
+template <int DT, bool WF32>
+static unsigned launch_bwd(const fp8_ctx *ctx, NormBwd p, bool want_w, bool want_b, cudaStream_t st)
+{
+    auto row = [&](const void *q, int64_t ld) { return !q || row_aligned(q, ld, DT, 16); };
+    const int sums = 2;   // (one output alone takes the same blocks, and gives the same bits)
+    const bool fast = p.cols % kPerVec<DT> == 0 && p.cols <= kMostHeld && row(p.dy, p.ld_dy) && row(p.h, p.ld_h) && row(p.dh, p.ld_dh) &&
+                      row(p.dx, p.ld_dx) && row(p.w, 0);
+    unsigned grid = 0;
+    auto lines = [&] {
+        if (want_w) p.part_w = ctx->d_partial;
+        if (want_b) p.part_b = ctx->d_partial + (int64_t)grid * p.cols;
+    };
     count_launch();
-    norm_bwd_any_kernel<DT><<<grid, kNormThreads, 0, st>>>(p);
+    if (fast) {
+        by_row_shape<true>(p.cols, [&](auto s) {
+            constexpr int kThreads = decltype(s)::kThreads, kBlock = kRowBlock<kThreads>, kGroups = kBlock / kThreads;
+            grid = bwd_blocks(ctx, (p.rows + kGroups - 1) / kGroups, kBlock <= 512 ? 512 / kBlock : 1, sums, p.cols);
+            lines();
+            norm_bwd_rows_kernel<DT, WF32, kThreads, decltype(s)::kElements><<<grid, kBlock, 0, st>>>(p);
+        });
+    } else {
+        grid = bwd_blocks(ctx, p.rows, 4, sums, p.cols);
+        lines();
+        norm_bwd_any_kernel<DT><<<grid, kNormThreads, 0, st>>>(p);
+    }
+    return grid;
 }
 
 }  // namespace fp8lin
@@ -217,10 +750,12 @@ fp8_status_t fp8_norm_fwd(fp8_ctx *ctx, const fp8_norm_fwd_t *a, void *stream)
                  {nullptr, a->d_amax, a->d_bias_out, ctx->d_status, FP8_E4, a->conv, a->margin}};
     if (a->d_amax || a->d_bias_out) p.sink.slot = take_slot(ctx);
     cudaStream_t st = (cudaStream_t)stream;
-    if (a->dt == FP8_BF16) launch_fwd<FP8_BF16>(ctx, p, two, st);
-    else if (a->dt == FP8_F16) launch_fwd<FP8_F16>(ctx, p, two, st);
-    else launch_fwd<FP8_F32>(ctx, p, two, st);
-    return cudaGetLastError() == cudaSuccess ? FP8_OK : FP8_ERR_CUDA;
+    const bool wide = a->w_dt == FP8_F32 && a->dt != FP8_F32;
+    const cudaError_t e = a->dt == FP8_F32    ? launch_fwd<FP8_F32, false>(ctx, p, two, st)
+                          : a->dt == FP8_BF16 ? (wide ? launch_fwd<FP8_BF16, true>(ctx, p, two, st) : launch_fwd<FP8_BF16, false>(ctx, p, two, st))
+                          : wide              ? launch_fwd<FP8_F16, true>(ctx, p, two, st)
+                                              : launch_fwd<FP8_F16, false>(ctx, p, two, st);
+    return e == cudaSuccess ? FP8_OK : FP8_ERR_CUDA;
 }
 
 fp8_status_t fp8_norm_bwd(fp8_ctx *ctx, const fp8_norm_bwd_t *a, void *stream)
@@ -239,26 +774,20 @@ fp8_status_t fp8_norm_bwd(fp8_ctx *ctx, const fp8_norm_bwd_t *a, void *stream)
         return FP8_ERR_ALIGN;
     const OnDevice on(ctx->device);
     cudaStream_t st = (cudaStream_t)stream;
-    unsigned grid = blocks_for_rows(ctx, a->rows, 4);
-    const int sums = (a->dw ? 1 : 0) + (a->db ? 1 : 0);
-    if (sums) {
-        const int64_t lines = (int64_t)(ctx->partial_bytes / sizeof(float)) / (sums * a->cols);   // at least two (cols up to 2^22)
-        if (grid > lines) grid = (unsigned)lines;
-    }
     NormBwd p = {a->dy, a->h, a->dh, a->weight, a->d_mean, a->d_rstd, a->dx, nullptr, nullptr, a->rows, a->ld_dy, a->ld_h, a->ld_dh,
                  a->ld_dx, (int)a->cols, a->w_dt, a->kind == FP8_NORM_LAYER, 1.0f / (float)a->cols,
                  {nullptr, a->d_amax, nullptr, ctx->d_status, FP8_E5, 0, 0}};
     if (a->d_amax) p.sink.slot = take_slot(ctx);
-    if (a->dw) p.part_w = ctx->d_partial;
-    if (a->db) p.part_b = ctx->d_partial + (a->dw ? (int64_t)grid * a->cols : 0);
-    if (a->dt == FP8_BF16) launch_bwd<FP8_BF16>(ctx, p, grid, st);
-    else if (a->dt == FP8_F16) launch_bwd<FP8_F16>(ctx, p, grid, st);
-    else launch_bwd<FP8_F32>(ctx, p, grid, st);
+    const bool wide = a->w_dt == FP8_F32 && a->dt != FP8_F32, w = a->dw != nullptr, b = a->db != nullptr;
+    const unsigned lines = a->dt == FP8_F32    ? launch_bwd<FP8_F32, false>(ctx, p, w, b, st)
+                           : a->dt == FP8_BF16 ? (wide ? launch_bwd<FP8_BF16, true>(ctx, p, w, b, st) : launch_bwd<FP8_BF16, false>(ctx, p, w, b, st))
+                           : wide              ? launch_bwd<FP8_F16, true>(ctx, p, w, b, st)
+                                               : launch_bwd<FP8_F16, false>(ctx, p, w, b, st);
     if (cudaGetLastError() != cudaSuccess) return FP8_ERR_CUDA;
-    if (sums) {
+    if (w || b) {
         count_launch();
-        norm_bwd_sum_kernel<<<dim3((unsigned)((a->cols + 31) / 32), 2), 256, 0, st>>>(p.part_w, p.part_b, (int)grid, (int)a->cols, a->w_dt,
-                                                                                   a->dw, a->db);
+        norm_bwd_sum_kernel<<<dim3((unsigned)((a->cols + 31) / 32), 2), 256, 0, st>>>(
+            ctx->d_partial, ctx->d_partial + (int64_t)lines * a->cols, (int)lines, (int)a->cols, a->w_dt, a->dw, a->db);
     }
     return cudaGetLastError() == cudaSuccess ? FP8_OK : FP8_ERR_CUDA;
 }

@@ -73,6 +73,34 @@ __device__ __forceinline__ float load_any(const void *x, int dt, int64_t i)
     return dt == FP8_BF16 ? load1<FP8_BF16>(x, i) : load1<FP8_F16>(x, i);
 }
 
+// A 16-byte vector's elements as floats, and the vector of floats rounded to the type.
+template <int DT, int N>
+__device__ __forceinline__ void unpack_vector(const uint4 &v, float (&f)[N])
+{
+    static_assert(N == (DT == FP8_F32 ? 4 : 8), "elements of 16 bytes");
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+        float g[4];
+        unpack4<DT>(w + i / 4 * InType<DT>::kWords4, g);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) f[i + k] = g[k];
+    }
+}
+template <int DT, int N>
+__device__ __forceinline__ uint4 pack_vector(const float (&f)[N])
+{
+    static_assert(N == (DT == FP8_F32 ? 4 : 8), "elements of 16 bytes");
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (DT == FP8_F32) w[i] = __float_as_uint(f[i]);
+        else if (DT == FP8_BF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(f[(2 * i + 1) % N]), "f"(f[2 * i % N]));
+        else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(f[(2 * i + 1) % N]), "f"(f[2 * i % N]));
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 // Magnitudes as unsigned numbers: NaN above infinity above what is finite.
 __device__ __forceinline__ uint32_t magnitude_key(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
 
@@ -95,6 +123,19 @@ __device__ __forceinline__ float block_sum(float v, float *part)
     v = part[0];
 #pragma unroll
     for (int i = 1; i < THREADS / 32; ++i) v += part[i];
+    return v;
+}
+
+template <int THREADS>
+__device__ __forceinline__ float2 block_sum2(float2 v, float2 *part)
+{
+    v = make_float2(warp_sum(v.x), warp_sum(v.y));
+    if (THREADS == 32) return v;
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = part[0];
+#pragma unroll
+    for (int i = 1; i < THREADS / 32; ++i) v = make_float2(v.x + part[i].x, v.y + part[i].y);
     return v;
 }
 
