@@ -6,7 +6,6 @@
 
 namespace fp8lin {
 
-constexpr int kLossThreads = 256, kLossWarps = kLossThreads / 32;
 constexpr int kTopBuffer = 2048;     // candidates for the top tokens of a row
 constexpr float kFloor = -200.0f;    // exponents (base 2) below it are zeros: 2^-200 is none of an FP32 sum
 constexpr float kLn2 = 0.693147180559945309f, kLog2e = 1.44269504088896341f;
@@ -26,17 +25,18 @@ __device__ __forceinline__ float max_nan(float a, float b)
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
-// a row as head elements up to the first 16-byte boundary, whole vectors, tail elements
+// a row, or a part of it, as head elements up to the first 16-byte boundary, whole vectors, tail elements
 // ---------------------------------------------------------------------------------------------------------------------
 template <int DT>
 struct Row {
     static constexpr int kVec = DT == FP8_F32 ? 4 : 8;
     const uint8_t *base;
-    int n, head, vecs, tail;   // tail: the first element behind the vectors
-    __device__ __forceinline__ Row(const void *logits, int64_t at, int count)
+    int first, n, head, vecs, tail;   // first: element 0's place in the whole row;  tail: the first element behind the vectors
+    __device__ __forceinline__ Row(const void *logits, int64_t at, int from, int count)
     {
         constexpr int kSize = InType<DT>::kBytes;
-        base = static_cast<const uint8_t *>(logits) + at * kSize;
+        base = static_cast<const uint8_t *>(logits) + (at + from) * kSize;
+        first = from;
         n = count;
         head = min(n, (int)((16 - (reinterpret_cast<uintptr_t>(base) & 15u)) & 15u) / kSize);
         vecs = (n - head) / kVec;
@@ -56,54 +56,6 @@ __device__ __forceinline__ uint4 no_vector()
     return make_uint4(w, w, w, w);
 }
 
-// Running sums over exp(scale (x - m)): with d = c (x - m), c = scale * log2 e:  s = sum 2^d,  t = sum 2^d d.
-struct Sums {
-    float m, s, t;
-    // the sums relative to a larger maximum
-    __device__ __forceinline__ void raise(float to, float c)
-    {
-        const float d = fmaxf((fmaxf(m, -FLT_MAX) - fmaxf(to, -FLT_MAX)) * c, kFloor), f = exp2_approx(d);
-        t = f * __fmaf_rn(d, s, t);
-        s *= f;
-        m = to;
-    }
-    template <bool ENTROPY>
-    __device__ __forceinline__ void add(float x, float c)
-    {
-        const float d = max_nan((x - fmaxf(m, -FLT_MAX)) * c, kFloor), e = exp2_approx(d);
-        s += e;
-        if (ENTROPY) t = __fmaf_rn(e, d, t);
-    }
-    __device__ __forceinline__ void join(const Sums &o, float c)
-    {
-        Sums b = o;
-        const float to = fmaxf(m, b.m);
-        raise(to, c);
-        b.raise(to, c);
-        s += b.s;
-        t += b.t;
-    }
-};
-
-// Sums over the block, to all threads, always in the same order.
-__device__ __forceinline__ Sums block_join(Sums a, float c, Sums *part)
-{
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        const Sums b = {__shfl_xor_sync(0xFFFFFFFFu, a.m, o), __shfl_xor_sync(0xFFFFFFFFu, a.s, o), __shfl_xor_sync(0xFFFFFFFFu, a.t, o)};
-        a.join(b, c);
-    }
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = a;
-    __syncthreads();
-    a = part[0];
-#pragma unroll
-    for (int i = 1; i < kLossWarps; ++i) a.join(part[i], c);
-    return a;
-}
-
-// ---------------------------------------------------------------------------------------------------------------------
-// top tokens
-// ---------------------------------------------------------------------------------------------------------------------
 // Orders like the numbers (-0 like 0); 0 is below every number's key.
 __device__ __forceinline__ uint32_t order_key(float x)
 {
@@ -111,44 +63,108 @@ __device__ __forceinline__ uint32_t order_key(float x)
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 __device__ __forceinline__ float order_value(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k); }
+__device__ __forceinline__ float warp_max(float x) { return order_value(__reduce_max_sync(0xFFFFFFFFu, order_key(x))); }
+
+// Sums over exp(scale (x - m)): with d = c (x - m), c = scale * log2 e:  s = sum 2^d,  t = sum 2^d d.  While a row is read, m
+// is not its largest number but one near it: it moves only when a term would pass 2^kLead, which most rows do once a thread
+// (moving it costs an exponential and a branch that a whole warp takes when one lane does).
+constexpr float kLead = 8.0f;
+struct Sums {
+    float m, s, t;
+    // the same sums relative to another number
+    __device__ __forceinline__ void relate(float to, float c)
+    {
+        const float d = fmaxf((m - to) * c, kFloor), f = exp2_approx(d);
+        t = f * __fmaf_rn(d, s, t);
+        s *= f;
+        m = to;
+    }
+    __device__ __forceinline__ void lead(float x, float c)
+    {
+        if ((x - m) * c > kLead) relate(x, c);
+    }
+    __device__ __forceinline__ void join(Sums b, float c)
+    {
+        const float to = fmaxf(m, b.m);
+        relate(to, c);
+        b.relate(to, c);
+        s += b.s;
+        t += b.t;
+    }
+};
+__device__ __forceinline__ Sums no_sums() { return Sums{-FLT_MAX, 0.0f, 0.0f}; }
+
+// One element.
+template <bool ENTROPY>
+__device__ __forceinline__ void add_element(Sums &a, float x, float c)
+{
+    a.lead(x, c);
+    const float d = max_nan((x - a.m) * c, kFloor), e = exp2_approx(d);
+    a.s += e;
+    if (ENTROPY) a.t = __fmaf_rn(e, d, a.t);
+}
+
+// Sums over the block relative to the largest number `top` of all threads, to all threads, always in the same order.  m is
+// -infinity where there is no number.
+template <int T>
+struct JoinShared {
+    float4 part[T / 32];
+};
+template <int T>
+__device__ __forceinline__ Sums block_join(Sums a, float top, float c, JoinShared<T> &sh)
+{
+    const int lane = threadIdx.x & 31;
+    a.relate(warp_max(a.m), c);
+    a.s = warp_sum(a.s);
+    a.t = warp_sum(a.t);
+    top = warp_max(top);
+    if (lane == 0) sh.part[threadIdx.x >> 5] = make_float4(a.m, a.s, a.t, top);
+    __syncthreads();
+    const float4 v = sh.part[lane % (T / 32)];
+    a = Sums{v.x, v.y, v.z};
+    a.relate(warp_max(a.m), c);
+#pragma unroll
+    for (int o = T / 64; o > 0; o >>= 1) {   // (each group of lanes holds all the parts)
+        a.s += __shfl_xor_sync(0xFFFFFFFFu, a.s, o);
+        a.t += __shfl_xor_sync(0xFFFFFFFFu, a.t, o);
+    }
+    top = warp_max(v.w);
+    if (a.s != 0.0f) a.relate(top, c);
+    a.m = top;
+    return a;
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// top tokens
+// ---------------------------------------------------------------------------------------------------------------------
 // larger logit first, then lower index
 __device__ __forceinline__ unsigned long long top_key(float x, int j) { return ((unsigned long long)order_key(x) << 32) | (uint32_t)~j; }
 
+template <int T>
 struct TopShared {
-    unsigned long long key[kTopBuffer];
-    uint32_t strip[kLossThreads];
+    unsigned long long key[kTopBuffer], best[FP8_LOSS_TOP_MAX];
+    uint32_t strip[T];
     int count;
     uint32_t bound;
 };
 
-// The k largest of sh.key[0 .. n), in order, to the front of the buffer.  Keys differ, so a key's place is the number
-// of larger ones.
-__device__ __forceinline__ void top_rank(TopShared &sh, int n, int k)
+// The k largest of sh.key[0 .. n), in order, to sh.best.  Keys differ, so a key's place is the number of larger ones.
+template <int T>
+__device__ __forceinline__ void top_rank(TopShared<T> &sh, int n, int k)
 {
-    constexpr int kMine = kTopBuffer / kLossThreads;
-    unsigned long long mine[kMine];
-    int place[kMine];
-#pragma unroll
-    for (int i = 0; i < kMine; ++i) {
-        const int at = threadIdx.x + i * kLossThreads;
-        place[i] = k;
-        if (i * kLossThreads >= n) continue;
-        mine[i] = at < n ? sh.key[at] : ~0ull;
+    for (int at = threadIdx.x; at < n; at += T) {
+        const unsigned long long mine = sh.key[at];
         int larger = 0;
-        for (int o = 0; o < n; ++o) larger += sh.key[o] > mine[i];
-        place[i] = at < n ? larger : k;
+        for (int o = 0; o < n; ++o) larger += sh.key[o] > mine;
+        if (larger < k) sh.best[larger] = mine;
     }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kMine; ++i)
-        if (place[i] < k) sh.key[place[i]] = mine[i];
     __syncthreads();
 }
 
-// The row's top k keys into sh.key[0 .. k).  m: the thread's own largest element (its strip: the vectors v = thread mod
-// block size, and its edge element).  A bound that k strips reach is reached by k elements; only those strips are read again.
-template <int DT>
-__device__ __forceinline__ void find_top(const Row<DT> &row, float m, int k, TopShared &sh)
+// The row's top k keys into sh.best.  m: the thread's own largest element (its strip: the vectors v = thread mod T, and its
+// edge element).  A bound that k strips reach is reached by k elements; only those strips are read again.
+template <int DT, int T>
+__device__ __forceinline__ void find_top(const Row<DT> &row, float m, int k, TopShared<T> &sh)
 {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int edge = row.edge(tid);
@@ -158,13 +174,13 @@ __device__ __forceinline__ void find_top(const Row<DT> &row, float m, int k, Top
     if (tid == 0) sh.count = 0;
     __syncthreads();
     if (warp == 0) {
-        uint32_t own[kLossWarps], bound = 0;
+        uint32_t own[T / 32], bound = 0;
 #pragma unroll
-        for (int i = 0; i < kLossWarps; ++i) own[i] = sh.strip[lane + 32 * i];
+        for (int i = 0; i < T / 32; ++i) own[i] = sh.strip[lane + 32 * i];
         for (uint32_t bit = 0x8000u; bit; bit >>= 1) {
             unsigned n = 0;
 #pragma unroll
-            for (int i = 0; i < kLossWarps; ++i) n += own[i] >= (bound | bit);
+            for (int i = 0; i < T / 32; ++i) n += own[i] >= (bound | bit);
             if (__reduce_add_sync(0xFFFFFFFFu, n) >= (unsigned)k) bound |= bit;
         }
         if (lane == 0) sh.bound = bound;
@@ -180,14 +196,14 @@ __device__ __forceinline__ void find_top(const Row<DT> &row, float m, int k, Top
     while (flagged) {
         const int owner = (warp << 5) + __ffs(flagged) - 1;
         flagged &= flagged - 1;
-        for (int v = owner + lane * kLossThreads; v < row.vecs; v += 32 * kLossThreads) {
+        for (int v = owner + lane * T; v < row.vecs; v += 32 * T) {
             float f[Row<DT>::kVec];
             unpack_vector<DT>(__ldg(row.vectors() + v), f);
 #pragma unroll
-            for (int i = 0; i < Row<DT>::kVec; ++i) offer(f[i], row.head + v * Row<DT>::kVec + i);
+            for (int i = 0; i < Row<DT>::kVec; ++i) offer(f[i], row.first + row.head + v * Row<DT>::kVec + i);
         }
     }
-    if (edge >= 0) offer(row.at(edge), edge);
+    if (edge >= 0) offer(row.at(edge), row.first + edge);
     __syncthreads();
     int n = sh.count;
     __syncthreads();
@@ -197,24 +213,25 @@ __device__ __forceinline__ void find_top(const Row<DT> &row, float m, int k, Top
     }
     // Many elements at the bound (equal logits, say): the row in order, 1024 elements at a time, against the k-th best so
     // far.  Equal logits come in rising index, so a full list rejects them.
+    constexpr int kStep = 1024;
     unsigned long long least = 0;
     if (tid == 0) sh.count = 0;
-    for (int base = 0; base < row.n; base += 4 * kLossThreads) {
+    for (int base = 0; base < row.n; base += kStep) {
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int j = base + tid + i * kLossThreads;
+        for (int i = 0; i < kStep / T; ++i) {
+            const int j = base + tid + i * T;
             if (j >= row.n) continue;
-            const unsigned long long key = top_key(row.at(j), j);
+            const unsigned long long key = top_key(row.at(j), row.first + j);
             if (key > least) sh.key[atomicAdd(&sh.count, 1)] = key;
         }
         __syncthreads();
         n = sh.count;
-        if (n <= k && base + 4 * kLossThreads < row.n) continue;
-        __syncthreads();
+        if (n <= k && base + kStep < row.n) continue;
         top_rank(sh, n, k);
+        if (tid < k && tid < n) sh.key[tid] = sh.best[tid];   // (a thread for each: k is at most T)
         if (tid == 0) sh.count = min(n, k);
-        if (n >= k) least = sh.key[k - 1];
+        if (n >= k) least = sh.best[k - 1];
     }
     __syncthreads();
 }
@@ -247,54 +264,187 @@ __device__ __forceinline__ int64_t load_index(const void *p, int it, int64_t i)
     return it == FP8_I64 ? static_cast<const int64_t *>(p)[i] : static_cast<const int32_t *>(p)[i];
 }
 
-// One row's elements through `sums`; `hide(v, vector)` may take elements out of a vector first.
-template <int DT, bool ENTROPY, typename Hide>
-__device__ __forceinline__ void stream_row(const Row<DT> &row, float c, Sums &sums, Hide hide)
+// The largest of a vector's packed elements, folded into two running ones (FP32: one); NaN is passed over.
+template <int DT>
+__device__ __forceinline__ uint32_t max_packed(uint32_t a, uint32_t b)
 {
-    constexpr int kVec = Row<DT>::kVec, kUnroll = 4;
-    for (int v0 = threadIdx.x; v0 < row.vecs; v0 += kUnroll * kLossThreads) {
-        uint4 raw[kUnroll];
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            const int v = v0 + u * kLossThreads;
-            raw[u] = v < row.vecs ? __ldg(row.vectors() + v) : no_vector<DT>();
-        }
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            float f[kVec];
-            hide(v0 + u * kLossThreads, raw[u]);
-            unpack_vector<DT>(raw[u], f);
-            float top = f[0];
-#pragma unroll
-            for (int i = 1; i < kVec; ++i) top = fmaxf(top, f[i]);
-            if (top > sums.m) sums.raise(top, c);
-#pragma unroll
-            for (int i = 0; i < kVec; ++i) sums.add<ENTROPY>(f[i], c);
-        }
-    }
+    uint32_t r;
+    if (DT == FP8_F32) return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+    if (DT == FP8_BF16) asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    else asm("max.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+template <int DT>
+__device__ __forceinline__ float packed_top(uint32_t a)
+{
+    return DT == FP8_F32 ? __uint_as_float(a) : fmaxf(element_value<DT>(a & 0xFFFFu), element_value<DT>(a >> 16));
 }
 
-template <int DT>
-__global__ void __launch_bounds__(kLossThreads) token_logprobs_kernel(const Logits p, const TokenOut o)
+// A row's vectors in batches of four a thread: whole ones, then what is left.  A batch is on its way while the one before is
+// worked on.  (Ordinary loads: a gradient may be written over its logits.)
+constexpr int kBatch = 4;
+template <int DT, int T>
+struct Batches {
+    const uint4 *src;     // the thread's first vector
+    int vecs, whole;      // whole: batches without a gap
+    __device__ __forceinline__ explicit Batches(const Row<DT> &row)
+        : src(row.vectors() + threadIdx.x), vecs(row.vecs), whole(row.vecs / (kBatch * T))
+    {
+    }
+    // batches in all; the vectors of batch b that some thread has
+    __device__ __forceinline__ int count() const { return (vecs + kBatch * T - 1) / (kBatch * T); }
+    __device__ __forceinline__ int filled(int b) const { return b < whole ? kBatch : (vecs - b * (kBatch * T) + T - 1) / T; }
+    __device__ __forceinline__ void load(int b, uint4 (&raw)[kBatch]) const
+    {
+        const uint4 *at = src + b * (kBatch * T);
+        if (b < whole) {
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) raw[u] = at[u * T];
+        } else if (b == whole) {
+            const int left = vecs - b * (kBatch * T) - (int)threadIdx.x;
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) raw[u] = u * T < left ? at[u * T] : no_vector<DT>();
+        }
+    }
+    // f(b, vectors) for all batches; `raw`: batch 0, loaded
+    template <typename F>
+    __device__ __forceinline__ void each(uint4 (&raw)[kBatch], F f) const
+    {
+        const int n = count();
+        uint4 other[kBatch];
+        for (int b = 0; b < n; b += 2) {
+            load(b + 1, other);
+            f(b, raw);
+            if (b + 1 >= n) break;
+            load(b + 2, raw);
+            f(b + 1, other);
+        }
+    }
+};
+
+// One row's elements into sums (relative to a number near the largest), and its largest element.  Bound by the memory as long
+// as an element costs few instructions (an SM issues ten of them in the time that an element's two bytes take): two of
+// everything an instruction where there is such a one, one exponential, the largest of 32 packed elements looked at once.
+// `hide(v, vector)` may take elements out of vector v.
+template <int DT, int T, bool ENTROPY, typename Hide>
+__device__ __forceinline__ Sums stream_row(const Row<DT> &row, float c, uint4 (&first)[kBatch], float &top, Hide hide)
 {
-    __shared__ TopShared top;
-    __shared__ Sums part[kLossWarps];
-    const int64_t r = blockIdx.x;
-    const Row<DT> row(p.x, r * p.ld, p.vocab);
-    Sums sums = {-INFINITY, 0.0f, 0.0f};
-    stream_row<DT, true>(row, p.c, sums, [](int, uint4 &) {});
+    constexpr int kPairs = kVecPairs<DT>;
+    const Pair c2 = pair_of(c);
+    Sums a = no_sums();
+    Pair s = pair_of(0.0f), t = pair_of(0.0f), less = pair_of(FLT_MAX);
+    top = -INFINITY;
+    const Batches<DT, T> batches(row);
+    batches.each(first, [&](int b, uint4 (&raw)[kBatch]) {
+        const int filled = batches.filled(b);
+        uint32_t most = no_vector<DT>().x;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            if (u >= filled) continue;
+            hide(b * (kBatch * T) + u * T, raw[u]);
+            most = max_packed<DT>(most, max_packed<DT>(max_packed<DT>(raw[u].x, raw[u].y), max_packed<DT>(raw[u].z, raw[u].w)));
+        }
+        const float here = packed_top<DT>(most);
+        top = fmaxf(top, here);
+        if ((here - a.m) * c > kLead) {
+            a.s = sum_of(s);
+            a.t = sum_of(t);
+            a.relate(here, c);
+            s = make_pair(a.s, 0.0f);
+            t = make_pair(a.t, 0.0f);
+            less = pair_of(-a.m);
+        }
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            if (u >= filled) continue;
+            Pair x[kPairs];
+            unpack_pairs<DT>(raw[u], x);
+#pragma unroll
+            for (int i = 0; i < kPairs; ++i) {
+                Pair d = (x[i] + less) * c2;
+                float lo, hi;
+                split(d, lo, hi);
+                if (ENTROPY) {   // (0 * -infinity)
+                    lo = max_nan(lo, kFloor);
+                    hi = max_nan(hi, kFloor);
+                    d = make_pair(lo, hi);
+                }
+                const Pair e = make_pair(exp2_approx(lo), exp2_approx(hi));
+                s = s + e;
+                if (ENTROPY) t = fma(e, d, t);
+            }
+        }
+    });
+    a.s = sum_of(s);
+    a.t = sum_of(t);
+    return a;
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// clusters: a row in as many parts as there are blocks
+// ---------------------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ void cluster_sync()
+{
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t cluster_address(const void *p, unsigned block)
+{
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(p)), "r"(block));
+    return r;
+}
+// The first elements of block b's part (b = blocks: the row's end): whole 64s.
+__device__ __forceinline__ int part_start(int vocab, int blocks, int b)
+{
+    if (blocks == 1) return b * vocab;
+    const int chunk = (vocab / blocks + 64) & ~63;
+    return min(vocab, b * chunk);
+}
+// Sums of all the parts, to every block.
+__device__ __forceinline__ Sums cluster_join(Sums own, int blocks, float c, float4 &word)
+{
+    if (blocks == 1) return own;
+    if (threadIdx.x == 0) word = make_float4(own.m, own.s, own.t, 0.0f);
+    cluster_sync();
+    Sums all = no_sums();
+    float most = -INFINITY;
+    for (int b = 0; b < blocks; ++b) {
+        Sums o;
+        const uint32_t at = cluster_address(&word, b);
+        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(o.m), "=f"(o.s), "=f"(o.t), "=f"(own.t) : "r"(at) : "memory");
+        most = fmaxf(most, o.m);
+        if (o.s != 0.0f) all.join(o, c);
+    }
+    all.m = most;
+    return all;
+}
+
+template <int DT, int T>
+__global__ void __launch_bounds__(T) token_logprobs_kernel(const Logits p, const TokenOut o, int blocks)
+{
+    __shared__ TopShared<T> top;
+    __shared__ JoinShared<T> part;
+    __shared__ float4 word;
+    const int64_t r = blockIdx.x / (unsigned)blocks;
+    const int own = (int)(blockIdx.x % (unsigned)blocks), from = part_start(p.vocab, blocks, own);
+    const Row<DT> row(p.x, r * p.ld, from, part_start(p.vocab, blocks, own + 1) - from);
+    uint4 raw[kBatch];
+    Batches<DT, T>(row).load(0, raw);
+    float strip;   // the thread's largest element
+    Sums sums = stream_row<DT, T, true>(row, p.c, raw, strip, [](int, uint4 &) {});
     const int edge = row.edge(threadIdx.x);
     if (edge >= 0) {
         const float x = row.at(edge);
-        if (x > sums.m) sums.raise(x, p.c);
-        sums.add<true>(x, p.c);
+        add_element<true>(sums, x, p.c);
+        strip = fmaxf(strip, x);
     }
-    const float strip = sums.m;
-    sums = block_join(sums, p.c, part);
+    sums = cluster_join(block_join<T>(sums, strip, p.c, part), blocks, p.c, word);
     // nothing but -infinity: s = 0;  a NaN or +infinity: s is NaN
     const bool none = sums.s == 0.0f, nan = !(sums.s >= 0.0f);
     const float logsum = none ? -INFINITY : logf(sums.s);
-    if (threadIdx.x == 0) {
+    if (own == 0 && threadIdx.x == 0) {
         const float h = none ? 0.0f : logsum - kLn2 * (sums.t / sums.s);
         if (o.entropy) o.entropy[r] = h;
         if (o.lse) o.lse[r] = none ? -INFINITY : __fmaf_rn(p.scale, sums.m, logsum);
@@ -306,21 +456,34 @@ __global__ void __launch_bounds__(kLossThreads) token_logprobs_kernel(const Logi
                 raise_flags(p.d_status, FP8_FLAG_BAD_INDEX);
                 lp = NAN;
             } else if (t >= 0) {
-                lp = none ? -INFINITY : p.scale * (row.at((int)t) - sums.m) - logsum;
+                lp = none ? -INFINITY : p.scale * (load1<DT>(p.x, r * p.ld + t) - sums.m) - logsum;
             }
             o.logprob[r] = lp;
         }
     }
-    if (o.top_k == 0) return;
-    if (!nan) find_top<DT>(row, strip, o.top_k, top);
-    for (int i = threadIdx.x; i < o.top_k; i += kLossThreads) {
-        const int64_t at = r * o.top_k + i;
-        const unsigned long long key = nan ? 0 : top.key[i];
-        const int j = nan ? -1 : (int)~(uint32_t)key;
-        o.top_logprob[at] = nan ? NAN : none ? -INFINITY : p.scale * (order_value((uint32_t)(key >> 32)) - sums.m) - logsum;
-        if (p.it == FP8_I64) static_cast<int64_t *>(o.top_index)[at] = j;
-        else static_cast<int32_t *>(o.top_index)[at] = j;
+    if (o.top_k > 0) {
+        if (!nan) find_top<DT, T>(row, strip, o.top_k, top);
+        if (blocks > 1) {
+            cluster_sync();
+            if (own == 0 && !nan) {
+                for (int i = threadIdx.x; i < blocks * o.top_k; i += T) {
+                    const uint32_t at = cluster_address(&top.best[i % o.top_k], i / o.top_k);
+                    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(top.key[i]) : "r"(at) : "memory");
+                }
+                __syncthreads();
+                top_rank(top, blocks * o.top_k, o.top_k);
+            }
+        }
+        for (int i = own == 0 ? threadIdx.x : o.top_k; i < o.top_k; i += T) {
+            const int64_t at = r * o.top_k + i;
+            const unsigned long long key = nan ? 0 : top.best[i];
+            const int j = nan ? -1 : (int)~(uint32_t)key;
+            o.top_logprob[at] = nan ? NAN : none ? -INFINITY : p.scale * (order_value((uint32_t)(key >> 32)) - sums.m) - logsum;
+            if (p.it == FP8_I64) static_cast<int64_t *>(o.top_index)[at] = j;
+            else static_cast<int32_t *>(o.top_index)[at] = j;
+        }
     }
+    if (blocks > 1) cluster_sync();   // (no block leaves while another reads its words)
 }
 
 // A row's list: thread i holds entry i.  Entries that count, their q and ln q, the sum Q of all q and the rest's q
@@ -336,14 +499,20 @@ struct ListEntry {
         rest = 0.0f;
     }
 };
+// (and a block's vectors more: a thread without a vector looks at its bits all the same)
+__host__ __device__ constexpr int list_words(int vocab) { return (vocab + 7 + 31) / 32 + 64; }
+template <int T>
 struct ListShared {
-    int index[kLossThreads];
-    float part[kLossWarps];
-    double sum[kLossWarps];
+    int index[T];
+    float part[T / 32];
+    double sum[T / 32];
 };
-__device__ __forceinline__ ListEntry load_list(const Logits &p, const TeacherList &l, int64_t r, ListShared &sh)
+// Also a bit for each token that is listed: token j at j + shift, so that a vector's bits lie in one word.
+template <int T>
+__device__ __forceinline__ ListEntry load_list(const Logits &p, const TeacherList &l, int64_t r, ListShared<T> &sh, uint32_t *bits, int shift)
 {
     const int tid = threadIdx.x;
+    for (int i = tid; i < list_words(p.vocab); i += T) bits[i] = 0u;
     ListEntry e = {-1, 0.0f, -INFINITY, 0.0f, 0.0f, 0.0f};
     float v = -INFINITY;
     if (tid < l.listed) {
@@ -353,14 +522,19 @@ __device__ __forceinline__ ListEntry load_list(const Logits &p, const TeacherLis
         else if (j >= 0) e.j = (int)j;
     }
     sh.index[tid] = e.j;
-    __syncthreads();
-    if (tid < l.listed && e.j >= 0) {
-        bool again = false;
+    __syncthreads();   // (the bits are zero)
+    bool again = false;
+    if (e.j >= 0) {
+        const uint32_t bit = 1u << ((e.j + shift) & 31);
+        again = atomicOr(&bits[(e.j + shift) >> 5], bit) & bit;
+    }
+    if (!__syncthreads_or(e.j >= 0)) return e;   // nothing listed
+    if (__syncthreads_or(again)) {               // a token that is listed twice: its first entry counts
+        again = false;
         for (int i = 0; i < tid; ++i) again = again || sh.index[i] == e.j;
         if (again) e.j = -1;
     }
     if (e.j < 0) v = -INFINITY;
-    if (!__syncthreads_or(e.j >= 0)) return e;   // nothing listed
     if (l.rest) {
         // 1 - sum of q loses what both have in common: in 64 bits
         double q = e.j >= 0 ? exp((double)v) : 0.0;
@@ -371,7 +545,7 @@ __device__ __forceinline__ ListEntry load_list(const Logits &p, const TeacherLis
         if ((tid & 31) == 0) sh.sum[tid >> 5] = q;
         __syncthreads();
         q = 0.0;
-        for (int i = 0; i < kLossWarps; ++i) q += sh.sum[i];
+        for (int i = 0; i < T / 32; ++i) q += sh.sum[i];
         const double rest = q >= 1.0 ? 0.0 : 1.0 - q;   // (NaN stays)
         e.mass = (float)q;
         e.rest = (float)rest;
@@ -383,11 +557,11 @@ __device__ __forceinline__ ListEntry load_list(const Logits &p, const TeacherLis
         if ((tid & 31) == 0) sh.part[tid >> 5] = top;
         __syncthreads();
         top = sh.part[0];
-        for (int i = 1; i < kLossWarps; ++i) top = max_nan(top, sh.part[i]);
+        for (int i = 1; i < T / 32; ++i) top = max_nan(top, sh.part[i]);
         __syncthreads();
         const bool none = top == -INFINITY;
         float q = none ? 0.0f : expf(v - top);
-        const float sum = block_sum<kLossThreads>(q, sh.part);
+        const float sum = block_sum<T>(q, sh.part);
         e.q = none ? 0.0f : q / sum;
         e.lnq = none ? -INFINITY : (v - top) - logf(sum);
         e.mass = e.total = none ? 0.0f : sum >= 0.0f ? 1.0f : NAN;
@@ -395,18 +569,13 @@ __device__ __forceinline__ ListEntry load_list(const Logits &p, const TeacherLis
     return e;
 }
 
-// The listed elements of a row, one bit each: bit of element j at j - head + 8, so that a vector's bits lie in one word.
-__host__ __device__ constexpr int list_words(int vocab) { return (vocab + 8 + 31) / 32 + 1; }
 template <int DT>
-__device__ __forceinline__ void note_listed(uint32_t *bits, const Row<DT> &row, int j)
-{
-    const int bit = j - row.head + 8;
-    atomicOr(&bits[bit >> 5], 1u << (bit & 31));
-}
+__device__ __forceinline__ int list_shift(const Row<DT> &row) { return -(row.first + row.head) & (Row<DT>::kVec - 1); }
+// `j`: place in this part of the row
 template <int DT>
 __device__ __forceinline__ bool is_listed(const uint32_t *bits, const Row<DT> &row, int j)
 {
-    const int bit = j - row.head + 8;
+    const int bit = row.first + j + list_shift<DT>(row);
     return bits[bit >> 5] >> (bit & 31) & 1u;
 }
 // Elements whose bit is set become -infinity.
@@ -423,63 +592,79 @@ __device__ __forceinline__ void hide_bits(uint32_t hidden, uint4 &raw)
     }
     raw = make_uint4(w[0], w[1], w[2], w[3]);
 }
+// The thread's view of the bits: those of its vectors lie at one place in words that are as far apart as the vectors.
 template <int DT>
-__device__ __forceinline__ void hide_listed(const uint32_t *bits, const Row<DT> &row, int v, uint4 &raw)
-{
-    constexpr int kVec = Row<DT>::kVec;
-    if (v >= row.vecs) return;
-    const int bit = v * kVec + 8;
-    const uint32_t hidden = (bits[bit >> 5] >> (bit & 31)) & ((1u << kVec) - 1u);
-    if (hidden) hide_bits<DT>(hidden, raw);
-}
+struct ListedVectors {
+    const uint32_t *word;
+    int place;
+    __device__ __forceinline__ ListedVectors(const uint32_t *bits, const Row<DT> &row)
+    {
+        const int bit = row.first + row.head + list_shift<DT>(row) + (int)threadIdx.x * Row<DT>::kVec;
+        word = bits + (bit >> 5);
+        place = bit & 31;
+    }
+    // ahead: vectors from the thread's first one (a multiple of the block's threads)
+    __device__ __forceinline__ void hide(int ahead, uint4 &raw) const
+    {
+        const uint32_t hidden = (word[ahead * Row<DT>::kVec / 32] >> place) & ((1u << Row<DT>::kVec) - 1u);
+        if (hidden) hide_bits<DT>(hidden, raw);
+    }
+};
 
-template <int DT>
-__global__ void __launch_bounds__(kLossThreads) distill_kernel(const Logits p, const TeacherList l, float *loss, float *saved)
+template <int DT, int T>
+__global__ void __launch_bounds__(T) distill_kernel(const Logits p, const TeacherList l, float *loss, float *saved, int blocks)
 {
     extern __shared__ __align__(16) uint32_t listed_bits[];
-    __shared__ ListShared sh;
-    __shared__ Sums part[2][kLossWarps];
-    __shared__ float terms[kLossWarps];
-    const int64_t r = blockIdx.x;
-    const Row<DT> row(p.x, r * p.ld, p.vocab);
-    for (int i = threadIdx.x; i < list_words(p.vocab); i += kLossThreads) listed_bits[i] = 0u;
-    ListEntry e = load_list(p, l, r, sh);   // (has barriers behind the zeros)
+    __shared__ ListShared<T> sh;
+    __shared__ JoinShared<T> part[2];
+    __shared__ float4 word;
+    __shared__ float terms[T / 32];
+    const int64_t r = blockIdx.x / (unsigned)blocks;
+    const int own = (int)(blockIdx.x % (unsigned)blocks), from = part_start(p.vocab, blocks, own);
+    const Row<DT> row(p.x, r * p.ld, from, part_start(p.vocab, blocks, own + 1) - from);
+    uint4 raw[kBatch];
+    Batches<DT, T>(row).load(0, raw);   // (on their way while the list is worked out)
+    ListEntry e = load_list(p, l, r, sh, listed_bits, list_shift<DT>(row));
     const bool counts = e.j >= 0;
-    float x = -INFINITY;
-    if (counts) {
-        note_listed<DT>(listed_bits, row, e.j);
-        x = row.at(e.j);
-    }
-    __syncthreads();
+    const float x = counts && own == 0 ? load1<DT>(p.x, r * p.ld + e.j) : -INFINITY;
     // the tokens that are not listed, apart from those that are: neither sum is a difference
-    Sums sums = {-INFINITY, 0.0f, 0.0f};
-    stream_row<DT, false>(row, p.c, sums, [&](int v, uint4 &raw) { hide_listed<DT>(listed_bits, row, v, raw); });
+    const ListedVectors<DT> listed(listed_bits, row);
+    float top;
+    Sums sums = stream_row<DT, T, false>(row, p.c, raw, top, [&](int ahead, uint4 &raw) { listed.hide(ahead, raw); });
     const int edge = row.edge(threadIdx.x);
     if (edge >= 0 && !is_listed<DT>(listed_bits, row, edge)) {
         const float y = row.at(edge);
-        if (y > sums.m) sums.raise(y, p.c);
-        sums.add<false>(y, p.c);
+        add_element<false>(sums, y, p.c);
+        top = fmaxf(top, y);
     }
-    const Sums others = block_join(sums, p.c, part[0]);
-    Sums own = {x, 0.0f, 0.0f};
-    if (counts) own.add<false>(x, p.c);
-    Sums all = block_join(own, p.c, part[1]);
-    all.join(others, p.c);
-    const bool none = all.s == 0.0f;
-    const float logsum = none ? -INFINITY : logf(all.s);
-    // ln of the others' sum relative to the row's largest logit, from the sum relative to their own: it may be far below
-    const float logrest = others.s == 0.0f ? -INFINITY : __fmaf_rn(p.scale, others.m - all.m, logf(others.s));
-    if (logrest == -INFINITY) e.drop_rest();
-    float term = 0.0f;
-    if (counts && e.q != 0.0f) term = e.q * (e.lnq - (none || x == -INFINITY ? -INFINITY : p.scale * (x - all.m) - logsum));
-    if (threadIdx.x == 0 && e.rest != 0.0f) term += e.rest * (logf(e.rest) - (logrest - logsum));
-    if (none && e.total != 0.0f && threadIdx.x == 0) term = INFINITY;
-    term = block_sum<kLossThreads>(term, terms);
-    if (threadIdx.x == 0) {
-        loss[r] = term;
-        if (saved)
-            reinterpret_cast<float4 *>(saved)[r] = make_float4(none ? 0.0f : all.m, none ? INFINITY : logsum, 0.0f, none ? INFINITY : logrest);
+    const Sums others = cluster_join(block_join<T>(sums, top, p.c, part[0]), blocks, p.c, word);
+    if (own == 0) {
+        sums = no_sums();
+        if (counts) add_element<false>(sums, x, p.c);
+        Sums all = block_join<T>(sums, x, p.c, part[1]);
+        const float most = fmaxf(all.m, others.m);
+        if (others.s != 0.0f) {
+            if (all.s == 0.0f) all = no_sums();
+            all.join(others, p.c);
+        }
+        all.m = most;
+        const bool none = all.s == 0.0f;
+        const float logsum = none ? -INFINITY : logf(all.s);
+        // ln of the others' sum relative to the row's largest logit, from the sum relative to their own: it may be far below
+        const float logrest = others.s == 0.0f ? -INFINITY : __fmaf_rn(p.scale, others.m - all.m, logf(others.s));
+        if (logrest == -INFINITY) e.drop_rest();
+        float term = 0.0f;
+        if (counts && e.q != 0.0f) term = e.q * (e.lnq - (none || x == -INFINITY ? -INFINITY : p.scale * (x - all.m) - logsum));
+        if (threadIdx.x == 0 && e.rest != 0.0f) term += e.rest * (logf(e.rest) - (logrest - logsum));
+        if (none && e.total != 0.0f && threadIdx.x == 0) term = INFINITY;
+        term = block_sum<T>(term, terms);
+        if (threadIdx.x == 0) {
+            loss[r] = term;
+            if (saved)
+                reinterpret_cast<float4 *>(saved)[r] = make_float4(none ? 0.0f : all.m, none ? INFINITY : logsum, 0.0f, none ? INFINITY : logrest);
+        }
     }
+    if (blocks > 1) cluster_sync();   // (no block leaves while another reads its words)
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
@@ -488,64 +673,85 @@ __global__ void __launch_bounds__(kLossThreads) distill_kernel(const Logits p, c
 struct GradOut {
     void *dx;
     int64_t ld;
-    int same;   // rows of logits and gradient lie alike relative to 16 bytes
+    int same;     // rows of logits and gradient lie alike relative to 16 bytes
+    int blocks;   // parts of a row
     AmaxSink sink;
 };
 
-// dx_j = 2^d (a + b d) with d = log2 p_j (p relative to the sum that log2sum is of), for all j of a row
-// that `hide(v, vector)` leaves (the others are written as zeros, and later by their own formula); `skip(j)` is the same
+// dx_j = 2^d (a + b d) with d = log2 p_j (p relative to the sum that log2sum is of), for all j of a part of a row
+// that `hide(ahead, vector)` leaves (the others are written as zeros, and later by their own formula); `skip(j)` is the same
 // for elements outside the vectors
-template <int DT, bool SLOPE, typename Hide, typename Skip>
-__device__ __forceinline__ void write_row(const Row<DT> &row, void *out, int64_t at, int same, float m, float c, float log2sum, float a,
-                                          float b, uint32_t &key, Hide hide, Skip skip)
+template <int DT, int T, bool SLOPE, typename Hide, typename Skip>
+__device__ __forceinline__ void write_row(const Row<DT> &row, uint4 (&first)[kBatch], void *out, int64_t at, int same, float m, float c,
+                                          float log2sum, float a, float b, uint32_t &key, Hide hide, Skip skip)
 {
-    constexpr int kVec = Row<DT>::kVec, kUnroll = 4, kSize = InType<DT>::kBytes;
+    constexpr int kPairs = kVecPairs<DT>, kSize = InType<DT>::kBytes;
     auto value = [&](float x) {
         const float d = max_nan(__fmaf_rn(x - m, c, -log2sum), kFloor), e = exp2_approx(d);
         const uint32_t bits = element_bits<DT>(e * (SLOPE ? __fmaf_rn(b, d, a) : a));
         key = max(key, magnitude_key(element_value<DT>(bits)));
         return bits;
     };
-    if (same) {
-        uint4 *dst = reinterpret_cast<uint4 *>(static_cast<uint8_t *>(out) + (at + row.head) * kSize);
-        for (int v0 = threadIdx.x; v0 < row.vecs; v0 += kUnroll * kLossThreads) {
-            uint4 raw[kUnroll];
-#pragma unroll
-            for (int u = 0; u < kUnroll; ++u)
-                if (v0 + u * kLossThreads < row.vecs) raw[u] = row.vectors()[v0 + u * kLossThreads];
-#pragma unroll
-            for (int u = 0; u < kUnroll; ++u) {
-                if (v0 + u * kLossThreads >= row.vecs) continue;
-                float f[kVec];
-                uint32_t w[4];
-                hide(v0 + u * kLossThreads, raw[u]);
-                unpack_vector<DT>(raw[u], f);
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    w[i] = DT == FP8_F32 ? value(f[i]) : value(f[2 * i % kVec]) | (value(f[(2 * i + 1) % kVec]) << 16);
-                dst[v0 + u * kLossThreads] = make_uint4(w[0], w[1], w[2], w[3]);
-            }
-        }
-        const int edge = row.edge(threadIdx.x);
-        if (edge >= 0 && !skip(edge)) store_bits<DT>(out, at + edge, value(row.at(edge)));
-    } else {
-        for (int j = threadIdx.x; j < row.n; j += kLossThreads)
+    if (!same) {
+        for (int j = threadIdx.x; j < row.n; j += T)
             if (!skip(j)) store_bits<DT>(out, at + j, value(row.at(j)));
+        return;
     }
+    uint32_t acc = 0;
+    uint4 *dst = reinterpret_cast<uint4 *>(static_cast<uint8_t *>(out) + (at + row.head) * kSize) + threadIdx.x;
+    const Pair less = pair_of(-m), c2 = pair_of(c), off = pair_of(-log2sum), a2 = pair_of(a), b2 = pair_of(b);
+    const Batches<DT, T> batches(row);
+    batches.each(first, [&](int n, uint4 (&raw)[kBatch]) {
+        const int left = row.vecs - n * (kBatch * T) - (int)threadIdx.x;
+        uint4 *to = dst + n * (kBatch * T);
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            if (u * T >= left) continue;
+            hide(n * (kBatch * T) + u * T, raw[u]);
+            Pair x[kPairs];
+            unpack_pairs<DT>(raw[u], x);
+#pragma unroll
+            for (int i = 0; i < kPairs; ++i) {
+                Pair d = fma(x[i] + less, c2, off);
+                float lo, hi;
+                split(d, lo, hi);
+                if (SLOPE) {   // (0 * -infinity)
+                    lo = max_nan(lo, kFloor);
+                    hi = max_nan(hi, kFloor);
+                    d = make_pair(lo, hi);
+                }
+                const Pair e = make_pair(exp2_approx(lo), exp2_approx(hi));
+                x[i] = e * (SLOPE ? fma(b2, d, a2) : a2);
+            }
+            const uint4 y = pack_pairs<DT>(x);
+            acc = fold_vector<DT>(acc, y);
+            to[u * T] = y;
+        }
+    });
+    key = max(key, folded_key<DT>(acc));
+    const int edge = row.edge(threadIdx.x);
+    if (edge >= 0 && !skip(edge)) store_bits<DT>(out, at + edge, value(row.at(edge)));
 }
 
-template <int DT>
+template <int DT, int T>
 __device__ __forceinline__ void write_zeros(void *out, int64_t at, int n)
 {
-    for (int j = threadIdx.x; j < n; j += kLossThreads) store_bits<DT>(out, at + j, 0u);
+    const Row<DT> row(out, at, 0, n);
+    uint4 *dst = const_cast<uint4 *>(row.vectors());
+    for (int v = threadIdx.x; v < row.vecs; v += T) dst[v] = make_uint4(0u, 0u, 0u, 0u);
+    const int edge = row.edge(threadIdx.x);
+    if (edge >= 0) store_bits<DT>(out, at + edge, 0u);
 }
 
-template <int DT>
-__global__ void __launch_bounds__(kLossThreads) token_logprobs_bwd_kernel(const Logits p, const void *targets, const float *saved,
+template <int DT, int T>
+__global__ void __launch_bounds__(T) token_logprobs_bwd_kernel(const Logits p, const void *targets, const float *saved,
                                                                           const float *g_lp, int64_t g_lp_stride, const float *g_h,
                                                                           int64_t g_h_stride, const GradOut o)
 {
-    const int64_t r = blockIdx.x, at = r * o.ld;
+    const int64_t r = blockIdx.x / (unsigned)o.blocks;
+    const int part = (int)(blockIdx.x % (unsigned)o.blocks), from = part_start(p.vocab, o.blocks, part);
+    const int count = part_start(p.vocab, o.blocks, part + 1) - from;
+    const int64_t at = r * o.ld + from;
     const float4 keep = reinterpret_cast<const float4 *>(saved)[r];
     int64_t t = g_lp && targets ? load_index(targets, p.it, r) : -1;
     if (t >= p.vocab) {
@@ -555,64 +761,73 @@ __global__ void __launch_bounds__(kLossThreads) token_logprobs_bwd_kernel(const 
     const float g = t >= 0 ? g_lp[r * g_lp_stride] : 0.0f, gh = g_h ? g_h[r * g_h_stride] : 0.0f;
     uint32_t key = 0;
     if ((g == 0.0f && gh == 0.0f) || keep.y == INFINITY) {
-        write_zeros<DT>(o.dx, at, p.vocab);
+        write_zeros<DT, T>(o.dx, at, count);
     } else {
-        const Row<DT> row(p.x, r * p.ld, p.vocab);
+        const Row<DT> row(p.x, r * p.ld, from, count);
+        uint4 raw[kBatch];
+        Batches<DT, T>(row).load(0, raw);
+        const int given = t >= from && t < from + count ? (int)t - from : -1;   // this part's
         uint32_t own = 0;
-        if (t >= 0 && threadIdx.x == 0) {
+        if (given >= 0 && threadIdx.x == 0) {
             // 1 - p of a token that is nearly certain: expm1 keeps its digits
-            const float lp = max_nan(p.scale * (row.at((int)t) - keep.x) - keep.y, -1e30f), prob = expf(lp);
+            const float lp = max_nan(p.scale * (row.at(given) - keep.x) - keep.y, -1e30f), prob = expf(lp);
             own = element_bits<DT>(p.scale * (-g * expm1f(lp) - gh * prob * (lp + keep.z)));
         }
         __syncthreads();   // (the gradient may overwrite the logits)
-        write_row<DT, true>(row, o.dx, at, o.same, keep.x, p.c, keep.y * kLog2e, p.scale * (-g - gh * keep.z), -p.scale * gh * kLn2, key,
-                            [&](int v, uint4 &raw) {
-                                const int i = (int)t - row.head - v * Row<DT>::kVec;
-                                if ((unsigned)i < (unsigned)Row<DT>::kVec) hide_bits<DT>(1u << i, raw);
+        const int given_vec = given >= row.head ? (given - row.head) / Row<DT>::kVec - (int)threadIdx.x : -1;
+        const int given_bit = (given - row.head) % Row<DT>::kVec;
+        write_row<DT, T, true>(row, raw, o.dx, at, o.same, keep.x, p.c, keep.y * kLog2e, p.scale * (-g - gh * keep.z), -p.scale * gh * kLn2, key,
+                            [&](int ahead, uint4 &raw) {
+                                if (ahead == given_vec) hide_bits<DT>(1u << given_bit, raw);
                             },
-                            [&](int j) { return j == (int)t; });
+                            [&](int j) { return j == given; });
         __syncthreads();
-        if (t >= 0 && threadIdx.x == 0) {
-            store_bits<DT>(o.dx, at + t, own);
+        if (given >= 0 && threadIdx.x == 0) {
+            store_bits<DT>(o.dx, at + given, own);
             key = max(key, magnitude_key(element_value<DT>(own)));
         }
     }
     sink_amax(key, o.sink);
 }
 
-template <int DT>
-__global__ void __launch_bounds__(kLossThreads) distill_bwd_kernel(const Logits p, const TeacherList l, const float *saved,
+template <int DT, int T>
+__global__ void __launch_bounds__(T) distill_bwd_kernel(const Logits p, const TeacherList l, const float *saved,
                                                                    const float *g_loss, int64_t g_stride, const GradOut o)
 {
     extern __shared__ __align__(16) uint32_t listed_bits[];
-    __shared__ ListShared sh;
-    const int64_t r = blockIdx.x, at = r * o.ld;
+    __shared__ ListShared<T> sh;
+    const int64_t r = blockIdx.x / (unsigned)o.blocks;
+    const int part = (int)(blockIdx.x % (unsigned)o.blocks), from = part_start(p.vocab, o.blocks, part);
+    const int count = part_start(p.vocab, o.blocks, part + 1) - from;
+    const int64_t at = r * o.ld + from;
     const float4 keep = reinterpret_cast<const float4 *>(saved)[r];
     const float g = g_loss[r * g_stride] * p.scale;
     uint32_t key = 0;
     if (g == 0.0f || keep.y == INFINITY) {
-        write_zeros<DT>(o.dx, at, p.vocab);
+        write_zeros<DT, T>(o.dx, at, count);
     } else {
-        const Row<DT> row(p.x, r * p.ld, p.vocab);
-        for (int i = threadIdx.x; i < list_words(p.vocab); i += kLossThreads) listed_bits[i] = 0u;
-        ListEntry e = load_list(p, l, r, sh);   // (has barriers behind the zeros)
+        const Row<DT> row(p.x, r * p.ld, from, count);
+        uint4 raw[kBatch];
+        Batches<DT, T>(row).load(0, raw);   // (on their way while the list is worked out)
+        ListEntry e = load_list(p, l, r, sh, listed_bits, list_shift<DT>(row));
         if (keep.w == -INFINITY) e.drop_rest();
+        const int own_j = e.j >= from && e.j < from + count ? e.j - from : -1;
         uint32_t own = 0;
-        if (e.j >= 0) {
-            note_listed<DT>(listed_bits, row, e.j);
-            const float prob = expf(p.scale * (row.at(e.j) - keep.x) - keep.y);
+        if (own_j >= 0) {
+            const float prob = expf(p.scale * (row.at(own_j) - keep.x) - keep.y);
             own = element_bits<DT>(g * __fmaf_rn(e.total, prob, -e.q));
         }
         // the others: p_j Q, or with s_j = p_j / p_r, s_j (Q p_r - q_r): s_j is one of a sum of 1 however small p_r is
         const float logsum = e.rest == 0.0f ? keep.y : keep.w;
         const float a = e.rest == 0.0f ? e.total : __fmaf_rn(e.total, expf(keep.w - keep.y), -e.rest);
+        const ListedVectors<DT> listed(listed_bits, row);
         __syncthreads();   // (the gradient may overwrite the logits)
-        write_row<DT, false>(row, o.dx, at, o.same, keep.x, p.c, logsum * kLog2e, g * a, 0.0f, key,
-                             [&](int v, uint4 &raw) { hide_listed<DT>(listed_bits, row, v, raw); },
+        write_row<DT, T, false>(row, raw, o.dx, at, o.same, keep.x, p.c, logsum * kLog2e, g * a, 0.0f, key,
+                             [&](int ahead, uint4 &raw) { listed.hide(ahead, raw); },
                              [&](int j) { return is_listed<DT>(listed_bits, row, j); });
         __syncthreads();
-        if (e.j >= 0) {
-            store_bits<DT>(o.dx, at + e.j, own);
+        if (own_j >= 0) {
+            store_bits<DT>(o.dx, at + own_j, own);
             key = max(key, magnitude_key(element_value<DT>(own)));
         }
     }
@@ -648,38 +863,71 @@ static Logits make_logits(const fp8_ctx *ctx, const void *x, int64_t ld, int64_t
     return Logits{x, ld, rows, (int)vocab, it, scale, scale * kLog2e, ctx->d_status};
 }
 
-static GradOut make_grad(fp8_ctx *ctx, const void *x, int64_t ld, int dt, void *dx, int64_t ld_d, float *d_amax)
+static GradOut make_grad(fp8_ctx *ctx, const void *x, int64_t ld, int dt, void *dx, int64_t ld_d, float *d_amax, int blocks)
 {
     const int64_t size = dt == FP8_F32 ? 4 : 2;
     const int64_t apart = (int64_t)(reinterpret_cast<uintptr_t>(x) & 15u) - (int64_t)(reinterpret_cast<uintptr_t>(dx) & 15u);
     const int same = apart == 0 && (ld - ld_d) * size % 16 == 0;
-    return GradOut{dx, ld_d, same, {d_amax ? take_slot(ctx) : nullptr, d_amax, nullptr, ctx->d_status, FP8_E5, 0, 0}};
+    return GradOut{dx, ld_d, same, blocks, {d_amax ? take_slot(ctx) : nullptr, d_amax, nullptr, ctx->d_status, FP8_E5, 0, 0}};
 }
 
-template <int DT>
+// In how many parts rows are read: as many blocks as give every SM two of them, of 2048 elements at least.
+static int row_blocks(const fp8_ctx *ctx, int64_t rows, int64_t vocab)
+{
+    int blocks = 1;
+    while (blocks < 8 && rows * blocks < (int64_t)ctx->sm_count * 2 && vocab / (2 * blocks) >= 2048) blocks *= 2;
+    return blocks;
+}
+
+// `cluster`: the blocks of a row are one.
+template <typename... KArgs, typename... Args>
+static fp8_status_t launch_rows(void (*kernel)(KArgs...), int threads, int64_t rows, int blocks, bool cluster, unsigned smem, void *stream, Args... args)
+{
+    if (rows * blocks > 0x7FFFFFFF) return FP8_ERR_SHAPE;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)blocks;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(rows * blocks));
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = (cudaStream_t)stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster && blocks > 1 ? 1 : 0;
+    count_launch();
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...) == cudaSuccess ? FP8_OK : FP8_ERR_CUDA;
+}
+
+template <int DT, int T>
 static cudaError_t allow_lists()
 {
     const int bytes = list_words(FP8_LOSS_VOCAB_MAX) * 4;
-    cudaError_t e = cudaFuncSetAttribute(distill_kernel<DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(distill_bwd_kernel<DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    return e;
+    const auto attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
+    cudaError_t e = cudaFuncSetAttribute(distill_kernel<DT, T>, attr, bytes);
+    return e == cudaSuccess ? cudaFuncSetAttribute(distill_bwd_kernel<DT, T>, attr, bytes) : e;
 }
 cudaError_t configure_loss_kernels()
 {
-    cudaError_t e = allow_lists<FP8_BF16>();
-    if (e == cudaSuccess) e = allow_lists<FP8_F16>();
-    return e == cudaSuccess ? allow_lists<FP8_F32>() : e;
+    cudaError_t e = allow_lists<FP8_BF16, 128>();
+    if (e == cudaSuccess) e = allow_lists<FP8_BF16, 256>();
+    if (e == cudaSuccess) e = allow_lists<FP8_F16, 128>();
+    if (e == cudaSuccess) e = allow_lists<FP8_F16, 256>();
+    if (e == cudaSuccess) e = allow_lists<FP8_F32, 128>();
+    return e == cudaSuccess ? allow_lists<FP8_F32, 256>() : e;
 }
 
 }  // namespace fp8lin
 
-#define FP8LIN_LAUNCH_BY_TYPE(KERNEL, GRID, SMEM, ...)                                                       \
-    do {                                                                                                     \
-        count_launch();                                                                                      \
-        if (dt == FP8_BF16) KERNEL<FP8_BF16><<<GRID, kLossThreads, SMEM, (cudaStream_t)stream>>>(__VA_ARGS__);    \
-        else if (dt == FP8_F16) KERNEL<FP8_F16><<<GRID, kLossThreads, SMEM, (cudaStream_t)stream>>>(__VA_ARGS__); \
-        else KERNEL<FP8_F32><<<GRID, kLossThreads, SMEM, (cudaStream_t)stream>>>(__VA_ARGS__);                    \
-    } while (0)
+#define FP8LIN_LAUNCH_OF(DT, T, KERNEL, ...) launch_rows(KERNEL<DT, T>, T, __VA_ARGS__)
+#define FP8LIN_LAUNCH_BY_TYPE(T, KERNEL, ...)                                                          \
+    (dt == FP8_BF16  ? FP8LIN_LAUNCH_OF(FP8_BF16, T, KERNEL, __VA_ARGS__)                              \
+     : dt == FP8_F16 ? FP8LIN_LAUNCH_OF(FP8_F16, T, KERNEL, __VA_ARGS__)                               \
+                     : FP8LIN_LAUNCH_OF(FP8_F32, T, KERNEL, __VA_ARGS__))
+// 128 threads a row: what a row costs beside its elements is paid by warp.  256 where a thread each is needed for more top
+// or listed tokens (top tokens: twice as many strips keep the candidates few).
+#define FP8LIN_LAUNCH_BY_SIZE(SMALL, KERNEL, ...) \
+    ((SMALL) ? FP8LIN_LAUNCH_BY_TYPE(128, KERNEL, __VA_ARGS__) : FP8LIN_LAUNCH_BY_TYPE(256, KERNEL, __VA_ARGS__))
 
 extern "C" {
 
@@ -701,8 +949,8 @@ fp8_status_t fp8_token_logprobs(fp8_ctx *ctx, const void *logits, fp8_dtype_t dt
     const OnDevice on(ctx->device);
     const Logits p = make_logits(ctx, logits, ld, rows, vocab, scale, (int)it);
     const TokenOut o = {targets, logprob, entropy, lse, saved, top_logprob, top_index, top_k};
-    FP8LIN_LAUNCH_BY_TYPE(token_logprobs_kernel, (unsigned)rows, 0, p, o);
-    return cudaGetLastError() == cudaSuccess ? FP8_OK : FP8_ERR_CUDA;
+    const int blocks = row_blocks(ctx, rows, vocab);
+    return FP8LIN_LAUNCH_BY_SIZE(top_k <= 32, token_logprobs_kernel, rows, blocks, true, 0u, stream, p, o, blocks);
 }
 
 fp8_status_t fp8_token_logprobs_bwd(fp8_ctx *ctx, const void *logits, fp8_dtype_t dt, int64_t ld, int64_t rows, int64_t vocab, float scale,
@@ -720,10 +968,10 @@ fp8_status_t fp8_token_logprobs_bwd(fp8_ctx *ctx, const void *logits, fp8_dtype_
         return FP8_ERR_ALIGN;
     const OnDevice on(ctx->device);
     const Logits p = make_logits(ctx, logits, ld, rows, vocab, scale, (int)it);
-    const GradOut o = make_grad(ctx, logits, ld, (int)dt, dlogits, ld_d, d_amax);
-    FP8LIN_LAUNCH_BY_TYPE(token_logprobs_bwd_kernel, (unsigned)rows, 0, p, targets, saved, g_logprob, g_logprob_stride, g_entropy,
-                          g_entropy_stride, o);
-    return cudaGetLastError() == cudaSuccess ? FP8_OK : FP8_ERR_CUDA;
+    const int blocks = row_blocks(ctx, rows, vocab);
+    const GradOut o = make_grad(ctx, logits, ld, (int)dt, dlogits, ld_d, d_amax, blocks);
+    return FP8LIN_LAUNCH_BY_TYPE(128, token_logprobs_bwd_kernel, rows, blocks, false, 0u, stream, p, targets, saved, g_logprob, g_logprob_stride,
+                                 g_entropy, g_entropy_stride, o);
 }
 
 fp8_status_t fp8_distill_fwd(fp8_ctx *ctx, const void *logits, fp8_dtype_t dt, int64_t ld, int64_t rows, int64_t vocab, float scale,
@@ -740,8 +988,8 @@ fp8_status_t fp8_distill_fwd(fp8_ctx *ctx, const void *logits, fp8_dtype_t dt, i
     const OnDevice on(ctx->device);
     const Logits p = make_logits(ctx, logits, ld, rows, vocab, scale, (int)it);
     const TeacherList l = {index, value, ld_index, ld_value, listed, mode == FP8_DISTILL_REST};
-    FP8LIN_LAUNCH_BY_TYPE(distill_kernel, (unsigned)rows, list_words((int)vocab) * 4, p, l, loss, saved);
-    return cudaGetLastError() == cudaSuccess ? FP8_OK : FP8_ERR_CUDA;
+    const int blocks = row_blocks(ctx, rows, vocab);
+    return FP8LIN_LAUNCH_BY_SIZE(listed <= 128, distill_kernel, rows, blocks, true, list_words((int)vocab) * 4u, stream, p, l, loss, saved, blocks);
 }
 
 fp8_status_t fp8_distill_bwd(fp8_ctx *ctx, const void *logits, fp8_dtype_t dt, int64_t ld, int64_t rows, int64_t vocab, float scale,
@@ -760,9 +1008,9 @@ fp8_status_t fp8_distill_bwd(fp8_ctx *ctx, const void *logits, fp8_dtype_t dt, i
     const OnDevice on(ctx->device);
     const Logits p = make_logits(ctx, logits, ld, rows, vocab, scale, (int)it);
     const TeacherList l = {index, value, ld_index, ld_value, listed, mode == FP8_DISTILL_REST};
-    const GradOut o = make_grad(ctx, logits, ld, (int)dt, dlogits, ld_d, d_amax);
-    FP8LIN_LAUNCH_BY_TYPE(distill_bwd_kernel, (unsigned)rows, list_words((int)vocab) * 4, p, l, saved, g_loss, g_loss_stride, o);
-    return cudaGetLastError() == cudaSuccess ? FP8_OK : FP8_ERR_CUDA;
+    const int blocks = row_blocks(ctx, rows, vocab);
+    const GradOut o = make_grad(ctx, logits, ld, (int)dt, dlogits, ld_d, d_amax, blocks);
+    return FP8LIN_LAUNCH_BY_SIZE(listed <= 128, distill_bwd_kernel, rows, blocks, false, list_words((int)vocab) * 4u, stream, p, l, saved, g_loss, g_loss_stride, o);
 }
 
 }  // extern "C"

@@ -144,22 +144,6 @@ __device__ __forceinline__ uint4 normalise_vector(const NormFwd &p, const float 
     return pack_vector<DT>(v);
 }
 
-// Largest magnitude of packed elements (as fp8_amax folds them), and its key.
-template <int DT>
-__device__ __forceinline__ uint32_t fold_vector(uint32_t acc, const uint4 &v)
-{
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) acc = DT == FP8_F32 ? max(acc, w[i] & 0x7FFFFFFFu) : __vmaxu2(acc, w[i] & 0x7FFF7FFFu);
-    return acc;
-}
-template <int DT>
-__device__ __forceinline__ uint32_t folded_key(uint32_t acc)
-{
-    if (DT == FP8_F32) return acc;
-    return magnitude_key(element_value<DT>(max(acc & 0xFFFFu, acc >> 16)));
-}
-
 // The E4 bytes of a vector of y, to y8 + at (8 or 4 bytes, aligned).
 template <int DT>
 __device__ __forceinline__ void store_bytes(uint8_t *y8, int64_t at, const uint4 &y, Pow2Pair scale, bool &sat)

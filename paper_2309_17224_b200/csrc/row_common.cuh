@@ -101,8 +101,102 @@ __device__ __forceinline__ uint4 pack_vector(const float (&f)[N])
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// Two FP32 numbers a instruction (a register pair).
+struct Pair {
+    unsigned long long v;
+};
+__device__ __forceinline__ Pair make_pair(float lo, float hi)
+{
+    Pair p;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(p.v) : "f"(lo), "f"(hi));
+    return p;
+}
+__device__ __forceinline__ Pair pair_of(float x) { return make_pair(x, x); }
+__device__ __forceinline__ void split(Pair p, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(p.v)); }
+__device__ __forceinline__ Pair operator+(Pair a, Pair b)
+{
+    Pair r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ Pair operator*(Pair a, Pair b)
+{
+    Pair r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ Pair fma(Pair a, Pair b, Pair c)
+{
+    Pair r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+__device__ __forceinline__ float sum_of(Pair p)
+{
+    float lo, hi;
+    split(p, lo, hi);
+    return lo + hi;
+}
+
+// Elements 2i, 2i + 1 of a 16-byte vector (FP32: of its four), and a vector of such pairs rounded to the type.
+template <int DT>
+constexpr int kVecPairs = DT == FP8_F32 ? 2 : 4;
+template <int DT>
+__device__ __forceinline__ void unpack_pairs(const uint4 &v, Pair (&f)[kVecPairs<DT>])
+{
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < kVecPairs<DT>; ++i) {
+        if (DT == FP8_F32) {
+            f[i] = make_pair(__uint_as_float(w[2 * i % 4]), __uint_as_float(w[(2 * i + 1) % 4]));
+        } else if (DT == FP8_BF16) {
+            f[i] = make_pair(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
+        } else {
+            float lo, hi;
+            asm("{ .reg .b16 lo, hi; mov.b32 {lo, hi}, %2; cvt.f32.f16 %0, lo; cvt.f32.f16 %1, hi; }" : "=f"(lo), "=f"(hi) : "r"(w[i]));
+            f[i] = make_pair(lo, hi);
+        }
+    }
+}
+template <int DT>
+__device__ __forceinline__ uint4 pack_pairs(const Pair (&f)[kVecPairs<DT>])
+{
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < kVecPairs<DT>; ++i) {
+        float lo, hi;
+        split(f[i], lo, hi);
+        if (DT == FP8_F32) {
+            w[2 * i % 4] = __float_as_uint(lo);
+            w[(2 * i + 1) % 4] = __float_as_uint(hi);
+        } else if (DT == FP8_BF16) {
+            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(hi), "f"(lo));
+        } else {
+            asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(hi), "f"(lo));
+        }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Largest magnitude of packed elements (as fp8_amax folds them), and its key.
+template <int DT>
+__device__ __forceinline__ uint32_t fold_vector(uint32_t acc, const uint4 &v)
+{
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc = DT == FP8_F32 ? max(acc, w[i] & 0x7FFFFFFFu) : __vmaxu2(acc, w[i] & 0x7FFF7FFFu);
+    return acc;
+}
+
 // Magnitudes as unsigned numbers: NaN above infinity above what is finite.
 __device__ __forceinline__ uint32_t magnitude_key(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+
+template <int DT>
+__device__ __forceinline__ uint32_t folded_key(uint32_t acc)
+{
+    if (DT == FP8_F32) return acc;
+    return magnitude_key(element_value<DT>(max(acc & 0xFFFFu, acc >> 16)));
+}
 
 __device__ __forceinline__ float warp_sum(float v)
 {
