@@ -264,22 +264,6 @@ __device__ __forceinline__ int64_t load_index(const void *p, int it, int64_t i)
     return it == FP8_I64 ? static_cast<const int64_t *>(p)[i] : static_cast<const int32_t *>(p)[i];
 }
 
-// The largest of a vector's packed elements, folded into two running ones (FP32: one); NaN is passed over.
-template <int DT>
-__device__ __forceinline__ uint32_t max_packed(uint32_t a, uint32_t b)
-{
-    uint32_t r;
-    if (DT == FP8_F32) return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
-    if (DT == FP8_BF16) asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-    else asm("max.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-    return r;
-}
-template <int DT>
-__device__ __forceinline__ float packed_top(uint32_t a)
-{
-    return DT == FP8_F32 ? __uint_as_float(a) : fmaxf(element_value<DT>(a & 0xFFFFu), element_value<DT>(a >> 16));
-}
-
 // A row's vectors in batches of four a thread: whole ones, then what is left.  A batch is on its way while the one before is
 // worked on.  (Ordinary loads: a gradient may be written over its logits.)
 constexpr int kBatch = 4;
@@ -432,6 +416,13 @@ __global__ void __launch_bounds__(T) token_logprobs_kernel(const Logits p, const
     const Row<DT> row(p.x, r * p.ld, from, part_start(p.vocab, blocks, own + 1) - from);
     uint4 raw[kBatch];
     Batches<DT, T>(row).load(0, raw);
+    // the given token's logit, on its way while the row is read
+    int64_t given = -1;
+    float given_logit = 0.0f;
+    if (o.logprob && own == 0 && threadIdx.x == 0) {
+        given = load_index(o.targets, p.it, r);
+        if (given >= 0 && given < p.vocab) given_logit = load1<DT>(p.x, r * p.ld + given);
+    }
     float strip;   // the thread's largest element
     Sums sums = stream_row<DT, T, true>(row, p.c, raw, strip, [](int, uint4 &) {});
     const int edge = row.edge(threadIdx.x);
@@ -450,13 +441,12 @@ __global__ void __launch_bounds__(T) token_logprobs_kernel(const Logits p, const
         if (o.lse) o.lse[r] = none ? -INFINITY : __fmaf_rn(p.scale, sums.m, logsum);
         if (o.saved) reinterpret_cast<float4 *>(o.saved)[r] = make_float4(none ? 0.0f : sums.m, none ? INFINITY : logsum, h, none ? INFINITY : logsum);
         if (o.logprob) {
-            const int64_t t = load_index(o.targets, p.it, r);
             float lp = 0.0f;
-            if (t >= p.vocab) {
+            if (given >= p.vocab) {
                 raise_flags(p.d_status, FP8_FLAG_BAD_INDEX);
                 lp = NAN;
-            } else if (t >= 0) {
-                lp = none ? -INFINITY : p.scale * (load1<DT>(p.x, r * p.ld + t) - sums.m) - logsum;
+            } else if (given >= 0) {
+                lp = none ? -INFINITY : p.scale * (given_logit - sums.m) - logsum;
             }
             o.logprob[r] = lp;
         }
@@ -486,10 +476,11 @@ __global__ void __launch_bounds__(T) token_logprobs_kernel(const Logits p, const
     if (blocks > 1) cluster_sync();   // (no block leaves while another reads its words)
 }
 
-// A row's list: thread i holds entry i.  Entries that count, their q and ln q, the sum Q of all q and the rest's q
-// (zeros where no entry counts).
+// A row's list: thread i holds entry i.  What of it is worked out in one exchange between the warps: q of the entries that
+// count, the sum Q of all q and the rest's q (zeros where no entry counts).
 struct ListEntry {
     int j;        // token, or -1
+    float v;      // its value
     float q, lnq;
     float mass, rest, total;   // sum of q over the list, q of the rest, both
     // no other token can come: what is left goes to none
@@ -504,71 +495,101 @@ __host__ __device__ constexpr int list_words(int vocab) { return (vocab + 7 + 31
 template <int T>
 struct ListShared {
     int index[T];
-    float part[T / 32];
-    double sum[T / 32];
+    double sum[T / 32];   // of q, or of exp(v - top)
+    float top[T / 32];
+    int any[T / 32];      // some entry counts, bit 1: a token came twice
 };
-// Also a bit for each token that is listed: token j at j + shift, so that a vector's bits lie in one word.
+// The entry, and a bit for each token that is listed: token j at j + shift, so that a vector's bits lie in one word.  Complete
+// for all threads after the next barrier.
 template <int T>
-__device__ __forceinline__ ListEntry load_list(const Logits &p, const TeacherList &l, int64_t r, ListShared<T> &sh, uint32_t *bits, int shift)
+__device__ __forceinline__ ListEntry note_list(const Logits &p, const TeacherList &l, int64_t r, ListShared<T> &sh, uint32_t *bits, int shift)
 {
     const int tid = threadIdx.x;
-    for (int i = tid; i < list_words(p.vocab); i += T) bits[i] = 0u;
-    ListEntry e = {-1, 0.0f, -INFINITY, 0.0f, 0.0f, 0.0f};
-    float v = -INFINITY;
+    ListEntry e = {-1, -INFINITY, 0.0f, -INFINITY, 0.0f, 0.0f, 0.0f};
+    int64_t j = -1;
     if (tid < l.listed) {
-        const int64_t j = load_index(l.index, p.it, r * l.ld_index + tid);
-        v = l.value[r * l.ld_value + tid];
-        if (j >= p.vocab) raise_flags(p.d_status, FP8_FLAG_BAD_INDEX);
-        else if (j >= 0) e.j = (int)j;
+        j = load_index(l.index, p.it, r * l.ld_index + tid);
+        e.v = l.value[r * l.ld_value + tid];
     }
+    for (int i = tid; i < list_words(p.vocab); i += T) bits[i] = 0u;
+    if (j >= p.vocab) raise_flags(p.d_status, FP8_FLAG_BAD_INDEX);
+    else if (j >= 0) e.j = (int)j;
     sh.index[tid] = e.j;
-    __syncthreads();   // (the bits are zero)
+    __syncthreads();
     bool again = false;
     if (e.j >= 0) {
         const uint32_t bit = 1u << ((e.j + shift) & 31);
         again = atomicOr(&bits[(e.j + shift) >> 5], bit) & bit;
     }
-    if (!__syncthreads_or(e.j >= 0)) return e;   // nothing listed
-    if (__syncthreads_or(again)) {               // a token that is listed twice: its first entry counts
-        again = false;
-        for (int i = 0; i < tid; ++i) again = again || sh.index[i] == e.j;
-        if (again) e.j = -1;
-    }
-    if (e.j < 0) v = -INFINITY;
-    if (l.rest) {
-        // 1 - sum of q loses what both have in common: in 64 bits
-        double q = e.j >= 0 ? exp((double)v) : 0.0;
-        e.q = (float)q;
-        e.lnq = v;
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) q += __shfl_xor_sync(0xFFFFFFFFu, q, o);
-        if ((tid & 31) == 0) sh.sum[tid >> 5] = q;
-        __syncthreads();
-        q = 0.0;
-        for (int i = 0; i < T / 32; ++i) q += sh.sum[i];
-        const double rest = q >= 1.0 ? 0.0 : 1.0 - q;   // (NaN stays)
-        e.mass = (float)q;
-        e.rest = (float)rest;
-        e.total = (float)(q + rest);
-    } else {
-        float top = v;
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-        if ((tid & 31) == 0) sh.part[tid >> 5] = top;
-        __syncthreads();
-        top = sh.part[0];
-        for (int i = 1; i < T / 32; ++i) top = max_nan(top, sh.part[i]);
-        __syncthreads();
-        const bool none = top == -INFINITY;
-        float q = none ? 0.0f : expf(v - top);
-        const float sum = block_sum<T>(q, sh.part);
-        e.q = none ? 0.0f : q / sum;
-        e.lnq = none ? -INFINITY : (v - top) - logf(sum);
-        e.mass = e.total = none ? 0.0f : sum >= 0.0f ? 1.0f : NAN;
-    }
+    const bool some = __any_sync(0xFFFFFFFFu, e.j >= 0), twice = __any_sync(0xFFFFFFFFu, again);
+    if ((tid & 31) == 0) sh.any[tid >> 5] = (some ? 1 : 0) | (twice ? 2 : 0);
     return e;
 }
-
+// The warp's part of the sums over the list, for `share_list` after the next barrier.
+template <int T>
+__device__ __forceinline__ void sum_list(const TeacherList &l, ListEntry &e, ListShared<T> &sh)
+{
+    // (64 bits: 1 - sum of q loses what both have in common)
+    double sum;
+    float top = 0.0f;
+    const float v = e.j >= 0 ? e.v : -INFINITY;
+    if (l.rest) {
+        sum = e.j >= 0 ? exp((double)v) : 0.0;
+    } else {
+        top = v;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+        sum = e.j >= 0 && top != -INFINITY ? (double)expf(v - top) : 0.0;
+    }
+    e.q = (float)sum;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+    if ((threadIdx.x & 31) == 0) {
+        sh.sum[threadIdx.x >> 5] = sum;
+        sh.top[threadIdx.x >> 5] = top;
+    }
+}
+template <int T>
+__device__ __forceinline__ void share_list(const TeacherList &l, ListEntry &e, ListShared<T> &sh)
+{
+    int any = sh.any[0];
+#pragma unroll
+    for (int i = 1; i < T / 32; ++i) any |= sh.any[i];
+    if (any & 2) {   // a token that is listed twice: its first entry counts, and the sums are taken again
+        bool again = false;
+        for (int i = 0; i < (int)threadIdx.x; ++i) again = again || sh.index[i] == e.j;
+        if (again) e.j = -1;
+        __syncthreads();
+        sum_list<T>(l, e, sh);
+        __syncthreads();
+    }
+    if (!(any & 1)) return;
+    double sum = 0.0;
+    if (l.rest) {
+#pragma unroll
+        for (int i = 0; i < T / 32; ++i) sum += sh.sum[i];
+        const double rest = sum >= 1.0 ? 0.0 : 1.0 - sum;   // (NaN stays)
+        e.lnq = e.v;
+        e.mass = (float)sum;
+        e.rest = (float)rest;
+        e.total = (float)(sum + rest);
+        return;
+    }
+    float top = sh.top[0];
+#pragma unroll
+    for (int i = 1; i < T / 32; ++i) top = max_nan(top, sh.top[i]);
+    if (top == -INFINITY) {   // q = 0 for all
+        e.q = 0.0f;
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < T / 32; ++i)
+        if (sh.top[i] != -INFINITY) sum += sh.sum[i] * (double)expf(sh.top[i] - top);
+    const float all = (float)sum;
+    e.q = e.j >= 0 ? expf(e.v - top) / all : 0.0f;
+    e.lnq = (e.v - top) - logf(all);
+    e.mass = e.total = all >= 0.0f ? 1.0f : NAN;
+}
 template <int DT>
 __device__ __forceinline__ int list_shift(const Row<DT> &row) { return -(row.first + row.head) & (Row<DT>::kVec - 1); }
 // `j`: place in this part of the row
@@ -624,9 +645,9 @@ __global__ void __launch_bounds__(T) distill_kernel(const Logits p, const Teache
     const Row<DT> row(p.x, r * p.ld, from, part_start(p.vocab, blocks, own + 1) - from);
     uint4 raw[kBatch];
     Batches<DT, T>(row).load(0, raw);   // (on their way while the list is worked out)
-    ListEntry e = load_list(p, l, r, sh, listed_bits, list_shift<DT>(row));
-    const bool counts = e.j >= 0;
-    const float x = counts && own == 0 ? load1<DT>(p.x, r * p.ld + e.j) : -INFINITY;
+    ListEntry e = note_list<T>(p, l, r, sh, listed_bits, list_shift<DT>(row));
+    const float x = e.j >= 0 && own == 0 ? load1<DT>(p.x, r * p.ld + e.j) : -INFINITY;
+    __syncthreads();
     // the tokens that are not listed, apart from those that are: neither sum is a difference
     const ListedVectors<DT> listed(listed_bits, row);
     float top;
@@ -637,11 +658,14 @@ __global__ void __launch_bounds__(T) distill_kernel(const Logits p, const Teache
         add_element<false>(sums, y, p.c);
         top = fmaxf(top, y);
     }
-    const Sums others = cluster_join(block_join<T>(sums, top, p.c, part[0]), blocks, p.c, word);
+    if (own == 0) sum_list<T>(l, e, sh);
+    const Sums others = cluster_join(block_join<T>(sums, top, p.c, part[0]), blocks, p.c, word);   // (a barrier)
     if (own == 0) {
+        share_list<T>(l, e, sh);
+        const bool counts = e.j >= 0;   // (of a token that came twice one entry is left)
         sums = no_sums();
         if (counts) add_element<false>(sums, x, p.c);
-        Sums all = block_join<T>(sums, x, p.c, part[1]);
+        Sums all = block_join<T>(sums, counts ? x : -INFINITY, p.c, part[1]);
         const float most = fmaxf(all.m, others.m);
         if (others.s != 0.0f) {
             if (all.s == 0.0f) all = no_sums();
@@ -809,19 +833,22 @@ __global__ void __launch_bounds__(T) distill_bwd_kernel(const Logits p, const Te
         const Row<DT> row(p.x, r * p.ld, from, count);
         uint4 raw[kBatch];
         Batches<DT, T>(row).load(0, raw);   // (on their way while the list is worked out)
-        ListEntry e = load_list(p, l, r, sh, listed_bits, list_shift<DT>(row));
+        ListEntry e = note_list<T>(p, l, r, sh, listed_bits, list_shift<DT>(row));
+        const float x = e.j >= from && e.j < from + count ? row.at(e.j - from) : 0.0f;
+        sum_list<T>(l, e, sh);
+        __syncthreads();   // (also: the gradient may overwrite the logits)
+        share_list<T>(l, e, sh);
         if (keep.w == -INFINITY) e.drop_rest();
         const int own_j = e.j >= from && e.j < from + count ? e.j - from : -1;
         uint32_t own = 0;
         if (own_j >= 0) {
-            const float prob = expf(p.scale * (row.at(own_j) - keep.x) - keep.y);
+            const float prob = expf(p.scale * (x - keep.x) - keep.y);
             own = element_bits<DT>(g * __fmaf_rn(e.total, prob, -e.q));
         }
         // the others: p_j Q, or with s_j = p_j / p_r, s_j (Q p_r - q_r): s_j is one of a sum of 1 however small p_r is
         const float logsum = e.rest == 0.0f ? keep.y : keep.w;
         const float a = e.rest == 0.0f ? e.total : __fmaf_rn(e.total, expf(keep.w - keep.y), -e.rest);
         const ListedVectors<DT> listed(listed_bits, row);
-        __syncthreads();   // (the gradient may overwrite the logits)
         write_row<DT, T, false>(row, raw, o.dx, at, o.same, keep.x, p.c, logsum * kLog2e, g * a, 0.0f, key,
                              [&](int ahead, uint4 &raw) { listed.hide(ahead, raw); },
                              [&](int j) { return is_listed<DT>(listed_bits, row, j); });
@@ -871,13 +898,19 @@ static GradOut make_grad(fp8_ctx *ctx, const void *x, int64_t ld, int dt, void *
     return GradOut{dx, ld_d, same, blocks, {d_amax ? take_slot(ctx) : nullptr, d_amax, nullptr, ctx->d_status, FP8_E5, 0, 0}};
 }
 
-// In how many parts rows are read: as many blocks as give every SM two of them, of 2048 elements at least.
-static int row_blocks(const fp8_ctx *ctx, int64_t rows, int64_t vocab)
+// In how many parts rows are read: as many blocks as give every SM two of them, of 2048 elements at least.  Parts of a
+// forward pass meet once more at the end, which costs more than a shorter last round of blocks gains (4096 rows of 50257: 74, 88
+// and 121 us in one, two and four parts); those of a gradient do not (2048 of 50257: 78, 72, 73 us; 4096 of 32000: 87, 84, 90).
+static int row_blocks(const fp8_ctx *ctx, int64_t rows, int64_t vocab, bool join)
 {
     int blocks = 1;
-    while (blocks < 8 && rows * blocks < (int64_t)ctx->sm_count * 2 && vocab / (2 * blocks) >= 2048) blocks *= 2;
+    while (blocks < 8 && ((rows * blocks < (int64_t)ctx->sm_count * 2 && vocab / (2 * blocks) >= 2048) || (!join && vocab / (2 * blocks) >= 16000)))
+        blocks *= 2;
     return blocks;
 }
+
+// Whether blocks of 128 threads still give an SM 1024.
+static bool many_rows(const fp8_ctx *ctx, int64_t rows, int blocks) { return rows * blocks >= (int64_t)ctx->sm_count * 8; }
 
 // `cluster`: the blocks of a row are one.
 template <typename... KArgs, typename... Args>
@@ -924,8 +957,8 @@ cudaError_t configure_loss_kernels()
     (dt == FP8_BF16  ? FP8LIN_LAUNCH_OF(FP8_BF16, T, KERNEL, __VA_ARGS__)                              \
      : dt == FP8_F16 ? FP8LIN_LAUNCH_OF(FP8_F16, T, KERNEL, __VA_ARGS__)                               \
                      : FP8LIN_LAUNCH_OF(FP8_F32, T, KERNEL, __VA_ARGS__))
-// 128 threads a row: what a row costs beside its elements is paid by warp.  256 where a thread each is needed for more top
-// or listed tokens (top tokens: twice as many strips keep the candidates few).
+// 128 threads a row: what a row costs beside its elements is paid by warp.  256 where there are few rows, or where a thread each
+// is needed for more top or listed tokens (top tokens: twice as many strips keep the candidates few).
 #define FP8LIN_LAUNCH_BY_SIZE(SMALL, KERNEL, ...) \
     ((SMALL) ? FP8LIN_LAUNCH_BY_TYPE(128, KERNEL, __VA_ARGS__) : FP8LIN_LAUNCH_BY_TYPE(256, KERNEL, __VA_ARGS__))
 
@@ -949,8 +982,8 @@ fp8_status_t fp8_token_logprobs(fp8_ctx *ctx, const void *logits, fp8_dtype_t dt
     const OnDevice on(ctx->device);
     const Logits p = make_logits(ctx, logits, ld, rows, vocab, scale, (int)it);
     const TokenOut o = {targets, logprob, entropy, lse, saved, top_logprob, top_index, top_k};
-    const int blocks = row_blocks(ctx, rows, vocab);
-    return FP8LIN_LAUNCH_BY_SIZE(top_k <= 32, token_logprobs_kernel, rows, blocks, true, 0u, stream, p, o, blocks);
+    const int blocks = row_blocks(ctx, rows, vocab, true);
+    return FP8LIN_LAUNCH_BY_SIZE(top_k <= 32 && many_rows(ctx, rows, blocks), token_logprobs_kernel, rows, blocks, true, 0u, stream, p, o, blocks);
 }
 
 fp8_status_t fp8_token_logprobs_bwd(fp8_ctx *ctx, const void *logits, fp8_dtype_t dt, int64_t ld, int64_t rows, int64_t vocab, float scale,
@@ -968,7 +1001,7 @@ fp8_status_t fp8_token_logprobs_bwd(fp8_ctx *ctx, const void *logits, fp8_dtype_
         return FP8_ERR_ALIGN;
     const OnDevice on(ctx->device);
     const Logits p = make_logits(ctx, logits, ld, rows, vocab, scale, (int)it);
-    const int blocks = row_blocks(ctx, rows, vocab);
+    const int blocks = row_blocks(ctx, rows, vocab, false);
     const GradOut o = make_grad(ctx, logits, ld, (int)dt, dlogits, ld_d, d_amax, blocks);
     return FP8LIN_LAUNCH_BY_TYPE(128, token_logprobs_bwd_kernel, rows, blocks, false, 0u, stream, p, targets, saved, g_logprob, g_logprob_stride,
                                  g_entropy, g_entropy_stride, o);
@@ -988,8 +1021,8 @@ fp8_status_t fp8_distill_fwd(fp8_ctx *ctx, const void *logits, fp8_dtype_t dt, i
     const OnDevice on(ctx->device);
     const Logits p = make_logits(ctx, logits, ld, rows, vocab, scale, (int)it);
     const TeacherList l = {index, value, ld_index, ld_value, listed, mode == FP8_DISTILL_REST};
-    const int blocks = row_blocks(ctx, rows, vocab);
-    return FP8LIN_LAUNCH_BY_SIZE(listed <= 128, distill_kernel, rows, blocks, true, list_words((int)vocab) * 4u, stream, p, l, loss, saved, blocks);
+    const int blocks = row_blocks(ctx, rows, vocab, true);
+    return FP8LIN_LAUNCH_BY_SIZE(listed <= 128 && many_rows(ctx, rows, blocks), distill_kernel, rows, blocks, true, list_words((int)vocab) * 4u, stream, p, l, loss, saved, blocks);
 }
 
 fp8_status_t fp8_distill_bwd(fp8_ctx *ctx, const void *logits, fp8_dtype_t dt, int64_t ld, int64_t rows, int64_t vocab, float scale,
@@ -1008,7 +1041,7 @@ fp8_status_t fp8_distill_bwd(fp8_ctx *ctx, const void *logits, fp8_dtype_t dt, i
     const OnDevice on(ctx->device);
     const Logits p = make_logits(ctx, logits, ld, rows, vocab, scale, (int)it);
     const TeacherList l = {index, value, ld_index, ld_value, listed, mode == FP8_DISTILL_REST};
-    const int blocks = row_blocks(ctx, rows, vocab);
+    const int blocks = row_blocks(ctx, rows, vocab, false);
     const GradOut o = make_grad(ctx, logits, ld, (int)dt, dlogits, ld_d, d_amax, blocks);
     return FP8LIN_LAUNCH_BY_SIZE(listed <= 128, distill_bwd_kernel, rows, blocks, false, list_words((int)vocab) * 4u, stream, p, l, saved, g_loss, g_loss_stride, o);
 }

@@ -112,54 +112,105 @@ template <int DT>
 constexpr int kPerVec = DT == FP8_F32 ? 4 : 8;
 template <int TPR>
 constexpr int kRowBlock = TPR < 128 ? 128 : TPR;   // threads of a block: four rows at a time where a warp holds one
+// Blocks that an SM holds at once, which is what the grids are made of: each walks its share of the rows, and a block more
+// than that would walk its share alone at the end.  They are what the registers allow: x and residual of the row behind
+// (FP32: not), the row, and in the backward pass two sums an element.
+template <int DT, int TPR, int EPT>
+constexpr int kFwdResident = TPR == 32 ? (EPT == 8 ? 6 : EPT == 16 ? 5 : 3) : TPR == 256 ? (EPT == 8 ? 4 : 3) : TPR == 512 ? 2 : 1;
+template <int DT, int TPR, int EPT>
+constexpr int kBwdResident = DT == FP8_F32 ? (TPR == 32 ? (EPT == 8 ? 4 : 2) : TPR == 128 ? 5 : TPR == 256 && EPT == 8 ? 2 : 1)
+                                           : (TPR == 32 ? (EPT == 8 ? 5 : 3) : TPR == 128 ? 7 : TPR == 256 ? (EPT == 8 ? 3 : 2) : 1);
 
-// `n` elements of a coefficient vector from col on (16-byte loads), `fill` where there is none.
+// A vector's coefficients from column col on (16-byte loads), `fill` where there are none.
 template <int DT, bool WF32>
-__device__ __forceinline__ void load_coefficients(const void *w, int col, float fill, float (&f)[kPerVec<DT>])
+__device__ __forceinline__ void load_coefficients(const void *w, int col, float fill, Pair (&f)[kVecPairs<DT>])
 {
-    constexpr int kN = kPerVec<DT>;
     if (!w) {
 #pragma unroll
-        for (int i = 0; i < kN; ++i) f[i] = fill;
+        for (int i = 0; i < kVecPairs<DT>; ++i) f[i] = pair_of(fill);
     } else if (WF32) {
 #pragma unroll
-        for (int i = 0; i < kN; i += 4) {
-            const float4 v = __ldg(reinterpret_cast<const float4 *>(static_cast<const float *>(w) + col + i));
-            f[i] = v.x; f[i + 1] = v.y; f[i + 2] = v.z; f[i + 3] = v.w;
+        for (int i = 0; i < kVecPairs<DT>; i += 2) {
+            const float4 v = __ldg(reinterpret_cast<const float4 *>(static_cast<const float *>(w) + col + 2 * i));
+            f[i] = make_pair(v.x, v.y);
+            f[i + 1] = make_pair(v.z, v.w);
         }
     } else {
-        unpack_vector<DT>(__ldg(reinterpret_cast<const uint4 *>(static_cast<const uint8_t *>(w) + (int64_t)col * InType<DT>::kBytes)), f);
+        unpack_pairs<DT>(__ldg(reinterpret_cast<const uint4 *>(static_cast<const uint8_t *>(w) + (int64_t)col * InType<DT>::kBytes)), f);
     }
 }
 
 // y of a vector, rounded to the tensors' type (the operations of `normalised`, in their order)
 template <int DT, bool WF32>
-__device__ __forceinline__ uint4 normalise_vector(const NormFwd &p, const float (&h)[kPerVec<DT>], float mean, float rstd, int col)
+__device__ __forceinline__ uint4 normalise_vector(const NormFwd &p, const Pair (&h)[kVecPairs<DT>], float mean, float rstd, int col)
 {
-    float w[kPerVec<DT>], b[kPerVec<DT>], v[kPerVec<DT>];
+    constexpr int kPairs = kVecPairs<DT>;
+    const Pair less = pair_of(-mean), by = pair_of(rstd);
+    Pair w[kPairs], b[kPairs], v[kPairs];
     load_coefficients<DT, WF32>(p.w, col, 1.0f, w);
     load_coefficients<DT, WF32>(p.b, col, 0.0f, b);
 #pragma unroll
-    for (int i = 0; i < kPerVec<DT>; ++i) v[i] = __fmaf_rn(__fmul_rn(__fsub_rn(h[i], mean), rstd), w[i], b[i]);
-    return pack_vector<DT>(v);
+    for (int i = 0; i < kPairs; ++i) v[i] = fma((h[i] + less) * by, w[i], b[i]);
+    return pack_pairs<DT>(v);
 }
 
-// The E4 bytes of a vector of y, to y8 + at (8 or 4 bytes, aligned).
+// h of a vector: x, or x + residual rounded to the type.
 template <int DT>
-__device__ __forceinline__ void store_bytes(uint8_t *y8, int64_t at, const uint4 &y, Pow2Pair scale, bool &sat)
+__device__ __forceinline__ void sum_vector(const uint4 &x, const uint4 &res, Pair (&h)[kVecPairs<DT>], uint4 &packed)
 {
-    const uint32_t w[4] = {y.x, y.y, y.z, y.w};
-    const uint32_t lo = cast4w<FP8_E4, DT, true>(w, scale, sat);
-    if (DT == FP8_F32) __stcs(reinterpret_cast<uint32_t *>(y8 + at), lo);
-    else __stcs(reinterpret_cast<uint2 *>(y8 + at), make_uint2(lo, cast4w<FP8_E4, DT, true>(w + 2, scale, sat)));
+    Pair f[kVecPairs<DT>];
+    unpack_pairs<DT>(x, h);
+    unpack_pairs<DT>(res, f);
+#pragma unroll
+    for (int i = 0; i < kVecPairs<DT>; ++i) h[i] = h[i] + f[i];
+    packed = pack_pairs<DT>(h);
+    unpack_pairs<DT>(packed, h);
 }
+
+// E4 bytes under one bias; `peak`: the largest magnitudes of y so far (packed), which say whether one was clipped.
+struct ByteScale {
+    float first, second;
+    bool two;   // (uniform: biases beyond what one FP32 power of two holds)
+    __device__ __forceinline__ explicit ByteScale(int shift)
+    {
+        const Pow2Pair p = make_pow2_pair(shift);
+        first = p.first;
+        second = p.second;
+        two = second != 1.0f;
+    }
+    __device__ __forceinline__ float of(float y) const { return y * first * second; }
+    // to y8 + at (8 or 4 bytes, aligned)
+    template <int DT>
+    __device__ __forceinline__ void store(uint8_t *y8, int64_t at, const uint4 &y, uint32_t &peak) const
+    {
+        const uint32_t words[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) peak = max_packed<DT>(peak, words[i] & (DT == FP8_F32 ? 0x7FFFFFFFu : 0x7FFF7FFFu));
+        Pair v[kVecPairs<DT>];
+        uint32_t pairs[4] = {};
+        unpack_pairs<DT>(y, v);
+#pragma unroll
+        for (int i = 0; i < kVecPairs<DT>; ++i) {
+            v[i] = v[i] * pair_of(first);
+            if (two) v[i] = v[i] * pair_of(second);
+            float lo, hi;
+            split(v[i], lo, hi);
+            pairs[i] = cvt_pair<FP8_E4>(hi, lo);
+        }
+        if (DT == FP8_F32) __stcs(reinterpret_cast<uint32_t *>(y8 + at), pairs[0] | (pairs[1] << 16));
+        else __stcs(reinterpret_cast<uint2 *>(y8 + at), make_uint2(pairs[0] | (pairs[1] << 16), pairs[2] | (pairs[3] << 16)));
+    }
+    template <int DT>
+    __device__ __forceinline__ bool clipped(uint32_t peak) const { return clips<FP8_E4>(of(packed_top<DT>(peak))); }
+};
 
 // CLUSTER: the blocks are one cluster that knows the amax when its rows are done, and casts them from shared memory in the
 // same launch.
 template <int DT, bool WF32, int TPR, int EPT, bool CLUSTER>
-__global__ void __launch_bounds__(kRowBlock<TPR>) norm_fwd_rows_kernel(const NormFwd p)
+__global__ void __launch_bounds__(kRowBlock<TPR>, kFwdResident<DT, TPR, EPT>) norm_fwd_rows_kernel(const NormFwd p)
 {
-    constexpr int kN = kPerVec<DT>, kVecs = EPT / kN, kSize = InType<DT>::kBytes, kGroups = kRowBlock<TPR> / TPR;
+    constexpr int kN = kPerVec<DT>, kPairs = kVecPairs<DT>, kVecs = EPT / kN, kSize = InType<DT>::kBytes, kGroups = kRowBlock<TPR> / TPR;
+    constexpr bool kAhead = DT != FP8_F32;
     extern __shared__ __align__(16) uint4 stage[];   // CLUSTER: y of this block's rows
     __shared__ float part[TPR / 32];
     __shared__ float2 part2[2][TPR / 32];
@@ -167,11 +218,9 @@ __global__ void __launch_bounds__(kRowBlock<TPR>) norm_fwd_rows_kernel(const Nor
     const int t = threadIdx.x % TPR, group = threadIdx.x / TPR;
     const int64_t first = (int64_t)blockIdx.x * kGroups + group, step = (int64_t)gridDim.x * kGroups;
     const int row_vecs = p.cols / kN;
-    uint32_t acc = 0;
-    bool sat = false;
+    uint32_t acc = 0, peak = 0;
     const bool bytes = !CLUSTER && p.y8 && p.bias, want_y = CLUSTER || p.y || bytes || p.sink.slot;
-    Pow2Pair scale = {1.0f, 1.0f};
-    if (bytes) scale = make_pow2_pair(*p.bias + p.delta);
+    ByteScale scale(bytes ? *p.bias + p.delta : 0);
     uint4 x[kVecs], res[kVecs];
     auto load = [&](int64_t r) {
         const uint4 *px = reinterpret_cast<const uint4 *>(static_cast<const uint8_t *>(p.x) + r * p.ld_x * kSize);
@@ -183,39 +232,34 @@ __global__ void __launch_bounds__(kRowBlock<TPR>) norm_fwd_rows_kernel(const Nor
             if (p.res) res[i] = __ldcs(pr + t + i * TPR);
         }
     };
-    if (first < p.rows) load(first);
+    if (kAhead && first < p.rows) load(first);
     for (int64_t r = first; r < p.rows; r += step, turn ^= 1) {
-        float h[kVecs][kN], s = 0.0f;
+        if (!kAhead) load(r);
+        Pair h[kVecs][kPairs], s = pair_of(0.0f), d1 = s, d2 = s;
 #pragma unroll
         for (int i = 0; i < kVecs; ++i) {
             if (t + i * TPR >= row_vecs) continue;
-            unpack_vector<DT>(x[i], h[i]);
-            if (p.res) {
-                float f[kN];
-                unpack_vector<DT>(res[i], f);
+            uint4 sum = x[i];
+            if (p.res) sum_vector<DT>(x[i], res[i], h[i], sum);
+            else unpack_pairs<DT>(sum, h[i]);
+            if (p.h) reinterpret_cast<uint4 *>(static_cast<uint8_t *>(p.h) + r * p.ld_h * kSize)[t + i * TPR] = sum;
 #pragma unroll
-                for (int k = 0; k < kN; ++k) f[k] += h[i][k];
-                const uint4 sum = pack_vector<DT>(f);
-                unpack_vector<DT>(sum, h[i]);
-                if (p.h) reinterpret_cast<uint4 *>(static_cast<uint8_t *>(p.h) + r * p.ld_h * kSize)[t + i * TPR] = sum;
-            } else if (p.h) {
-                reinterpret_cast<uint4 *>(static_cast<uint8_t *>(p.h) + r * p.ld_h * kSize)[t + i * TPR] = x[i];
-            }
-#pragma unroll
-            for (int k = 0; k < kN; ++k) s += h[i][k];
+            for (int k = 0; k < kPairs; ++k) s = s + h[i][k];
         }
-        if (r + step < p.rows) load(r + step);   // (while this row is reduced)
-        float mean = p.layer ? block_sum<TPR>(s, part) * p.inv_cols : 0.0f;
-        float2 q = make_float2(0.0f, 0.0f);
+        if (kAhead && r + step < p.rows) load(r + step);   // (while this row is reduced)
+        float mean = p.layer ? block_sum<TPR>(sum_of(s), part) * p.inv_cols : 0.0f;
+        const Pair less = pair_of(-mean);
 #pragma unroll
         for (int i = 0; i < kVecs; ++i) {
             if (t + i * TPR >= row_vecs) continue;
 #pragma unroll
-            for (int k = 0; k < kN; ++k) {
-                const float d = h[i][k] - mean;
-                q = make_float2(q.x + d, __fmaf_rn(d, d, q.y));
+            for (int k = 0; k < kPairs; ++k) {
+                const Pair d = h[i][k] + less;
+                d1 = d1 + d;
+                d2 = fma(d, d, d2);
             }
         }
+        float2 q = make_float2(sum_of(d1), sum_of(d2));
         q = block_sum2<TPR>(q, part2[turn]);
         if (p.layer) {
             q = corrected(mean, q, p.cols, p.inv_cols);
@@ -235,7 +279,7 @@ __global__ void __launch_bounds__(kRowBlock<TPR>) norm_fwd_rows_kernel(const Nor
                 acc = fold_vector<DT>(acc, y);
                 if (p.y) reinterpret_cast<uint4 *>(static_cast<uint8_t *>(p.y) + r * p.ld_y * kSize)[v] = y;
                 if (CLUSTER) stage[((r - first) / gridDim.x + group) * row_vecs + v] = y;
-                if (bytes) store_bytes<DT>(p.y8, r * p.cols + v * kN, y, scale, sat);
+                if (bytes) scale.store<DT>(p.y8, r * p.cols + v * kN, y, peak);
             }
         }
     }
@@ -267,14 +311,14 @@ __global__ void __launch_bounds__(kRowBlock<TPR>) norm_fwd_rows_kernel(const Nor
             *p.sink.d_bias = bias;
             if (flags) raise_flags(p.sink.d_status, flags);
         }
-        scale = make_pow2_pair(bias + p.delta);
+        scale = ByteScale(bias + p.delta);
         for (int64_t r = first; r < p.rows; r += step)
             for (int v = t; v < row_vecs; v += TPR)
-                store_bytes<DT>(p.y8, r * p.cols + v * kN, stage[((r - first) / gridDim.x + group) * row_vecs + v], scale, sat);
+                scale.store<DT>(p.y8, r * p.cols + v * kN, stage[((r - first) / gridDim.x + group) * row_vecs + v], peak);
         __syncwarp();
         if (blocks > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     }
-    if (sat) raise_flags(p.sink.d_status, FP8_FLAG_SATURATED);
+    if (scale.clipped<DT>(peak)) raise_flags(p.sink.d_status, FP8_FLAG_SATURATED);
     if (!CLUSTER) sink_amax(folded_key<DT>(acc), p.sink);
 }
 
@@ -310,23 +354,18 @@ __global__ void __launch_bounds__(kNormThreads) norm_cast_rows_kernel(const Norm
         mean[i] = p.layer ? p.mean[r] : 0.0f;
         rstd[i] = p.rstd[r];
     }
-    const Pow2Pair scale = make_pow2_pair(*p.bias + p.delta);
-    bool sat = false;
+    const ByteScale scale(*p.bias + p.delta);
+    uint32_t peak = 0;
 #pragma unroll
     for (int i = 0; i < kRows; ++i) {
         if (r0 + i >= p.rows) continue;
-        float h[kN];
-        unpack_vector<DT>(x[i], h);
-        if (sum) {
-            float f[kN];
-            unpack_vector<DT>(res[i], f);
-#pragma unroll
-            for (int k = 0; k < kN; ++k) f[k] += h[k];
-            unpack_vector<DT>(pack_vector<DT>(f), h);
-        }
-        store_bytes<DT>(p.y8, (r0 + i) * p.cols + v * kN, normalise_vector<DT, WF32>(p, h, mean[i], rstd[i], v * kN), scale, sat);
+        Pair h[kVecPairs<DT>];
+        uint4 packed;
+        if (sum) sum_vector<DT>(x[i], res[i], h, packed);
+        else unpack_pairs<DT>(x[i], h);
+        scale.store<DT>(p.y8, (r0 + i) * p.cols + v * kN, normalise_vector<DT, WF32>(p, h, mean[i], rstd[i], v * kN), peak);
     }
-    if (sat) raise_flags(p.sink.d_status, FP8_FLAG_SATURATED);
+    if (scale.clipped<DT>(peak)) raise_flags(p.sink.d_status, FP8_FLAG_SATURATED);
 }
 
 struct NormBwd {
@@ -380,9 +419,9 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_any_kernel(const NormBw
 // The same for rows of whole vectors: TPR threads hold a row, and for all rows of a block the sums of their own columns; the
 // next row is on its way while this one is reduced, where the registers allow.
 template <int DT, bool WF32, int TPR, int EPT>
-__global__ void __launch_bounds__(kRowBlock<TPR>) norm_bwd_rows_kernel(const NormBwd p)
+__global__ void __launch_bounds__(kRowBlock<TPR>, kBwdResident<DT, TPR, EPT>) norm_bwd_rows_kernel(const NormBwd p)
 {
-    constexpr int kN = kPerVec<DT>, kVecs = EPT / kN, kSize = InType<DT>::kBytes, kGroups = kRowBlock<TPR> / TPR;
+    constexpr int kN = kPerVec<DT>, kPairs = kVecPairs<DT>, kVecs = EPT / kN, kSize = InType<DT>::kBytes, kGroups = kRowBlock<TPR> / TPR;
     constexpr bool kAhead = TPR * (DT == FP8_F32 ? 2 : 1) <= 512;
     __shared__ float2 part[2][TPR / 32];
     const int t = threadIdx.x % TPR, group = threadIdx.x / TPR;
@@ -390,7 +429,21 @@ __global__ void __launch_bounds__(kRowBlock<TPR>) norm_bwd_rows_kernel(const Nor
     const int row_vecs = p.cols / kN;
     uint32_t acc = 0;
     int turn = 0;
-    float sum_w[kVecs][kN] = {}, sum_b[kVecs][kN] = {};
+    Pair sum_w[kVecs][kPairs], sum_b[kVecs][kPairs];
+    uint4 weight[WF32 ? 1 : kVecs];   // (of the tensors' type: held; FP32: read again for each row)
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+#pragma unroll
+        for (int k = 0; k < kPairs; ++k) sum_w[i][k] = sum_b[i][k] = pair_of(0.0f);
+        if (!WF32 && t + i * TPR < row_vecs) {
+            const uint32_t one = DT == FP8_F32 ? 0x3F800000u : DT == FP8_BF16 ? 0x3F803F80u : 0x3C003C00u;
+            weight[WF32 ? 0 : i] = p.w ? reinterpret_cast<const uint4 *>(p.w)[t + i * TPR] : make_uint4(one, one, one, one);
+        }
+    }
+    auto weights = [&](int i, Pair (&w)[kPairs]) {
+        if (WF32) load_coefficients<DT, WF32>(p.w, (t + i * TPR) * kN, 1.0f, w);
+        else unpack_pairs<DT>(weight[WF32 ? 0 : i], w);
+    };
     uint4 dy[kVecs], h[kVecs], dh[kVecs];
     float mean = 0.0f, rstd = 0.0f;
     auto vectors = [&](const void *q, int64_t r, int64_t ld) {
@@ -415,24 +468,25 @@ __global__ void __launch_bounds__(kRowBlock<TPR>) norm_bwd_rows_kernel(const Nor
         float mean2 = 0.0f, rstd2 = 0.0f;
         if (!kAhead) load(r, dy, h, dh, mean, rstd);
         else if (r + step < p.rows) load(r + step, dy2, h2, dh2, mean2, rstd2);
-        float s1 = 0.0f, s2 = 0.0f;
+        const Pair less = pair_of(-mean), by = pair_of(rstd);
+        Pair p1 = pair_of(0.0f), p2 = p1;
 #pragma unroll
         for (int i = 0; i < kVecs; ++i) {
-            const int v = t + i * TPR;
-            if (v >= row_vecs) continue;
-            float y[kN], x[kN], w[kN];
-            unpack_vector<DT>(dy[i], y);
-            unpack_vector<DT>(h[i], x);
-            load_coefficients<DT, WF32>(p.w, v * kN, 1.0f, w);
+            if (t + i * TPR >= row_vecs) continue;
+            Pair y[kPairs], x[kPairs], w[kPairs];
+            unpack_pairs<DT>(dy[i], y);
+            unpack_pairs<DT>(h[i], x);
+            weights(i, w);
 #pragma unroll
-            for (int k = 0; k < kN; ++k) {
-                const float xh = (x[k] - mean) * rstd, g = y[k] * w[k];
-                s1 += g;
-                s2 = __fmaf_rn(g, xh, s2);
-                sum_w[i][k] = __fmaf_rn(y[k], xh, sum_w[i][k]);
-                sum_b[i][k] += y[k];
+            for (int k = 0; k < kPairs; ++k) {
+                const Pair xh = (x[k] + less) * by, g = y[k] * w[k];
+                p1 = p1 + g;
+                p2 = fma(g, xh, p2);
+                sum_w[i][k] = fma(y[k], xh, sum_w[i][k]);
+                sum_b[i][k] = sum_b[i][k] + y[k];
             }
         }
+        float s1 = sum_of(p1), s2 = sum_of(p2);
         if (p.dx) {
             s1 = warp_sum(s1);
             s2 = warp_sum(s2);
@@ -446,27 +500,24 @@ __global__ void __launch_bounds__(kRowBlock<TPR>) norm_bwd_rows_kernel(const Nor
                     s2 += part[turn][i].y;
                 }
             }
-            const float c1 = p.layer ? s1 * p.inv_cols : 0.0f, c2 = s2 * p.inv_cols;
+            const Pair c1 = pair_of(p.layer ? -s1 * p.inv_cols : 0.0f), c2 = pair_of(-s2 * p.inv_cols);
             uint4 *px = reinterpret_cast<uint4 *>(static_cast<uint8_t *>(p.dx) + r * p.ld_dx * kSize);
 #pragma unroll
             for (int i = 0; i < kVecs; ++i) {
                 const int v = t + i * TPR;
                 if (v >= row_vecs) continue;
-                float y[kN], x[kN], w[kN];
-                unpack_vector<DT>(dy[i], y);
-                unpack_vector<DT>(h[i], x);
-                load_coefficients<DT, WF32>(p.w, v * kN, 1.0f, w);
+                Pair y[kPairs], x[kPairs], w[kPairs];
+                unpack_pairs<DT>(dy[i], y);
+                unpack_pairs<DT>(h[i], x);
+                weights(i, w);
 #pragma unroll
-                for (int k = 0; k < kN; ++k) {
-                    const float xh = (x[k] - mean) * rstd;
-                    y[k] = rstd * (y[k] * w[k] - c1 - xh * c2);
-                }
+                for (int k = 0; k < kPairs; ++k) y[k] = (fma((x[k] + less) * by, c2, y[k] * w[k]) + c1) * by;
                 if (p.dh) {
-                    unpack_vector<DT>(kAhead ? dh[i] : __ldcs(vectors(p.dh, r, p.ld_dh) + v), x);
+                    unpack_pairs<DT>(kAhead ? dh[i] : __ldcs(vectors(p.dh, r, p.ld_dh) + v), x);
 #pragma unroll
-                    for (int k = 0; k < kN; ++k) y[k] += x[k];
+                    for (int k = 0; k < kPairs; ++k) y[k] = y[k] + x[k];
                 }
-                const uint4 out = pack_vector<DT>(y);
+                const uint4 out = pack_pairs<DT>(y);
                 acc = fold_vector<DT>(acc, out);
                 px[v] = out;
             }
@@ -496,8 +547,9 @@ __global__ void __launch_bounds__(kRowBlock<TPR>) norm_bwd_rows_kernel(const Nor
                 if (v >= row_vecs) continue;
 #pragma unroll
                 for (int k = 0; k < kN; k += 4) {
-                    const float(&s)[kN] = which ? sum_b[i] : sum_w[i];
-                    const float4 f = make_float4(s[k], s[k + 1], s[k + 2], s[k + 3]);
+                    float4 f;
+                    split(which ? sum_b[i][k / 2] : sum_w[i][k / 2], f.x, f.y);
+                    split(which ? sum_b[i][k / 2 + 1] : sum_w[i][k / 2 + 1], f.z, f.w);
                     if (kGroups > 1) lines[group][(v * kN + k) / 4] = f;
                     else reinterpret_cast<float4 *>(out)[(v * kN + k) / 4] = f;
                 }
@@ -596,7 +648,7 @@ static cudaError_t launch_fwd_rows(const fp8_ctx *ctx, NormFwd p, bool two, cuda
     }
     const int32_t *bias = p.bias;
     if (two) p.bias = nullptr;
-    const int64_t most = (int64_t)ctx->sm_count * (1024 / kBlock);
+    const int64_t most = (int64_t)ctx->sm_count * kFwdResident<DT, TPR, EPT>;
     count_launch();
     norm_fwd_rows_kernel<DT, WF32, TPR, EPT, false><<<(unsigned)(blocks < most ? blocks : most), kBlock, 0, st>>>(p);
     if (two) {
@@ -691,7 +743,7 @@ static unsigned launch_bwd(const fp8_ctx *ctx, NormBwd p, bool want_w, bool want
     if (fast) {
         by_row_shape<true>(p.cols, [&](auto s) {
             constexpr int kThreads = decltype(s)::kThreads, kBlock = kRowBlock<kThreads>, kGroups = kBlock / kThreads;
-            grid = bwd_blocks(ctx, (p.rows + kGroups - 1) / kGroups, kBlock <= 512 ? 512 / kBlock : 1, sums, p.cols);
+            grid = bwd_blocks(ctx, (p.rows + kGroups - 1) / kGroups, kBwdResident<DT, kThreads, decltype(s)::kElements>, sums, p.cols);
             lines();
             norm_bwd_rows_kernel<DT, WF32, kThreads, decltype(s)::kElements><<<grid, kBlock, 0, st>>>(p);
         });

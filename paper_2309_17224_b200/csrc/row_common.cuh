@@ -73,7 +73,7 @@ __device__ __forceinline__ float load_any(const void *x, int dt, int64_t i)
     return dt == FP8_BF16 ? load1<FP8_BF16>(x, i) : load1<FP8_F16>(x, i);
 }
 
-// A 16-byte vector's elements as floats, and the vector of floats rounded to the type.
+// A 16-byte vector's elements as floats.
 template <int DT, int N>
 __device__ __forceinline__ void unpack_vector(const uint4 &v, float (&f)[N])
 {
@@ -87,21 +87,8 @@ __device__ __forceinline__ void unpack_vector(const uint4 &v, float (&f)[N])
         for (int k = 0; k < 4; ++k) f[i + k] = g[k];
     }
 }
-template <int DT, int N>
-__device__ __forceinline__ uint4 pack_vector(const float (&f)[N])
-{
-    static_assert(N == (DT == FP8_F32 ? 4 : 8), "elements of 16 bytes");
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if (DT == FP8_F32) w[i] = __float_as_uint(f[i]);
-        else if (DT == FP8_BF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(f[(2 * i + 1) % N]), "f"(f[2 * i % N]));
-        else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(f[(2 * i + 1) % N]), "f"(f[2 * i % N]));
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
-}
 
-// Two FP32 numbers a instruction (a register pair).
+// Two FP32 numbers an instruction (a register pair).
 struct Pair {
     unsigned long long v;
 };
@@ -176,6 +163,22 @@ __device__ __forceinline__ uint4 pack_pairs(const Pair (&f)[kVecPairs<DT>])
         }
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// The largest of packed elements; NaN is passed over.
+template <int DT>
+__device__ __forceinline__ uint32_t max_packed(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    if (DT == FP8_F32) return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+    if (DT == FP8_BF16) asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    else asm("max.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+template <int DT>
+__device__ __forceinline__ float packed_top(uint32_t a)
+{
+    return DT == FP8_F32 ? __uint_as_float(a) : fmaxf(element_value<DT>(a & 0xFFFFu), element_value<DT>(a >> 16));
 }
 
 // Largest magnitude of packed elements (as fp8_amax folds them), and its key.
