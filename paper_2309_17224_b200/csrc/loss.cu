@@ -144,7 +144,8 @@ template <int T>
 struct TopShared {
     unsigned long long key[kTopBuffer], best[FP8_LOSS_TOP_MAX];
     uint32_t strip[T];
-    int count;
+    int owner[T];   // strips that reach the bound
+    int count, strips;
     uint32_t bound;
 };
 
@@ -166,14 +167,14 @@ __device__ __forceinline__ void top_rank(TopShared<T> &sh, int n, int k)
 template <int DT, int T>
 __device__ __forceinline__ void find_top(const Row<DT> &row, float m, int k, TopShared<T> &sh)
 {
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x, lane = tid & 31;
     const int edge = row.edge(tid);
     // sixteen bits of the key are enough of a bound
     const uint32_t mine = tid < row.vecs || edge >= 0 ? order_key(m) >> 16 : 0u;
     sh.strip[tid] = mine;
-    if (tid == 0) sh.count = 0;
+    if (tid == 0) sh.count = sh.strips = 0;
     __syncthreads();
-    if (warp == 0) {
+    if (tid < 32) {
         uint32_t own[T / 32], bound = 0;
 #pragma unroll
         for (int i = 0; i < T / 32; ++i) own[i] = sh.strip[lane + 32 * i];
@@ -192,15 +193,26 @@ __device__ __forceinline__ void find_top(const Row<DT> &row, float m, int k, Top
         const int at = atomicAdd(&sh.count, 1);
         if (at < kTopBuffer) sh.key[at] = top_key(x, j);
     };
-    unsigned flagged = __ballot_sync(0xFFFFFFFFu, mine >= bound);
-    while (flagged) {
-        const int owner = (warp << 5) + __ffs(flagged) - 1;
-        flagged &= flagged - 1;
-        for (int v = owner + lane * T; v < row.vecs; v += 32 * T) {
-            float f[Row<DT>::kVec];
-            unpack_vector<DT>(__ldg(row.vectors() + v), f);
+    // all vectors of the strips that reach the bound, four a thread on their way
+    if (mine >= bound) sh.owner[atomicAdd(&sh.strips, 1)] = tid;
+    __syncthreads();
+    const int length = (row.vecs + T - 1) / T, items = sh.strips * length;
+    for (int at = tid; at < items; at += 4 * T) {
+        uint4 raw[4];
+        int v[4];
 #pragma unroll
-            for (int i = 0; i < Row<DT>::kVec; ++i) offer(f[i], row.first + row.head + v * Row<DT>::kVec + i);
+        for (int u = 0; u < 4; ++u) {
+            const int item = at + u * T;
+            v[u] = item < items ? sh.owner[item / length] + item % length * T : row.vecs;
+            if (v[u] < row.vecs) raw[u] = row.vectors()[v[u]];
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (v[u] >= row.vecs) continue;
+            float f[Row<DT>::kVec];
+            unpack_vector<DT>(raw[u], f);
+#pragma unroll
+            for (int i = 0; i < Row<DT>::kVec; ++i) offer(f[i], row.first + row.head + v[u] * Row<DT>::kVec + i);
         }
     }
     if (edge >= 0) offer(row.at(edge), row.first + edge);
@@ -406,7 +418,7 @@ __device__ __forceinline__ Sums cluster_join(Sums own, int blocks, float c, floa
 }
 
 template <int DT, int T>
-__global__ void __launch_bounds__(T) token_logprobs_kernel(const Logits p, const TokenOut o, int blocks)
+__global__ void __launch_bounds__(T, 1024 / T) token_logprobs_kernel(const Logits p, const TokenOut o, int blocks)
 {
     __shared__ TopShared<T> top;
     __shared__ JoinShared<T> part;

@@ -2,6 +2,7 @@
 // backward.
 #include "fp8_norm.h"
 #include "kv_common.cuh"
+#include "ptx.cuh"
 #include "row_common.cuh"
 
 namespace fp8lin {
@@ -112,14 +113,73 @@ template <int DT>
 constexpr int kPerVec = DT == FP8_F32 ? 4 : 8;
 template <int TPR>
 constexpr int kRowBlock = TPR < 128 ? 128 : TPR;   // threads of a block: four rows at a time where a warp holds one
-// Blocks that an SM holds at once, which is what the grids are made of: each walks its share of the rows, and a block more
-// than that would walk its share alone at the end.  They are what the registers allow: x and residual of the row behind
-// (FP32: not), the row, and in the backward pass two sums an element.
-template <int DT, int TPR, int EPT>
-constexpr int kFwdResident = TPR == 32 ? (EPT == 8 ? 6 : EPT == 16 ? 5 : 3) : TPR == 256 ? (EPT == 8 ? 4 : 3) : TPR == 512 ? 2 : 1;
-template <int DT, int TPR, int EPT>
-constexpr int kBwdResident = DT == FP8_F32 ? (TPR == 32 ? (EPT == 8 ? 4 : 2) : TPR == 128 ? 5 : TPR == 256 && EPT == 8 ? 2 : 1)
-                                           : (TPR == 32 ? (EPT == 8 ? 5 : 3) : TPR == 128 ? 7 : TPR == 256 ? (EPT == 8 ? 3 : 2) : 1);
+// Blocks that an SM's registers hold at once, which the grids are made of (as far as shared memory allows): each walks its
+// share of the rows, and a block more than that would walk its share alone at the end.
+template <int TPR, int EPT, bool SUMS>
+constexpr int kResident = SUMS ? (TPR == 32 ? (EPT == 8 ? 6 : EPT == 16 ? 5 : 3) : TPR == 128 ? (EPT == 16 ? 5 : 3) : TPR == 256 ? 2 : 1)
+                               : (TPR == 32 ? (EPT == 8 ? 8 : EPT == 16 ? 6 : 4) : TPR == 128 ? (EPT == 16 ? 6 : 4) : TPR == 256 ? 2 : 1);
+
+// The launch behind may start when no block of this one waits for a place any more; it waits for this one's end itself.
+__device__ __forceinline__ void launch_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_launch_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+// The rows that a group of TPR threads walks, on their way into shared memory `depth` rows ahead: bulk copies that one thread
+// starts.  Neither registers nor a barrier wait for the memory, and a row's 32 elements a thread leave time for little else.
+constexpr int kMostAhead = 4;
+template <int TPR>
+struct RowRing {
+    static constexpr int kGroups = kRowBlock<TPR> / TPR;
+    uint64_t full[kGroups][kMostAhead];
+    int abort_flag;
+};
+struct RowSource {
+    const uint8_t *base[3];   // rows, NULL for one that is not there
+    int64_t stride[3];        // in bytes
+    uint32_t row_bytes;
+    int inputs;               // of the three, those that are there
+};
+template <int TPR>
+struct RowWalk {
+    const RowSource &src;
+    RowRing<TPR> &ring;
+    uint8_t *slots;           // this group's
+    uint32_t slot_bytes;
+    int depth, group;
+    unsigned *d_status;
+    __device__ __forceinline__ RowWalk(const RowSource &s, RowRing<TPR> &r, uint8_t *smem, int ahead, unsigned *status)
+        : src(s), ring(r), slot_bytes(s.row_bytes * s.inputs), depth(ahead), group(threadIdx.x / TPR), d_status(status)
+    {
+        slots = smem + (uint64_t)group * depth * slot_bytes;
+        if (threadIdx.x == 0) {
+            for (int g = 0; g < RowRing<TPR>::kGroups; ++g)
+                for (int i = 0; i < kMostAhead; ++i) mbar_init(smem_u32(&ring.full[g][i]), 1);
+            ring.abort_flag = 0;
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        }
+        __syncthreads();
+    }
+    // one thread of the group: row r into slot s
+    __device__ __forceinline__ void start(int64_t r, int s) const
+    {
+        const uint32_t bar = smem_u32(&ring.full[group][s]);
+        uint32_t to = smem_u32(slots + s * slot_bytes);
+        mbar_expect_tx(bar, slot_bytes);
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+            if (!src.base[i]) continue;
+            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to),
+                         "l"(src.base[i] + r * src.stride[i]), "r"(src.row_bytes), "r"(bar)
+                         : "memory");
+            to += src.row_bytes;
+        }
+    }
+    // (a wait that runs out raises the flag; the walk goes on with what is there, without waiting again)
+    __device__ __forceinline__ const uint4 *wait(int s, uint32_t parity) const
+    {
+        mbar_wait(smem_u32(&ring.full[group][s]), parity, &ring.abort_flag, d_status);
+        return reinterpret_cast<const uint4 *>(slots + s * slot_bytes);
+    }
+};
 
 // A vector's coefficients from column col on (16-byte loads), `fill` where there are none.
 template <int DT, bool WF32>
@@ -141,17 +201,23 @@ __device__ __forceinline__ void load_coefficients(const void *w, int col, float 
 }
 
 // y of a vector, rounded to the tensors' type (the operations of `normalised`, in their order)
+template <int DT>
+__device__ __forceinline__ uint4 normalise_vector(const Pair (&h)[kVecPairs<DT>], float mean, float rstd, const Pair (&w)[kVecPairs<DT>],
+                                                  const Pair (&b)[kVecPairs<DT>])
+{
+    const Pair less = pair_of(-mean), by = pair_of(rstd);
+    Pair v[kVecPairs<DT>];
+#pragma unroll
+    for (int i = 0; i < kVecPairs<DT>; ++i) v[i] = fma((h[i] + less) * by, w[i], b[i]);
+    return pack_pairs<DT>(v);
+}
 template <int DT, bool WF32>
 __device__ __forceinline__ uint4 normalise_vector(const NormFwd &p, const Pair (&h)[kVecPairs<DT>], float mean, float rstd, int col)
 {
-    constexpr int kPairs = kVecPairs<DT>;
-    const Pair less = pair_of(-mean), by = pair_of(rstd);
-    Pair w[kPairs], b[kPairs], v[kPairs];
+    Pair w[kVecPairs<DT>], b[kVecPairs<DT>];
     load_coefficients<DT, WF32>(p.w, col, 1.0f, w);
     load_coefficients<DT, WF32>(p.b, col, 0.0f, b);
-#pragma unroll
-    for (int i = 0; i < kPairs; ++i) v[i] = fma((h[i] + less) * by, w[i], b[i]);
-    return pack_pairs<DT>(v);
+    return normalise_vector<DT>(h, mean, rstd, w, b);
 }
 
 // h of a vector: x, or x + residual rounded to the type.
@@ -204,71 +270,167 @@ struct ByteScale {
     __device__ __forceinline__ bool clipped(uint32_t peak) const { return clips<FP8_E4>(of(packed_top<DT>(peak))); }
 };
 
-// CLUSTER: the blocks are one cluster that knows the amax when its rows are done, and casts them from shared memory in the
-// same launch.
-template <int DT, bool WF32, int TPR, int EPT, bool CLUSTER>
-__global__ void __launch_bounds__(kRowBlock<TPR>, kFwdResident<DT, TPR, EPT>) norm_fwd_rows_kernel(const NormFwd p)
+// From a row's elements and the first estimate of its mean: mean and 1 / standard deviation.  `left`: row_vecs - t.
+template <int TPR, int VECS, int PAIRS>
+__device__ __forceinline__ void row_statistics(const NormFwd &p, const Pair (&h)[VECS][PAIRS], int left, float &mean, float &rstd, float2 *part)
+{
+    const Pair less = pair_of(-mean);
+    Pair d1 = pair_of(0.0f), d2 = d1;
+#pragma unroll
+    for (int i = 0; i < VECS; ++i) {
+        if (i * TPR >= left) continue;
+#pragma unroll
+        for (int k = 0; k < PAIRS; ++k) {
+            const Pair d = h[i][k] + less;
+            d1 = d1 + d;
+            d2 = fma(d, d, d2);
+        }
+    }
+    float2 q = block_sum2<TPR>(make_float2(sum_of(d1), sum_of(d2)), part);
+    if (p.layer) {
+        q = corrected(mean, q, p.cols, p.inv_cols);
+        mean = q.x;
+    }
+    rstd = 1.0f / sqrtf(__fmaf_rn(q.y, p.inv_cols, p.eps));
+}
+
+// Few rows whose bytes are wanted: the blocks are one cluster that knows the amax when its rows are done, and casts them from
+// shared memory in the same launch.
+template <int DT, bool WF32, int TPR, int EPT>
+__global__ void __launch_bounds__(kRowBlock<TPR>) norm_fwd_cluster_kernel(const NormFwd p)
 {
     constexpr int kN = kPerVec<DT>, kPairs = kVecPairs<DT>, kVecs = EPT / kN, kSize = InType<DT>::kBytes, kGroups = kRowBlock<TPR> / TPR;
-    constexpr bool kAhead = DT != FP8_F32;
-    extern __shared__ __align__(16) uint4 stage[];   // CLUSTER: y of this block's rows
+    extern __shared__ __align__(16) uint4 stage[];   // y of this block's rows
     __shared__ float part[TPR / 32];
     __shared__ float2 part2[2][TPR / 32];
+    __shared__ uint32_t block_key;
     int turn = 0;
     const int t = threadIdx.x % TPR, group = threadIdx.x / TPR;
     const int64_t first = (int64_t)blockIdx.x * kGroups + group, step = (int64_t)gridDim.x * kGroups;
     const int row_vecs = p.cols / kN;
-    uint32_t acc = 0, peak = 0;
-    const bool bytes = !CLUSTER && p.y8 && p.bias, want_y = CLUSTER || p.y || bytes || p.sink.slot;
-    ByteScale scale(bytes ? *p.bias + p.delta : 0);
-    uint4 x[kVecs], res[kVecs];
-    auto load = [&](int64_t r) {
+    uint32_t acc = 0;
+    if (threadIdx.x == 0) block_key = 0u;
+    for (int64_t r = first; r < p.rows; r += step, turn ^= 1) {
         const uint4 *px = reinterpret_cast<const uint4 *>(static_cast<const uint8_t *>(p.x) + r * p.ld_x * kSize);
         const uint4 *pr = reinterpret_cast<const uint4 *>(static_cast<const uint8_t *>(p.res) + r * p.ld_res * kSize);
+        uint4 *ph = reinterpret_cast<uint4 *>(static_cast<uint8_t *>(p.h) + r * p.ld_h * kSize);
+        Pair h[kVecs][kPairs], s = pair_of(0.0f);
+        uint4 x[kVecs], res[kVecs];
 #pragma unroll
         for (int i = 0; i < kVecs; ++i) {
             if (t + i * TPR >= row_vecs) continue;
-            x[i] = __ldcs(px + t + i * TPR);
-            if (p.res) res[i] = __ldcs(pr + t + i * TPR);
+            x[i] = px[t + i * TPR];
+            if (p.res) res[i] = pr[t + i * TPR];
         }
-    };
-    if (kAhead && first < p.rows) load(first);
-    for (int64_t r = first; r < p.rows; r += step, turn ^= 1) {
-        if (!kAhead) load(r);
-        Pair h[kVecs][kPairs], s = pair_of(0.0f), d1 = s, d2 = s;
 #pragma unroll
         for (int i = 0; i < kVecs; ++i) {
             if (t + i * TPR >= row_vecs) continue;
-            uint4 sum = x[i];
-            if (p.res) sum_vector<DT>(x[i], res[i], h[i], sum);
-            else unpack_pairs<DT>(sum, h[i]);
-            if (p.h) reinterpret_cast<uint4 *>(static_cast<uint8_t *>(p.h) + r * p.ld_h * kSize)[t + i * TPR] = sum;
+            if (p.res) sum_vector<DT>(x[i], res[i], h[i], x[i]);
+            else unpack_pairs<DT>(x[i], h[i]);
+            if (p.h) ph[t + i * TPR] = x[i];
 #pragma unroll
             for (int k = 0; k < kPairs; ++k) s = s + h[i][k];
         }
-        if (kAhead && r + step < p.rows) load(r + step);   // (while this row is reduced)
-        float mean = p.layer ? block_sum<TPR>(sum_of(s), part) * p.inv_cols : 0.0f;
-        const Pair less = pair_of(-mean);
-#pragma unroll
-        for (int i = 0; i < kVecs; ++i) {
-            if (t + i * TPR >= row_vecs) continue;
-#pragma unroll
-            for (int k = 0; k < kPairs; ++k) {
-                const Pair d = h[i][k] + less;
-                d1 = d1 + d;
-                d2 = fma(d, d, d2);
-            }
-        }
-        float2 q = make_float2(sum_of(d1), sum_of(d2));
-        q = block_sum2<TPR>(q, part2[turn]);
-        if (p.layer) {
-            q = corrected(mean, q, p.cols, p.inv_cols);
-            mean = q.x;
-        }
-        const float rstd = 1.0f / sqrtf(__fmaf_rn(q.y, p.inv_cols, p.eps));
+        float mean = p.layer ? block_sum<TPR>(sum_of(s), part) * p.inv_cols : 0.0f, rstd;
+        row_statistics<TPR, kVecs, kPairs>(p, h, row_vecs - t, mean, rstd, part2[turn]);
         if (t == 0) {
             if (p.mean) p.mean[r] = mean;
             if (p.rstd) p.rstd[r] = rstd;
+        }
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) {
+            const int v = t + i * TPR;
+            if (v >= row_vecs) continue;
+            const uint4 y = normalise_vector<DT, WF32>(p, h[i], mean, rstd, v * kN);
+            acc = fold_vector<DT>(acc, y);
+            if (p.y) reinterpret_cast<uint4 *>(static_cast<uint8_t *>(p.y) + r * p.ld_y * kSize)[v] = y;
+            stage[((r - first) / gridDim.x + group) * row_vecs + v] = y;
+        }
+    }
+    const unsigned blocks = gridDim.x;
+    uint32_t key = __reduce_max_sync(0xFFFFFFFFu, folded_key<DT>(acc));
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) atomicMax(&block_key, key);
+    __syncthreads();
+    key = block_key;
+    if (blocks > 1) {
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        for (unsigned b = 0; b < blocks; ++b) {
+            uint32_t remote, other;
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(smem_u32(&block_key)), "r"(b));
+            asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(other) : "r"(remote) : "memory");
+            key = max(key, other);
+        }
+        // (no block leaves while another reads its word)
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    }
+    unsigned flags = 0;
+    const int bias = bias_from_amax_bits(key, FP8_E4, p.sink.conv, p.sink.margin, &flags);
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        if (p.sink.d_amax) *p.sink.d_amax = __uint_as_float(key);
+        *p.sink.d_bias = bias;
+        if (flags) raise_flags(p.sink.d_status, flags);
+    }
+    const ByteScale scale(bias + p.delta);
+    uint32_t peak = 0;
+    for (int64_t r = first; r < p.rows; r += step)
+        for (int v = t; v < row_vecs; v += TPR)
+            scale.store<DT>(p.y8, r * p.cols + v * kN, stage[((r - first) / gridDim.x + group) * row_vecs + v], peak);
+    if (scale.clipped<DT>(peak)) raise_flags(p.sink.d_status, FP8_FLAG_SATURATED);
+    __syncwarp();
+    if (blocks > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// Any number of rows: one reading, whatever is asked for but bytes under a bias that the call itself finds.  Bound by the memory
+// where a row's fixed cost (two sums over its threads, 150 instructions a thread) meets 32 elements a thread; with 16 it was
+// bound by its instructions.
+template <int DT, bool WF32, int TPR, int EPT>
+__global__ void __launch_bounds__(kRowBlock<TPR>, kResident<TPR, EPT, false>) norm_fwd_rows_kernel(const NormFwd p, const RowSource src, int depth)
+{
+    constexpr int kN = kPerVec<DT>, kPairs = kVecPairs<DT>, kVecs = EPT / kN, kSize = InType<DT>::kBytes, kGroups = kRowBlock<TPR> / TPR;
+    extern __shared__ __align__(16) uint8_t slots[];
+    __shared__ RowRing<TPR> ring;
+    __shared__ float part[TPR / 32];
+    __shared__ float2 part2[2][TPR / 32];
+    launch_next();
+    const RowWalk<TPR> walk(src, ring, slots, depth, p.sink.d_status);
+    const int t = threadIdx.x % TPR, group = threadIdx.x / TPR;
+    const int64_t step = (int64_t)gridDim.x * kGroups;
+    const int row_vecs = p.cols / kN;
+    uint32_t acc = 0, peak = 0, parity = 0;
+    int slot = 0, turn = 0;
+    const bool bytes = p.y8 && p.bias, want_y = p.y || bytes || p.sink.slot;
+    const ByteScale scale(bytes ? *p.bias + p.delta : 0);
+    int64_t r = (int64_t)blockIdx.x * kGroups + group;
+    if (t == 0)
+        for (int i = 0; i < depth && r + i * step < p.rows; ++i) walk.start(r + i * step, i);
+    for (; r < p.rows; r += step, turn ^= 1) {
+        const uint4 *in = walk.wait(slot, parity);
+        Pair h[kVecs][kPairs], s = pair_of(0.0f);
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) {
+            const int v = t + i * TPR;
+            if (v >= row_vecs) continue;
+            uint4 x = in[v];
+            if (p.res) sum_vector<DT>(x, in[row_vecs + v], h[i], x);
+            else unpack_pairs<DT>(x, h[i]);
+            if (p.h) reinterpret_cast<uint4 *>(static_cast<uint8_t *>(p.h) + r * p.ld_h * kSize)[v] = x;
+#pragma unroll
+            for (int k = 0; k < kPairs; ++k) s = s + h[i][k];
+        }
+        float mean = p.layer ? block_sum<TPR>(sum_of(s), part) * p.inv_cols : 0.0f, rstd;
+        row_statistics<TPR, kVecs, kPairs>(p, h, row_vecs - t, mean, rstd, part2[turn]);
+        // every thread has read its part of the slot (a barrier, or the warp's exchange, lies behind it)
+        if (TPR == 32) __syncwarp();
+        if (t == 0) {
+            if (r + depth * step < p.rows) walk.start(r + depth * step, slot);
+            if (p.mean) p.mean[r] = mean;
+            if (p.rstd) p.rstd[r] = rstd;
+        }
+        if (++slot == depth) {
+            slot = 0;
+            parity ^= 1u;
         }
         if (want_y) {
 #pragma unroll
@@ -278,92 +440,67 @@ __global__ void __launch_bounds__(kRowBlock<TPR>, kFwdResident<DT, TPR, EPT>) no
                 const uint4 y = normalise_vector<DT, WF32>(p, h[i], mean, rstd, v * kN);
                 acc = fold_vector<DT>(acc, y);
                 if (p.y) reinterpret_cast<uint4 *>(static_cast<uint8_t *>(p.y) + r * p.ld_y * kSize)[v] = y;
-                if (CLUSTER) stage[((r - first) / gridDim.x + group) * row_vecs + v] = y;
                 if (bytes) scale.store<DT>(p.y8, r * p.cols + v * kN, y, peak);
             }
         }
     }
-    if (CLUSTER) {
-        const unsigned blocks = gridDim.x;
-        __shared__ uint32_t block_key;
-        uint32_t key = __reduce_max_sync(0xFFFFFFFFu, folded_key<DT>(acc));
-        if (threadIdx.x == 0) block_key = 0u;
-        __syncthreads();
-        if ((threadIdx.x & 31) == 0) atomicMax(&block_key, key);
-        __syncthreads();
-        key = block_key;
-        if (blocks > 1) {
-            asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-            asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-            for (unsigned b = 0; b < blocks; ++b) {
-                uint32_t remote, other;
-                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(smem_u32(&block_key)), "r"(b));
-                asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(other) : "r"(remote) : "memory");
-                key = max(key, other);
-            }
-            // (no block leaves while another reads its word)
-            asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-        }
-        unsigned flags = 0;
-        const int bias = bias_from_amax_bits(key, FP8_E4, p.sink.conv, p.sink.margin, &flags);
-        if (blockIdx.x == 0 && threadIdx.x == 0) {
-            if (p.sink.d_amax) *p.sink.d_amax = __uint_as_float(key);
-            *p.sink.d_bias = bias;
-            if (flags) raise_flags(p.sink.d_status, flags);
-        }
-        scale = ByteScale(bias + p.delta);
-        for (int64_t r = first; r < p.rows; r += step)
-            for (int v = t; v < row_vecs; v += TPR)
-                scale.store<DT>(p.y8, r * p.cols + v * kN, stage[((r - first) / gridDim.x + group) * row_vecs + v], peak);
-        __syncwarp();
-        if (blocks > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-    }
     if (scale.clipped<DT>(peak)) raise_flags(p.sink.d_status, FP8_FLAG_SATURATED);
-    if (!CLUSTER) sink_amax(folded_key<DT>(acc), p.sink);
+    sink_amax(folded_key<DT>(acc), p.sink);
 }
 
-// The bytes of y from the sums and the statistics of the launch before, under the bias that it left: four rows of one vector a
+// The bytes of y from the sums and the statistics of the launch before, under the bias that it left: eight rows of one vector a
 // thread, last rows first (what the launch before wrote last is what L2 holds).
+constexpr int kCastRows = 8;
 template <int DT, bool WF32>
-__global__ void __launch_bounds__(kNormThreads) norm_cast_rows_kernel(const NormFwd p)
+__global__ void __launch_bounds__(kNormThreads, 3) norm_cast_rows_kernel(const NormFwd p)
 {
-    constexpr int kN = kPerVec<DT>, kSize = InType<DT>::kBytes, kRows = 4;
+    constexpr int kN = kPerVec<DT>, kPairs = kVecPairs<DT>, kSize = InType<DT>::kBytes, kHalf = kCastRows / 2;
     const unsigned row_vecs = p.cols / kN;
     const uint64_t at = (uint64_t)(gridDim.x - 1 - blockIdx.x) * kNormThreads + threadIdx.x;
     int64_t r0;
     int v;
     if (gridDim.x < (1u << 24)) {   // (divisions of 32 bits where they do)
-        r0 = (int64_t)((unsigned)at / row_vecs) * kRows;
+        r0 = (int64_t)((unsigned)at / row_vecs) * kCastRows;
         v = (int)((unsigned)at % row_vecs);
     } else {
-        r0 = (int64_t)(at / row_vecs) * kRows;
+        r0 = (int64_t)(at / row_vecs) * kCastRows;
         v = (int)(at % row_vecs);
     }
     if (r0 >= p.rows) return;
-    uint4 x[kRows], res[kRows];
-    float mean[kRows], rstd[kRows];
     const bool sum = p.res && !p.h;
-    const uint8_t *src = static_cast<const uint8_t *>(p.h ? p.h : p.x);
-    const int64_t ld = p.h ? p.ld_h : p.ld_x;
-#pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-        const int64_t r = r0 + i;
-        if (r >= p.rows) continue;
-        x[i] = __ldcs(reinterpret_cast<const uint4 *>(src + r * ld * kSize) + v);
-        if (sum) res[i] = __ldcs(reinterpret_cast<const uint4 *>(static_cast<const uint8_t *>(p.res) + r * p.ld_res * kSize) + v);
-        mean[i] = p.layer ? p.mean[r] : 0.0f;
-        rstd[i] = p.rstd[r];
-    }
-    const ByteScale scale(*p.bias + p.delta);
+    const int64_t stride = (p.h ? p.ld_h : p.ld_x) * kSize;
+    const uint8_t *src = static_cast<const uint8_t *>(p.h ? p.h : p.x) + r0 * stride + (int64_t)v * 16;
+    const uint8_t *src_res = static_cast<const uint8_t *>(p.res) + r0 * p.ld_res * kSize + (int64_t)v * 16;
+    uint8_t *dst = p.y8 + r0 * p.cols + (int64_t)v * kN;
+    const int rows = (int)min((int64_t)kCastRows, p.rows - r0);
+    Pair w[kPairs], b[kPairs];
+    load_coefficients<DT, WF32>(p.w, v * kN, 1.0f, w);
+    load_coefficients<DT, WF32>(p.b, v * kN, 0.0f, b);
+    wait_for_launch_before();
+    const ByteScale scale(__ldcg(p.bias) + p.delta);
     uint32_t peak = 0;
+    for (int first = 0; first < rows; first += kHalf) {
+        uint4 x[kHalf], res[kHalf];
+        float mean[kHalf], rstd[kHalf];
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-        if (r0 + i >= p.rows) continue;
-        Pair h[kVecPairs<DT>];
-        uint4 packed;
-        if (sum) sum_vector<DT>(x[i], res[i], h, packed);
-        else unpack_pairs<DT>(x[i], h);
-        scale.store<DT>(p.y8, (r0 + i) * p.cols + v * kN, normalise_vector<DT, WF32>(p, h, mean[i], rstd[i], v * kN), peak);
+        for (int i = 0; i < kHalf; ++i) {
+            if (first + i >= rows) continue;
+            x[i] = __ldcs(reinterpret_cast<const uint4 *>(src + i * stride));
+            if (sum) res[i] = __ldcs(reinterpret_cast<const uint4 *>(src_res + i * p.ld_res * kSize));
+            mean[i] = p.layer ? __ldcg(p.mean + r0 + first + i) : 0.0f;
+            rstd[i] = __ldcg(p.rstd + r0 + first + i);
+        }
+#pragma unroll
+        for (int i = 0; i < kHalf; ++i) {
+            if (first + i >= rows) continue;
+            Pair h[kPairs];
+            if (sum) sum_vector<DT>(x[i], res[i], h, x[i]);
+            else unpack_pairs<DT>(x[i], h);
+            scale.store<DT>(dst, (int64_t)i * p.cols, normalise_vector<DT>(h, mean[i], rstd[i], w, b), peak);
+        }
+        src += kHalf * stride;
+        src_res += kHalf * p.ld_res * kSize;
+        dst += (int64_t)kHalf * p.cols;
     }
     if (scale.clipped<DT>(peak)) raise_flags(p.sink.d_status, FP8_FLAG_SATURATED);
 }
@@ -416,19 +553,21 @@ __global__ void __launch_bounds__(kNormThreads) norm_bwd_any_kernel(const NormBw
     sink_amax(key, p.sink);
 }
 
-// The same for rows of whole vectors: TPR threads hold a row, and for all rows of a block the sums of their own columns; the
-// next row is on its way while this one is reduced, where the registers allow.
+// The same for rows of whole vectors: TPR threads hold, for all rows of their block, the sums of their own columns.
 template <int DT, bool WF32, int TPR, int EPT>
-__global__ void __launch_bounds__(kRowBlock<TPR>, kBwdResident<DT, TPR, EPT>) norm_bwd_rows_kernel(const NormBwd p)
+__global__ void __launch_bounds__(kRowBlock<TPR>, kResident<TPR, EPT, true>) norm_bwd_rows_kernel(const NormBwd p, const RowSource src, int depth)
 {
     constexpr int kN = kPerVec<DT>, kPairs = kVecPairs<DT>, kVecs = EPT / kN, kSize = InType<DT>::kBytes, kGroups = kRowBlock<TPR> / TPR;
-    constexpr bool kAhead = TPR * (DT == FP8_F32 ? 2 : 1) <= 512;
+    extern __shared__ __align__(16) uint8_t slots[];
+    __shared__ RowRing<TPR> ring;
     __shared__ float2 part[2][TPR / 32];
+    launch_next();
+    const RowWalk<TPR> walk(src, ring, slots, depth, p.sink.d_status);
     const int t = threadIdx.x % TPR, group = threadIdx.x / TPR;
     const int64_t step = (int64_t)gridDim.x * kGroups;
     const int row_vecs = p.cols / kN;
-    uint32_t acc = 0;
-    int turn = 0;
+    uint32_t acc = 0, parity = 0;
+    int slot = 0, turn = 0;
     Pair sum_w[kVecs][kPairs], sum_b[kVecs][kPairs];
     uint4 weight[WF32 ? 1 : kVecs];   // (of the tensors' type: held; FP32: read again for each row)
 #pragma unroll
@@ -444,38 +583,20 @@ __global__ void __launch_bounds__(kRowBlock<TPR>, kBwdResident<DT, TPR, EPT>) no
         if (WF32) load_coefficients<DT, WF32>(p.w, (t + i * TPR) * kN, 1.0f, w);
         else unpack_pairs<DT>(weight[WF32 ? 0 : i], w);
     };
-    uint4 dy[kVecs], h[kVecs], dh[kVecs];
-    float mean = 0.0f, rstd = 0.0f;
-    auto vectors = [&](const void *q, int64_t r, int64_t ld) {
-        return reinterpret_cast<const uint4 *>(static_cast<const uint8_t *>(q) + r * ld * kSize);
-    };
-    auto load = [&](int64_t r, uint4 (&dy)[kVecs], uint4 (&h)[kVecs], uint4 (&dh)[kVecs], float &mean, float &rstd) {
-        const uint4 *py = vectors(p.dy, r, p.ld_dy), *ph = vectors(p.h, r, p.ld_h), *pd = vectors(p.dh, r, p.ld_dh);
-#pragma unroll
-        for (int i = 0; i < kVecs; ++i) {
-            if (t + i * TPR >= row_vecs) continue;
-            dy[i] = __ldcs(py + t + i * TPR);
-            h[i] = __ldcs(ph + t + i * TPR);
-            if (p.dh && kAhead) dh[i] = __ldcs(pd + t + i * TPR);
-        }
-        mean = p.layer ? p.mean[r] : 0.0f;
-        rstd = p.rstd[r];
-    };
     int64_t r = (int64_t)blockIdx.x * kGroups + group;
-    if (kAhead && r < p.rows) load(r, dy, h, dh, mean, rstd);
-    for (; r < p.rows; r += step, turn ^= 1) {
-        uint4 dy2[kVecs], h2[kVecs], dh2[kVecs];
-        float mean2 = 0.0f, rstd2 = 0.0f;
-        if (!kAhead) load(r, dy, h, dh, mean, rstd);
-        else if (r + step < p.rows) load(r + step, dy2, h2, dh2, mean2, rstd2);
+    if (t == 0)
+        for (int i = 0; i < depth && r + i * step < p.rows; ++i) walk.start(r + i * step, i);
+    for (bool behind = false; r < p.rows; r += step, turn ^= 1, behind = true) {
+        const float mean = p.layer ? p.mean[r] : 0.0f, rstd = p.rstd[r];
+        const uint4 *in = walk.wait(slot, parity);
         const Pair less = pair_of(-mean), by = pair_of(rstd);
         Pair p1 = pair_of(0.0f), p2 = p1;
 #pragma unroll
         for (int i = 0; i < kVecs; ++i) {
             if (t + i * TPR >= row_vecs) continue;
             Pair y[kPairs], x[kPairs], w[kPairs];
-            unpack_pairs<DT>(dy[i], y);
-            unpack_pairs<DT>(h[i], x);
+            unpack_pairs<DT>(in[t + i * TPR], y);
+            unpack_pairs<DT>(in[row_vecs + t + i * TPR], x);
             weights(i, w);
 #pragma unroll
             for (int k = 0; k < kPairs; ++k) {
@@ -486,34 +607,25 @@ __global__ void __launch_bounds__(kRowBlock<TPR>, kBwdResident<DT, TPR, EPT>) no
                 sum_b[i][k] = sum_b[i][k] + y[k];
             }
         }
-        float s1 = sum_of(p1), s2 = sum_of(p2);
+        const float2 s = block_sum2<TPR>(make_float2(sum_of(p1), sum_of(p2)), part[turn]);
+        // every thread is done with the row before (a barrier, or the warp's exchange, lies behind it): its slot is free
+        if (TPR == 32) __syncwarp();
+        if (t == 0 && behind && r + (depth - 1) * step < p.rows) walk.start(r + (depth - 1) * step, slot == 0 ? depth - 1 : slot - 1);
         if (p.dx) {
-            s1 = warp_sum(s1);
-            s2 = warp_sum(s2);
-            if (TPR > 32) {
-                if ((threadIdx.x & 31) == 0) part[turn][threadIdx.x >> 5] = make_float2(s1, s2);
-                __syncthreads();
-                s1 = s2 = 0.0f;
-#pragma unroll
-                for (int i = 0; i < TPR / 32; ++i) {
-                    s1 += part[turn][i].x;
-                    s2 += part[turn][i].y;
-                }
-            }
-            const Pair c1 = pair_of(p.layer ? -s1 * p.inv_cols : 0.0f), c2 = pair_of(-s2 * p.inv_cols);
+            const Pair c1 = pair_of(p.layer ? -s.x * p.inv_cols : 0.0f), c2 = pair_of(-s.y * p.inv_cols);
             uint4 *px = reinterpret_cast<uint4 *>(static_cast<uint8_t *>(p.dx) + r * p.ld_dx * kSize);
 #pragma unroll
             for (int i = 0; i < kVecs; ++i) {
                 const int v = t + i * TPR;
                 if (v >= row_vecs) continue;
                 Pair y[kPairs], x[kPairs], w[kPairs];
-                unpack_pairs<DT>(dy[i], y);
-                unpack_pairs<DT>(h[i], x);
+                unpack_pairs<DT>(in[v], y);
+                unpack_pairs<DT>(in[row_vecs + v], x);
                 weights(i, w);
 #pragma unroll
                 for (int k = 0; k < kPairs; ++k) y[k] = (fma((x[k] + less) * by, c2, y[k] * w[k]) + c1) * by;
                 if (p.dh) {
-                    unpack_pairs<DT>(kAhead ? dh[i] : __ldcs(vectors(p.dh, r, p.ld_dh) + v), x);
+                    unpack_pairs<DT>(in[2 * row_vecs + v], x);
 #pragma unroll
                     for (int k = 0; k < kPairs; ++k) y[k] = y[k] + x[k];
                 }
@@ -522,15 +634,9 @@ __global__ void __launch_bounds__(kRowBlock<TPR>, kBwdResident<DT, TPR, EPT>) no
                 px[v] = out;
             }
         }
-        if (kAhead) {
-#pragma unroll
-            for (int i = 0; i < kVecs; ++i) {
-                dy[i] = dy2[i];
-                h[i] = h2[i];
-                dh[i] = dh2[i];
-            }
-            mean = mean2;
-            rstd = rstd2;
+        if (++slot == depth) {
+            slot = 0;
+            parity ^= 1u;
         }
     }
     if (p.part_w || p.part_b) {
@@ -570,26 +676,37 @@ __global__ void __launch_bounds__(kRowBlock<TPR>, kBwdResident<DT, TPR, EPT>) no
     sink_amax(folded_key<DT>(acc), p.sink);
 }
 
-// Sums of the blocks' lines, in their order: 32 columns a block, eight lines at a time.
-__global__ void __launch_bounds__(256) norm_bwd_sum_kernel(const float *part_w, const float *part_b, int lines, int cols, int w_dt,
-                                                           void *dw, void *db)
+// Sums of the blocks' lines, in one order: 32 columns a block, 32 lines at a time, eight of a thread's on their way.
+constexpr int kSumThreads = 1024;
+__global__ void __launch_bounds__(kSumThreads) norm_bwd_sum_kernel(const float *part_w, const float *part_b, int lines, int cols, int w_dt,
+                                                                   void *dw, void *db, int chunks)
 {
-    __shared__ float sums[8][33];
-    const int lane = threadIdx.x & 31, group = threadIdx.x >> 5, j = blockIdx.x * 32 + lane;
-    const float *part = blockIdx.y ? part_b : part_w;
-    void *out = blockIdx.y ? db : dw;
+    __shared__ float sums[32][33];
+    const int lane = threadIdx.x & 31, group = threadIdx.x >> 5;
+    const bool second = (int)blockIdx.x >= chunks;
+    const int j = ((int)blockIdx.x - (second ? chunks : 0)) * 32 + lane;
+    const float *part = (second ? part_b : part_w) + j;
+    void *out = second ? db : dw;
     if (!out) return;
+    wait_for_launch_before();
     float s = 0.0f;
-    if (j < cols)
-        for (int i = group; i < lines; i += 8) s += part[(int64_t)i * cols + j];
+    if (j < cols) {
+        for (int i = group; i < lines; i += 8 * 32) {
+            float v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = i + k * 32 < lines ? __ldcg(part + (int64_t)(i + k * 32) * cols) : 0.0f;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) s += v[k];
+        }
+    }
     sums[group][lane] = s;
     __syncthreads();
-    if (group != 0 || j >= cols) return;
-#pragma unroll
-    for (int i = 1; i < 8; ++i) s += sums[i][lane];
-    if (w_dt == FP8_F32) store_bits<FP8_F32>(out, j, element_bits<FP8_F32>(s));
-    else if (w_dt == FP8_BF16) store_bits<FP8_BF16>(out, j, element_bits<FP8_BF16>(s));
-    else store_bits<FP8_F16>(out, j, element_bits<FP8_F16>(s));
+    s = warp_sum(sums[lane][group]);
+    const int column = j - lane + group;
+    if (lane != 0 || column >= cols) return;
+    if (w_dt == FP8_F32) store_bits<FP8_F32>(out, column, element_bits<FP8_F32>(s));
+    else if (w_dt == FP8_BF16) store_bits<FP8_BF16>(out, column, element_bits<FP8_BF16>(s));
+    else store_bits<FP8_F16>(out, column, element_bits<FP8_F16>(s));
 }
 
 static unsigned blocks_for_rows(const fp8_ctx *ctx, int64_t rows, int per_sm)
@@ -604,81 +721,112 @@ struct RowHold {
     static constexpr int kThreads = TPR, kElements = EPT;
 };
 constexpr int kMostHeld = 16384;
-// A warp per row as long as 32 elements a lane hold it (SUMS: the backward pass, which holds two sums beside each element;
-// 16), then as few threads as 16 elements a thread allow.
-template <bool SUMS, typename F>
+// A warp per row as long as 32 elements a lane hold it, then as few threads as that allow.  All kernels for whole rows share the
+// shapes, so that a row's sums are taken in one order, whatever is asked for and however many rows there are.
+template <typename F>
 static void by_row_shape(int cols, F f)
 {
     if (cols <= 256) f(RowHold<32, 8>{});
     else if (cols <= 512) f(RowHold<32, 16>{});
-    else if (cols <= 1024) f(RowHold<SUMS ? 128 : 32, SUMS ? 8 : 32>{});
-    else if (cols <= 2048) f(RowHold<256, 8>{});
-    else if (cols <= 4096) f(RowHold<256, 16>{});
-    else if (cols <= 8192) f(RowHold<512, 16>{});
-    else f(RowHold<1024, 16>{});
+    else if (cols <= 1024) f(RowHold<32, 32>{});
+    else if (cols <= 2048) f(RowHold<128, 16>{});
+    else if (cols <= 4096) f(RowHold<128, 32>{});
+    else if (cols <= 8192) f(RowHold<256, 32>{});
+    else f(RowHold<512, 32>{});
 }
+// Blocks an SM, and rows on their way for each group, that shared memory allows; false where not two rows fit.
+static bool ring_size(int most_blocks, int groups, int64_t slot, int &blocks, int &depth)
+{
+    for (blocks = most_blocks; blocks > 0; --blocks) {
+        const int64_t each = (227 << 10) / blocks - 2048 - (blocks > 1 ? 1024 : 0);   // (beside the fixed part)
+        depth = (int)(each / (groups * slot));
+        if (depth > kMostAhead) depth = kMostAhead;
+        if (depth >= 2) return true;
+    }
+    return false;
+}
+constexpr int kRingBytes = (227 << 10) - 2048;
 
 // Two passes as one launch of one cluster: up to eight blocks, whose rows of y fit their shared memory.
 constexpr int kClusterBlocks = 8, kClusterStage = 96 << 10;
 
-template <int DT, bool WF32, int TPR, int EPT>
-static cudaError_t launch_fwd_rows(const fp8_ctx *ctx, NormFwd p, bool two, cudaStream_t st)
+template <int DT, bool WF32>
+static bool launch_fwd_cluster(const NormFwd &p, cudaStream_t st, cudaError_t &e)
 {
-    constexpr int kBlock = kRowBlock<TPR>, kGroups = kBlock / TPR;
-    const int64_t blocks = (p.rows + kGroups - 1) / kGroups;
-    if (two) {
+    bool done = false;
+    by_row_shape(p.cols, [&](auto s) {
+        constexpr int kThreads = decltype(s)::kThreads, kBlock = kRowBlock<kThreads>, kGroups = kBlock / kThreads;
+        const int64_t blocks = (p.rows + kGroups - 1) / kGroups;
         int cluster = 1;
         while (cluster < kClusterBlocks && cluster < blocks) cluster *= 2;
         const int64_t stage = (blocks + cluster - 1) / cluster * kGroups * p.cols * InType<DT>::kBytes;
-        if (stage <= kClusterStage) {
-            cudaLaunchAttribute attr[1];
-            attr[0].id = cudaLaunchAttributeClusterDimension;
-            attr[0].val.clusterDim.x = (unsigned)cluster;
-            attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-            cudaLaunchConfig_t cfg = {};
-            cfg.gridDim = dim3((unsigned)cluster);
-            cfg.blockDim = dim3(kBlock);
-            cfg.dynamicSmemBytes = (size_t)stage;
-            cfg.stream = st;
-            cfg.attrs = attr;
-            cfg.numAttrs = 1;
-            count_launch();
-            return cudaLaunchKernelEx(&cfg, norm_fwd_rows_kernel<DT, WF32, TPR, EPT, true>, p);
-        }
-    }
-    const int32_t *bias = p.bias;
-    if (two) p.bias = nullptr;
-    const int64_t most = (int64_t)ctx->sm_count * kFwdResident<DT, TPR, EPT>;
-    count_launch();
-    norm_fwd_rows_kernel<DT, WF32, TPR, EPT, false><<<(unsigned)(blocks < most ? blocks : most), kBlock, 0, st>>>(p);
-    if (two) {
-        p.bias = bias;
-        const int64_t work = (p.rows + 3) / 4 * (p.cols / kPerVec<DT>);
+        if (stage > kClusterStage) return;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = (unsigned)cluster;
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)cluster);
+        cfg.blockDim = dim3(kBlock);
+        cfg.dynamicSmemBytes = (size_t)stage;
+        cfg.stream = st;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
         count_launch();
-        norm_cast_rows_kernel<DT, WF32><<<(unsigned)((work + kNormThreads - 1) / kNormThreads), kNormThreads, 0, st>>>(p);
-    }
-    return cudaGetLastError();
+        e = cudaLaunchKernelEx(&cfg, norm_fwd_cluster_kernel<DT, WF32, kThreads, decltype(s)::kElements>, p);
+        done = true;
+    });
+    return done;
+}
+
+static RowSource row_source(int dt, int64_t cols, const void *a, int64_t ld_a, const void *b, int64_t ld_b, const void *c, int64_t ld_c)
+{
+    const int64_t size = dt == FP8_F32 ? 4 : 2;
+    return RowSource{{static_cast<const uint8_t *>(a), static_cast<const uint8_t *>(b), static_cast<const uint8_t *>(c)},
+                     {ld_a * size, ld_b * size, ld_c * size}, (uint32_t)(cols * size), 1 + (b ? 1 : 0) + (c ? 1 : 0)};
+}
+
+// One reading of all rows; false where the rows do not fit.
+template <int DT, bool WF32>
+static bool launch_fwd_rows(const fp8_ctx *ctx, const NormFwd &p, cudaStream_t st)
+{
+    bool done = false;
+    const RowSource src = row_source(DT, p.cols, p.x, p.ld_x, p.res, p.ld_res, nullptr, 0);
+    by_row_shape(p.cols, [&](auto s) {
+        constexpr int kThreads = decltype(s)::kThreads, kElements = decltype(s)::kElements, kBlock = kRowBlock<kThreads>, kGroups = kBlock / kThreads;
+        int resident, depth;
+        if (!ring_size(kResident<kThreads, kElements, false>, kGroups, (int64_t)src.row_bytes * src.inputs, resident, depth)) return;
+        const int64_t blocks = (p.rows + kGroups - 1) / kGroups, most = (int64_t)ctx->sm_count * resident;
+        count_launch();
+        norm_fwd_rows_kernel<DT, WF32, kThreads, kElements>
+            <<<(unsigned)(blocks < most ? blocks : most), kBlock, (size_t)kGroups * depth * src.row_bytes * src.inputs, st>>>(p, src, depth);
+        done = true;
+    });
+    return done;
 }
 
 template <int DT, bool WF32>
-static cudaError_t allow_stage()
+static cudaError_t allow_shared()
 {
     cudaError_t e = cudaSuccess;
-    for (int cols : {256, 512, 1024, 2048, 4096, 8192, kMostHeld})
-        by_row_shape<false>(cols, [&](auto s) {
-            if (e == cudaSuccess)
-                e = cudaFuncSetAttribute(norm_fwd_rows_kernel<DT, WF32, decltype(s)::kThreads, decltype(s)::kElements, true>,
-                                         cudaFuncAttributeMaxDynamicSharedMemorySize, kClusterStage);
+    const auto attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
+    for (int cols : {256, 512, 1024, 2048, 4096, 8192, kMostHeld}) {
+        by_row_shape(cols, [&](auto s) {
+            if (e == cudaSuccess) e = cudaFuncSetAttribute(norm_fwd_cluster_kernel<DT, WF32, decltype(s)::kThreads, decltype(s)::kElements>, attr, kClusterStage);
+            if (e == cudaSuccess) e = cudaFuncSetAttribute(norm_fwd_rows_kernel<DT, WF32, decltype(s)::kThreads, decltype(s)::kElements>, attr, kRingBytes);
+            constexpr int kBwdBytes = kRingBytes - (decltype(s)::kThreads == 32 ? 17 << 10 : 0);
+            if (e == cudaSuccess) e = cudaFuncSetAttribute(norm_bwd_rows_kernel<DT, WF32, decltype(s)::kThreads, decltype(s)::kElements>, attr, kBwdBytes);
         });
+    }
     return e;
 }
 cudaError_t configure_norm_kernels()
 {
-    cudaError_t e = allow_stage<FP8_BF16, false>();
-    if (e == cudaSuccess) e = allow_stage<FP8_BF16, true>();
-    if (e == cudaSuccess) e = allow_stage<FP8_F16, false>();
-    if (e == cudaSuccess) e = allow_stage<FP8_F16, true>();
-    return e == cudaSuccess ? allow_stage<FP8_F32, false>() : e;
+    cudaError_t e = allow_shared<FP8_BF16, false>();
+    if (e == cudaSuccess) e = allow_shared<FP8_BF16, true>();
+    if (e == cudaSuccess) e = allow_shared<FP8_F16, false>();
+    if (e == cudaSuccess) e = allow_shared<FP8_F16, true>();
+    return e == cudaSuccess ? allow_shared<FP8_F32, false>() : e;
 }
 
 // Whether every row, and every coefficient vector, consists of whole aligned vectors.
@@ -691,7 +839,7 @@ static bool fast_rows(const NormFwd &p, int dt)
     auto row = [&](const void *q, int64_t ld) { return !q || row_aligned(q, ld, dt, 16); };
     return whole_vectors(dt, p.cols) && p.cols <= kMostHeld && row(p.x, p.ld_x) && row(p.res, p.ld_res) && row(p.h, p.ld_h) && row(p.y, p.ld_y) &&
            row(p.w, 0) && row(p.b, 0) && (reinterpret_cast<uintptr_t>(p.y8) & 7u) == 0 &&
-           (p.rows + 3) / 4 * (int64_t)p.cols / (dt == FP8_F32 ? 4 : 8) / kNormThreads < 0x7FFFFFFF;
+           (p.rows + kCastRows - 1) / kCastRows * (int64_t)p.cols / (dt == FP8_F32 ? 4 : 8) / kNormThreads < 0x7FFFFFFF;
 }
 
 template <int DT, bool WF32>
@@ -699,8 +847,16 @@ static cudaError_t launch_fwd(const fp8_ctx *ctx, NormFwd p, bool two, cudaStrea
 {
     if (fast_rows(p, DT)) {
         cudaError_t e = cudaSuccess;
-        by_row_shape<false>(p.cols, [&](auto s) { e = launch_fwd_rows<DT, WF32, decltype(s)::kThreads, decltype(s)::kElements>(ctx, p, two, st); });
-        return e;
+        if (two && launch_fwd_cluster<DT, WF32>(p, st, e)) return e;
+        NormFwd once = p;
+        if (two) once.bias = nullptr;
+        if (launch_fwd_rows<DT, WF32>(ctx, once, st)) {
+            if (two) {
+                const int64_t work = (p.rows + kCastRows - 1) / kCastRows * (p.cols / kPerVec<DT>);
+                return launch_dependent(norm_cast_rows_kernel<DT, WF32>, (unsigned)((work + kNormThreads - 1) / kNormThreads), kNormThreads, st, p);
+            }
+            return cudaGetLastError();
+        }
     }
     const unsigned grid = blocks_for_rows(ctx, p.rows, 8);
     const int32_t *bias = p.bias;
@@ -739,17 +895,25 @@ static unsigned launch_bwd(const fp8_ctx *ctx, NormBwd p, bool want_w, bool want
         if (want_w) p.part_w = ctx->d_partial;
         if (want_b) p.part_b = ctx->d_partial + (int64_t)grid * p.cols;
     };
-    count_launch();
-    if (fast) {
-        by_row_shape<true>(p.cols, [&](auto s) {
-            constexpr int kThreads = decltype(s)::kThreads, kBlock = kRowBlock<kThreads>, kGroups = kBlock / kThreads;
-            grid = bwd_blocks(ctx, (p.rows + kGroups - 1) / kGroups, kBwdResident<DT, kThreads, decltype(s)::kElements>, sums, p.cols);
+    bool done = false;
+    const RowSource src = row_source(DT, p.cols, p.dy, p.ld_dy, p.h, p.ld_h, p.dh, p.ld_dh);
+    if (fast)
+        by_row_shape(p.cols, [&](auto s) {
+            constexpr int kThreads = decltype(s)::kThreads, kElements = decltype(s)::kElements, kBlock = kRowBlock<kThreads>, kGroups = kBlock / kThreads;
+            int resident, depth;
+            // (a warp's rows: the blocks' sums meet in 16 KB more)
+            const int64_t slot = (int64_t)src.row_bytes * src.inputs + (kThreads == 32 ? 2048 : 0);
+            if (!ring_size(kResident<kThreads, kElements, true>, kGroups, slot, resident, depth)) return;
+            grid = bwd_blocks(ctx, (p.rows + kGroups - 1) / kGroups, resident, sums, p.cols);
             lines();
-            norm_bwd_rows_kernel<DT, WF32, kThreads, decltype(s)::kElements><<<grid, kBlock, 0, st>>>(p);
+            count_launch();
+            norm_bwd_rows_kernel<DT, WF32, kThreads, kElements><<<grid, kBlock, (size_t)kGroups * depth * src.row_bytes * src.inputs, st>>>(p, src, depth);
+            done = true;
         });
-    } else {
+    if (!done) {
         grid = bwd_blocks(ctx, p.rows, 4, sums, p.cols);
         lines();
+        count_launch();
         norm_bwd_any_kernel<DT><<<grid, kNormThreads, 0, st>>>(p);
     }
     return grid;
@@ -821,9 +985,10 @@ fp8_status_t fp8_norm_bwd(fp8_ctx *ctx, const fp8_norm_bwd_t *a, void *stream)
                                                : launch_bwd<FP8_F16, false>(ctx, p, w, b, st);
     if (cudaGetLastError() != cudaSuccess) return FP8_ERR_CUDA;
     if (w || b) {
-        count_launch();
-        norm_bwd_sum_kernel<<<dim3((unsigned)((a->cols + 31) / 32), 2), 256, 0, st>>>(
-            ctx->d_partial, ctx->d_partial + (int64_t)lines * a->cols, (int)lines, (int)a->cols, a->w_dt, a->dw, a->db);
+        const int chunks = (int)((a->cols + 31) / 32);
+        if (launch_dependent(norm_bwd_sum_kernel, 2u * chunks, kSumThreads, st, ctx->d_partial, ctx->d_partial + (int64_t)lines * a->cols,
+                             (int)lines, (int)a->cols, a->w_dt, a->dw, a->db, chunks) != cudaSuccess)
+            return FP8_ERR_CUDA;
     }
     return cudaGetLastError() == cudaSuccess ? FP8_OK : FP8_ERR_CUDA;
 }
