@@ -93,8 +93,8 @@ inline void count_launch(int n = 1) { g_kernel_launches.fetch_add((unsigned long
 // Launch allowed to start while the launch before it on the stream drains (programmatic dependent launch); the
 // kernel itself waits (griddepcontrol.wait) before it touches anything an earlier launch may have written.
 template <typename... KArgs, typename... Args>
-inline cudaError_t launch_dependent(void (*kernel)(KArgs...), unsigned grid, unsigned block, cudaStream_t stream,
-                                    Args... args)
+inline cudaError_t launch_dependent_with(void (*kernel)(KArgs...), unsigned grid, unsigned block, size_t smem, cudaStream_t stream,
+                                         Args... args)
 {
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -102,11 +102,18 @@ inline cudaError_t launch_dependent(void (*kernel)(KArgs...), unsigned grid, uns
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(grid);
     cfg.blockDim = dim3(block);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     count_launch();
     return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
+}
+template <typename... KArgs, typename... Args>
+inline cudaError_t launch_dependent(void (*kernel)(KArgs...), unsigned grid, unsigned block, cudaStream_t stream,
+                                    Args... args)
+{
+    return launch_dependent_with(kernel, grid, block, 0, stream, args...);
 }
 
 cudaError_t launch_amax_bias(fp8_ctx *ctx, const void *x, int dt, int64_t rows, int64_t cols, int64_t ld, float *d_amax,

@@ -1,5 +1,7 @@
 // Layer norm and its root-mean-square form, forward (with the residual sum, and the E4 bytes and amax of the output) and
 // backward.
+#include <algorithm>
+
 #include "fp8_norm.h"
 #include "kv_common.cuh"
 #include "ptx.cuh"
@@ -81,7 +83,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_fwd_any_kernel(const NormFw
                 q = corrected(mean, q, p.cols, p.inv_cols);
                 mean = q.x;
             }
-            rstd = 1.0f / sqrtf(__fmaf_rn(q.y, p.inv_cols, p.eps));
+            rstd = __frsqrt_rn(__fmaf_rn(q.y, p.inv_cols, p.eps));
             if (threadIdx.x == 0) {
                 if (p.mean) p.mean[r] = mean;
                 if (p.rstd) p.rstd[r] = rstd;
@@ -161,14 +163,15 @@ struct RowWalk {
     // one thread of the group: row r into slot s
     __device__ __forceinline__ void start(int64_t r, int s) const
     {
+        const uint64_t once = l2_policy_evict_first();   // (what is written stays in L2 for the launch behind)
         const uint32_t bar = smem_u32(&ring.full[group][s]);
         uint32_t to = smem_u32(slots + s * slot_bytes);
         mbar_expect_tx(bar, slot_bytes);
 #pragma unroll
         for (int i = 0; i < 3; ++i) {
             if (!src.base[i]) continue;
-            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to),
-                         "l"(src.base[i] + r * src.stride[i]), "r"(src.row_bytes), "r"(bar)
+            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;" ::"r"(to),
+                         "l"(src.base[i] + r * src.stride[i]), "r"(src.row_bytes), "r"(bar), "l"(once)
                          : "memory");
             to += src.row_bytes;
         }
@@ -199,6 +202,30 @@ __device__ __forceinline__ void load_coefficients(const void *w, int col, float 
         unpack_pairs<DT>(__ldg(reinterpret_cast<const uint4 *>(static_cast<const uint8_t *>(w) + (int64_t)col * InType<DT>::kBytes)), f);
     }
 }
+
+// Coefficients of a thread's own vectors: of the tensors' type they are held packed, FP32 ones are read again for each row.
+template <int DT, bool WF32, int VECS>
+struct HeldCoefficients {
+    uint4 raw[WF32 ? 1 : VECS];
+    const void *source;
+    float fill;
+    __device__ __forceinline__ HeldCoefficients(const void *w, float f, int t, int threads, int row_vecs) : source(w), fill(f)
+    {
+        if (WF32) return;
+        const uint32_t one = DT == FP8_F32 ? 0x3F800000u : DT == FP8_BF16 ? 0x3F803F80u : 0x3C003C00u, all = f == 1.0f ? one : 0u;
+#pragma unroll
+        for (int i = 0; i < VECS; ++i) {
+            raw[WF32 ? 0 : i] = make_uint4(all, all, all, all);
+            if (w && t + i * threads < row_vecs) raw[WF32 ? 0 : i] = __ldg(reinterpret_cast<const uint4 *>(w) + t + i * threads);
+        }
+    }
+    // of vector i, whose first column is col
+    __device__ __forceinline__ void get(int i, int col, Pair (&f)[kVecPairs<DT>]) const
+    {
+        if (WF32) load_coefficients<DT, WF32>(source, col, fill, f);
+        else unpack_pairs<DT>(raw[WF32 ? 0 : i], f);
+    }
+};
 
 // y of a vector, rounded to the tensors' type (the operations of `normalised`, in their order)
 template <int DT>
@@ -255,12 +282,13 @@ struct ByteScale {
         Pair v[kVecPairs<DT>];
         uint32_t pairs[4] = {};
         unpack_pairs<DT>(y, v);
+        if (two)
+#pragma unroll
+            for (int i = 0; i < kVecPairs<DT>; ++i) v[i] = v[i] * pair_of(second);
 #pragma unroll
         for (int i = 0; i < kVecPairs<DT>; ++i) {
-            v[i] = v[i] * pair_of(first);
-            if (two) v[i] = v[i] * pair_of(second);
             float lo, hi;
-            split(v[i], lo, hi);
+            split(v[i] * pair_of(first), lo, hi);
             pairs[i] = cvt_pair<FP8_E4>(hi, lo);
         }
         if (DT == FP8_F32) __stcs(reinterpret_cast<uint32_t *>(y8 + at), pairs[0] | (pairs[1] << 16));
@@ -291,7 +319,7 @@ __device__ __forceinline__ void row_statistics(const NormFwd &p, const Pair (&h)
         q = corrected(mean, q, p.cols, p.inv_cols);
         mean = q.x;
     }
-    rstd = 1.0f / sqrtf(__fmaf_rn(q.y, p.inv_cols, p.eps));
+    rstd = __frsqrt_rn(__fmaf_rn(q.y, p.inv_cols, p.eps));
 }
 
 // Few rows whose bytes are wanted: the blocks are one cluster that knows the amax when its rows are done, and casts them from
@@ -402,6 +430,7 @@ __global__ void __launch_bounds__(kRowBlock<TPR>, kResident<TPR, EPT, false>) no
     int slot = 0, turn = 0;
     const bool bytes = p.y8 && p.bias, want_y = p.y || bytes || p.sink.slot;
     const ByteScale scale(bytes ? *p.bias + p.delta : 0);
+    const HeldCoefficients<DT, WF32, kVecs> weight(p.w, 1.0f, t, TPR, row_vecs), shift(p.b, 0.0f, t, TPR, row_vecs);
     int64_t r = (int64_t)blockIdx.x * kGroups + group;
     if (t == 0)
         for (int i = 0; i < depth && r + i * step < p.rows; ++i) walk.start(r + i * step, i);
@@ -437,8 +466,11 @@ __global__ void __launch_bounds__(kRowBlock<TPR>, kResident<TPR, EPT, false>) no
             for (int i = 0; i < kVecs; ++i) {
                 const int v = t + i * TPR;
                 if (v >= row_vecs) continue;
-                const uint4 y = normalise_vector<DT, WF32>(p, h[i], mean, rstd, v * kN);
-                acc = fold_vector<DT>(acc, y);
+                Pair w[kPairs], b[kPairs];
+                weight.get(i, v * kN, w);
+                shift.get(i, v * kN, b);
+                const uint4 y = normalise_vector<DT>(h[i], mean, rstd, w, b);
+                if (p.sink.slot) acc = fold_vector<DT>(acc, y);
                 if (p.y) reinterpret_cast<uint4 *>(static_cast<uint8_t *>(p.y) + r * p.ld_y * kSize)[v] = y;
                 if (bytes) scale.store<DT>(p.y8, r * p.cols + v * kN, y, peak);
             }
@@ -448,59 +480,56 @@ __global__ void __launch_bounds__(kRowBlock<TPR>, kResident<TPR, EPT, false>) no
     sink_amax(folded_key<DT>(acc), p.sink);
 }
 
-// The bytes of y from the sums and the statistics of the launch before, under the bias that it left: eight rows of one vector a
-// thread, last rows first (what the launch before wrote last is what L2 holds).
-constexpr int kCastRows = 8;
-template <int DT, bool WF32>
-__global__ void __launch_bounds__(kNormThreads, 3) norm_cast_rows_kernel(const NormFwd p)
+// The bytes of y from the sums and the statistics of the launch before, under the bias that it left.  Last rows first: what the
+// launch before wrote last is what L2 holds.
+template <int DT, bool WF32, int TPR, int EPT>
+__global__ void __launch_bounds__(kRowBlock<TPR>, kResident<TPR, EPT, false>) norm_cast_rows_kernel(const NormFwd p, const RowSource src, int depth)
 {
-    constexpr int kN = kPerVec<DT>, kPairs = kVecPairs<DT>, kSize = InType<DT>::kBytes, kHalf = kCastRows / 2;
-    const unsigned row_vecs = p.cols / kN;
-    const uint64_t at = (uint64_t)(gridDim.x - 1 - blockIdx.x) * kNormThreads + threadIdx.x;
-    int64_t r0;
-    int v;
-    if (gridDim.x < (1u << 24)) {   // (divisions of 32 bits where they do)
-        r0 = (int64_t)((unsigned)at / row_vecs) * kCastRows;
-        v = (int)((unsigned)at % row_vecs);
-    } else {
-        r0 = (int64_t)(at / row_vecs) * kCastRows;
-        v = (int)(at % row_vecs);
-    }
-    if (r0 >= p.rows) return;
-    const bool sum = p.res && !p.h;
-    const int64_t stride = (p.h ? p.ld_h : p.ld_x) * kSize;
-    const uint8_t *src = static_cast<const uint8_t *>(p.h ? p.h : p.x) + r0 * stride + (int64_t)v * 16;
-    const uint8_t *src_res = static_cast<const uint8_t *>(p.res) + r0 * p.ld_res * kSize + (int64_t)v * 16;
-    uint8_t *dst = p.y8 + r0 * p.cols + (int64_t)v * kN;
-    const int rows = (int)min((int64_t)kCastRows, p.rows - r0);
-    Pair w[kPairs], b[kPairs];
-    load_coefficients<DT, WF32>(p.w, v * kN, 1.0f, w);
-    load_coefficients<DT, WF32>(p.b, v * kN, 0.0f, b);
+    constexpr int kN = kPerVec<DT>, kPairs = kVecPairs<DT>, kVecs = EPT / kN, kGroups = kRowBlock<TPR> / TPR;
+    extern __shared__ __align__(16) uint8_t slots[];
+    __shared__ RowRing<TPR> ring;
+    const RowWalk<TPR> walk(src, ring, slots, depth, p.sink.d_status);
+    const int t = threadIdx.x % TPR, group = threadIdx.x / TPR;
+    const int64_t step = (int64_t)gridDim.x * kGroups;
+    const int row_vecs = p.cols / kN;
+    const HeldCoefficients<DT, WF32, kVecs> weight(p.w, 1.0f, t, TPR, row_vecs), shift(p.b, 0.0f, t, TPR, row_vecs);
     wait_for_launch_before();
+    int64_t r = p.rows - 1 - ((int64_t)blockIdx.x * kGroups + group);
+    if (t == 0)
+        for (int i = 0; i < depth && r - i * step >= 0; ++i) walk.start(r - i * step, i);
     const ByteScale scale(__ldcg(p.bias) + p.delta);
-    uint32_t peak = 0;
-    for (int first = 0; first < rows; first += kHalf) {
-        uint4 x[kHalf], res[kHalf];
-        float mean[kHalf], rstd[kHalf];
+    uint32_t peak = 0, parity = 0;
+    int slot = 0;
+    float mean = 0.0f, rstd = 0.0f;
+    auto statistics = [&](int64_t row) {
+        mean = p.layer ? __ldcg(p.mean + row) : 0.0f;
+        rstd = __ldcg(p.rstd + row);
+    };
+    if (r >= 0) statistics(r);
+    for (bool behind = false; r >= 0; r -= step, behind = true) {
+        const uint4 *in = walk.wait(slot, parity);
+        // (all are done with the row before: its slot is free)
+        if (TPR == 32) __syncwarp();
+        else __syncthreads();
+        if (t == 0 && behind && r - (depth - 1) * step >= 0) walk.start(r - (depth - 1) * step, slot == 0 ? depth - 1 : slot - 1);
+        const float m = mean, s = rstd;
+        if (r - step >= 0) statistics(r - step);
 #pragma unroll
-        for (int i = 0; i < kHalf; ++i) {
-            if (first + i >= rows) continue;
-            x[i] = __ldcs(reinterpret_cast<const uint4 *>(src + i * stride));
-            if (sum) res[i] = __ldcs(reinterpret_cast<const uint4 *>(src_res + i * p.ld_res * kSize));
-            mean[i] = p.layer ? __ldcg(p.mean + r0 + first + i) : 0.0f;
-            rstd[i] = __ldcg(p.rstd + r0 + first + i);
+        for (int i = 0; i < kVecs; ++i) {
+            const int v = t + i * TPR;
+            if (v >= row_vecs) continue;
+            Pair h[kPairs], w[kPairs], b[kPairs];
+            uint4 x = in[v];
+            if (src.inputs == 2) sum_vector<DT>(x, in[row_vecs + v], h, x);
+            else unpack_pairs<DT>(x, h);
+            weight.get(i, v * kN, w);
+            shift.get(i, v * kN, b);
+            scale.store<DT>(p.y8, r * p.cols + v * kN, normalise_vector<DT>(h, m, s, w, b), peak);
         }
-#pragma unroll
-        for (int i = 0; i < kHalf; ++i) {
-            if (first + i >= rows) continue;
-            Pair h[kPairs];
-            if (sum) sum_vector<DT>(x[i], res[i], h, x[i]);
-            else unpack_pairs<DT>(x[i], h);
-            scale.store<DT>(dst, (int64_t)i * p.cols, normalise_vector<DT>(h, mean[i], rstd[i], w, b), peak);
+        if (++slot == depth) {
+            slot = 0;
+            parity ^= 1u;
         }
-        src += kHalf * stride;
-        src_res += kHalf * p.ld_res * kSize;
-        dst += (int64_t)kHalf * p.cols;
     }
     if (scale.clipped<DT>(peak)) raise_flags(p.sink.d_status, FP8_FLAG_SATURATED);
 }
@@ -569,25 +598,23 @@ __global__ void __launch_bounds__(kRowBlock<TPR>, kResident<TPR, EPT, true>) nor
     uint32_t acc = 0, parity = 0;
     int slot = 0, turn = 0;
     Pair sum_w[kVecs][kPairs], sum_b[kVecs][kPairs];
-    uint4 weight[WF32 ? 1 : kVecs];   // (of the tensors' type: held; FP32: read again for each row)
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
+    for (int i = 0; i < kVecs; ++i)
 #pragma unroll
         for (int k = 0; k < kPairs; ++k) sum_w[i][k] = sum_b[i][k] = pair_of(0.0f);
-        if (!WF32 && t + i * TPR < row_vecs) {
-            const uint32_t one = DT == FP8_F32 ? 0x3F800000u : DT == FP8_BF16 ? 0x3F803F80u : 0x3C003C00u;
-            weight[WF32 ? 0 : i] = p.w ? reinterpret_cast<const uint4 *>(p.w)[t + i * TPR] : make_uint4(one, one, one, one);
-        }
-    }
-    auto weights = [&](int i, Pair (&w)[kPairs]) {
-        if (WF32) load_coefficients<DT, WF32>(p.w, (t + i * TPR) * kN, 1.0f, w);
-        else unpack_pairs<DT>(weight[WF32 ? 0 : i], w);
-    };
+    const HeldCoefficients<DT, WF32, kVecs> weight(p.w, 1.0f, t, TPR, row_vecs);
     int64_t r = (int64_t)blockIdx.x * kGroups + group;
     if (t == 0)
         for (int i = 0; i < depth && r + i * step < p.rows; ++i) walk.start(r + i * step, i);
+    float next_mean = 0.0f, next_rstd = 0.0f;
+    auto statistics = [&](int64_t row) {
+        next_mean = p.layer ? p.mean[row] : 0.0f;
+        next_rstd = p.rstd[row];
+    };
+    if (r < p.rows) statistics(r);
     for (bool behind = false; r < p.rows; r += step, turn ^= 1, behind = true) {
-        const float mean = p.layer ? p.mean[r] : 0.0f, rstd = p.rstd[r];
+        const float mean = next_mean, rstd = next_rstd;
+        if (r + step < p.rows) statistics(r + step);
         const uint4 *in = walk.wait(slot, parity);
         const Pair less = pair_of(-mean), by = pair_of(rstd);
         Pair p1 = pair_of(0.0f), p2 = p1;
@@ -597,7 +624,7 @@ __global__ void __launch_bounds__(kRowBlock<TPR>, kResident<TPR, EPT, true>) nor
             Pair y[kPairs], x[kPairs], w[kPairs];
             unpack_pairs<DT>(in[t + i * TPR], y);
             unpack_pairs<DT>(in[row_vecs + t + i * TPR], x);
-            weights(i, w);
+            weight.get(i, (t + i * TPR) * kN, w);
 #pragma unroll
             for (int k = 0; k < kPairs; ++k) {
                 const Pair xh = (x[k] + less) * by, g = y[k] * w[k];
@@ -621,7 +648,7 @@ __global__ void __launch_bounds__(kRowBlock<TPR>, kResident<TPR, EPT, true>) nor
                 Pair y[kPairs], x[kPairs], w[kPairs];
                 unpack_pairs<DT>(in[v], y);
                 unpack_pairs<DT>(in[row_vecs + v], x);
-                weights(i, w);
+                weight.get(i, v * kN, w);
 #pragma unroll
                 for (int k = 0; k < kPairs; ++k) y[k] = (fma((x[k] + less) * by, c2, y[k] * w[k]) + c1) * by;
                 if (p.dh) {
@@ -630,7 +657,7 @@ __global__ void __launch_bounds__(kRowBlock<TPR>, kResident<TPR, EPT, true>) nor
                     for (int k = 0; k < kPairs; ++k) y[k] = y[k] + x[k];
                 }
                 const uint4 out = pack_pairs<DT>(y);
-                acc = fold_vector<DT>(acc, out);
+                if (p.sink.slot) acc = fold_vector<DT>(acc, out);
                 px[v] = out;
             }
         }
@@ -786,21 +813,29 @@ static RowSource row_source(int dt, int64_t cols, const void *a, int64_t ld_a, c
                      {ld_a * size, ld_b * size, ld_c * size}, (uint32_t)(cols * size), 1 + (b ? 1 : 0) + (c ? 1 : 0)};
 }
 
-// One reading of all rows; false where the rows do not fit.
+// One reading of all rows (two: and a second one for the bytes); false where the rows do not fit.
 template <int DT, bool WF32>
-static bool launch_fwd_rows(const fp8_ctx *ctx, const NormFwd &p, cudaStream_t st)
+static bool launch_fwd_rows(const fp8_ctx *ctx, const NormFwd &p, bool two, cudaStream_t st, cudaError_t &e)
 {
     bool done = false;
     const RowSource src = row_source(DT, p.cols, p.x, p.ld_x, p.res, p.ld_res, nullptr, 0);
     by_row_shape(p.cols, [&](auto s) {
         constexpr int kThreads = decltype(s)::kThreads, kElements = decltype(s)::kElements, kBlock = kRowBlock<kThreads>, kGroups = kBlock / kThreads;
+        const int64_t blocks = (p.rows + kGroups - 1) / kGroups;
         int resident, depth;
+        auto grid = [&] { return (unsigned)std::min(blocks, (int64_t)ctx->sm_count * resident); };
+        auto bytes = [&](const RowSource &from) { return (size_t)kGroups * depth * from.row_bytes * from.inputs; };
         if (!ring_size(kResident<kThreads, kElements, false>, kGroups, (int64_t)src.row_bytes * src.inputs, resident, depth)) return;
-        const int64_t blocks = (p.rows + kGroups - 1) / kGroups, most = (int64_t)ctx->sm_count * resident;
+        NormFwd once = p;
+        if (two) once.bias = nullptr;
         count_launch();
-        norm_fwd_rows_kernel<DT, WF32, kThreads, kElements>
-            <<<(unsigned)(blocks < most ? blocks : most), kBlock, (size_t)kGroups * depth * src.row_bytes * src.inputs, st>>>(p, src, depth);
+        norm_fwd_rows_kernel<DT, WF32, kThreads, kElements><<<grid(), kBlock, bytes(src), st>>>(once, src, depth);
+        e = cudaGetLastError();
         done = true;
+        if (!two || e != cudaSuccess) return;
+        const RowSource sums = p.h ? row_source(DT, p.cols, p.h, p.ld_h, nullptr, 0, nullptr, 0) : src;
+        ring_size(kResident<kThreads, kElements, false>, kGroups, (int64_t)sums.row_bytes * sums.inputs, resident, depth);
+        e = launch_dependent_with(norm_cast_rows_kernel<DT, WF32, kThreads, kElements>, grid(), kBlock, bytes(sums), st, p, sums, depth);
     });
     return done;
 }
@@ -814,6 +849,7 @@ static cudaError_t allow_shared()
         by_row_shape(cols, [&](auto s) {
             if (e == cudaSuccess) e = cudaFuncSetAttribute(norm_fwd_cluster_kernel<DT, WF32, decltype(s)::kThreads, decltype(s)::kElements>, attr, kClusterStage);
             if (e == cudaSuccess) e = cudaFuncSetAttribute(norm_fwd_rows_kernel<DT, WF32, decltype(s)::kThreads, decltype(s)::kElements>, attr, kRingBytes);
+            if (e == cudaSuccess) e = cudaFuncSetAttribute(norm_cast_rows_kernel<DT, WF32, decltype(s)::kThreads, decltype(s)::kElements>, attr, kRingBytes);
             constexpr int kBwdBytes = kRingBytes - (decltype(s)::kThreads == 32 ? 17 << 10 : 0);
             if (e == cudaSuccess) e = cudaFuncSetAttribute(norm_bwd_rows_kernel<DT, WF32, decltype(s)::kThreads, decltype(s)::kElements>, attr, kBwdBytes);
         });
@@ -838,8 +874,7 @@ static bool fast_rows(const NormFwd &p, int dt)
 {
     auto row = [&](const void *q, int64_t ld) { return !q || row_aligned(q, ld, dt, 16); };
     return whole_vectors(dt, p.cols) && p.cols <= kMostHeld && row(p.x, p.ld_x) && row(p.res, p.ld_res) && row(p.h, p.ld_h) && row(p.y, p.ld_y) &&
-           row(p.w, 0) && row(p.b, 0) && (reinterpret_cast<uintptr_t>(p.y8) & 7u) == 0 &&
-           (p.rows + kCastRows - 1) / kCastRows * (int64_t)p.cols / (dt == FP8_F32 ? 4 : 8) / kNormThreads < 0x7FFFFFFF;
+           row(p.w, 0) && row(p.b, 0) && (reinterpret_cast<uintptr_t>(p.y8) & 7u) == 0;
 }
 
 template <int DT, bool WF32>
@@ -848,15 +883,7 @@ static cudaError_t launch_fwd(const fp8_ctx *ctx, NormFwd p, bool two, cudaStrea
     if (fast_rows(p, DT)) {
         cudaError_t e = cudaSuccess;
         if (two && launch_fwd_cluster<DT, WF32>(p, st, e)) return e;
-        NormFwd once = p;
-        if (two) once.bias = nullptr;
-        if (launch_fwd_rows<DT, WF32>(ctx, once, st)) {
-            if (two) {
-                const int64_t work = (p.rows + kCastRows - 1) / kCastRows * (p.cols / kPerVec<DT>);
-                return launch_dependent(norm_cast_rows_kernel<DT, WF32>, (unsigned)((work + kNormThreads - 1) / kNormThreads), kNormThreads, st, p);
-            }
-            return cudaGetLastError();
-        }
+        if (launch_fwd_rows<DT, WF32>(ctx, p, two, st, e)) return e;
     }
     const unsigned grid = blocks_for_rows(ctx, p.rows, 8);
     const int32_t *bias = p.bias;
@@ -986,7 +1013,7 @@ fp8_status_t fp8_norm_bwd(fp8_ctx *ctx, const fp8_norm_bwd_t *a, void *stream)
     if (cudaGetLastError() != cudaSuccess) return FP8_ERR_CUDA;
     if (w || b) {
         const int chunks = (int)((a->cols + 31) / 32);
-        if (launch_dependent(norm_bwd_sum_kernel, 2u * chunks, kSumThreads, st, ctx->d_partial, ctx->d_partial + (int64_t)lines * a->cols,
+        if (launch_dependent_with(norm_bwd_sum_kernel, 2u * chunks, kSumThreads, 0, st, ctx->d_partial, ctx->d_partial + (int64_t)lines * a->cols,
                              (int)lines, (int)a->cols, a->w_dt, a->dw, a->db, chunks) != cudaSuccess)
             return FP8_ERR_CUDA;
     }
