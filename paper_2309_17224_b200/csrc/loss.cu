@@ -178,7 +178,15 @@ __device__ __forceinline__ void find_top(const Row<DT> &row, float m, int k, Top
         uint32_t own[T / 32], bound = 0;
 #pragma unroll
         for (int i = 0; i < T / 32; ++i) own[i] = sh.strip[lane + 32 * i];
-        for (uint32_t bit = 0x8000u; bit; bit >>= 1) {
+        for (int i = 0; k <= 8 && i < k; ++i) {   // few: the largest, k times (equal ones go together: a lower bound then)
+            uint32_t most = 0;
+#pragma unroll
+            for (int n = 0; n < T / 32; ++n) most = max(most, own[n]);
+            bound = __reduce_max_sync(0xFFFFFFFFu, most);
+#pragma unroll
+            for (int n = 0; n < T / 32; ++n) own[n] = own[n] == bound ? 0u : own[n];
+        }
+        for (uint32_t bit = k <= 8 ? 0u : 0x8000u; bit; bit >>= 1) {
             unsigned n = 0;
 #pragma unroll
             for (int i = 0; i < T / 32; ++i) n += own[i] >= (bound | bit);
@@ -398,18 +406,20 @@ __device__ __forceinline__ int part_start(int vocab, int blocks, int b)
     const int chunk = (vocab / blocks + 64) & ~63;
     return min(vocab, b * chunk);
 }
-// Sums of all the parts, to every block.
-__device__ __forceinline__ Sums cluster_join(Sums own, int blocks, float c, float4 &word)
+// Sums of all the parts, for the first block, behind a cluster_sync that follows the parts' words.
+__device__ __forceinline__ void cluster_note(const Sums &own, float4 &word)
 {
-    if (blocks == 1) return own;
     if (threadIdx.x == 0) word = make_float4(own.m, own.s, own.t, 0.0f);
-    cluster_sync();
+}
+__device__ __forceinline__ Sums cluster_join(int blocks, float c, const float4 &word)
+{
     Sums all = no_sums();
     float most = -INFINITY;
     for (int b = 0; b < blocks; ++b) {
         Sums o;
         const uint32_t at = cluster_address(&word, b);
-        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(o.m), "=f"(o.s), "=f"(o.t), "=f"(own.t) : "r"(at) : "memory");
+        asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(o.m), "=f"(o.s) : "r"(at) : "memory");
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(o.t) : "r"(at + 8) : "memory");
         most = fmaxf(most, o.m);
         if (o.s != 0.0f) all.join(o, c);
     }
@@ -443,7 +453,13 @@ __global__ void __launch_bounds__(T, 1024 / T) token_logprobs_kernel(const Logit
         add_element<true>(sums, x, p.c);
         strip = fmaxf(strip, x);
     }
-    sums = cluster_join(block_join<T>(sums, strip, p.c, part), blocks, p.c, word);
+    sums = block_join<T>(sums, strip, p.c, part);
+    if (o.top_k > 0) find_top<DT, T>(row, strip, o.top_k, top);   // (of a row with a NaN too: what it finds there is not used)
+    if (blocks > 1) {
+        cluster_note(sums, word);
+        cluster_sync();
+        if (own == 0) sums = cluster_join(blocks, p.c, word);
+    }
     // nothing but -infinity: s = 0;  a NaN or +infinity: s is NaN
     const bool none = sums.s == 0.0f, nan = !(sums.s >= 0.0f);
     const float logsum = none ? -INFINITY : logf(sums.s);
@@ -463,20 +479,16 @@ __global__ void __launch_bounds__(T, 1024 / T) token_logprobs_kernel(const Logit
             o.logprob[r] = lp;
         }
     }
-    if (o.top_k > 0) {
-        if (!nan) find_top<DT, T>(row, strip, o.top_k, top);
+    if (o.top_k > 0 && own == 0) {
         if (blocks > 1) {
-            cluster_sync();
-            if (own == 0 && !nan) {
-                for (int i = threadIdx.x; i < blocks * o.top_k; i += T) {
-                    const uint32_t at = cluster_address(&top.best[i % o.top_k], i / o.top_k);
-                    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(top.key[i]) : "r"(at) : "memory");
-                }
-                __syncthreads();
-                top_rank(top, blocks * o.top_k, o.top_k);
+            for (int i = threadIdx.x; i < blocks * o.top_k; i += T) {
+                const uint32_t at = cluster_address(&top.best[i % o.top_k], i / o.top_k);
+                asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(top.key[i]) : "r"(at) : "memory");
             }
+            __syncthreads();
+            top_rank(top, blocks * o.top_k, o.top_k);
         }
-        for (int i = own == 0 ? threadIdx.x : o.top_k; i < o.top_k; i += T) {
+        for (int i = threadIdx.x; i < o.top_k; i += T) {
             const int64_t at = r * o.top_k + i;
             const unsigned long long key = nan ? 0 : top.best[i];
             const int j = nan ? -1 : (int)~(uint32_t)key;
@@ -671,7 +683,12 @@ __global__ void __launch_bounds__(T) distill_kernel(const Logits p, const Teache
         top = fmaxf(top, y);
     }
     if (own == 0) sum_list<T>(l, e, sh);
-    const Sums others = cluster_join(block_join<T>(sums, top, p.c, part[0]), blocks, p.c, word);   // (a barrier)
+    Sums others = block_join<T>(sums, top, p.c, part[0]);   // (a barrier)
+    if (blocks > 1) {
+        cluster_note(others, word);
+        cluster_sync();
+        if (own == 0) others = cluster_join(blocks, p.c, word);
+    }
     if (own == 0) {
         share_list<T>(l, e, sh);
         const bool counts = e.j >= 0;   // (of a token that came twice one entry is left)

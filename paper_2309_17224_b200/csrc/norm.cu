@@ -9,7 +9,6 @@
 
 namespace fp8lin {
 
-constexpr int kNormThreads = 256;
 constexpr int kMaxCols = 1 << 30;
 
 struct NormFwd {
@@ -35,50 +34,82 @@ __device__ __forceinline__ float2 corrected(float estimate, float2 sums, int col
 }
 
 template <int DT>
-__device__ __forceinline__ float normalised(const NormFwd &p, float h, float mean, float rstd, int j)
+__device__ __forceinline__ float normalised(float h, float mean, float rstd, float w, float b)
 {
-    float v = __fmul_rn(__fsub_rn(h, mean), rstd);
-    const float w = p.w ? load_any(p.w, p.w_dt, j) : 1.0f, b = p.b ? load_any(p.b, p.w_dt, j) : 0.0f;
-    return element_value<DT>(element_bits<DT>(__fmaf_rn(v, w, b)));
+    return element_value<DT>(element_bits<DT>(__fmaf_rn(__fmul_rn(__fsub_rn(h, mean), rstd), w, b)));
 }
+__device__ __forceinline__ float weight_at(const void *w, int w_dt, int j) { return w ? load_any(w, w_dt, j) : 1.0f; }
+__device__ __forceinline__ float shift_at(const void *b, int w_dt, int j) { return b ? load_any(b, w_dt, j) : 0.0f; }
 
-// Any sizes and alignment: a block per row, three walks over it.  CAST_ONLY: the statistics are there, bytes are wanted.
-template <int DT, bool CAST_ONLY>
-__global__ void __launch_bounds__(kNormThreads) norm_fwd_any_kernel(const NormFwd p)
+// Any sizes and alignment, element by element: T threads a row.  HELD > 0: a thread holds that many elements (T * HELD >= cols) and
+// the row is read once; 0: any length, three walks over it.  CAST_ONLY: the statistics are there, bytes are wanted.
+template <int DT, bool CAST_ONLY, int T, int HELD>
+__global__ void __launch_bounds__(T) norm_fwd_any_kernel(const NormFwd p)
 {
-    __shared__ float part[kNormThreads / 32];
-    __shared__ float2 part2[kNormThreads / 32];
+    constexpr int kTurns = HELD ? HELD : 1;
+    __shared__ float part[T / 32];
+    __shared__ float2 part2[T / 32];
     uint32_t key = 0;
     bool sat = false;
     const bool bytes = p.y8 && p.bias;
     Pow2Pair scale = {1.0f, 1.0f};
     if (bytes) scale = make_pow2_pair(*p.bias + p.delta);
+    // (up to eight of each, the coefficients too are held: they would be waited for behind each row's sums)
+    constexpr bool kHoldCoefficients = HELD > 0 && HELD <= 8;
+    float held_w[kTurns], held_b[kTurns];
+    if (kHoldCoefficients) {
+#pragma unroll
+        for (int i = 0; i < kTurns; ++i) {
+            const int j = (int)threadIdx.x + i * T;
+            held_w[i] = j < p.cols ? weight_at(p.w, p.w_dt, j) : 0.0f;
+            held_b[i] = j < p.cols ? shift_at(p.b, p.w_dt, j) : 0.0f;
+        }
+    }
     for (int64_t r = blockIdx.x; r < p.rows; r += gridDim.x) {
+        float held[kTurns];
         auto sum_at = [&](int j) {
             float v = load1<DT>(p.x, r * p.ld_x + j);
             if (p.res) v = element_value<DT>(element_bits<DT>(v + load1<DT>(p.res, r * p.ld_res + j)));
             return v;
         };
-        auto h_at = [&](int j) { return p.h ? load1<DT>(p.h, r * p.ld_h + j) : sum_at(j); };
+        // f(element, its column, its place), for all of the thread's
+        auto each = [&](auto f) {
+            if (HELD) {
+#pragma unroll
+                for (int i = 0; i < kTurns; ++i)
+                    if ((int)threadIdx.x + i * T < p.cols) f(held[i], (int)threadIdx.x + i * T, i);
+            } else {
+                for (int j = threadIdx.x; j < p.cols; j += T) f(p.h ? load1<DT>(p.h, r * p.ld_h + j) : sum_at(j), j, 0);
+            }
+        };
+        if (HELD) {
+            const bool from_h = CAST_ONLY && p.h;
+#pragma unroll
+            for (int i = 0; i < kTurns; ++i) {
+                const int j = (int)threadIdx.x + i * T;
+                if (j < p.cols) held[i] = from_h ? load1<DT>(p.h, r * p.ld_h + j) : sum_at(j);
+            }
+        }
         float mean = 0.0f, rstd;
         if (CAST_ONLY) {
             mean = p.layer ? p.mean[r] : 0.0f;
             rstd = p.rstd[r];
         } else {
             float s = 0.0f;
-            for (int j = threadIdx.x; j < p.cols; j += kNormThreads) {
-                const float v = sum_at(j);
-                if (p.h) store_bits<DT>(p.h, r * p.ld_h + j, element_bits<DT>(v));
+            if (!HELD && p.h)
+                for (int j = threadIdx.x; j < p.cols; j += T) store_bits<DT>(p.h, r * p.ld_h + j, element_bits<DT>(sum_at(j)));
+            each([&](float v, int j, int) {
+                if (HELD && p.h) store_bits<DT>(p.h, r * p.ld_h + j, element_bits<DT>(v));
                 s += v;
-            }
-            s = block_sum<kNormThreads>(s, part);
+            });
+            s = block_sum<T>(s, part);
             if (p.layer) mean = s * p.inv_cols;
             float2 q = make_float2(0.0f, 0.0f);
-            for (int j = threadIdx.x; j < p.cols; j += kNormThreads) {
-                const float d = h_at(j) - mean;
+            each([&](float v, int, int) {
+                const float d = v - mean;
                 q = make_float2(q.x + d, __fmaf_rn(d, d, q.y));
-            }
-            q = block_sum2<kNormThreads>(q, part2);
+            });
+            q = block_sum2<T>(q, part2);
             if (p.layer) {
                 q = corrected(mean, q, p.cols, p.inv_cols);
                 mean = q.x;
@@ -90,8 +121,10 @@ __global__ void __launch_bounds__(kNormThreads) norm_fwd_any_kernel(const NormFw
             }
         }
         if (p.y || bytes || p.sink.slot) {
-            for (int j = threadIdx.x; j < p.cols; j += kNormThreads) {
-                const float v = normalised<DT>(p, h_at(j), mean, rstd, j);
+            each([&](float h, int j, int i) {
+                const float w = kHoldCoefficients ? held_w[i] : weight_at(p.w, p.w_dt, j);
+                const float b = kHoldCoefficients ? held_b[i] : shift_at(p.b, p.w_dt, j);
+                const float v = normalised<DT>(h, mean, rstd, w, b);
                 key = max(key, magnitude_key(v));
                 if (p.y && !CAST_ONLY) store_bits<DT>(p.y, r * p.ld_y + j, element_bits<DT>(v));
                 if (bytes) {
@@ -99,7 +132,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_fwd_any_kernel(const NormFw
                     sat = sat || clips<FP8_E4>(z);
                     p.y8[r * p.cols + j] = (uint8_t)(cvt_pair<FP8_E4>(0.0f, z) & 0xFFu);
                 }
-            }
+            });
         }
     }
     if (sat) raise_flags(p.sink.d_status, FP8_FLAG_SATURATED);
@@ -238,15 +271,6 @@ __device__ __forceinline__ uint4 normalise_vector(const Pair (&h)[kVecPairs<DT>]
     for (int i = 0; i < kVecPairs<DT>; ++i) v[i] = fma((h[i] + less) * by, w[i], b[i]);
     return pack_pairs<DT>(v);
 }
-template <int DT, bool WF32>
-__device__ __forceinline__ uint4 normalise_vector(const NormFwd &p, const Pair (&h)[kVecPairs<DT>], float mean, float rstd, int col)
-{
-    Pair w[kVecPairs<DT>], b[kVecPairs<DT>];
-    load_coefficients<DT, WF32>(p.w, col, 1.0f, w);
-    load_coefficients<DT, WF32>(p.b, col, 0.0f, b);
-    return normalise_vector<DT>(h, mean, rstd, w, b);
-}
-
 // h of a vector: x, or x + residual rounded to the type.
 template <int DT>
 __device__ __forceinline__ void sum_vector(const uint4 &x, const uint4 &res, Pair (&h)[kVecPairs<DT>], uint4 &packed)
@@ -338,6 +362,7 @@ __global__ void __launch_bounds__(kRowBlock<TPR>) norm_fwd_cluster_kernel(const 
     const int row_vecs = p.cols / kN;
     uint32_t acc = 0;
     if (threadIdx.x == 0) block_key = 0u;
+    const HeldCoefficients<DT, WF32, kVecs> weight(p.w, 1.0f, t, TPR, row_vecs), shift(p.b, 0.0f, t, TPR, row_vecs);
     for (int64_t r = first; r < p.rows; r += step, turn ^= 1) {
         const uint4 *px = reinterpret_cast<const uint4 *>(static_cast<const uint8_t *>(p.x) + r * p.ld_x * kSize);
         const uint4 *pr = reinterpret_cast<const uint4 *>(static_cast<const uint8_t *>(p.res) + r * p.ld_res * kSize);
@@ -369,7 +394,10 @@ __global__ void __launch_bounds__(kRowBlock<TPR>) norm_fwd_cluster_kernel(const 
         for (int i = 0; i < kVecs; ++i) {
             const int v = t + i * TPR;
             if (v >= row_vecs) continue;
-            const uint4 y = normalise_vector<DT, WF32>(p, h[i], mean, rstd, v * kN);
+            Pair w[kPairs], b[kPairs];
+            weight.get(i, v * kN, w);
+            shift.get(i, v * kN, b);
+            const uint4 y = normalise_vector<DT>(h[i], mean, rstd, w, b);
             acc = fold_vector<DT>(acc, y);
             if (p.y) reinterpret_cast<uint4 *>(static_cast<uint8_t *>(p.y) + r * p.ld_y * kSize)[v] = y;
             stage[((r - first) / gridDim.x + group) * row_vecs + v] = y;
@@ -545,38 +573,73 @@ struct NormBwd {
     AmaxSink sink;
 };
 
-// Any sizes and alignment: a block per row at a time; the rows of a block add up in its own line of the workspace.
-template <int DT>
-__global__ void __launch_bounds__(kNormThreads) norm_bwd_any_kernel(const NormBwd p)
+// Any sizes and alignment, element by element: T threads a row at a time.  HELD > 0: a thread holds that many elements and the
+// sums of their columns; 0: any length, the sums of a block's rows grow in its own line of the workspace.
+template <int DT, int T, int HELD>
+__global__ void __launch_bounds__(T) norm_bwd_any_kernel(const NormBwd p)
 {
-    __shared__ float part[2][2][kNormThreads / 32];
+    constexpr int kTurns = HELD ? HELD : 1;
+    __shared__ float2 part[2][T / 32];
     uint32_t key = 0;
     int turn = 0;
     float *pw = p.part_w ? p.part_w + (int64_t)blockIdx.x * p.cols : nullptr;
     float *pb = p.part_b ? p.part_b + (int64_t)blockIdx.x * p.cols : nullptr;
+    float sum_w[kTurns], sum_b[kTurns], held_dy[kTurns], held_h[kTurns];
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) sum_w[i] = sum_b[i] = 0.0f;
     for (int64_t r = blockIdx.x; r < p.rows; r += gridDim.x, turn ^= 1) {
-        const float mean = p.layer ? p.mean[r] : 0.0f, rstd = p.rstd[r];
         const bool first = r == blockIdx.x;
-        float s1 = 0.0f, s2 = 0.0f;
-        for (int j = threadIdx.x; j < p.cols; j += kNormThreads) {
-            const float dy = load1<DT>(p.dy, r * p.ld_dy + j), xh = (load1<DT>(p.h, r * p.ld_h + j) - mean) * rstd;
-            const float g = p.w ? dy * load_any(p.w, p.w_dt, j) : dy;
-            s1 += g;
-            s2 = __fmaf_rn(g, xh, s2);
-            if (pw) pw[j] = __fmaf_rn(dy, xh, first ? 0.0f : pw[j]);
-            if (pb) pb[j] = first ? dy : pb[j] + dy;
+        // f(dy, h, column, place), for all of the thread's
+        auto each = [&](auto f) {
+            if (HELD) {
+#pragma unroll
+                for (int i = 0; i < kTurns; ++i)
+                    if ((int)threadIdx.x + i * T < p.cols) f(held_dy[i], held_h[i], (int)threadIdx.x + i * T, i);
+            } else {
+                for (int j = threadIdx.x; j < p.cols; j += T) f(load1<DT>(p.dy, r * p.ld_dy + j), load1<DT>(p.h, r * p.ld_h + j), j, 0);
+            }
+        };
+        if (HELD) {
+#pragma unroll
+            for (int i = 0; i < kTurns; ++i) {
+                const int j = (int)threadIdx.x + i * T;
+                if (j >= p.cols) continue;
+                held_dy[i] = load1<DT>(p.dy, r * p.ld_dy + j);
+                held_h[i] = load1<DT>(p.h, r * p.ld_h + j);
+            }
         }
+        const float mean = p.layer ? p.mean[r] : 0.0f, rstd = p.rstd[r];
+        float2 s = make_float2(0.0f, 0.0f);
+        each([&](float dy, float h, int j, int i) {
+            const float xh = (h - mean) * rstd, g = p.w ? dy * load_any(p.w, p.w_dt, j) : dy;
+            s = make_float2(s.x + g, __fmaf_rn(g, xh, s.y));
+            if (HELD) {
+                sum_w[i] = __fmaf_rn(dy, xh, sum_w[i]);
+                sum_b[i] += dy;
+            } else {
+                if (pw) pw[j] = __fmaf_rn(dy, xh, first ? 0.0f : pw[j]);
+                if (pb) pb[j] = first ? dy : pb[j] + dy;
+            }
+        });
         if (!p.dx) continue;
-        const float c1 = p.layer ? block_sum<kNormThreads>(s1, part[turn][0]) * p.inv_cols : 0.0f;
-        const float c2 = block_sum<kNormThreads>(s2, part[turn][1]) * p.inv_cols;
-        for (int j = threadIdx.x; j < p.cols; j += kNormThreads) {
-            const float dy = load1<DT>(p.dy, r * p.ld_dy + j), xh = (load1<DT>(p.h, r * p.ld_h + j) - mean) * rstd;
-            const float g = p.w ? dy * load_any(p.w, p.w_dt, j) : dy;
+        s = block_sum2<T>(s, part[turn]);
+        const float c1 = p.layer ? s.x * p.inv_cols : 0.0f, c2 = s.y * p.inv_cols;
+        each([&](float dy, float h, int j, int) {
+            const float xh = (h - mean) * rstd, g = p.w ? dy * load_any(p.w, p.w_dt, j) : dy;
             float v = rstd * (g - c1 - xh * c2);
             if (p.dh) v += load1<DT>(p.dh, r * p.ld_dh + j);
             const uint32_t bits = element_bits<DT>(v);
             key = max(key, magnitude_key(element_value<DT>(bits)));
             store_bits<DT>(p.dx, r * p.ld_dx + j, bits);
+        });
+    }
+    if (HELD) {
+#pragma unroll
+        for (int i = 0; i < kTurns; ++i) {
+            const int j = (int)threadIdx.x + i * T;
+            if (j >= p.cols) continue;
+            if (pw) pw[j] = sum_w[i];
+            if (pb) pb[j] = sum_b[i];
         }
     }
     sink_amax(key, p.sink);
@@ -761,6 +824,19 @@ static void by_row_shape(int cols, F f)
     else if (cols <= 8192) f(RowHold<256, 32>{});
     else f(RowHold<512, 32>{});
 }
+// Rows that are no whole vectors, or too long: threads, and elements that each of them holds (none: the row is walked).
+template <typename F>
+static void by_element_shape(int cols, F f)
+{
+    if (cols <= 512) f(RowHold<64, 8>{});
+    else if (cols <= 1024) f(RowHold<128, 8>{});
+    else if (cols <= 2048) f(RowHold<256, 8>{});
+    else if (cols <= 4096) f(RowHold<512, 8>{});
+    else if (cols <= 8192) f(RowHold<1024, 8>{});
+    else if (cols <= 16384) f(RowHold<1024, 16>{});
+    else f(RowHold<256, 0>{});
+}
+
 // Blocks an SM, and rows on their way for each group, that shared memory allows; false where not two rows fit.
 static bool ring_size(int most_blocks, int groups, int64_t slot, int &blocks, int &depth)
 {
@@ -774,8 +850,8 @@ static bool ring_size(int most_blocks, int groups, int64_t slot, int &blocks, in
 }
 constexpr int kRingBytes = (227 << 10) - 2048;
 
-// Two passes as one launch of one cluster: up to eight blocks, whose rows of y fit their shared memory.
-constexpr int kClusterBlocks = 8, kClusterStage = 96 << 10;
+// Two passes as one launch of one cluster: up to eight blocks with two rows (or two times four) one after the other.
+constexpr int kClusterBlocks = 8, kClusterRows = 2, kClusterStage = 96 << 10;
 
 template <int DT, bool WF32>
 static bool launch_fwd_cluster(const NormFwd &p, cudaStream_t st, cudaError_t &e)
@@ -786,8 +862,8 @@ static bool launch_fwd_cluster(const NormFwd &p, cudaStream_t st, cudaError_t &e
         const int64_t blocks = (p.rows + kGroups - 1) / kGroups;
         int cluster = 1;
         while (cluster < kClusterBlocks && cluster < blocks) cluster *= 2;
-        const int64_t stage = (blocks + cluster - 1) / cluster * kGroups * p.cols * InType<DT>::kBytes;
-        if (stage > kClusterStage) return;
+        const int64_t each = (blocks + cluster - 1) / cluster, stage = each * kGroups * p.cols * InType<DT>::kBytes;
+        if (each > kClusterRows || stage > kClusterStage) return;
         cudaLaunchAttribute attr[1];
         attr[0].id = cudaLaunchAttributeClusterDimension;
         attr[0].val.clusterDim.x = (unsigned)cluster;
@@ -885,16 +961,17 @@ static cudaError_t launch_fwd(const fp8_ctx *ctx, NormFwd p, bool two, cudaStrea
         if (two && launch_fwd_cluster<DT, WF32>(p, st, e)) return e;
         if (launch_fwd_rows<DT, WF32>(ctx, p, two, st, e)) return e;
     }
-    const unsigned grid = blocks_for_rows(ctx, p.rows, 8);
-    const int32_t *bias = p.bias;
-    if (two) p.bias = nullptr;
-    count_launch();
-    norm_fwd_any_kernel<DT, false><<<grid, kNormThreads, 0, st>>>(p);
-    if (two) {
-        p.bias = bias;
+    NormFwd once = p;
+    if (two) once.bias = nullptr;
+    by_element_shape(p.cols, [&](auto s) {
+        constexpr int kThreads = decltype(s)::kThreads, kElements = decltype(s)::kElements;
+        const unsigned grid = blocks_for_rows(ctx, p.rows, 1536 / kThreads);
         count_launch();
-        norm_fwd_any_kernel<DT, true><<<grid, kNormThreads, 0, st>>>(p);
-    }
+        norm_fwd_any_kernel<DT, false, kThreads, kElements><<<grid, kThreads, 0, st>>>(once);
+        if (!two) return;
+        count_launch();
+        norm_fwd_any_kernel<DT, true, kThreads, kElements><<<grid, kThreads, 0, st>>>(p);
+    });
     return cudaGetLastError();
 }
 
@@ -938,10 +1015,13 @@ static unsigned launch_bwd(const fp8_ctx *ctx, NormBwd p, bool want_w, bool want
             done = true;
         });
     if (!done) {
-        grid = bwd_blocks(ctx, p.rows, 4, sums, p.cols);
-        lines();
-        count_launch();
-        norm_bwd_any_kernel<DT><<<grid, kNormThreads, 0, st>>>(p);
+        by_element_shape(p.cols, [&](auto s) {
+            constexpr int kThreads = decltype(s)::kThreads, kElements = decltype(s)::kElements;
+            grid = bwd_blocks(ctx, p.rows, 1024 / kThreads, sums, p.cols);
+            lines();
+            count_launch();
+            norm_bwd_any_kernel<DT, kThreads, kElements><<<grid, kThreads, 0, st>>>(p);
+        });
     }
     return grid;
 }

@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from ctypes import c_int, c_int32, c_int64, c_uint, c_uint64, c_void_p, c_float, c_char_p, POINTER, byref
 
 import torch
@@ -126,23 +127,12 @@ _lib.fp8_attn_paged.argtypes = [_P, POINTER(KvCacheDesc), POINTER(SeqBatchDesc),
                                 c_float, c_int32, c_int, _P]
 
 
-class NormFwdDesc(ctypes.Structure):
-    """``fp8_norm_fwd_t``."""
-    _fields_ = [(n, c_void_p) for n in ("x", "residual", "weight", "bias_vec", "h", "y", "d_mean", "d_rstd", "y8", "d_bias_in",
-                                        "d_amax", "d_bias_out")] + \
-               [(n, c_int64) for n in ("rows", "cols", "ld_x", "ld_residual", "ld_h", "ld_y")] + \
-               [(n, c_int32) for n in ("kind", "dt", "w_dt", "conv", "margin")] + [("eps", c_float)]
+# ``fp8_norm_fwd_t`` and ``fp8_norm_bwd_t``, field by field (packing is several times quicker than a ctypes.Structure)
+_NORM_FWD = struct.Struct("@12P6q5if")
+_NORM_BWD = struct.Struct("@10P6q4i")
 
-
-class NormBwdDesc(ctypes.Structure):
-    """``fp8_norm_bwd_t``."""
-    _fields_ = [(n, c_void_p) for n in ("dy", "h", "dh", "weight", "d_mean", "d_rstd", "dx", "dw", "db", "d_amax")] + \
-               [(n, c_int64) for n in ("rows", "cols", "ld_dy", "ld_h", "ld_dh", "ld_dx")] + \
-               [(n, c_int32) for n in ("kind", "dt", "w_dt", "reserved")]
-
-
-_lib.fp8_norm_fwd.argtypes = [_P, POINTER(NormFwdDesc), _P]
-_lib.fp8_norm_bwd.argtypes = [_P, POINTER(NormBwdDesc), _P]
+_lib.fp8_norm_fwd.argtypes = [_P, c_char_p, _P]
+_lib.fp8_norm_bwd.argtypes = [_P, c_char_p, _P]
 _logits_args = [_P, _P, c_int, c_int64, c_int64, c_int64, c_float]
 _list_args = [_P, c_int, c_int64, _P, c_int64, c_int32, c_int]
 _lib.fp8_token_logprobs.argtypes = _logits_args + [_P, c_int, _P, _P, _P, _P, c_int32, _P, _P, _P]
@@ -315,6 +305,9 @@ _IT = {torch.int32: I32, torch.int64: I64}
 
 def _matrix(t, shape, dtypes, what, device):
     """Check a 2-D tensor (shape, one of the types, contiguous rows, the context's GPU); its row distance in elements."""
+    own = t.shape
+    if t.get_device() == device and t.dtype in dtypes and len(own) == 2 and (shape is None or own == shape) and t.is_contiguous():
+        return own[1]
     if t.get_device() != device:
         raise ValueError(f"{what}: a tensor on GPU {device} expected, got one on {t.device}")
     if t.dtype not in dtypes:
@@ -331,6 +324,8 @@ def _matrix(t, shape, dtypes, what, device):
 
 def _vector(t, n, dtypes, what, device, strided=False):
     """Check a 1-D tensor of n elements (contiguous, or any distance with ``strided``); the distance of its elements."""
+    if t.get_device() == device and t.dtype in dtypes and t.dim() == 1 and t.numel() == n and t.is_contiguous():
+        return 1
     if t.get_device() != device:
         raise ValueError(f"{what}: a tensor on GPU {device} expected, got one on {t.device}")
     if t.dtype not in dtypes:
@@ -344,7 +339,8 @@ def _address(t):
     return None if t is None else t.data_ptr()
 
 
-_F32 = (torch.float32,)
+_F32, _U8, _INT32 = (torch.float32,), (torch.uint8,), (torch.int32,)
+_WITH_F32 = {torch.bfloat16: (torch.bfloat16, torch.float32), torch.float16: (torch.float16, torch.float32), torch.float32: _F32}
 
 MATMUL_FWD, MATMUL_DGRAD, MATMUL_WGRAD = 0, 1, 2
 
@@ -653,62 +649,94 @@ class Context:
                  d_rstd=None, y8=None, d_bias=None, d_amax_out=None, d_bias_out=None, conv=CONV_PAPER, margin=0):
         """``fp8_norm_fwd``: x, residual, h, y [rows, cols] of one type; weight, bias_vec [cols] of that type or float32;
         y8 uint8 [rows, cols]; d_bias: the bias to cast under, None for that of Eq. 3 (d_bias_out)."""
-        dev = self.device
+        dev, dtype = self.device, x.dtype
         ld_x = _matrix(x, None, _DT, "x", dev)
-        shape, dt = x.shape, (x.dtype,)
+        shape, dt = x.shape, (dtype,)
         rows, cols = shape
-        lds = [0 if t is None else _matrix(t, shape, dt, what, dev) for t, what in ((residual, "residual"), (h, "h"), (y, "y"))]
-        w_dt = self._vectors(((weight, "weight"), (bias_vec, "bias_vec")), cols, x.dtype)
-        for t, n, want, what in ((d_mean, rows, _F32, "d_mean"), (d_rstd, rows, _F32, "d_rstd"), (d_amax_out, 1, _F32, "d_amax_out"),
-                                 (d_bias, 1, (torch.int32,), "d_bias"), (d_bias_out, 1, (torch.int32,), "d_bias_out")):
-            if t is not None:
-                _vector(t, n, want, what, dev)
-        if y8 is not None and _matrix(y8, shape, (torch.uint8,), "y8", dev) != cols:
-            raise ValueError("y8: contiguous bytes expected")
+        ld_r = ld_h = ld_y = p_r = p_h = p_y = p_y8 = p_mean = p_rstd = p_b = p_a = p_o = 0
+        if residual is not None:
+            ld_r, p_r = _matrix(residual, shape, dt, "residual", dev), residual.data_ptr()
+        if h is not None:
+            ld_h, p_h = _matrix(h, shape, dt, "h", dev), h.data_ptr()
+        if y is not None:
+            ld_y, p_y = _matrix(y, shape, dt, "y", dev), y.data_ptr()
+        if y8 is not None:
+            if _matrix(y8, shape, _U8, "y8", dev) != cols:
+                raise ValueError("y8: contiguous bytes expected")
+            p_y8 = y8.data_ptr()
+        w_dt, p_w = self._coefficients(weight, cols, dtype, None, "weight")
+        w_dt, p_v = self._coefficients(bias_vec, cols, dtype, w_dt, "bias_vec")
+        if d_mean is not None:
+            _vector(d_mean, rows, _F32, "d_mean", dev)
+            p_mean = d_mean.data_ptr()
+        if d_rstd is not None:
+            _vector(d_rstd, rows, _F32, "d_rstd", dev)
+            p_rstd = d_rstd.data_ptr()
+        if d_bias is not None:
+            _vector(d_bias, 1, _INT32, "d_bias", dev)
+            p_b = d_bias.data_ptr()
+        if d_amax_out is not None:
+            _vector(d_amax_out, 1, _F32, "d_amax_out", dev)
+            p_a = d_amax_out.data_ptr()
+        if d_bias_out is not None:
+            _vector(d_bias_out, 1, _INT32, "d_bias_out", dev)
+            p_o = d_bias_out.data_ptr()
         if rows == 0:
             return
-        desc = NormFwdDesc(x.data_ptr(), _address(residual), _address(weight), _address(bias_vec), _address(h), _address(y),
-                           _address(d_mean), _address(d_rstd), _address(y8), _address(d_bias), _address(d_amax_out),
-                           _address(d_bias_out), rows, cols, ld_x, *lds, kind, _DT[x.dtype], w_dt, conv, margin, eps)
-        status = _lib.fp8_norm_fwd(self._h, byref(desc), _raw_stream(dev))
+        code = _DT[dtype]
+        status = _lib.fp8_norm_fwd(self._h, _NORM_FWD.pack(x.data_ptr(), p_r, p_w, p_v, p_h, p_y, p_mean, p_rstd, p_y8, p_b, p_a, p_o, rows,
+                                                           cols, ld_x, ld_r, ld_h, ld_y, kind, code, code if w_dt is None else _DT[w_dt],
+                                                           conv, margin, eps), _raw_stream(dev))
         if status:
             _check(status, "fp8_norm_fwd")
 
     def norm_bwd(self, dy, h, weight, d_mean, d_rstd, dx, dh=None, dw=None, db=None, d_amax=None, kind=NORM_LAYER):
         """``fp8_norm_bwd``: dy, h, dh, dx [rows, cols] of one type; weight, dw, db [cols] of that type or float32; d_mean
         (None for NORM_RMS), d_rstd float32 [rows]."""
-        dev = self.device
+        dev, dtype = self.device, dy.dtype
         ld_dy = _matrix(dy, None, _DT, "dy", dev)
-        shape, dt = dy.shape, (dy.dtype,)
+        shape, dt = dy.shape, (dtype,)
         rows, cols = shape
+        ld_dh = ld_dx = p_dh = p_dx = p_mean = p_rstd = p_a = 0
         ld_h = _matrix(h, shape, dt, "h", dev)
-        ld_dh, ld_dx = [0 if t is None else _matrix(t, shape, dt, what, dev) for t, what in ((dh, "dh"), (dx, "dx"))]
-        w_dt = self._vectors(((weight, "weight"), (dw, "dw"), (db, "db")), cols, dy.dtype)
-        for t, n, what in ((d_mean, rows, "d_mean"), (d_rstd, rows, "d_rstd"), (d_amax, 1, "d_amax")):
-            if t is not None:
-                _vector(t, n, _F32, what, dev)
+        if dh is not None:
+            ld_dh, p_dh = _matrix(dh, shape, dt, "dh", dev), dh.data_ptr()
+        if dx is not None:
+            ld_dx, p_dx = _matrix(dx, shape, dt, "dx", dev), dx.data_ptr()
+        w_dt, p_w = self._coefficients(weight, cols, dtype, None, "weight")
+        w_dt, p_dw = self._coefficients(dw, cols, dtype, w_dt, "dw")
+        w_dt, p_db = self._coefficients(db, cols, dtype, w_dt, "db")
+        if d_mean is not None:
+            _vector(d_mean, rows, _F32, "d_mean", dev)
+            p_mean = d_mean.data_ptr()
+        if d_rstd is not None:
+            _vector(d_rstd, rows, _F32, "d_rstd", dev)
+            p_rstd = d_rstd.data_ptr()
+        if d_amax is not None:
+            _vector(d_amax, 1, _F32, "d_amax", dev)
+            p_a = d_amax.data_ptr()
         if rows == 0:
             for t in (dw, db):
                 if t is not None:
                     t.zero_()
             return
-        desc = NormBwdDesc(dy.data_ptr(), h.data_ptr(), _address(dh), _address(weight), _address(d_mean), _address(d_rstd),
-                           _address(dx), _address(dw), _address(db), _address(d_amax), rows, cols, ld_dy, ld_h, ld_dh, ld_dx, kind,
-                           _DT[dy.dtype], w_dt, 0)
-        status = _lib.fp8_norm_bwd(self._h, byref(desc), _raw_stream(dev))
+        code = _DT[dtype]
+        status = _lib.fp8_norm_bwd(self._h, _NORM_BWD.pack(dy.data_ptr(), h.data_ptr(), p_dh, p_w, p_mean, p_rstd, p_dx, p_dw, p_db, p_a, rows,
+                                                           cols, ld_dy, ld_h, ld_dh, ld_dx, kind, code, code if w_dt is None else _DT[w_dt],
+                                                           0), _raw_stream(dev))
         if status:
             _check(status, "fp8_norm_bwd")
 
-    def _vectors(self, named, cols, dtype):
-        """Check vectors of ``cols`` elements, all of one type: ``dtype`` or float32; that type."""
-        w_dt = None
-        for t, what in named:
-            if t is not None:
-                _vector(t, cols, (dtype,) if dtype == torch.float32 else (dtype, torch.float32), what, self.device)
-                if w_dt not in (None, t.dtype):
-                    raise ValueError(f"{what}: the type of the other vectors ({w_dt}) expected, got {t.dtype}")
-                w_dt = t.dtype
-        return _DT[w_dt or dtype]
+    def _coefficients(self, t, cols, dtype, others, what):
+        """Check a vector of ``cols`` elements of ``dtype`` or float32, all of a call's of one type (``others``, None: the
+        first); that type and the address."""
+        if t is None:
+            return others, 0
+        own = t.dtype
+        _vector(t, cols, _WITH_F32[dtype], what, self.device)
+        if others is not None and own != others:
+            raise ValueError(f"{what}: the type of the other vectors ({others}) expected, got {own}")
+        return own, t.data_ptr()
 
     # -- a head's losses (include/fp8_loss.h); calls without rows check their arguments and launch nothing -----------------
     def _logits(self, logits, scale):

@@ -117,20 +117,37 @@ HANDLE = ctypes.cast(FAKE, ctypes.c_void_p)
 A = 1 << 20   # an aligned address that is never read
 
 
+class NormFwdDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("x", "residual", "weight", "bias_vec", "h", "y", "d_mean", "d_rstd", "y8", "d_bias_in", "d_amax",
+                                               "d_bias_out")] + \
+               [(n, ctypes.c_int64) for n in ("rows", "cols", "ld_x", "ld_residual", "ld_h", "ld_y")] + \
+               [(n, ctypes.c_int32) for n in ("kind", "dt", "w_dt", "conv", "margin")] + [("eps", ctypes.c_float)]
+
+
+class NormBwdDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("dy", "h", "dh", "weight", "d_mean", "d_rstd", "dx", "dw", "db", "d_amax")] + \
+               [(n, ctypes.c_int64) for n in ("rows", "cols", "ld_dy", "ld_h", "ld_dh", "ld_dx")] + \
+               [(n, ctypes.c_int32) for n in ("kind", "dt", "w_dt", "reserved")]
+
+
+def test_the_binding_packs_the_structures():
+    assert fp8lin._NORM_FWD.size == ctypes.sizeof(NormFwdDesc) and fp8lin._NORM_BWD.size == ctypes.sizeof(NormBwdDesc)
+
+
 def norm_fwd(ctx=HANDLE, **change):
-    d = fp8lin.NormFwdDesc(x=A, residual=A, weight=A, bias_vec=A, h=A, y=A, d_mean=A, d_rstd=A, y8=A, d_bias_in=None, d_amax=A, d_bias_out=A,
-                           rows=4, cols=32, ld_x=32, ld_residual=32, ld_h=32, ld_y=32, kind=0, dt=0, w_dt=0, conv=0, margin=0, eps=1e-5)
+    d = NormFwdDesc(x=A, residual=A, weight=A, bias_vec=A, h=A, y=A, d_mean=A, d_rstd=A, y8=A, d_bias_in=None, d_amax=A, d_bias_out=A,
+                    rows=4, cols=32, ld_x=32, ld_residual=32, ld_h=32, ld_y=32, kind=0, dt=0, w_dt=0, conv=0, margin=0, eps=1e-5)
     for k, v in change.items():
         setattr(d, k, v)
-    return fp8lin._lib.fp8_norm_fwd(ctx, ctypes.byref(d), None)
+    return fp8lin._lib.fp8_norm_fwd(ctx, bytes(d), None)
 
 
 def norm_bwd(ctx=HANDLE, **change):
-    d = fp8lin.NormBwdDesc(dy=A, h=A, dh=A, weight=A, d_mean=A, d_rstd=A, dx=A, dw=A, db=A, d_amax=A, rows=4, cols=32, ld_dy=32, ld_h=32,
-                           ld_dh=32, ld_dx=32, kind=0, dt=0, w_dt=0, reserved=0)
+    d = NormBwdDesc(dy=A, h=A, dh=A, weight=A, d_mean=A, d_rstd=A, dx=A, dw=A, db=A, d_amax=A, rows=4, cols=32, ld_dy=32, ld_h=32,
+                    ld_dh=32, ld_dx=32, kind=0, dt=0, w_dt=0, reserved=0)
     for k, v in change.items():
         setattr(d, k, v)
-    return fp8lin._lib.fp8_norm_bwd(ctx, ctypes.byref(d), None)
+    return fp8lin._lib.fp8_norm_bwd(ctx, bytes(d), None)
 
 
 E = fp8lin
