@@ -22,6 +22,9 @@ Scaling policies (``scaling=``):
 mode the weight is quantised once and cached until ``train()`` is called again
 or ``requantise()`` is asked for (post-training quantisation); activations of at
 most 64 KB are then quantised inside the matmul's own launch.
+
+``Norm`` and ``Fp8NormLinear`` put the decoder's norm in front of it (``include/fp8_norm.h``): the residual sum, layer norm or
+its root-mean-square form, and, in the second, the linear whose FP8 input the norm writes itself.
 """
 from __future__ import annotations
 
@@ -45,6 +48,27 @@ def default_context(device: int) -> "fp8lin.Context":
 def _out_dtype(dt):
     """The library writes bf16 or fp32: fp16 tensors get bf16 results."""
     return dt if dt in (torch.bfloat16, torch.float32) else torch.bfloat16
+
+
+def _backward_matmuls(layer, g8, x8, w8, b_fwd, dx_dtype, want_dw):
+    """(dX [T, K] of ``dx_dtype``, or None without one; dW in the weight's type, or None) from the FP8 bytes of a step."""
+    lib, bg, (T, N), K = layer.ctx, layer.bias_words[_G:_G + 1], g8.shape, layer.in_features
+    dx = dw = None
+    if dx_dtype is not None:
+        dx = torch.empty((T, K), dtype=dx_dtype, device=g8.device)
+    if want_dw:
+        dw = torch.empty((N, K), dtype=_out_dtype(layer.weight.dtype), device=g8.device)
+    if dx is not None and dw is not None:
+        # the two backward matmuls share dY8 and do not depend on each other (Section 2.2): one launch
+        lib.linear_group([(fp8lin.MATMUL_DGRAD, g8, bg, w8, b_fwd[_W:_W + 1], dx),
+                          (fp8lin.MATMUL_WGRAD, g8, bg, x8, b_fwd[_X:_X + 1], dw)], conv=layer.conv)
+    elif dx is not None:
+        lib.linear_dgrad(g8, bg, w8, None, b_fwd[_W:_W + 1], dx, conv=layer.conv)
+    elif dw is not None:
+        lib.linear_wgrad(g8, None, bg, x8, None, b_fwd[_X:_X + 1], dw, T, conv=layer.conv)
+    if dw is not None and dw.dtype != layer.weight.dtype:
+        dw = dw.to(layer.weight.dtype)
+    return dx, dw
 
 
 class _Fp8LinearFn(torch.autograd.Function):
@@ -92,8 +116,7 @@ class _Fp8LinearFn(torch.autograd.Function):
     @staticmethod
     def backward(fn, dy):
         layer = fn.layer
-        lib = layer.ctx
-        K, N = layer.in_features, layer.out_features
+        N = layer.out_features
         x8, w8, b_fwd = fn.saved_tensors
         T = x8.shape[0]
         dy2 = dy.reshape(T, N)
@@ -101,24 +124,11 @@ class _Fp8LinearFn(torch.autograd.Function):
             dy2 = dy2.contiguous()
         g8 = torch.empty((T, N), dtype=torch.uint8, device=dy2.device)
         layer._quantise(fp8lin.E5, dy2, _G, g8, margin=layer.margin)
-        bg = layer.bias_words[_G:_G + 1]
-        dx = dw = db = None
-        if fn.needs_input_grad[0]:
-            dx = torch.empty((T, K), dtype=_out_dtype(dy.dtype), device=dy2.device)
-        if fn.needs_input_grad[1]:
-            dw = torch.empty((N, K), dtype=_out_dtype(layer.weight.dtype), device=dy2.device)
-        if dx is not None and dw is not None:
-            # the two backward matmuls share dY8 and do not depend on each other (Section 2.2): one launch
-            lib.linear_group([(fp8lin.MATMUL_DGRAD, g8, bg, w8, b_fwd[_W:_W + 1], dx),
-                              (fp8lin.MATMUL_WGRAD, g8, bg, x8, b_fwd[_X:_X + 1], dw)], conv=layer.conv)
-        elif dx is not None:
-            lib.linear_dgrad(g8, bg, w8, None, b_fwd[_W:_W + 1], dx, conv=layer.conv)
-        elif dw is not None:
-            lib.linear_wgrad(g8, None, bg, x8, None, b_fwd[_X:_X + 1], dw, T, conv=layer.conv)
+        dx, dw = _backward_matmuls(layer, g8, x8, w8, b_fwd, _out_dtype(dy.dtype) if fn.needs_input_grad[0] else None,
+                                   fn.needs_input_grad[1])
+        db = None
         if dx is not None:
             dx = dx.reshape(fn.x_shape)
-        if dw is not None and dw.dtype != layer.weight.dtype:
-            dw = dw.to(layer.weight.dtype)
         if fn.has_bias and fn.needs_input_grad[2]:
             db = dy2.sum(0, dtype=torch.float32).to(layer.bias.dtype)   # not part of the paper's layer
         return dx, dw, db, None
@@ -196,3 +206,169 @@ class Fp8Linear(torch.nn.Module):
     def extra_repr(self):
         return (f"in_features={self.in_features}, out_features={self.out_features}, bias={self.bias is not None}, "
                 f"scaling={self.scaling}, margin={self.margin}")
+
+
+# -- the norm in front of a linear -----------------------------------------------------------------------------------------
+_NORM_KINDS = {"layer": fp8lin.NORM_LAYER, "rms": fp8lin.NORM_RMS}
+
+
+def _norm_rows(x, residual, features):
+    """x and the residual as [rows, features] with contiguous rows."""
+    if x.shape[-1] != features or (residual is not None and (residual.shape != x.shape or residual.dtype != x.dtype)):
+        raise ValueError(f"x [..., {features}] and a residual of its shape and type expected, got {tuple(x.shape)} {x.dtype}"
+                         + ("" if residual is None else f" and {tuple(residual.shape)} {residual.dtype}"))
+    return [None if t is None else t.reshape(-1, features) if t.stride(-1) == 1 else t.reshape(-1, features).contiguous()
+            for t in (x, residual)]
+
+
+def _norm_statistics(rows, kind, device):
+    """Buffers of a forward pass: (mean or None, 1 / standard deviation)."""
+    f32 = dict(dtype=torch.float32, device=device)
+    return (torch.empty(rows, **f32) if kind == fp8lin.NORM_LAYER else None), torch.empty(rows, **f32)
+
+
+def _norm_backward(layer, dy, h, weight, mean, rstd, dh, want_w, want_b):
+    """(gradient of the sum, of the weight, of the additive vector) in h's and the weight's types."""
+    dx = torch.empty(h.shape, dtype=h.dtype, device=h.device)
+    dw = torch.empty_like(weight) if want_w else None
+    db = torch.empty_like(weight) if want_b else None
+    if dh is not None:
+        dh = dh.reshape(h.shape)
+        dh = dh if dh.stride(-1) == 1 else dh.contiguous()
+    layer.ctx.norm_bwd(dy, h, weight, mean, rstd, dx, dh=dh, dw=dw, db=db, kind=layer.norm_kind)
+    return dx, dw, db
+
+
+class _NormFn(torch.autograd.Function):
+    """(y, h); h is x itself where there is no residual (and then not an output)."""
+
+    @staticmethod
+    def forward(fn, x, residual, weight, bias, layer):
+        x2, r2 = _norm_rows(x, residual, layer.features)
+        h = x2 if r2 is None else torch.empty(x2.shape, dtype=x.dtype, device=x.device)
+        y = torch.empty(x2.shape, dtype=x.dtype, device=x.device)
+        mean, rstd = _norm_statistics(x2.shape[0], layer.norm_kind, x.device)
+        layer.ctx.norm_fwd(x2, weight.detach(), None if bias is None else bias.detach(), residual=r2, eps=layer.eps, kind=layer.norm_kind,
+                           h=None if r2 is None else h, y=y, d_mean=mean, d_rstd=rstd)
+        fn.layer, fn.shape, fn.with_h = layer, x.shape, r2 is not None
+        fn.set_materialize_grads(False)
+        fn.save_for_backward(h, weight, mean, rstd)
+        y = y.reshape(x.shape)
+        return (y, h.reshape(x.shape)) if fn.with_h else y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(fn, dy, dh=None):
+        h, weight, mean, rstd = fn.saved_tensors
+        if dy is None:
+            return dh, dh if fn.with_h else None, None, None, None
+        dy = dy.reshape(h.shape)
+        dx, dw, db = _norm_backward(fn.layer, dy if dy.stride(-1) == 1 else dy.contiguous(), h, weight, mean, rstd, dh,
+                                    fn.needs_input_grad[2], fn.needs_input_grad[3])
+        dx = dx.reshape(fn.shape)
+        return dx, dx if fn.with_h else None, dw, db, None
+
+
+class Norm(torch.nn.Module):
+    """Layer norm (``kind="layer"``, with an additive vector) or its root-mean-square form (``"rms"``) over the last dimension.
+
+    ``forward(x)`` gives y; ``forward(x, residual)`` gives (y, x + residual), both from one call.  x bf16, fp16 or fp32, y of
+    its type; weight and bias of that type or float32."""
+
+    def __init__(self, features: int, kind: str = "layer", eps: float = 1e-5, device="cuda", dtype=torch.bfloat16,
+                 ctx: Optional["fp8lin.Context"] = None):
+        super().__init__()
+        if kind not in _NORM_KINDS:
+            raise ValueError("kind must be 'layer' or 'rms'")
+        dev = torch.device(device)
+        self.features, self.kind, self.norm_kind, self.eps = features, kind, _NORM_KINDS[kind], float(eps)
+        self.ctx = ctx if ctx is not None else default_context(dev.index or 0)
+        self.weight = torch.nn.Parameter(torch.ones(features, device=dev, dtype=dtype))
+        self.bias = torch.nn.Parameter(torch.zeros(features, device=dev, dtype=dtype)) if kind == "layer" else None
+
+    def forward(self, x, residual=None):
+        return _NormFn.apply(x, residual, self.weight, self.bias, self)
+
+    def extra_repr(self):
+        return f"{self.features}, kind={self.kind}, eps={self.eps}"
+
+
+class _Fp8NormLinearFn(torch.autograd.Function):
+    """(linear(norm(x + residual)), x + residual); the sum is an output only where there is a residual."""
+
+    @staticmethod
+    def forward(fn, x, residual, norm_weight, norm_bias, weight, bias_vec, layer):
+        lib, K, N = layer.ctx, layer.in_features, layer.out_features
+        x2, r2 = _norm_rows(x, residual, K)
+        T, dev = x2.shape[0], x2.device
+        h = x2 if r2 is None else torch.empty(x2.shape, dtype=x.dtype, device=dev)
+        x8 = torch.empty((T, K), dtype=torch.uint8, device=dev)
+        y = torch.empty((T, N), dtype=layer.out_dtype or _out_dtype(x.dtype), device=dev)
+        mean, rstd = _norm_statistics(T, layer.norm_kind, dev)
+        am, bi = layer.amax, layer.bias_words
+        constant = layer.scaling == "constant"
+        w8, w8_is_old = layer._quantised_weight(weight)
+        lib.norm_fwd(x2, norm_weight.detach(), None if norm_bias is None else norm_bias.detach(), residual=r2, eps=layer.eps,
+                     kind=layer.norm_kind, h=None if r2 is None else h, d_mean=mean, d_rstd=rstd, y8=x8,
+                     d_bias=bi[_X:_X + 1] if constant else None, d_amax_out=None if constant else am[_X:_X + 1],
+                     d_bias_out=None if constant else bi[_X:_X + 1], conv=layer.conv)
+        run = lib.linear_infer if (not layer.training) and w8_is_old else lib.linear_fwd
+        run(x8, bi[_X:_X + 1], w8, bi[_W:_W + 1], y, bias_vec=bias_vec, conv=layer.conv)
+        fn.layer, fn.shape, fn.with_h, fn.has_bias = layer, x.shape, r2 is not None, bias_vec is not None
+        fn.set_materialize_grads(False)
+        fn.save_for_backward(h, norm_weight, mean, rstd, x8, w8, bi[:2].clone())
+        y = y.reshape(*x.shape[:-1], N)
+        return (y, h.reshape(x.shape)) if fn.with_h else y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(fn, dy, dh=None):
+        layer = fn.layer
+        h, norm_weight, mean, rstd, x8, w8, b_fwd = fn.saved_tensors
+        if dy is None:
+            return dh, dh if fn.with_h else None, None, None, None, None, None
+        T, N = x8.shape[0], layer.out_features
+        dy2 = dy.reshape(T, N)
+        if not dy2.is_contiguous():
+            dy2 = dy2.contiguous()
+        g8 = torch.empty((T, N), dtype=torch.uint8, device=dy2.device)
+        layer._quantise(fp8lin.E5, dy2, _G, g8, margin=layer.margin)
+        need = fn.needs_input_grad
+        # the gradient of the norm's output has the sum's type (FP16: by way of FP32, the library writes no FP16)
+        through = need[0] or need[1] or need[2] or need[3]
+        dn, dw = _backward_matmuls(layer, g8, x8, w8, b_fwd, (torch.float32 if h.dtype == torch.float16 else h.dtype) if through else None,
+                                   need[4])
+        dx = d_norm_w = d_norm_b = db = None
+        if through:
+            dn = dn.to(h.dtype)
+            dx, d_norm_w, d_norm_b = _norm_backward(layer, dn, h, norm_weight, mean, rstd, dh, need[2], need[3])
+            dx = dx.reshape(fn.shape)
+        if fn.has_bias and need[5]:
+            db = dy2.sum(0, dtype=torch.float32).to(layer.bias.dtype)   # not part of the paper's layer
+        return dx, dx if fn.with_h else None, d_norm_w, d_norm_b, dw, db, None
+
+
+class Fp8NormLinear(Fp8Linear):
+    """``Norm`` and ``Fp8Linear`` as one: the norm writes the FP8 bytes that the matmul reads, under the bias of their amax
+    (``scaling="amax"``, Eq. 3 just in time) or a constant one, and its 16-bit output does not exist.
+
+    ``forward(x)`` gives the linear's output, ``forward(x, residual)`` that and x + residual.  Parameters: those of
+    ``Fp8Linear`` and ``norm_weight`` and, with ``kind="layer"``, ``norm_bias``."""
+
+    def __init__(self, in_features: int, out_features: int, kind: str = "layer", eps: float = 1e-5, norm_dtype=None, device="cuda",
+                 dtype=torch.bfloat16, scaling: str = "amax", **kw):
+        if kind not in _NORM_KINDS:
+            raise ValueError("kind must be 'layer' or 'rms'")
+        if scaling == "predicted":
+            raise ValueError("scaling must be 'amax' or 'constant': the norm has no bytes before its amax to guess for")
+        super().__init__(in_features, out_features, device=device, dtype=dtype, scaling=scaling, **kw)
+        self.kind, self.norm_kind, self.eps = kind, _NORM_KINDS[kind], float(eps)
+        like = dict(device=self.weight.device, dtype=norm_dtype or dtype)
+        self.norm_weight = torch.nn.Parameter(torch.ones(in_features, **like))
+        self.norm_bias = torch.nn.Parameter(torch.zeros(in_features, **like)) if kind == "layer" else None
+
+    def forward(self, x, residual=None):
+        return _Fp8NormLinearFn.apply(x, residual, self.norm_weight, self.norm_bias, self.weight, self.bias, self)
+
+    def extra_repr(self):
+        return f"{super().extra_repr()}, kind={self.kind}, eps={self.eps}"

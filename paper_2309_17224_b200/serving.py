@@ -18,7 +18,7 @@ from typing import Callable, Dict, List, Optional, Sequence
 import torch
 
 from . import fp8lin
-from .module import Fp8Linear, default_context
+from .module import Fp8Linear, Fp8NormLinear, default_context
 
 
 class PagePool:
@@ -93,11 +93,14 @@ class Fp8SelfAttention(torch.nn.Module):
     The tokens are those of ``batch`` (``PagePool.batch``), sequence after sequence; their keys and values enter ``cache``
     and each attends causally to its sequence's cached tokens.  Calls that share ``ctx`` (by default the device's
     ``default_context``) must not overlap on the GPU: a program that runs prefill and decoding on two streams gives the layers
-    of each a context of its own."""
+    of each a context of its own.
+
+    With ``norm`` ("layer" or "rms") the layer's norm is in front of the QKV linear and writes its FP8 input; ``forward`` then
+    takes the residual as well, and gives the layer's output and the sum x + residual (x without one)."""
 
     def __init__(self, hidden: int, q_heads: int, kv_heads: int, head_dim: int, cache: "fp8lin.KvCache", device="cuda",
                  rotate: Optional[Callable[[torch.Tensor, torch.Tensor, "fp8lin.SeqBatch"], None]] = None,
-                 ctx: Optional["fp8lin.Context"] = None):
+                 ctx: Optional["fp8lin.Context"] = None, norm: Optional[str] = None, eps: float = 1e-5):
         super().__init__()
         if q_heads % kv_heads or (cache.kv_heads, cache.head_dim) != (kv_heads, head_dim):
             raise ValueError("q_heads a multiple of kv_heads; the cache has this layer's kv_heads and head_dim")
@@ -105,20 +108,30 @@ class Fp8SelfAttention(torch.nn.Module):
         self.cache, self.rotate = cache, rotate
         self.ctx = ctx if ctx is not None else default_context(torch.device(device).index or 0)
         # (attention reads bf16 queries whatever x is)
-        self.qkv = Fp8Linear(hidden, (q_heads + 2 * kv_heads) * head_dim, device=device, out_dtype=torch.bfloat16, ctx=self.ctx)
+        self.norm = norm
+        qkv = dict(device=device, out_dtype=torch.bfloat16, ctx=self.ctx)
+        if norm is None:
+            self.qkv = Fp8Linear(hidden, (q_heads + 2 * kv_heads) * head_dim, **qkv)
+        else:
+            self.qkv = Fp8NormLinear(hidden, (q_heads + 2 * kv_heads) * head_dim, kind=norm, eps=eps, norm_dtype=torch.float32, **qkv)
         self.out = Fp8Linear(q_heads * head_dim, hidden, device=device, ctx=self.ctx)
         self.eval()
 
     @torch.no_grad()
-    def forward(self, x: torch.Tensor, batch: "fp8lin.SeqBatch") -> torch.Tensor:
+    def forward(self, x: torch.Tensor, batch: "fp8lin.SeqBatch", residual: Optional[torch.Tensor] = None):
+        if residual is not None and self.norm is None:
+            raise ValueError("a residual goes with a layer that has a norm")
         if x.shape[0] == 0:                  # no sequence has new tokens
-            return torch.empty(x.shape, dtype=torch.bfloat16, device=x.device)
+            y = torch.empty(x.shape, dtype=torch.bfloat16, device=x.device)
+            return y if self.norm is None else (y, x)
         hq, hk = self.q_heads, self.kv_heads
-        qkv = self.qkv(x).unflatten(1, (hq + 2 * hk, self.head_dim))
+        qkv, h = (self.qkv(x), x) if residual is None else self.qkv(x, residual)
+        qkv = qkv.unflatten(1, (hq + 2 * hk, self.head_dim))
         q, k, v = qkv[:, :hq], qkv[:, hq:hq + hk], qkv[:, hq + hk:]
         if self.rotate is not None:
             self.rotate(q, k, batch)
         self.ctx.kv_append(self.cache, batch, k, v)
         o = torch.empty((x.shape[0], hq, self.head_dim), dtype=torch.bfloat16, device=x.device)
         self.ctx.attn_paged(self.cache, batch, q, o, causal=True)
-        return self.out(o.flatten(1))
+        y = self.out(o.flatten(1))
+        return y if self.norm is None else (y, h)
