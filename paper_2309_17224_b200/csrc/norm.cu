@@ -44,9 +44,10 @@ __device__ __forceinline__ float shift_at(const void *b, int w_dt, int j) { retu
 // Any sizes and alignment, element by element: T threads a row.  HELD > 0: a thread holds that many elements (T * HELD >= cols) and
 // the row is read once; 0: any length, three walks over it.  CAST_ONLY: the statistics are there, bytes are wanted.
 template <int DT, bool CAST_ONLY, int T, int HELD>
-__global__ void __launch_bounds__(T) norm_fwd_any_kernel(const NormFwd p)
+__global__ void __launch_bounds__(T, 1024 / T) norm_fwd_any_kernel(const NormFwd p)
 {
     constexpr int kTurns = HELD ? HELD : 1;
+    constexpr bool kAhead = HELD > 0 && HELD <= 8;   // the next row's elements are on their way while this one is reduced
     __shared__ float part[T / 32];
     __shared__ float2 part2[T / 32];
     uint32_t key = 0;
@@ -65,8 +66,22 @@ __global__ void __launch_bounds__(T) norm_fwd_any_kernel(const NormFwd p)
             held_b[i] = j < p.cols ? shift_at(p.b, p.w_dt, j) : 0.0f;
         }
     }
+    const bool from_h = CAST_ONLY && p.h;
+    float x[kTurns], res[kTurns];
+    auto fetch = [&](int64_t r) {
+#pragma unroll
+        for (int i = 0; i < kTurns; ++i) {
+            const int j = (int)threadIdx.x + i * T;
+            x[i] = res[i] = 0.0f;
+            if (j >= p.cols) continue;
+            x[i] = from_h ? load1<DT>(p.h, r * p.ld_h + j) : load1<DT>(p.x, r * p.ld_x + j);
+            if (p.res && !from_h) res[i] = load1<DT>(p.res, r * p.ld_res + j);
+        }
+    };
+    if (kAhead && blockIdx.x < p.rows) fetch(blockIdx.x);
     for (int64_t r = blockIdx.x; r < p.rows; r += gridDim.x) {
         float held[kTurns];
+        const int64_t next = r + gridDim.x;
         auto sum_at = [&](int j) {
             float v = load1<DT>(p.x, r * p.ld_x + j);
             if (p.res) v = element_value<DT>(element_bits<DT>(v + load1<DT>(p.res, r * p.ld_res + j)));
@@ -83,12 +98,13 @@ __global__ void __launch_bounds__(T) norm_fwd_any_kernel(const NormFwd p)
             }
         };
         if (HELD) {
-            const bool from_h = CAST_ONLY && p.h;
+            if (!kAhead) fetch(r);
 #pragma unroll
             for (int i = 0; i < kTurns; ++i) {
-                const int j = (int)threadIdx.x + i * T;
-                if (j < p.cols) held[i] = from_h ? load1<DT>(p.h, r * p.ld_h + j) : sum_at(j);
+                held[i] = x[i];
+                if (p.res && !from_h) held[i] = element_value<DT>(element_bits<DT>(x[i] + res[i]));
             }
+            if (kAhead && next < p.rows) fetch(next);
         }
         float mean = 0.0f, rstd;
         if (CAST_ONLY) {
@@ -148,11 +164,14 @@ template <int DT>
 constexpr int kPerVec = DT == FP8_F32 ? 4 : 8;
 template <int TPR>
 constexpr int kRowBlock = TPR < 128 ? 128 : TPR;   // threads of a block: four rows at a time where a warp holds one
-// Blocks that an SM's registers hold at once, which the grids are made of (as far as shared memory allows): each walks its
-// share of the rows, and a block more than that would walk its share alone at the end.
-template <int TPR, int EPT, bool SUMS>
-constexpr int kResident = SUMS ? (TPR == 32 ? (EPT == 8 ? 6 : EPT == 16 ? 5 : 3) : TPR == 128 ? (EPT == 16 ? 5 : 3) : TPR == 256 ? 2 : 1)
-                               : (TPR == 32 ? (EPT == 8 ? 8 : EPT == 16 ? 6 : 4) : TPR == 128 ? (EPT == 16 ? 6 : 4) : TPR == 256 ? 2 : 1);
+// Blocks of the forward kernels that an SM's registers hold at once, which their grids are made of (as far as shared memory
+// allows): each walks its share of the rows, and a block more than that would walk its share alone at the end.
+template <int TPR, int EPT>
+constexpr int kResident = TPR == 32 ? (EPT == 8 ? 8 : EPT == 16 ? 6 : 4) : TPR == 128 ? (EPT == 16 ? 6 : 4) : TPR == 256 ? 2 : 1;
+// Groups of TPR threads of the backward kernel's block, of which an SM has one: the sums of its rows leave it as one line.
+template <int TPR, int EPT>
+constexpr int kSumGroups = TPR == 32 ? (EPT == 8 ? 24 : EPT == 16 ? 16 : 12) : TPR == 128 ? (EPT == 16 ? 5 : 3) : TPR == 256 ? 2 : 1;
+constexpr int kMostGroups = 24;
 
 // The launch behind may start when no block of this one waits for a place any more; it waits for this one's end itself.
 __device__ __forceinline__ void launch_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
@@ -161,10 +180,8 @@ __device__ __forceinline__ void wait_for_launch_before() { asm volatile("griddep
 // The rows that a group of TPR threads walks, on their way into shared memory `depth` rows ahead: bulk copies that one thread
 // starts.  Neither registers nor a barrier wait for the memory, and a row's 32 elements a thread leave time for little else.
 constexpr int kMostAhead = 4;
-template <int TPR>
 struct RowRing {
-    static constexpr int kGroups = kRowBlock<TPR> / TPR;
-    uint64_t full[kGroups][kMostAhead];
+    uint64_t full[kMostGroups][kMostAhead];
     int abort_flag;
 };
 struct RowSource {
@@ -176,17 +193,17 @@ struct RowSource {
 template <int TPR>
 struct RowWalk {
     const RowSource &src;
-    RowRing<TPR> &ring;
+    RowRing &ring;
     uint8_t *slots;           // this group's
     uint32_t slot_bytes;
     int depth, group;
     unsigned *d_status;
-    __device__ __forceinline__ RowWalk(const RowSource &s, RowRing<TPR> &r, uint8_t *smem, int ahead, unsigned *status)
+    __device__ __forceinline__ RowWalk(const RowSource &s, RowRing &r, uint8_t *smem, int ahead, unsigned *status)
         : src(s), ring(r), slot_bytes(s.row_bytes * s.inputs), depth(ahead), group(threadIdx.x / TPR), d_status(status)
     {
         slots = smem + (uint64_t)group * depth * slot_bytes;
         if (threadIdx.x == 0) {
-            for (int g = 0; g < RowRing<TPR>::kGroups; ++g)
+            for (int g = 0; g < (int)blockDim.x / TPR; ++g)
                 for (int i = 0; i < kMostAhead; ++i) mbar_init(smem_u32(&ring.full[g][i]), 1);
             ring.abort_flag = 0;
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -442,11 +459,11 @@ __global__ void __launch_bounds__(kRowBlock<TPR>) norm_fwd_cluster_kernel(const 
 // where a row's fixed cost (two sums over its threads, 150 instructions a thread) meets 32 elements a thread; with 16 it was
 // bound by its instructions.
 template <int DT, bool WF32, int TPR, int EPT>
-__global__ void __launch_bounds__(kRowBlock<TPR>, kResident<TPR, EPT, false>) norm_fwd_rows_kernel(const NormFwd p, const RowSource src, int depth)
+__global__ void __launch_bounds__(kRowBlock<TPR>, kResident<TPR, EPT>) norm_fwd_rows_kernel(const NormFwd p, const RowSource src, int depth)
 {
     constexpr int kN = kPerVec<DT>, kPairs = kVecPairs<DT>, kVecs = EPT / kN, kSize = InType<DT>::kBytes, kGroups = kRowBlock<TPR> / TPR;
     extern __shared__ __align__(16) uint8_t slots[];
-    __shared__ RowRing<TPR> ring;
+    __shared__ RowRing ring;
     __shared__ float part[TPR / 32];
     __shared__ float2 part2[2][TPR / 32];
     launch_next();
@@ -511,11 +528,11 @@ __global__ void __launch_bounds__(kRowBlock<TPR>, kResident<TPR, EPT, false>) no
 // The bytes of y from the sums and the statistics of the launch before, under the bias that it left.  Last rows first: what the
 // launch before wrote last is what L2 holds.
 template <int DT, bool WF32, int TPR, int EPT>
-__global__ void __launch_bounds__(kRowBlock<TPR>, kResident<TPR, EPT, false>) norm_cast_rows_kernel(const NormFwd p, const RowSource src, int depth)
+__global__ void __launch_bounds__(kRowBlock<TPR>, kResident<TPR, EPT>) norm_cast_rows_kernel(const NormFwd p, const RowSource src, int depth)
 {
     constexpr int kN = kPerVec<DT>, kPairs = kVecPairs<DT>, kVecs = EPT / kN, kGroups = kRowBlock<TPR> / TPR;
     extern __shared__ __align__(16) uint8_t slots[];
-    __shared__ RowRing<TPR> ring;
+    __shared__ RowRing ring;
     const RowWalk<TPR> walk(src, ring, slots, depth, p.sink.d_status);
     const int t = threadIdx.x % TPR, group = threadIdx.x / TPR;
     const int64_t step = (int64_t)gridDim.x * kGroups;
@@ -576,7 +593,7 @@ struct NormBwd {
 // Any sizes and alignment, element by element: T threads a row at a time.  HELD > 0: a thread holds that many elements and the
 // sums of their columns; 0: any length, the sums of a block's rows grow in its own line of the workspace.
 template <int DT, int T, int HELD>
-__global__ void __launch_bounds__(T) norm_bwd_any_kernel(const NormBwd p)
+__global__ void __launch_bounds__(T, 1024 / T) norm_bwd_any_kernel(const NormBwd p)
 {
     constexpr int kTurns = HELD ? HELD : 1;
     __shared__ float2 part[2][T / 32];
@@ -645,18 +662,20 @@ __global__ void __launch_bounds__(T) norm_bwd_any_kernel(const NormBwd p)
     sink_amax(key, p.sink);
 }
 
-// The same for rows of whole vectors: TPR threads hold, for all rows of their block, the sums of their own columns.
+// The same for rows of whole vectors: groups of TPR threads, each with rows of its own, for all of which a thread holds the sums of
+// its columns.
 template <int DT, bool WF32, int TPR, int EPT>
-__global__ void __launch_bounds__(kRowBlock<TPR>, kResident<TPR, EPT, true>) norm_bwd_rows_kernel(const NormBwd p, const RowSource src, int depth)
+__global__ void __launch_bounds__(kSumGroups<TPR, EPT> * TPR, 1) norm_bwd_rows_kernel(const NormBwd p, const RowSource src, int depth)
 {
-    constexpr int kN = kPerVec<DT>, kPairs = kVecPairs<DT>, kVecs = EPT / kN, kSize = InType<DT>::kBytes, kGroups = kRowBlock<TPR> / TPR;
+    constexpr int kN = kPerVec<DT>, kPairs = kVecPairs<DT>, kVecs = EPT / kN, kSize = InType<DT>::kBytes;
     extern __shared__ __align__(16) uint8_t slots[];
-    __shared__ RowRing<TPR> ring;
-    __shared__ float2 part[2][TPR / 32];
+    __shared__ RowRing ring;
+    __shared__ float2 part[kSumGroups<TPR, EPT>][2][TPR / 32];
     launch_next();
     const RowWalk<TPR> walk(src, ring, slots, depth, p.sink.d_status);
     const int t = threadIdx.x % TPR, group = threadIdx.x / TPR;
-    const int64_t step = (int64_t)gridDim.x * kGroups;
+    const int groups = (int)blockDim.x / TPR;
+    const int64_t step = (int64_t)gridDim.x * groups;
     const int row_vecs = p.cols / kN;
     uint32_t acc = 0, parity = 0;
     int slot = 0, turn = 0;
@@ -666,7 +685,7 @@ __global__ void __launch_bounds__(kRowBlock<TPR>, kResident<TPR, EPT, true>) nor
 #pragma unroll
         for (int k = 0; k < kPairs; ++k) sum_w[i][k] = sum_b[i][k] = pair_of(0.0f);
     const HeldCoefficients<DT, WF32, kVecs> weight(p.w, 1.0f, t, TPR, row_vecs);
-    int64_t r = (int64_t)blockIdx.x * kGroups + group;
+    int64_t r = (int64_t)blockIdx.x * groups + group;
     if (t == 0)
         for (int i = 0; i < depth && r + i * step < p.rows; ++i) walk.start(r + i * step, i);
     float next_mean = 0.0f, next_rstd = 0.0f;
@@ -697,7 +716,7 @@ __global__ void __launch_bounds__(kRowBlock<TPR>, kResident<TPR, EPT, true>) nor
                 sum_b[i][k] = sum_b[i][k] + y[k];
             }
         }
-        const float2 s = block_sum2<TPR>(make_float2(sum_of(p1), sum_of(p2)), part[turn]);
+        const float2 s = group_sum2<TPR>(make_float2(sum_of(p1), sum_of(p2)), part[group][turn], group);
         // every thread is done with the row before (a barrier, or the warp's exchange, lies behind it): its slot is free
         if (TPR == 32) __syncwarp();
         if (t == 0 && behind && r + (depth - 1) * step < p.rows) walk.start(r + (depth - 1) * step, slot == 0 ? depth - 1 : slot - 1);
@@ -729,38 +748,30 @@ __global__ void __launch_bounds__(kRowBlock<TPR>, kResident<TPR, EPT, true>) nor
             parity ^= 1u;
         }
     }
-    if (p.part_w || p.part_b) {
-        __shared__ float4 lines[kGroups > 1 ? kGroups : 1][kGroups > 1 ? TPR * EPT / 4 : 1];
+    // the groups' sums meet where their rows were, and leave as one line
+    float *lines = reinterpret_cast<float *>(slots);
 #pragma unroll
-        for (int which = 0; which < 2; ++which) {
-            float *out = which ? p.part_b : p.part_w;
-            if (!out) continue;
-            out += (int64_t)blockIdx.x * p.cols;
-            if (kGroups > 1) __syncthreads();
+    for (int which = 0; which < 2; ++which) {
+        float *out = which ? p.part_b : p.part_w;
+        if (!out) continue;
+        __syncthreads();
 #pragma unroll
-            for (int i = 0; i < kVecs; ++i) {
-                const int v = t + i * TPR;
-                if (v >= row_vecs) continue;
+        for (int i = 0; i < kVecs; ++i) {
+            const int v = t + i * TPR;
+            if (v >= row_vecs) continue;
 #pragma unroll
-                for (int k = 0; k < kN; k += 4) {
-                    float4 f;
-                    split(which ? sum_b[i][k / 2] : sum_w[i][k / 2], f.x, f.y);
-                    split(which ? sum_b[i][k / 2 + 1] : sum_w[i][k / 2 + 1], f.z, f.w);
-                    if (kGroups > 1) lines[group][(v * kN + k) / 4] = f;
-                    else reinterpret_cast<float4 *>(out)[(v * kN + k) / 4] = f;
-                }
+            for (int k = 0; k < kN; k += 4) {
+                float4 f;
+                split(which ? sum_b[i][k / 2] : sum_w[i][k / 2], f.x, f.y);
+                split(which ? sum_b[i][k / 2 + 1] : sum_w[i][k / 2 + 1], f.z, f.w);
+                reinterpret_cast<float4 *>(lines + (int64_t)group * p.cols)[(v * kN + k) / 4] = f;
             }
-            if (kGroups > 1) {
-                __syncthreads();
-                for (int j = threadIdx.x; j < p.cols / 4; j += kRowBlock<TPR>) {
-                    float4 f = lines[0][j];
-#pragma unroll
-                    for (int g = 1; g < kGroups; ++g) {
-                        f.x += lines[g][j].x; f.y += lines[g][j].y; f.z += lines[g][j].z; f.w += lines[g][j].w;
-                    }
-                    reinterpret_cast<float4 *>(out)[j] = f;
-                }
-            }
+        }
+        __syncthreads();
+        for (int j = threadIdx.x; j < p.cols; j += (int)blockDim.x) {
+            float s = lines[j];
+            for (int g = 1; g < groups; ++g) s += lines[(int64_t)g * p.cols + j];
+            out[(int64_t)blockIdx.x * p.cols + j] = s;
         }
     }
     sink_amax(folded_key<DT>(acc), p.sink);
@@ -841,14 +852,14 @@ static void by_element_shape(int cols, F f)
 static bool ring_size(int most_blocks, int groups, int64_t slot, int &blocks, int &depth)
 {
     for (blocks = most_blocks; blocks > 0; --blocks) {
-        const int64_t each = (227 << 10) / blocks - 2048 - (blocks > 1 ? 1024 : 0);   // (beside the fixed part)
+        const int64_t each = (227 << 10) / blocks - 3072 - (blocks > 1 ? 1024 : 0);   // (beside the fixed part)
         depth = (int)(each / (groups * slot));
         if (depth > kMostAhead) depth = kMostAhead;
         if (depth >= 2) return true;
     }
     return false;
 }
-constexpr int kRingBytes = (227 << 10) - 2048;
+constexpr int kRingBytes = (227 << 10) - 3072;
 
 // Two passes as one launch of one cluster: up to eight blocks with two rows (or two times four) one after the other.
 constexpr int kClusterBlocks = 8, kClusterRows = 2, kClusterStage = 96 << 10;
@@ -901,7 +912,7 @@ static bool launch_fwd_rows(const fp8_ctx *ctx, const NormFwd &p, bool two, cuda
         int resident, depth;
         auto grid = [&] { return (unsigned)std::min(blocks, (int64_t)ctx->sm_count * resident); };
         auto bytes = [&](const RowSource &from) { return (size_t)kGroups * depth * from.row_bytes * from.inputs; };
-        if (!ring_size(kResident<kThreads, kElements, false>, kGroups, (int64_t)src.row_bytes * src.inputs, resident, depth)) return;
+        if (!ring_size(kResident<kThreads, kElements>, kGroups, (int64_t)src.row_bytes * src.inputs, resident, depth)) return;
         NormFwd once = p;
         if (two) once.bias = nullptr;
         count_launch();
@@ -910,7 +921,7 @@ static bool launch_fwd_rows(const fp8_ctx *ctx, const NormFwd &p, bool two, cuda
         done = true;
         if (!two || e != cudaSuccess) return;
         const RowSource sums = p.h ? row_source(DT, p.cols, p.h, p.ld_h, nullptr, 0, nullptr, 0) : src;
-        ring_size(kResident<kThreads, kElements, false>, kGroups, (int64_t)sums.row_bytes * sums.inputs, resident, depth);
+        ring_size(kResident<kThreads, kElements>, kGroups, (int64_t)sums.row_bytes * sums.inputs, resident, depth);
         e = launch_dependent_with(norm_cast_rows_kernel<DT, WF32, kThreads, kElements>, grid(), kBlock, bytes(sums), st, p, sums, depth);
     });
     return done;
@@ -926,8 +937,7 @@ static cudaError_t allow_shared()
             if (e == cudaSuccess) e = cudaFuncSetAttribute(norm_fwd_cluster_kernel<DT, WF32, decltype(s)::kThreads, decltype(s)::kElements>, attr, kClusterStage);
             if (e == cudaSuccess) e = cudaFuncSetAttribute(norm_fwd_rows_kernel<DT, WF32, decltype(s)::kThreads, decltype(s)::kElements>, attr, kRingBytes);
             if (e == cudaSuccess) e = cudaFuncSetAttribute(norm_cast_rows_kernel<DT, WF32, decltype(s)::kThreads, decltype(s)::kElements>, attr, kRingBytes);
-            constexpr int kBwdBytes = kRingBytes - (decltype(s)::kThreads == 32 ? 17 << 10 : 0);
-            if (e == cudaSuccess) e = cudaFuncSetAttribute(norm_bwd_rows_kernel<DT, WF32, decltype(s)::kThreads, decltype(s)::kElements>, attr, kBwdBytes);
+            if (e == cudaSuccess) e = cudaFuncSetAttribute(norm_bwd_rows_kernel<DT, WF32, decltype(s)::kThreads, decltype(s)::kElements>, attr, kRingBytes);
         });
     }
     return e;
@@ -965,7 +975,7 @@ static cudaError_t launch_fwd(const fp8_ctx *ctx, NormFwd p, bool two, cudaStrea
     if (two) once.bias = nullptr;
     by_element_shape(p.cols, [&](auto s) {
         constexpr int kThreads = decltype(s)::kThreads, kElements = decltype(s)::kElements;
-        const unsigned grid = blocks_for_rows(ctx, p.rows, 1536 / kThreads);
+        const unsigned grid = blocks_for_rows(ctx, p.rows, 1024 / kThreads);
         count_launch();
         norm_fwd_any_kernel<DT, false, kThreads, kElements><<<grid, kThreads, 0, st>>>(once);
         if (!two) return;
@@ -1003,15 +1013,16 @@ static unsigned launch_bwd(const fp8_ctx *ctx, NormBwd p, bool want_w, bool want
     const RowSource src = row_source(DT, p.cols, p.dy, p.ld_dy, p.h, p.ld_h, p.dh, p.ld_dh);
     if (fast)
         by_row_shape(p.cols, [&](auto s) {
-            constexpr int kThreads = decltype(s)::kThreads, kElements = decltype(s)::kElements, kBlock = kRowBlock<kThreads>, kGroups = kBlock / kThreads;
-            int resident, depth;
-            // (a warp's rows: the blocks' sums meet in 16 KB more)
-            const int64_t slot = (int64_t)src.row_bytes * src.inputs + (kThreads == 32 ? 2048 : 0);
-            if (!ring_size(kResident<kThreads, kElements, true>, kGroups, slot, resident, depth)) return;
-            grid = bwd_blocks(ctx, (p.rows + kGroups - 1) / kGroups, resident, sums, p.cols);
+            constexpr int kThreads = decltype(s)::kThreads, kElements = decltype(s)::kElements;
+            // as many groups as have rows and two slots each
+            const int64_t slot = (int64_t)src.row_bytes * src.inputs;
+            int groups = (int)std::min((int64_t)kSumGroups<kThreads, kElements>, (p.rows + ctx->sm_count - 1) / ctx->sm_count), blocks, depth = 0;
+            while (groups > 0 && !ring_size(1, groups, slot, blocks, depth)) --groups;
+            if (groups == 0) return;
+            grid = bwd_blocks(ctx, (p.rows + groups - 1) / groups, 1, sums, p.cols);
             lines();
             count_launch();
-            norm_bwd_rows_kernel<DT, WF32, kThreads, kElements><<<grid, kBlock, (size_t)kGroups * depth * src.row_bytes * src.inputs, st>>>(p, src, depth);
+            norm_bwd_rows_kernel<DT, WF32, kThreads, kElements><<<grid, groups * kThreads, (size_t)groups * depth * slot, st>>>(p, src, depth);
             done = true;
         });
     if (!done) {

@@ -236,6 +236,21 @@ __device__ __forceinline__ float2 block_sum2(float2 v, float2 *part)
     return v;
 }
 
+// The same over a group of THREADS of a block with several groups (each has its own `part`, and barrier).
+template <int THREADS>
+__device__ __forceinline__ float2 group_sum2(float2 v, float2 *part, int group)
+{
+    v = make_float2(warp_sum(v.x), warp_sum(v.y));
+    if (THREADS == 32) return v;
+    const int warp = (threadIdx.x % THREADS) >> 5;
+    if ((threadIdx.x & 31) == 0) part[warp] = v;
+    asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(THREADS) : "memory");
+    v = part[0];
+#pragma unroll
+    for (int i = 1; i < THREADS / 32; ++i) v = make_float2(v.x + part[i].x, v.y + part[i].y);
+    return v;
+}
+
 // Fold a thread's magnitude key into the sink; every thread of every block calls it once, at the end.
 __device__ __forceinline__ void sink_amax(uint32_t key, const AmaxSink &o)
 {
