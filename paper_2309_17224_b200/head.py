@@ -16,7 +16,7 @@ from typing import Optional
 
 import torch
 
-from .module import Fp8NormLinear, default_context
+from .module import Fp8NormLinear, default_context, matrix_rows
 
 
 def _tokens(logits, vocab):
@@ -25,8 +25,7 @@ def _tokens(logits, vocab):
     vocab = columns if vocab is None else vocab
     if not 0 < vocab <= columns:
         raise ValueError(f"vocab 1 .. {columns} expected, got {vocab}")
-    flat = logits.reshape(-1, columns)
-    return (flat if flat.stride(-1) == 1 else flat.contiguous())[:, :vocab]
+    return matrix_rows(logits, columns)[:, :vocab]
 
 
 def _gradient(logits, vocab):
@@ -134,6 +133,7 @@ class Fp8Head(Fp8NormLinear):
     def logprobs(self, x, targets, residual=None, scale: float = 1.0):
         return token_logprobs(self._logits(x, residual), targets, scale, self.vocab, self.ctx)
 
+    @torch.no_grad()
     def top(self, x, k: int, residual=None, scale: float = 1.0):
         return top_tokens(self._logits(x, residual), k, scale, self.vocab, self.ctx)
 

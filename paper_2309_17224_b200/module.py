@@ -212,13 +212,19 @@ class Fp8Linear(torch.nn.Module):
 _NORM_KINDS = {"layer": fp8lin.NORM_LAYER, "rms": fp8lin.NORM_RMS}
 
 
+def matrix_rows(t, columns):
+    """t as [rows, columns] with contiguous rows that do not overlap (gradients of sums and means are expanded numbers)."""
+    t = t.reshape(-1, columns)
+    plain = t.shape[0] <= 1 or t.stride(0) >= columns
+    return t if plain and (columns == 1 or t.stride(1) == 1) else t.contiguous()
+
+
 def _norm_rows(x, residual, features):
     """x and the residual as [rows, features] with contiguous rows."""
     if x.shape[-1] != features or (residual is not None and (residual.shape != x.shape or residual.dtype != x.dtype)):
         raise ValueError(f"x [..., {features}] and a residual of its shape and type expected, got {tuple(x.shape)} {x.dtype}"
                          + ("" if residual is None else f" and {tuple(residual.shape)} {residual.dtype}"))
-    return [None if t is None else t.reshape(-1, features) if t.stride(-1) == 1 else t.reshape(-1, features).contiguous()
-            for t in (x, residual)]
+    return matrix_rows(x, features), None if residual is None else matrix_rows(residual, features)
 
 
 def _norm_statistics(rows, kind, device):
@@ -233,8 +239,7 @@ def _norm_backward(layer, dy, h, weight, mean, rstd, dh, want_w, want_b):
     dw = torch.empty_like(weight) if want_w else None
     db = torch.empty_like(weight) if want_b else None
     if dh is not None:
-        dh = dh.reshape(h.shape)
-        dh = dh if dh.stride(-1) == 1 else dh.contiguous()
+        dh = matrix_rows(dh, h.shape[1])
     layer.ctx.norm_bwd(dy, h, weight, mean, rstd, dx, dh=dh, dw=dw, db=db, kind=layer.norm_kind)
     return dx, dw, db
 
@@ -262,9 +267,8 @@ class _NormFn(torch.autograd.Function):
         h, weight, mean, rstd = fn.saved_tensors
         if dy is None:
             return dh, dh if fn.with_h else None, None, None, None
-        dy = dy.reshape(h.shape)
-        dx, dw, db = _norm_backward(fn.layer, dy if dy.stride(-1) == 1 else dy.contiguous(), h, weight, mean, rstd, dh,
-                                    fn.needs_input_grad[2], fn.needs_input_grad[3])
+        dx, dw, db = _norm_backward(fn.layer, matrix_rows(dy, h.shape[1]), h, weight, mean, rstd, dh, fn.needs_input_grad[2],
+                                    fn.needs_input_grad[3])
         dx = dx.reshape(fn.shape)
         return dx, dx if fn.with_h else None, dw, db, None
 

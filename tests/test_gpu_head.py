@@ -53,6 +53,16 @@ def test_norm_module(M, kind, shape, dtype, w_dtype):
     if db is not None and norm.bias is not None:
         torch.testing.assert_close(norm.bias.grad.double(), db, rtol=half, atol=half * 8)
     assert torch.equal(xs.grad, rs.grad) and xs.grad.data_ptr() != rs.grad.data_ptr()
+    # inputs and gradients that are expanded numbers or rows
+    row = x.reshape(-1, n)[:1].expand(5, n)
+    a = row.detach().requires_grad_(True)
+    z, h1 = norm(a, row)
+    assert torch.equal(z[0], z[4]) and torch.equal(z[:1], norm(row[:1].clone(), row[:1].clone())[0])
+    (z.sum() + h1.mean(0).sum()).backward()
+    b = row.detach().clone().requires_grad_(True)
+    z, h1 = norm(b, row.clone())
+    torch.autograd.backward((z, h1), (torch.ones_like(z), torch.full_like(h1, 0.2)))
+    torch.testing.assert_close(a.grad.float(), b.grad.float(), rtol=2.0 ** -6, atol=2.0 ** -6)   # (a fifth is no bf16 number)
     # without a residual, and with one of the two outputs unused
     xs.grad = None
     y1 = norm(xs)
@@ -227,7 +237,7 @@ def test_a_training_step_from_a_graph(H):
 
     def step():
         loss = head.distill(fixed[0], fixed[2], fixed[3], residual=fixed[1]).mean()
-        return loss, torch.autograd.grad(loss, params)
+        return loss.detach(), torch.autograd.grad(loss, params)   # (no autograd graph outlives the step)
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):
@@ -242,7 +252,7 @@ def test_a_training_step_from_a_graph(H):
         graph.replay()
         replayed = [loss.clone()] + [g.clone() for g in grads]
         want, want_grads = step()
-        assert torch.equal(replayed[0], want.detach()) and all(torch.equal(g, w) for g, w in zip(replayed[1:], want_grads))
+        assert torch.equal(replayed[0], want) and all(torch.equal(g, w) for g, w in zip(replayed[1:], want_grads))
 
 
 @pytest.mark.parametrize("norm", ["layer", "rms"])

@@ -1,7 +1,10 @@
 """fp8_norm_fwd and fp8_norm_bwd against the definitions in 64 bits.
 
-Tolerances count roundings of 2^-24 (FP32) and one of the output's type.  A sum of n terms adds at most n/256 + 16 of them on
-one path (a thread's terms one after the other in blocks of 256 threads or more, then at most 16 joins)."""
+Tolerances count roundings of 2^-24 (FP32) and one of the output's type.  A sum of n terms adds at most n/256 + 32 of them on
+one path: a thread adds its terms (32 as two sums of 16: 17), a warp joins its lanes in 5, a block its warps one after the other.
+Whole vectors: a warp alone 22 (up to 1024 terms), 128 threads 25 (4096), 256 threads 29, 512 threads 37 (from 8193 on: 64 allowed).
+Element by element: 64 threads 14, 256 threads 20, 512 threads 28, 1024 threads 44 (from 4097 on: 48 allowed) or 52 (from 8193
+on); walked rows n/256 + 5 + 7."""
 import pytest
 import torch
 
@@ -43,7 +46,7 @@ def inputs(rows, cols, dtype, w_dtype, seed, residual, ld=None):
 
 def path(cols):
     """Roundings on the longest path of a sum over a row."""
-    return cols / 256 + 16
+    return cols / 256 + 32
 
 
 def check_norm(h, y, mean, rstd, w, b, layer, dtype, got_h, got_y, got_mean, got_rstd):
