@@ -19,18 +19,25 @@ struct NormFwd {
     const int32_t *bias;   // of y8: given, or what the first pass left
     int64_t rows, ld_x, ld_res, ld_h, ld_y;
     int cols, w_dt, delta, layer;
-    float eps, inv_cols;
+    double inv_cols;   // (averages are one product of 64 bits: an FP32 reciprocal would be off for all rows alike)
+    float eps;
     AmaxSink sink;
 };
 
 // Mean and sum of squared deviations of a row from its first estimate of the mean and the sums {d, d^2} of the deviations
 // from that.  The estimate carries the rounding of a sum of whole numbers; where the mean is far above the spread (eight times,
 // say), the mean of the small deviations corrects it, which is what keeps the spread's digits.
-__device__ __forceinline__ float2 corrected(float estimate, float2 sums, int cols, float inv_cols)
+__device__ __forceinline__ float average(float sum, double inv_cols) { return (float)((double)sum * inv_cols); }
+__device__ __forceinline__ float2 corrected(float estimate, float2 sums, int cols, double inv_cols)
 {
-    if (estimate * estimate <= 64.0f * sums.y * inv_cols) return make_float2(estimate, sums.y);
-    const float mean = __fmaf_rn(sums.x, inv_cols, estimate), e = mean - estimate;
+    if (estimate * estimate <= 64.0f * average(sums.y, inv_cols)) return make_float2(estimate, sums.y);
+    const float mean = estimate + average(sums.x, inv_cols), e = mean - estimate;
     return make_float2(mean, fmaxf(0.0f, __fmaf_rn(-e, __fmaf_rn(-(float)cols, e, 2.0f * sums.x), sums.y)));
+}
+
+__device__ __forceinline__ float inverse_deviation(float squares, const double inv_cols, float eps)
+{
+    return __frsqrt_rn((float)((double)squares * inv_cols + (double)eps));
 }
 
 template <int DT>
@@ -119,7 +126,7 @@ __global__ void __launch_bounds__(T, 1024 / T) norm_fwd_any_kernel(const NormFwd
                 s += v;
             });
             s = block_sum<T>(s, part);
-            if (p.layer) mean = s * p.inv_cols;
+            if (p.layer) mean = average(s, p.inv_cols);
             float2 q = make_float2(0.0f, 0.0f);
             each([&](float v, int, int) {
                 const float d = v - mean;
@@ -130,7 +137,7 @@ __global__ void __launch_bounds__(T, 1024 / T) norm_fwd_any_kernel(const NormFwd
                 q = corrected(mean, q, p.cols, p.inv_cols);
                 mean = q.x;
             }
-            rstd = __frsqrt_rn(__fmaf_rn(q.y, p.inv_cols, p.eps));
+            rstd = inverse_deviation(q.y, p.inv_cols, p.eps);
             if (threadIdx.x == 0) {
                 if (p.mean) p.mean[r] = mean;
                 if (p.rstd) p.rstd[r] = rstd;
@@ -360,7 +367,7 @@ __device__ __forceinline__ void row_statistics(const NormFwd &p, const Pair (&h)
         q = corrected(mean, q, p.cols, p.inv_cols);
         mean = q.x;
     }
-    rstd = __frsqrt_rn(__fmaf_rn(q.y, p.inv_cols, p.eps));
+    rstd = inverse_deviation(q.y, p.inv_cols, p.eps);
 }
 
 // Few rows whose bytes are wanted: the blocks are one cluster that knows the amax when its rows are done, and casts them from
@@ -401,7 +408,7 @@ __global__ void __launch_bounds__(kRowBlock<TPR>) norm_fwd_cluster_kernel(const 
 #pragma unroll
             for (int k = 0; k < kPairs; ++k) s = s + h[i][k];
         }
-        float mean = p.layer ? block_sum<TPR>(sum_of(s), part) * p.inv_cols : 0.0f, rstd;
+        float mean = p.layer ? average(block_sum<TPR>(sum_of(s), part), p.inv_cols) : 0.0f, rstd;
         row_statistics<TPR, kVecs, kPairs>(p, h, row_vecs - t, mean, rstd, part2[turn]);
         if (t == 0) {
             if (p.mean) p.mean[r] = mean;
@@ -493,7 +500,7 @@ __global__ void __launch_bounds__(kRowBlock<TPR>, kResident<TPR, EPT>) norm_fwd_
 #pragma unroll
             for (int k = 0; k < kPairs; ++k) s = s + h[i][k];
         }
-        float mean = p.layer ? block_sum<TPR>(sum_of(s), part) * p.inv_cols : 0.0f, rstd;
+        float mean = p.layer ? average(block_sum<TPR>(sum_of(s), part), p.inv_cols) : 0.0f, rstd;
         row_statistics<TPR, kVecs, kPairs>(p, h, row_vecs - t, mean, rstd, part2[turn]);
         // every thread has read its part of the slot (a barrier, or the warp's exchange, lies behind it)
         if (TPR == 32) __syncwarp();
@@ -1064,7 +1071,7 @@ fp8_status_t fp8_norm_fwd(fp8_ctx *ctx, const fp8_norm_fwd_t *a, void *stream)
     if (two && (!a->d_rstd || (a->kind == FP8_NORM_LAYER && !a->d_mean))) return FP8_ERR_NULL;
     NormFwd p = {a->x, a->residual, a->weight, a->bias_vec, a->h, a->y, a->d_mean, a->d_rstd, a->y8, two ? a->d_bias_out : a->d_bias_in,
                  a->rows, a->ld_x, a->ld_residual, a->ld_h, a->ld_y, (int)a->cols, a->w_dt, format_delta(FP8_E4, a->conv),
-                 a->kind == FP8_NORM_LAYER, a->eps, 1.0f / (float)a->cols,
+                 a->kind == FP8_NORM_LAYER, 1.0 / (double)a->cols, a->eps,
                  {nullptr, a->d_amax, a->d_bias_out, ctx->d_status, FP8_E4, a->conv, a->margin}};
     if (a->d_amax || a->d_bias_out) p.sink.slot = take_slot(ctx);
     cudaStream_t st = (cudaStream_t)stream;
