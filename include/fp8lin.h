@@ -90,13 +90,13 @@ typedef struct fp8_ctx fp8_ctx;
 
 /* Create / destroy a context on `device`.  The context owns its device
  * workspace: a status word, reduction slots and a 64 MB FP32 buffer for the
- * partial sums of split-contraction (decode-size) matmuls.  fp8_create is the
- * only call that allocates device memory; it also raises the dynamic
- * shared-memory limit of the matmul kernels.  It must not be called during
+ * partial sums of split-contraction (decode-size) matmuls and of a norm's
+ * weight gradient.  fp8_create is the only call that allocates device memory;
+ * it also raises the dynamic shared-memory limit of the kernels.  It must not be called during
  * stream capture.  The context-taking calls that enqueue work (fp8_amax,
- * fp8_scaling_bias, fp8_cast_*, fp8_ptq_weights, fp8_linear_*) neither
- * synchronise nor allocate, so a whole step of them can be captured into a
- * CUDA graph and replayed. */
+ * fp8_scaling_bias, fp8_cast_*, fp8_ptq_weights, fp8_linear_*, fp8_norm_*,
+ * fp8_token_logprobs*, fp8_distill_*) neither synchronise nor allocate, so a
+ * whole step of them can be captured into a CUDA graph and replayed. */
 FP8_API fp8_status_t fp8_create(fp8_ctx **ctx, int device);
 FP8_API fp8_status_t fp8_destroy(fp8_ctx *ctx);
 

@@ -24,10 +24,10 @@ struct NormFwd {
     AmaxSink sink;
 };
 
+__device__ __forceinline__ float average(float sum, double inv_cols) { return (float)((double)sum * inv_cols); }
 // Mean and sum of squared deviations of a row from its first estimate of the mean and the sums {d, d^2} of the deviations
 // from that.  The estimate carries the rounding of a sum of whole numbers; where the mean is far above the spread (eight times,
 // say), the mean of the small deviations corrects it, which is what keeps the spread's digits.
-__device__ __forceinline__ float average(float sum, double inv_cols) { return (float)((double)sum * inv_cols); }
 __device__ __forceinline__ float2 corrected(float estimate, float2 sums, int cols, double inv_cols)
 {
     if (estimate * estimate <= 64.0f * average(sums.y, inv_cols)) return make_float2(estimate, sums.y);
@@ -49,7 +49,9 @@ __device__ __forceinline__ float weight_at(const void *w, int w_dt, int j) { ret
 __device__ __forceinline__ float shift_at(const void *b, int w_dt, int j) { return b ? load_any(b, w_dt, j) : 0.0f; }
 
 // Any sizes and alignment, element by element: T threads a row.  HELD > 0: a thread holds that many elements (T * HELD >= cols) and
-// the row is read once; 0: any length, three walks over it.  CAST_ONLY: the statistics are there, bytes are wanted.
+// the row is read once; 0: any length, three walks over it.  CAST_ONLY: the statistics are there, bytes are wanted.  Bound by the
+// chain of a row (loads, two sums, stores): 1531 x 1027 FP32 in 10.4 us from a graph, of which an empty launch is 4.3 (1.2 TB/s);
+// 1098 x 969 BF16 with a residual 8.5, by three walks 10.5.
 template <int DT, bool CAST_ONLY, int T, int HELD>
 __global__ void __launch_bounds__(T, 1024 / T) norm_fwd_any_kernel(const NormFwd p)
 {
@@ -371,7 +373,8 @@ __device__ __forceinline__ void row_statistics(const NormFwd &p, const Pair (&h)
 }
 
 // Few rows whose bytes are wanted: the blocks are one cluster that knows the amax when its rows are done, and casts them from
-// shared memory in the same launch.
+// shared memory in the same launch.  Bound by the chain of one row (6.2 us from a graph for one row of 8192 BF16 with a residual,
+// an empty launch is 4.3); from the third row of a block on two launches are quicker (549 x 128: 22 us so, 8.4 in two).
 template <int DT, bool WF32, int TPR, int EPT>
 __global__ void __launch_bounds__(kRowBlock<TPR>) norm_fwd_cluster_kernel(const NormFwd p)
 {
@@ -462,9 +465,11 @@ __global__ void __launch_bounds__(kRowBlock<TPR>) norm_fwd_cluster_kernel(const 
     if (blocks > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// Any number of rows: one reading, whatever is asked for but bytes under a bias that the call itself finds.  Bound by the memory
-// where a row's fixed cost (two sums over its threads, 150 instructions a thread) meets 32 elements a thread; with 16 it was
-// bound by its instructions.
+// Any number of rows: one reading, whatever is asked for but bytes under a bias that the call itself finds.  A row's fixed cost
+// (two sums over its threads, some 150 instructions a thread) wants many elements a thread: 8192 x 4096 BF16 with a residual,
+// the sum stored and the amax taken, 201 MB, took 55 us at 16 elements a thread and takes 40 at 32 with the coefficients held
+// (5.0 TB/s).  Now bound by the chain of a row in sixteen warps an SM (issue slots 56 % used, memory 77 % of a plain copy's rate).
+// Coefficients in shared memory and six rows a block at once: 44 us; five blocks an SM: 44.
 template <int DT, bool WF32, int TPR, int EPT>
 __global__ void __launch_bounds__(kRowBlock<TPR>, kResident<TPR, EPT>) norm_fwd_rows_kernel(const NormFwd p, const RowSource src, int depth)
 {
@@ -533,7 +538,8 @@ __global__ void __launch_bounds__(kRowBlock<TPR>, kResident<TPR, EPT>) norm_fwd_
 }
 
 // The bytes of y from the sums and the statistics of the launch before, under the bias that it left.  Last rows first: what the
-// launch before wrote last is what L2 holds.
+// launch before wrote last is what L2 holds.  8192 x 4096, 100 MB: 22 us (4.5 TB/s, L2 flushed), bound like the launch before; a
+// thread per vector column and eight rows, without copies ahead, took 28.
 template <int DT, bool WF32, int TPR, int EPT>
 __global__ void __launch_bounds__(kRowBlock<TPR>, kResident<TPR, EPT>) norm_cast_rows_kernel(const NormFwd p, const RowSource src, int depth)
 {
@@ -670,7 +676,9 @@ __global__ void __launch_bounds__(T, 1024 / T) norm_bwd_any_kernel(const NormBwd
 }
 
 // The same for rows of whole vectors: groups of TPR threads, each with rows of its own, for all of which a thread holds the sums of
-// its columns.
+// its columns: 64 registers at 32 elements, so rows wait in shared memory and are read from there twice.  8192 x 4096 BF16 with dh,
+// 268 MB: 43 us (6.2 TB/s), bound by the memory; with rows in registers and 16 elements a thread 57.  A block an SM, because each
+// block's sums are 32 KB that the launch behind has to read: with three it took 55 us in all, with one 52.
 template <int DT, bool WF32, int TPR, int EPT>
 __global__ void __launch_bounds__(kSumGroups<TPR, EPT> * TPR, 1) norm_bwd_rows_kernel(const NormBwd p, const RowSource src, int depth)
 {
@@ -859,14 +867,14 @@ static void by_element_shape(int cols, F f)
 static bool ring_size(int most_blocks, int groups, int64_t slot, int &blocks, int &depth)
 {
     for (blocks = most_blocks; blocks > 0; --blocks) {
-        const int64_t each = (227 << 10) / blocks - 3072 - (blocks > 1 ? 1024 : 0);   // (beside the fixed part)
+        const int64_t each = (227 << 10) / blocks - 4096 - (blocks > 1 ? 1024 : 0);   // (beside the fixed part)
         depth = (int)(each / (groups * slot));
         if (depth > kMostAhead) depth = kMostAhead;
         if (depth >= 2) return true;
     }
     return false;
 }
-constexpr int kRingBytes = (227 << 10) - 3072;
+constexpr int kRingBytes = (227 << 10) - 4096;
 
 // Two passes as one launch of one cluster: up to eight blocks with two rows (or two times four) one after the other.
 constexpr int kClusterBlocks = 8, kClusterRows = 2, kClusterStage = 96 << 10;

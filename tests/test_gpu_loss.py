@@ -446,3 +446,46 @@ def test_neighbours_stay(ctx):
         for view, old in zip(d, before[8:]):
             view.copy_(old[1:rows + 1, 8:vocab + 8])
         assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(flat + grads, before))
+
+
+def test_largest_and_smallest_sizes(ctx, L):
+    """The longest vocabulary of a list, more rows than a grid's second dimension has, one token."""
+    x = logits_of(2, L.LOSS_VOCAB_MAX, F32, 22)
+    index, value = teacher(2, L.LOSS_VOCAB_MAX, 256, 23, x, 1.0)
+    index[1, :3] = torch.tensor([0, L.LOSS_VOCAB_MAX - 1, L.LOSS_VOCAB_MAX - 2], device="cuda")
+    check_distill(ctx, x, index, value, True, 1.0, F32)
+    check_tokens(ctx, x, torch.tensor([0, L.LOSS_VOCAB_MAX - 1], device="cuda"), 1.0, 128)
+    for rows, vocab in ((70001, 7), (70001, 1)):
+        x = logits_of(rows, vocab, BF16, 24)
+        t = torch.arange(rows, device="cuda") % vocab
+        saved, _ = check_tokens(ctx, x, t, 1.0, 1)
+        dx, one = new(rows, vocab, dtype=BF16), torch.ones(1, device="cuda").expand(rows)
+        ctx.token_logprobs_bwd(x, t, saved, dx, g_logprob=one)
+        want = R.token_grad(x, t, one.double(), None, 1.0)
+        torch.testing.assert_close(dx.double(), want, rtol=2.0 ** -7, atol=2.0 ** -19)
+
+
+def test_calls_on_two_streams_at_once(ctx):
+    """These calls have no workspace: two streams may make them on one context at the same time."""
+    x = [logits_of(n, 32000, BF16, 25 + n) for n in (300, 40)]
+    t = [torch.arange(n, device="cuda") for n in (300, 40)]
+    lists = [teacher(n, 32000, 20, 26, a, 1.0) for n, a in zip((300, 40), x)]
+
+    def run(i):
+        n = x[i].shape[0]
+        a, s, lp, ti, b, s2, d, amax = new(n), new(n, 4), new(n, 6), new(n, 6, dtype=torch.int64), new(n), new(n, 4), new(n, 32000, dtype=BF16), new(1)
+        ctx.token_logprobs(x[i], t[i], logprob=a, saved=s, top_logprob=lp, top_index=ti)
+        ctx.distill_fwd(x[i], *lists[i], b, saved=s2)
+        ctx.distill_bwd(x[i], *lists[i], s2, torch.ones(n, device="cuda"), d, d_amax=amax)
+        return a, s, lp, ti, b, s2, d, amax
+    want = run(0), run(1)
+    torch.cuda.synchronize()
+    streams = torch.cuda.Stream(), torch.cuda.Stream()
+    got = [], []
+    for _ in range(10):
+        for i, stream in enumerate(streams):
+            with torch.cuda.stream(stream):
+                got[i].append(run(i))
+    torch.cuda.synchronize()
+    for i in (0, 1):
+        assert all(torch.equal(a, b) for r in got[i] for a, b in zip(r, want[i]))

@@ -308,3 +308,43 @@ def test_neighbours_stay(L, ctx):
                                                                 *[b[8:8 + len(part[k])] for k, b in zip(part, before[4:])])):
             t.copy_(old)
         assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip((*big.values(), bytes_, *vec.values()), before))
+
+
+def test_many_short_rows_and_long_ones(L, ctx):
+    for rows, cols, dtype in ((200001, 8, BF16), (100003, 3, F32), (2, 1 << 20, BF16), (2, (1 << 20) + 1, F16), (3, 16384, F32)):
+        x, res, w, b = inputs(rows, cols, dtype, dtype, 15, True)
+        h, y, mean, rstd = new(rows, cols, dtype=dtype), new(rows, cols, dtype=dtype), new(rows), new(rows)
+        ctx.norm_fwd(x, w, b, residual=res, h=h, y=y, d_mean=mean, d_rstd=rstd)
+        check_norm(*R.norm(x, w, b, res), w, b, True, dtype, h, y, mean, rstd)
+        dx, dw, db = new(rows, cols, dtype=dtype), new(cols, dtype=dtype), new(cols, dtype=dtype)
+        ctx.norm_bwd(x, h, w, mean, rstd, dx, dh=res, dw=dw, db=db)
+        want, want_w, want_b = R.norm_grad(x, h, w, res)
+        check_grad(dx, want, res, x, h, w, rstd, dtype)
+        xh = ((h.double() - mean.double().unsqueeze(-1)).abs() + h.double().abs()) * rstd.double().unsqueeze(-1)
+        for got, ref, size in ((dw, want_w, (x.double().abs() * xh).sum(0)), (db, want_b, x.double().abs().sum(0))):
+            # (a block's rows one after the other, then 32 sums of the blocks' lines)
+            d = size * (rows / 100 + 80) * U + ref.abs() * R.HALF[dtype] + R.TINY[dtype]
+            assert bool(((got.double() - ref).abs() <= d).all()), float(((got.double() - ref).abs() / d).max())
+
+
+def test_forward_calls_on_two_streams_at_once(L, ctx):
+    """The forward call has no workspace: two streams may make it on one context at the same time."""
+    sets = [inputs(n, 2048, BF16, BF16, 16 + n, True) for n in (600, 9)]
+
+    def run(i):
+        x, res, w, b = sets[i]
+        n = x.shape[0]
+        out = [new(n, 2048, dtype=BF16), new(n, 2048, dtype=torch.uint8), new(n), new(n), new(1), new(1, dtype=torch.int32)]
+        ctx.norm_fwd(x, w, b, residual=res, h=out[0], y8=out[1], d_mean=out[2], d_rstd=out[3], d_amax_out=out[4], d_bias_out=out[5])
+        return out
+    want = run(0), run(1)
+    torch.cuda.synchronize()
+    streams = torch.cuda.Stream(), torch.cuda.Stream()
+    got = [], []
+    for _ in range(15):
+        for i, stream in enumerate(streams):
+            with torch.cuda.stream(stream):
+                got[i].append(run(i))
+    torch.cuda.synchronize()
+    for i in (0, 1):
+        assert all(torch.equal(a, b) for r in got[i] for a, b in zip(r, want[i]))
