@@ -52,7 +52,7 @@ FP8_API fp8_status_t fp8_token_logprobs(fp8_ctx *ctx, const void *logits, fp8_dt
  *     dlogits_j = scale * (g_logprob (1[j = t] - p_j) - g_entropy p_j (lp_j + entropy))
  *   g_logprob, g_entropy   in float, elements g_logprob_stride / g_entropy_stride apart (0: one number for all rows);
  *               NULL counts as zero, not both.  A row without a valid given token has no part of g_logprob.
- *   dlogits     out, of dt, rows ld_d apart; may be logits itself
+ *   dlogits     out, of dt, rows ld_d apart; may be logits itself (ld_d = ld then)
  *   d_amax      NULL, or out: amax of dlogits (for the E5 cast of the linear below)
  * Rows whose gradients are zero are written as zeros and their logits are not read. */
 FP8_API fp8_status_t fp8_token_logprobs_bwd(fp8_ctx *ctx, const void *logits, fp8_dtype_t dt, int64_t ld, int64_t rows,
@@ -86,7 +86,7 @@ FP8_API fp8_status_t fp8_distill_fwd(fp8_ctx *ctx, const void *logits, fp8_dtype
 
 /* Its gradient, g the gradient of the row's loss and Q the sum of the row's q:
  *     dlogits_j = g * scale * (Q p_j - q_j)   for listed tokens,   g * scale * p_j (Q - q_r / p_r)   for the others
- * (q_r = 0 with FP8_DISTILL_TOP).  g_loss, dlogits, d_amax as in fp8_token_logprobs_bwd. */
+ * (q_r = 0 with FP8_DISTILL_TOP); zeros where no entry counts.  g_loss, dlogits, d_amax as in fp8_token_logprobs_bwd. */
 FP8_API fp8_status_t fp8_distill_bwd(fp8_ctx *ctx, const void *logits, fp8_dtype_t dt, int64_t ld, int64_t rows,
                                      int64_t vocab, float scale, const void *index, fp8_itype_t it, int64_t ld_index,
                                      const float *value, int64_t ld_value, int32_t listed, fp8_distill_mode_t mode,

@@ -876,6 +876,11 @@ __global__ void __launch_bounds__(T) distill_bwd_kernel(const Logits p, const Te
         __syncthreads();   // (also: the gradient may overwrite the logits)
         share_list<T>(l, e, sh);
         if (keep.w == -INFINITY) e.drop_rest();
+        if (e.total == 0.0f) {   // no entry counts: the loss is 0, whatever the logits are
+            write_zeros<DT, T>(o.dx, at, count);
+            sink_amax(key, o.sink);
+            return;
+        }
         const int own_j = e.j >= from && e.j < from + count ? e.j - from : -1;
         uint32_t own = 0;
         if (own_j >= 0) {
@@ -1034,6 +1039,7 @@ fp8_status_t fp8_token_logprobs_bwd(fp8_ctx *ctx, const void *logits, fp8_dtype_
     if (s != FP8_OK) return s;
     if (!saved || !dlogits || (!g_logprob && !g_entropy) || (g_logprob && !targets)) return FP8_ERR_NULL;
     if (ld_d < vocab || g_logprob_stride < 0 || g_entropy_stride < 0) return FP8_ERR_SHAPE;
+    if (dlogits == logits && ld_d != ld && rows > 1) return FP8_ERR_SHAPE;
     if (!index_aligned(targets, (int)it) || !saved_aligned(saved) || !float_aligned(g_logprob) || !float_aligned(g_entropy) ||
         !element_aligned(dlogits, (int)dt) || !float_aligned(d_amax))
         return FP8_ERR_ALIGN;
@@ -1074,6 +1080,7 @@ fp8_status_t fp8_distill_bwd(fp8_ctx *ctx, const void *logits, fp8_dtype_t dt, i
     if (s != FP8_OK) return s;
     if (!saved || !g_loss || !dlogits) return FP8_ERR_NULL;
     if (ld_d < vocab || g_loss_stride < 0) return FP8_ERR_SHAPE;
+    if (dlogits == logits && ld_d != ld && rows > 1) return FP8_ERR_SHAPE;
     if (vocab > FP8_LOSS_VOCAB_MAX) return FP8_ERR_UNSUPPORTED;
     if (!saved_aligned(saved) || !float_aligned(g_loss) || !element_aligned(dlogits, (int)dt) || !float_aligned(d_amax)) return FP8_ERR_ALIGN;
     const OnDevice on(ctx->device);

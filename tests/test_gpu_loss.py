@@ -489,3 +489,20 @@ def test_calls_on_two_streams_at_once(ctx):
     torch.cuda.synchronize()
     for i in (0, 1):
         assert all(torch.equal(a, b) for r in got[i] for a, b in zip(r, want[i]))
+
+
+@pytest.mark.parametrize("rest", [True, False])
+@pytest.mark.parametrize("vocab", [1003, 50257])
+def test_padding_rows_may_hold_anything(ctx, vocab, rest):
+    """A row whose list is padding has loss 0 and a gradient of zeros, whatever its logits are; in place too."""
+    x = logits_of(4, vocab, BF16, 27)
+    index, value = teacher(4, vocab, 5, 28, x, 1.0)
+    index[1:3] = -1
+    x[1], x[2, 17], value[1] = NAN, INF, NAN
+    loss, saved, dx, amax = new(4), new(4, 4), new(4, vocab, dtype=BF16), new(1)
+    ctx.distill_fwd(x, index, value, loss, rest=rest, saved=saved)
+    ctx.distill_bwd(x, index, value, saved, torch.ones(4, device="cuda"), dx, rest=rest, d_amax=amax)
+    assert loss[1:3].tolist() == [0.0, 0.0] and bool((dx[1:3] == 0).all()) and bool((dx[[0, 3]] != 0).any(1).all())
+    assert float(amax) == float(dx.abs().max())
+    ctx.distill_bwd(x, index, value, saved, torch.ones(4, device="cuda"), x, rest=rest)
+    assert torch.equal(x, dx)
