@@ -29,7 +29,8 @@ typedef enum { FP8_NORM_LAYER = 0, FP8_NORM_RMS = 1 } fp8_norm_kind_t;
  *   x            in
  *   residual     NULL, or in
  *   weight       NULL (ones), or in;   bias_vec   NULL (zeros), or in
- *   h            NULL, or out: x + residual.  May be x or residual itself; no other output may overlap an input.
+ *   h            NULL, or out: x + residual.  May be x or residual itself (rows as far apart); no other output
+ *                may overlap an input.
  *   y            NULL, or out
  *   d_mean       NULL, or out float [rows] (zeros for FP8_NORM_RMS);   d_rstd   NULL, or out float [rows]
  *   y8           NULL, or out, [rows][cols] contiguous E4 bytes
@@ -62,7 +63,7 @@ FP8_API fp8_status_t fp8_norm_fwd(fp8_ctx *ctx, const fp8_norm_fwd_t *args, void
  *   dy, h        in, [rows][cols] of dt;   dh   NULL, or in: the gradient that reaches h beside the norm
  *   weight       NULL (ones), or in, of w_dt
  *   d_mean       in, float [rows] (not read for FP8_NORM_RMS, may be NULL);   d_rstd   in, float [rows]
- *   dx           NULL, or out, of dt.  May be dy or dh itself.
+ *   dx           NULL, or out, of dt.  May be dy or dh itself (rows as far apart).
  *   dw, db       NULL, or out, [cols] of w_dt.  Sums over rows are taken in an order that depends on the sizes only:
  *                equal inputs give equal bits.
  *   d_amax       NULL, or out: amax of dx (its E5 cast in the linear below needs no pass of its own; needs dx)

@@ -92,8 +92,8 @@ typedef struct fp8_ctx fp8_ctx;
  * workspace: a status word, reduction slots and a 64 MB FP32 buffer for the
  * partial sums of split-contraction (decode-size) matmuls and of a norm's
  * weight gradient.  fp8_create is the only call that allocates device memory;
- * it also raises the dynamic shared-memory limit of the kernels.  It must not be called during
- * stream capture.  The context-taking calls that enqueue work (fp8_amax,
+ * it also raises the dynamic shared-memory limit of the kernels.  It must not
+ * be called during stream capture.  The context-taking calls that enqueue work (fp8_amax,
  * fp8_scaling_bias, fp8_cast_*, fp8_ptq_weights, fp8_linear_*, fp8_norm_*,
  * fp8_token_logprobs*, fp8_distill_*) neither synchronise nor allocate, so a
  * whole step of them can be captured into a CUDA graph and replayed. */

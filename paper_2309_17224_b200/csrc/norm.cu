@@ -207,6 +207,7 @@ struct RowWalk {
     uint32_t slot_bytes;
     int depth, group;
     unsigned *d_status;
+    bool in_time = true;      // no wait of this thread's has run out
     __device__ __forceinline__ RowWalk(const RowSource &s, RowRing &r, uint8_t *smem, int ahead, unsigned *status)
         : src(s), ring(r), slot_bytes(s.row_bytes * s.inputs), depth(ahead), group(threadIdx.x / TPR), d_status(status)
     {
@@ -219,9 +220,10 @@ struct RowWalk {
         }
         __syncthreads();
     }
-    // one thread of the group: row r into slot s
+    // one thread of the group: row r into slot s (none any more behind a wait that ran out)
     __device__ __forceinline__ void start(int64_t r, int s) const
     {
+        if (!in_time) return;
         const uint64_t once = l2_policy_evict_first();   // (what is written stays in L2 for the launch behind)
         const uint32_t bar = smem_u32(&ring.full[group][s]);
         uint32_t to = smem_u32(slots + s * slot_bytes);
@@ -236,10 +238,15 @@ struct RowWalk {
         }
     }
     // (a wait that runs out raises the flag; the walk goes on with what is there, without waiting again)
-    __device__ __forceinline__ const uint4 *wait(int s, uint32_t parity) const
+    __device__ __forceinline__ const uint4 *wait(int s, uint32_t parity)
     {
-        mbar_wait(smem_u32(&ring.full[group][s]), parity, &ring.abort_flag, d_status);
+        in_time = mbar_wait(smem_u32(&ring.full[group][s]), parity, &ring.abort_flag, d_status) && in_time;
         return reinterpret_cast<const uint4 *>(slots + s * slot_bytes);
+    }
+    // the block's shared memory is given up only when copies on their way have had time to arrive
+    __device__ __forceinline__ void finish() const
+    {
+        if (*reinterpret_cast<volatile int *>(&ring.abort_flag)) __nanosleep(1000000);
     }
 };
 
@@ -479,7 +486,7 @@ __global__ void __launch_bounds__(kRowBlock<TPR>, kResident<TPR, EPT>) norm_fwd_
     __shared__ float part[TPR / 32];
     __shared__ float2 part2[2][TPR / 32];
     launch_next();
-    const RowWalk<TPR> walk(src, ring, slots, depth, p.sink.d_status);
+    RowWalk<TPR> walk(src, ring, slots, depth, p.sink.d_status);
     const int t = threadIdx.x % TPR, group = threadIdx.x / TPR;
     const int64_t step = (int64_t)gridDim.x * kGroups;
     const int row_vecs = p.cols / kN;
@@ -533,6 +540,7 @@ __global__ void __launch_bounds__(kRowBlock<TPR>, kResident<TPR, EPT>) norm_fwd_
             }
         }
     }
+    walk.finish();
     if (scale.clipped<DT>(peak)) raise_flags(p.sink.d_status, FP8_FLAG_SATURATED);
     sink_amax(folded_key<DT>(acc), p.sink);
 }
@@ -546,7 +554,7 @@ __global__ void __launch_bounds__(kRowBlock<TPR>, kResident<TPR, EPT>) norm_cast
     constexpr int kN = kPerVec<DT>, kPairs = kVecPairs<DT>, kVecs = EPT / kN, kGroups = kRowBlock<TPR> / TPR;
     extern __shared__ __align__(16) uint8_t slots[];
     __shared__ RowRing ring;
-    const RowWalk<TPR> walk(src, ring, slots, depth, p.sink.d_status);
+    RowWalk<TPR> walk(src, ring, slots, depth, p.sink.d_status);
     const int t = threadIdx.x % TPR, group = threadIdx.x / TPR;
     const int64_t step = (int64_t)gridDim.x * kGroups;
     const int row_vecs = p.cols / kN;
@@ -589,6 +597,7 @@ __global__ void __launch_bounds__(kRowBlock<TPR>, kResident<TPR, EPT>) norm_cast
             parity ^= 1u;
         }
     }
+    walk.finish();
     if (scale.clipped<DT>(peak)) raise_flags(p.sink.d_status, FP8_FLAG_SATURATED);
 }
 
@@ -687,7 +696,7 @@ __global__ void __launch_bounds__(kSumGroups<TPR, EPT> * TPR, 1) norm_bwd_rows_k
     __shared__ RowRing ring;
     __shared__ float2 part[kSumGroups<TPR, EPT>][2][TPR / 32];
     launch_next();
-    const RowWalk<TPR> walk(src, ring, slots, depth, p.sink.d_status);
+    RowWalk<TPR> walk(src, ring, slots, depth, p.sink.d_status);
     const int t = threadIdx.x % TPR, group = threadIdx.x / TPR;
     const int groups = (int)blockDim.x / TPR;
     const int64_t step = (int64_t)gridDim.x * groups;
@@ -763,6 +772,7 @@ __global__ void __launch_bounds__(kSumGroups<TPR, EPT> * TPR, 1) norm_bwd_rows_k
             parity ^= 1u;
         }
     }
+    walk.finish();
     // the groups' sums meet where their rows were, and leave as one line
     float *lines = reinterpret_cast<float *>(slots);
 #pragma unroll
@@ -823,6 +833,12 @@ __global__ void __launch_bounds__(kSumThreads) norm_bwd_sum_kernel(const float *
     if (w_dt == FP8_F32) store_bits<FP8_F32>(out, column, element_bits<FP8_F32>(s));
     else if (w_dt == FP8_BF16) store_bits<FP8_BF16>(out, column, element_bits<FP8_BF16>(s));
     else store_bits<FP8_F16>(out, column, element_bits<FP8_F16>(s));
+}
+
+// An output in an input's place lies as the input does.
+static bool in_place(const void *out, int64_t ld_out, const void *in, int64_t ld_in, int64_t rows)
+{
+    return !out || out != in || rows == 1 || ld_out == ld_in;
 }
 
 static unsigned blocks_for_rows(const fp8_ctx *ctx, int64_t rows, int per_sm)
@@ -1068,6 +1084,7 @@ fp8_status_t fp8_norm_fwd(fp8_ctx *ctx, const fp8_norm_fwd_t *a, void *stream)
     if (a->rows <= 0 || a->cols <= 0 || a->cols > kMaxCols || !(a->eps >= 0.0f && a->eps <= FLT_MAX)) return FP8_ERR_SHAPE;
     if (a->ld_x < a->cols || (a->residual && a->ld_residual < a->cols) || (a->h && a->ld_h < a->cols) || (a->y && a->ld_y < a->cols))
         return FP8_ERR_SHAPE;
+    if (!in_place(a->h, a->ld_h, a->x, a->ld_x, a->rows) || !in_place(a->h, a->ld_h, a->residual, a->ld_residual, a->rows)) return FP8_ERR_SHAPE;
     if (!element_aligned(a->x, a->dt) || !element_aligned(a->residual, a->dt) || !element_aligned(a->h, a->dt) ||
         !element_aligned(a->y, a->dt) || !element_aligned(a->weight, a->w_dt) || !element_aligned(a->bias_vec, a->w_dt) ||
         !element_aligned(a->d_mean, FP8_F32) || !element_aligned(a->d_rstd, FP8_F32) || !element_aligned(a->d_bias_in, FP8_F32) ||
@@ -1101,6 +1118,7 @@ fp8_status_t fp8_norm_bwd(fp8_ctx *ctx, const fp8_norm_bwd_t *a, void *stream)
     if (a->rows <= 0 || a->cols <= 0 || a->cols > kMaxCols) return FP8_ERR_SHAPE;
     if ((a->dw || a->db) && a->cols > (int64_t)1 << 22) return FP8_ERR_SHAPE;
     if (a->ld_dy < a->cols || a->ld_h < a->cols || (a->dh && a->ld_dh < a->cols) || (a->dx && a->ld_dx < a->cols)) return FP8_ERR_SHAPE;
+    if (!in_place(a->dx, a->ld_dx, a->dy, a->ld_dy, a->rows) || !in_place(a->dx, a->ld_dx, a->dh, a->ld_dh, a->rows)) return FP8_ERR_SHAPE;
     if (!element_aligned(a->dy, a->dt) || !element_aligned(a->h, a->dt) || !element_aligned(a->dh, a->dt) || !element_aligned(a->dx, a->dt) ||
         !element_aligned(a->weight, a->w_dt) || !element_aligned(a->dw, a->w_dt) || !element_aligned(a->db, a->w_dt) ||
         !element_aligned(a->d_mean, FP8_F32) || !element_aligned(a->d_rstd, FP8_F32) || !element_aligned(a->d_amax, FP8_F32))

@@ -223,3 +223,12 @@ def test_library_refuses_lists(name):
                            (dict(vocab=(1 << 20) + 1, ld=1 << 21, ld_d=1 << 21), E.ERR_UNSUPPORTED), (dict(index=A + 4), E.ERR_ALIGN),
                            (dict(value=A + 2), E.ERR_ALIGN)):
         assert call(name, CALLS[name], change) == status, change
+
+
+def test_library_refuses_other_distances_in_place():
+    """An output in an input's place lies as the input does (one row has no distance)."""
+    B = 1 << 24
+    assert norm_fwd(residual=B, ld_x=40) == E.ERR_SHAPE and norm_fwd(x=B, ld_residual=40) == E.ERR_SHAPE
+    assert norm_bwd(dh=B, ld_dy=40) == E.ERR_SHAPE and norm_bwd(dy=B, ld_dh=40) == E.ERR_SHAPE
+    assert call("fp8_token_logprobs_bwd", CALLS["fp8_token_logprobs_bwd"], dict(ld=104)) == E.ERR_SHAPE
+    assert call("fp8_distill_bwd", CALLS["fp8_distill_bwd"], dict(ld=104)) == E.ERR_SHAPE
