@@ -1,5 +1,7 @@
 // Log probabilities of given tokens with entropy and top tokens, and the divergence from a teacher's listed tokens, each
 // with the gradient of the logits.
+#include <algorithm>
+
 #include "fp8_loss.h"
 #include "kv_common.cuh"
 #include "row_common.cuh"
@@ -148,6 +150,9 @@ struct TopShared {
     int count, strips;
     uint32_t bound;
 };
+
+template <>
+struct TopShared<64> {};   // 64 threads: a kernel without top tokens, so that shared memory holds as many blocks as registers
 
 // The k largest of sh.key[0 .. n), in order, to sh.best.  Keys differ, so a key's place is the number of larger ones.
 template <int T>
@@ -427,10 +432,11 @@ __device__ __forceinline__ Sums cluster_join(int blocks, float c, const float4 &
     return all;
 }
 
-// A row (or a part of one) a block.  4096 x 50257 BF16, 412 MB: 82 us (5.0 TB/s); an element takes 7.4 instructions and one
-// exponential, which is 49 us of the units for those at 1.76 GHz, and rows of eight blocks an SM come in 3.5 rounds.  512 x 128256
-// FP32 with 20 top tokens, 263 MB: 60 us.  Tried: batches of 2, 3 and 6 vectors, 10 and 12 blocks an SM (no better); copies to a
-// ring in shared memory instead of registers (8.4 instructions an element, 2 to 5 % slower).
+// A row (or a part of one) a block.  4096 x 50257 BF16, 412 MB: 74 us from a graph (5.6 TB/s); an element takes 7.4 instructions
+// and one exponential, which is 49 us of the units for those at 1.76 GHz, and rows of sixteen blocks an SM come in 1.7 rounds.
+// 512 x 128256 FP32 with 20 top tokens, 263 MB: 60 us.  Tried: 32 threads a row (as quick, slower where an SM has few rows); batches
+// of 2, 3 and 6 vectors, 10 and 12 blocks of 128 threads an SM (no better); copies to a ring in shared memory instead of registers
+// (8.4 instructions an element, 2 to 5 % slower).
 template <int DT, int T>
 __global__ void __launch_bounds__(T, 1024 / T) token_logprobs_kernel(const Logits p, const TokenOut o, int blocks)
 {
@@ -458,7 +464,8 @@ __global__ void __launch_bounds__(T, 1024 / T) token_logprobs_kernel(const Logit
         strip = fmaxf(strip, x);
     }
     sums = block_join<T>(sums, strip, p.c, part);
-    if (o.top_k > 0) find_top<DT, T>(row, strip, o.top_k, top);   // (of a row with a NaN too: what it finds there is not used)
+    if constexpr (T > 64)
+        if (o.top_k > 0) find_top<DT, T>(row, strip, o.top_k, top);   // (of a row with a NaN too: what it finds there is not used)
     if (blocks > 1) {
         cluster_note(sums, word);
         cluster_sync();
@@ -483,22 +490,24 @@ __global__ void __launch_bounds__(T, 1024 / T) token_logprobs_kernel(const Logit
             o.logprob[r] = lp;
         }
     }
-    if (o.top_k > 0 && own == 0) {
-        if (blocks > 1) {
-            for (int i = threadIdx.x; i < blocks * o.top_k; i += T) {
-                const uint32_t at = cluster_address(&top.best[i % o.top_k], i / o.top_k);
-                asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(top.key[i]) : "r"(at) : "memory");
+    if constexpr (T > 64) {
+        if (o.top_k > 0 && own == 0) {
+            if (blocks > 1) {
+                for (int i = threadIdx.x; i < blocks * o.top_k; i += T) {
+                    const uint32_t at = cluster_address(&top.best[i % o.top_k], i / o.top_k);
+                    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(top.key[i]) : "r"(at) : "memory");
+                }
+                __syncthreads();
+                top_rank(top, blocks * o.top_k, o.top_k);
             }
-            __syncthreads();
-            top_rank(top, blocks * o.top_k, o.top_k);
-        }
-        for (int i = threadIdx.x; i < o.top_k; i += T) {
-            const int64_t at = r * o.top_k + i;
-            const unsigned long long key = nan ? 0 : top.best[i];
-            const int j = nan ? -1 : (int)~(uint32_t)key;
-            o.top_logprob[at] = nan ? NAN : none ? -INFINITY : p.scale * (order_value((uint32_t)(key >> 32)) - sums.m) - logsum;
-            if (p.it == FP8_I64) static_cast<int64_t *>(o.top_index)[at] = j;
-            else static_cast<int32_t *>(o.top_index)[at] = j;
+            for (int i = threadIdx.x; i < o.top_k; i += T) {
+                const int64_t at = r * o.top_k + i;
+                const unsigned long long key = nan ? 0 : top.best[i];
+                const int j = nan ? -1 : (int)~(uint32_t)key;
+                o.top_logprob[at] = nan ? NAN : none ? -INFINITY : p.scale * (order_value((uint32_t)(key >> 32)) - sums.m) - logsum;
+                if (p.it == FP8_I64) static_cast<int64_t *>(o.top_index)[at] = j;
+                else static_cast<int32_t *>(o.top_index)[at] = j;
+            }
         }
     }
     if (blocks > 1) cluster_sync();   // (no block leaves while another reads its words)
@@ -660,8 +669,8 @@ struct ListedVectors {
     }
 };
 
-// 2048 x 32000 BF16 with lists of 64, 131 MB: 35 us (3.8 TB/s).  Bound by what a row costs beside its elements (the list, two
-// joins: some 4 us of latency, covered by the other blocks of the SM as far as two rounds of rows go).
+// 2048 x 32000 BF16 with lists of 64, 131 MB: 32.5 us (4.0 TB/s).  Bound by what a row costs beside its elements (the list, two
+// joins: some 4 us of latency, which nothing covers at the start and the end of the one round of rows).
 template <int DT, int T>
 __global__ void __launch_bounds__(T) distill_kernel(const Logits p, const TeacherList l, float *loss, float *saved, int blocks)
 {
@@ -952,8 +961,18 @@ static int row_blocks(const fp8_ctx *ctx, int64_t rows, int64_t vocab, bool join
     return blocks;
 }
 
-// Whether blocks of 128 threads still give an SM 1024 (512 rows of 128256 with top tokens: 103 us with 128 threads, 60 with 256).
-static bool many_rows(const fp8_ctx *ctx, int64_t rows, int blocks) { return rows * blocks >= (int64_t)ctx->sm_count * 8; }
+// Threads of a row's block: `least` of them at least, and as many as let an SM's shared memory (`shared` bytes a block) hold 1024
+// threads.  Sixteen rows an SM by 64 threads come in half as many rounds as eight by 128, each of which has its latencies at both
+// ends (forward, 8192 rows of 50257: 134 and 144 us; 4096: 74 and 78; 2048 of 32000 with lists of 64: 32.5 and 35).  By shared
+// memory: 2048 rows of 262144 with lists take 178 us by 256 threads and 220 by 128, their gradient 325 and 406.
+static int row_threads(int least, unsigned shared)
+{
+    int threads = least <= 64 ? 64 : least <= 128 ? 128 : 256;
+    while (threads < 256 && 1024u / threads * (shared + 2048u) > 227u << 10) threads *= 2;
+    return threads;
+}
+// Where there are no eight rows an SM, 256 (forward, 512 rows of 128256 with top tokens: 60 us; by 128 threads 103).
+static int few_row_threads(const fp8_ctx *ctx, int64_t rows, int blocks) { return rows * blocks < (int64_t)ctx->sm_count * 8 ? 256 : 1; }
 
 // `cluster`: the blocks of a row are one.
 template <typename... KArgs, typename... Args>
@@ -980,12 +999,16 @@ static cudaError_t allow_lists()
 {
     const int bytes = list_words(FP8_LOSS_VOCAB_MAX) * 4;
     const auto attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
-    cudaError_t e = cudaFuncSetAttribute(distill_kernel<DT, T>, attr, bytes);
-    return e == cudaSuccess ? cudaFuncSetAttribute(distill_bwd_kernel<DT, T>, attr, bytes) : e;
+    const cudaError_t e = cudaFuncSetAttribute(distill_kernel<DT, T>, attr, bytes);
+    if constexpr (T > 64) return e == cudaSuccess ? cudaFuncSetAttribute(distill_bwd_kernel<DT, T>, attr, bytes) : e;
+    return e;
 }
 cudaError_t configure_loss_kernels()
 {
-    cudaError_t e = allow_lists<FP8_BF16, 128>();
+    cudaError_t e = allow_lists<FP8_BF16, 64>();
+    if (e == cudaSuccess) e = allow_lists<FP8_F16, 64>();
+    if (e == cudaSuccess) e = allow_lists<FP8_F32, 64>();
+    if (e == cudaSuccess) e = allow_lists<FP8_BF16, 128>();
     if (e == cudaSuccess) e = allow_lists<FP8_BF16, 256>();
     if (e == cudaSuccess) e = allow_lists<FP8_F16, 128>();
     if (e == cudaSuccess) e = allow_lists<FP8_F16, 256>();
@@ -1000,10 +1023,10 @@ cudaError_t configure_loss_kernels()
     (dt == FP8_BF16  ? FP8LIN_LAUNCH_OF(FP8_BF16, T, KERNEL, __VA_ARGS__)                              \
      : dt == FP8_F16 ? FP8LIN_LAUNCH_OF(FP8_F16, T, KERNEL, __VA_ARGS__)                               \
                      : FP8LIN_LAUNCH_OF(FP8_F32, T, KERNEL, __VA_ARGS__))
-// 128 threads a row: what a row costs beside its elements is paid by warp.  256 where there are few rows, or where a thread each
-// is needed for more top or listed tokens (top tokens: twice as many strips keep the candidates few).
-#define FP8LIN_LAUNCH_BY_SIZE(SMALL, KERNEL, ...) \
-    ((SMALL) ? FP8LIN_LAUNCH_BY_TYPE(128, KERNEL, __VA_ARGS__) : FP8LIN_LAUNCH_BY_TYPE(256, KERNEL, __VA_ARGS__))
+#define FP8LIN_LAUNCH_BY_SIZE(THREADS, KERNEL, ...)               \
+    ((THREADS) == 64    ? FP8LIN_LAUNCH_BY_TYPE(64, KERNEL, __VA_ARGS__)  \
+     : (THREADS) == 128 ? FP8LIN_LAUNCH_BY_TYPE(128, KERNEL, __VA_ARGS__) \
+                        : FP8LIN_LAUNCH_BY_TYPE(256, KERNEL, __VA_ARGS__))
 
 extern "C" {
 
@@ -1026,7 +1049,9 @@ fp8_status_t fp8_token_logprobs(fp8_ctx *ctx, const void *logits, fp8_dtype_t dt
     const Logits p = make_logits(ctx, logits, ld, rows, vocab, scale, (int)it);
     const TokenOut o = {targets, logprob, entropy, lse, saved, top_logprob, top_index, top_k};
     const int blocks = row_blocks(ctx, rows, vocab, true);
-    return FP8LIN_LAUNCH_BY_SIZE(top_k <= 32 && many_rows(ctx, rows, blocks), token_logprobs_kernel, rows, blocks, true, 0u, stream, p, o, blocks);
+    // (top tokens: 64 threads have no place for them, and twice as many strips keep the candidates of a long list few)
+    const int threads = row_threads(std::max(few_row_threads(ctx, rows, blocks), top_k == 0 ? 64 : top_k <= 32 ? 128 : 256), 0u);
+    return FP8LIN_LAUNCH_BY_SIZE(threads, token_logprobs_kernel, rows, blocks, true, 0u, stream, p, o, blocks);
 }
 
 fp8_status_t fp8_token_logprobs_bwd(fp8_ctx *ctx, const void *logits, fp8_dtype_t dt, int64_t ld, int64_t rows, int64_t vocab, float scale,
@@ -1066,7 +1091,9 @@ fp8_status_t fp8_distill_fwd(fp8_ctx *ctx, const void *logits, fp8_dtype_t dt, i
     const Logits p = make_logits(ctx, logits, ld, rows, vocab, scale, (int)it);
     const TeacherList l = {index, value, ld_index, ld_value, listed, mode == FP8_DISTILL_REST};
     const int blocks = row_blocks(ctx, rows, vocab, true);
-    return FP8LIN_LAUNCH_BY_SIZE(listed <= 128 && many_rows(ctx, rows, blocks), distill_kernel, rows, blocks, true, list_words((int)vocab) * 4u, stream, p, l, loss, saved, blocks);
+    const unsigned shared = list_words((int)vocab) * 4u;
+    const int threads = row_threads(std::max(few_row_threads(ctx, rows, blocks), (int)listed), shared);
+    return FP8LIN_LAUNCH_BY_SIZE(threads, distill_kernel, rows, blocks, true, shared, stream, p, l, loss, saved, blocks);
 }
 
 fp8_status_t fp8_distill_bwd(fp8_ctx *ctx, const void *logits, fp8_dtype_t dt, int64_t ld, int64_t rows, int64_t vocab, float scale,
@@ -1088,7 +1115,11 @@ fp8_status_t fp8_distill_bwd(fp8_ctx *ctx, const void *logits, fp8_dtype_t dt, i
     const TeacherList l = {index, value, ld_index, ld_value, listed, mode == FP8_DISTILL_REST};
     const int blocks = row_blocks(ctx, rows, vocab, false);
     const GradOut o = make_grad(ctx, logits, ld, (int)dt, dlogits, ld_d, d_amax, blocks);
-    return FP8LIN_LAUNCH_BY_SIZE(listed <= 128, distill_bwd_kernel, rows, blocks, false, list_words((int)vocab) * 4u, stream, p, l, saved, g_loss, g_loss_stride, o);
+    const unsigned shared = list_words((int)vocab) * 4u;
+    // (64 threads: 76 us for 2048 rows of 50257 FP16, by 128 they take 72)
+    return row_threads(std::max(128, (int)listed), shared) == 128
+               ? FP8LIN_LAUNCH_BY_TYPE(128, distill_bwd_kernel, rows, blocks, false, shared, stream, p, l, saved, g_loss, g_loss_stride, o)
+               : FP8LIN_LAUNCH_BY_TYPE(256, distill_bwd_kernel, rows, blocks, false, shared, stream, p, l, saved, g_loss, g_loss_stride, o);
 }
 
 }  // extern "C"

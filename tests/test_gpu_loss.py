@@ -1,8 +1,8 @@
 """Token log probabilities and distillation against the definitions in 64 bits.
 
 Tolerances count FP32 roundings U = 2^-24.  With d = (x - m) * scale * log2 e: a term 2^d is off by 3 U |d| ln 2 from d and by
-2^-22 from the exponential; a sum's terms are joined in at most n / 256 + 24 additions and as many changes of the maximum as
-a thread meets vectors (n / 1024 at most, each one more exponential).  So ln sum is off by SUM(n) + 2^-22 * E, E the mean of
+2^-22 from the exponential; a sum's terms are joined in at most n / 2T + 24 additions and as many changes of the maximum as
+a thread meets vectors (n / 8T at most, each one more exponential), T the threads of a row: 128 at least, 64 of many rows.  So ln sum is off by SUM(n) + 2^-22 * E, E the mean of
 (largest z - z), and a log probability by that and 4 U times its size."""
 import math
 
@@ -44,13 +44,13 @@ def logits_of(rows, vocab, dtype, seed, spread=2.0, ld=None, first=0):
     return x
 
 
-def log_error(lp, z_scale):
+def log_error(lp, z_scale, threads=128):
     """Bound of |error of ln sum|, per row: 64-bit log probabilities in, see above."""
     n = lp.shape[-1]
     p = lp.exp()
     lead = lp.amax(-1, keepdim=True)
     far = torch.where(p > 0, p * (lead - lp), torch.zeros_like(p)).sum(-1)
-    return (n / 256 + 24) * U + (n / 1024 + 16) * 2.0 ** -22 + 2.0 ** -22 * far
+    return (n / (2 * threads) + 24) * U + (n / (8 * threads) + 16) * 2.0 ** -22 + 2.0 ** -22 * far
 
 
 def near(got, want, bound):
@@ -65,13 +65,13 @@ def near(got, want, bound):
     assert bool((off[fine] <= bound[fine]).all()), (float(off[fine].max()), float((off[fine] / bound[fine]).max()))
 
 
-def check_tokens(ctx, x, targets, scale, k, itype=torch.int64):
+def check_tokens(ctx, x, targets, scale, k, itype=torch.int64, threads=128):
     rows, vocab = x.shape
     out = {n: new(rows) for n in ("logprob", "entropy", "lse")}
     saved, top_lp, top_i = new(rows, 4), new(rows, k) if k else None, new(rows, k, dtype=itype) if k else None
     ctx.token_logprobs(x, targets, scale=scale, saved=saved, top_logprob=top_lp, top_index=top_i, **out)
     lp, lse = R.log_softmax(x, scale)
-    err = log_error(lp, scale)
+    err = log_error(lp, scale, threads)
     given = (targets >= 0) & (targets < vocab)
     want = torch.where(given, lp.gather(1, targets.clamp(0, vocab - 1).long().unsqueeze(1)).squeeze(1), torch.zeros_like(lse))
     want = torch.where(targets >= vocab, torch.full_like(want, NAN), want)
@@ -219,18 +219,19 @@ def teacher(rows, vocab, listed, seed, x, scale, itype=torch.int64):
     return index.to(itype), value.contiguous()
 
 
-def check_distill(ctx, x, index, value, rest, scale, dtype):
+def check_distill(ctx, x, index, value, rest, scale, dtype, threads=128, pick=slice(None)):
     rows, vocab = x.shape
     loss, saved, dx, amax = new(rows), new(rows, 4), new(rows, vocab, dtype=dtype), new(1)
     ctx.distill_fwd(x, index, value, loss, rest=rest, scale=scale, saved=saved)
-    want, grad = R.distill(x, index, value, rest, scale)
-    lp, _ = R.log_softmax(x, scale)
+    some = x[pick], index[pick], value[pick]   # the rows that are compared
+    want, grad = R.distill(*some, rest, scale)
+    lp, _ = R.log_softmax(some[0], scale)
     p = lp.exp()
-    err = 4 * log_error(lp, scale) + 64 * U
+    err = 4 * log_error(lp, scale, threads) + 64 * U
     # terms q (ln q - lp): sizes of the parts, each off by err and 4 U of its size; q_r ln q_r by 2^-24 of q_r's logarithm
-    reach = torch.where(torch.isfinite(value), value.abs(), torch.zeros_like(value)).double().amax(-1) + 1
-    far = lp.clamp(min=-700).gather(1, index.long().clamp(0, vocab - 1)).abs().amax(-1)
-    near(loss, want, (err + 8 * U * (reach + far + 30)) * 2)
+    reach = torch.where(torch.isfinite(some[2]), some[2].abs(), torch.zeros_like(some[2])).double().amax(-1) + 1
+    far = lp.clamp(min=-700).gather(1, some[1].long().clamp(0, vocab - 1)).abs().amax(-1)
+    near(loss[pick], want, (err + 8 * U * (reach + far + 30)) * 2)
     plain = new(rows)
     ctx.distill_fwd(x, index, value, plain, rest=rest, scale=scale)
     assert torch.equal(plain, loss) or bool(torch.isnan(loss).any())
@@ -238,17 +239,17 @@ def check_distill(ctx, x, index, value, rest, scale, dtype):
     gl = torch.rand(rows, generator=g, device="cuda") + 0.5
     for up in (gl, gl[:1].expand(rows)):
         ctx.distill_bwd(x, index, value, saved, up, dx, rest=rest, scale=scale, d_amax=amax)
-        full = up.double().unsqueeze(1) * grad
+        full = up[pick].double().unsqueeze(1) * grad
         q = torch.zeros_like(p)
-        for r in range(rows):
-            for j, (a, _) in R.teacher_of(index[r].tolist(), value[r].tolist(), vocab, rest)[0].items():
+        for r in range(len(want)):
+            for j, (a, _) in R.teacher_of(some[1][r].tolist(), some[2][r].tolist(), vocab, rest)[0].items():
                 q[r, j] = a
         left = (1 - q.sum(-1, keepdim=True)).clamp(min=0) if rest else torch.zeros_like(p[:, :1])
         others = torch.where(q > 0, torch.zeros_like(p), p)
         spread = left * others / others.sum(-1, keepdim=True).clamp(min=1e-300)
-        size = up.double().unsqueeze(1) * scale * (p + q + spread)
+        size = up[pick].double().unsqueeze(1) * scale * (p + q + spread)
         finite = torch.isfinite(full).all(1)
-        check_gradient(dx[finite], full[finite], size[finite], err[finite], dtype)
+        check_gradient(dx[pick][finite], full[finite], size[finite], err[finite], dtype)
         assert float(amax) == float(dx.float().abs().max()) or bool(torch.isnan(dx).any())
     return saved, dx
 
@@ -506,3 +507,15 @@ def test_padding_rows_may_hold_anything(ctx, vocab, rest):
     assert float(amax) == float(dx.abs().max())
     ctx.distill_bwd(x, index, value, saved, torch.ones(4, device="cuda"), x, rest=rest)
     assert torch.equal(x, dx)
+
+
+@pytest.mark.parametrize("rows,vocab,listed,dtype", [
+    (1184, 1003, 20, BF16), (1183, 1003, 20, BF16), (2500, 1003, 64, F32), (2500, 1003, 65, F16), (1300, 515, 130, BF16), (1190, 131072, 7, BF16),
+    (1190, 200003, 7, F16)])
+def test_many_rows(ctx, rows, vocab, listed, dtype):
+    """Both sides of each number of threads that a row may have: by rows, by listed tokens, by the list's shared memory."""
+    x = logits_of(rows, vocab, dtype, 29)
+    check_tokens(ctx, x, torch.arange(rows, device="cuda") * 7 % vocab, 1.0, 0, threads=64)
+    index, value = teacher(rows, vocab, listed, 30, x, 1.0)
+    for rest in (True, False):
+        check_distill(ctx, x, index, value, rest, 1.0, dtype, threads=64, pick=slice(0, rows, 97))
