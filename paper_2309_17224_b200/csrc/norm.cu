@@ -48,6 +48,10 @@ __device__ __forceinline__ float normalised(float h, float mean, float rstd, flo
 __device__ __forceinline__ float weight_at(const void *w, int w_dt, int j) { return w ? load_any(w, w_dt, j) : 1.0f; }
 __device__ __forceinline__ float shift_at(const void *b, int w_dt, int j) { return b ? load_any(b, w_dt, j) : 0.0f; }
 
+// The launch behind may start when no block of this one waits for a place any more; it waits for this one's end itself.
+__device__ __forceinline__ void launch_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_launch_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 // Any sizes and alignment, element by element: T threads a row.  HELD > 0: a thread holds that many elements (T * HELD >= cols) and
 // the row is read once; 0: any length, three walks over it.  CAST_ONLY: the statistics are there, bytes are wanted.  Bound by the
 // chain of a row (loads, two sums, stores): 1531 x 1027 FP32 in 10.4 us from a graph, of which an empty launch is 4.3 (1.2 TB/s);
@@ -62,8 +66,7 @@ __global__ void __launch_bounds__(T, 1024 / T) norm_fwd_any_kernel(const NormFwd
     uint32_t key = 0;
     bool sat = false;
     const bool bytes = p.y8 && p.bias;
-    Pow2Pair scale = {1.0f, 1.0f};
-    if (bytes) scale = make_pow2_pair(*p.bias + p.delta);
+    if (!CAST_ONLY) launch_next();
     // (up to eight of each, the coefficients too are held: they would be waited for behind each row's sums)
     constexpr bool kHoldCoefficients = HELD > 0 && HELD <= 8;
     float held_w[kTurns], held_b[kTurns];
@@ -75,6 +78,9 @@ __global__ void __launch_bounds__(T, 1024 / T) norm_fwd_any_kernel(const NormFwd
             held_b[i] = j < p.cols ? shift_at(p.b, p.w_dt, j) : 0.0f;
         }
     }
+    if (CAST_ONLY) wait_for_launch_before();
+    Pow2Pair scale = {1.0f, 1.0f};
+    if (bytes) scale = make_pow2_pair(__ldcg(p.bias) + p.delta);
     const bool from_h = CAST_ONLY && p.h;
     float x[kTurns], res[kTurns];
     auto fetch = [&](int64_t r) {
@@ -117,8 +123,8 @@ __global__ void __launch_bounds__(T, 1024 / T) norm_fwd_any_kernel(const NormFwd
         }
         float mean = 0.0f, rstd;
         if (CAST_ONLY) {
-            mean = p.layer ? p.mean[r] : 0.0f;
-            rstd = p.rstd[r];
+            mean = p.layer ? __ldcg(p.mean + r) : 0.0f;
+            rstd = __ldcg(p.rstd + r);
         } else {
             float s = 0.0f;
             if (!HELD && p.h)
@@ -181,10 +187,6 @@ constexpr int kResident = TPR == 32 ? (EPT == 8 ? 8 : EPT == 16 ? 6 : 4) : TPR =
 template <int TPR, int EPT>
 constexpr int kSumGroups = TPR == 32 ? (EPT == 8 ? 24 : EPT == 16 ? 16 : 12) : TPR == 128 ? (EPT == 16 ? 5 : 3) : TPR == 256 ? 2 : 1;
 constexpr int kMostGroups = 24;
-
-// The launch behind may start when no block of this one waits for a place any more; it waits for this one's end itself.
-__device__ __forceinline__ void launch_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-__device__ __forceinline__ void wait_for_launch_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 // The rows that a group of TPR threads walks, on their way into shared memory `depth` rows ahead: bulk copies that one thread
 // starts.  Neither registers nor a barrier wait for the memory, and a row's 32 elements a thread leave time for little else.
@@ -1004,16 +1006,16 @@ static cudaError_t launch_fwd(const fp8_ctx *ctx, NormFwd p, bool two, cudaStrea
     }
     NormFwd once = p;
     if (two) once.bias = nullptr;
+    cudaError_t e = cudaSuccess;
     by_element_shape(p.cols, [&](auto s) {
         constexpr int kThreads = decltype(s)::kThreads, kElements = decltype(s)::kElements;
         const unsigned grid = blocks_for_rows(ctx, p.rows, 1024 / kThreads);
         count_launch();
         norm_fwd_any_kernel<DT, false, kThreads, kElements><<<grid, kThreads, 0, st>>>(once);
-        if (!two) return;
-        count_launch();
-        norm_fwd_any_kernel<DT, true, kThreads, kElements><<<grid, kThreads, 0, st>>>(p);
+        e = cudaGetLastError();
+        if (two && e == cudaSuccess) e = launch_dependent_with(norm_fwd_any_kernel<DT, true, kThreads, kElements>, grid, kThreads, 0, st, p);
     });
-    return cudaGetLastError();
+    return e;
 }
 
 // Lines of the workspace that a call's row sums take (as many blocks as its kernel has), within the workspace.
