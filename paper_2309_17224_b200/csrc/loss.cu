@@ -432,7 +432,7 @@ __device__ __forceinline__ Sums cluster_join(int blocks, float c, const float4 &
     return all;
 }
 
-// A row (or a part of one) a block.  4096 x 50257 BF16, 412 MB: 74 us from a graph (5.6 TB/s); an element takes 7.4 instructions
+// A row (or a part of one) a block.  4096 x 50257 BF16, 412 MB: 74 us from a graph (5.6 TB/s); an element takes 7.6 instructions
 // and one exponential, which is 49 us of the units for those at 1.76 GHz, and rows of sixteen blocks an SM come in 1.7 rounds.
 // 512 x 128256 FP32 with 20 top tokens, 263 MB: 60 us.  Tried: 32 threads a row (as quick, slower where an SM has few rows); batches
 // of 2, 3 and 6 vectors, 10 and 12 blocks of 128 threads an SM (no better); copies to a ring in shared memory instead of registers
