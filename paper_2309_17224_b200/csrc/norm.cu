@@ -32,7 +32,8 @@ __device__ __forceinline__ float2 corrected(float estimate, float2 sums, int col
 {
     if (estimate * estimate <= 64.0f * average(sums.y, inv_cols)) return make_float2(estimate, sums.y);
     const float mean = estimate + average(sums.x, inv_cols), e = mean - estimate;
-    return make_float2(mean, fmaxf(0.0f, __fmaf_rn(-e, __fmaf_rn(-(float)cols, e, 2.0f * sums.x), sums.y)));
+    const float squares = __fmaf_rn(-e, __fmaf_rn(-(float)cols, e, 2.0f * sums.x), sums.y);
+    return make_float2(mean, squares < 0.0f ? 0.0f : squares);   // (NaN stays)
 }
 
 __device__ __forceinline__ float inverse_deviation(float squares, const double inv_cols, float eps)
