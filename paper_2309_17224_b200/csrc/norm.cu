@@ -36,9 +36,22 @@ __device__ __forceinline__ float2 corrected(float estimate, float2 sums, int col
     return make_float2(mean, squares < 0.0f ? 0.0f : squares);   // (NaN stays)
 }
 
-__device__ __forceinline__ float inverse_deviation(float squares, const double inv_cols, float eps)
+__device__ __forceinline__ float variance(float squares, double inv_cols, float eps) { return (float)((double)squares * inv_cols + (double)eps); }
+// Squares that FP32 holds, with their digits.  Where they pass it, or come near its subnormal numbers, a row's statistics are taken
+// again from its elements times a power of two (2^-96, 2^96), which is exact for all that count: a row of any finite size is
+// normalised.  (NaN goes the same way and comes back.)
+constexpr float kLeastVariance = 0x1p-90f, kFarDown = 0x1p-96f, kFarUp = 0x1p96f;
+__device__ __forceinline__ bool held_by_fp32(float variance)   // (from kLeastVariance to FLT_MAX: one comparison of the bits)
 {
-    return __frsqrt_rn((float)((double)squares * inv_cols + (double)eps));
+    return __builtin_expect(__float_as_uint(variance) - __float_as_uint(kLeastVariance) <= __float_as_uint(FLT_MAX) - __float_as_uint(kLeastVariance), 1);
+}
+__device__ __forceinline__ float far_factor(float rstd) { return rstd >= 0x1p45f ? kFarUp : kFarDown; }   // (rstd: of such a variance)
+// {mean, 1 / standard deviation} from what the row times `by` has: mean and sum of squared deviations.
+__device__ __forceinline__ float2 far_statistics(float by, float mean, float squares, double inv_cols, float eps)
+{
+    const double back = 1.0 / (double)by, var = (double)squares * inv_cols * back * back + (double)eps;
+    const float f = var < (double)kLeastVariance ? kFarUp : var > (double)FLT_MAX ? kFarDown : 1.0f;
+    return make_float2((float)((double)mean * back), __frsqrt_rn((float)(var * (double)f * (double)f)) * f);
 }
 
 template <int DT>
@@ -146,7 +159,28 @@ __global__ void __launch_bounds__(T, 1024 / T) norm_fwd_any_kernel(const NormFwd
                 q = corrected(mean, q, p.cols, p.inv_cols);
                 mean = q.x;
             }
-            rstd = inverse_deviation(q.y, p.inv_cols, p.eps);
+            const float var = variance(q.y, p.inv_cols, p.eps);
+            rstd = __frsqrt_rn(var);
+            if (!held_by_fp32(var)) {
+                const float by = far_factor(rstd);
+                s = 0.0f;
+                each([&](float v, int, int) { s = __fmaf_rn(v, by, s); });
+                s = block_sum<T>(s, part);
+                mean = p.layer ? average(s, p.inv_cols) : 0.0f;
+                q = make_float2(0.0f, 0.0f);
+                each([&](float v, int, int) {
+                    const float d = __fmaf_rn(v, by, -mean);
+                    q = make_float2(q.x + d, __fmaf_rn(d, d, q.y));
+                });
+                q = block_sum2<T>(q, part2);
+                if (p.layer) {
+                    q = corrected(mean, q, p.cols, p.inv_cols);
+                    mean = q.x;
+                }
+                q = far_statistics(by, mean, q.y, p.inv_cols, p.eps);
+                mean = q.x;
+                rstd = q.y;
+            }
             if (threadIdx.x == 0) {
                 if (p.mean) p.mean[r] = mean;
                 if (p.rstd) p.rstd[r] = rstd;
@@ -358,28 +392,55 @@ struct ByteScale {
     __device__ __forceinline__ bool clipped(uint32_t peak) const { return clips<FP8_E4>(of(packed_top<DT>(peak))); }
 };
 
-// From a row's elements and the first estimate of its mean: mean and 1 / standard deviation.  `left`: row_vecs - t.
-template <int TPR, int VECS, int PAIRS>
-__device__ __forceinline__ void row_statistics(const NormFwd &p, const Pair (&h)[VECS][PAIRS], int left, float &mean, float &rstd, float2 *part)
+// From a row's elements and the first estimate of its mean: mean and sum of squared deviations.  FAR: elements times `by`.
+// `left`: row_vecs - t.
+template <int TPR, bool FAR, int VECS, int PAIRS>
+__device__ __forceinline__ float2 row_deviations(const NormFwd &p, const Pair (&h)[VECS][PAIRS], int left, float by, float mean, float2 *part)
 {
-    const Pair less = pair_of(-mean);
+    const Pair less = pair_of(-mean), by2 = pair_of(by);
     Pair d1 = pair_of(0.0f), d2 = d1;
 #pragma unroll
     for (int i = 0; i < VECS; ++i) {
         if (i * TPR >= left) continue;
 #pragma unroll
         for (int k = 0; k < PAIRS; ++k) {
-            const Pair d = h[i][k] + less;
+            const Pair d = FAR ? fma(h[i][k], by2, less) : h[i][k] + less;
             d1 = d1 + d;
             d2 = fma(d, d, d2);
         }
     }
-    float2 q = block_sum2<TPR>(make_float2(sum_of(d1), sum_of(d2)), part);
-    if (p.layer) {
-        q = corrected(mean, q, p.cols, p.inv_cols);
-        mean = q.x;
+    const float2 q = block_sum2<TPR>(make_float2(sum_of(d1), sum_of(d2)), part);
+    return p.layer ? corrected(mean, q, p.cols, p.inv_cols) : make_float2(0.0f, q.y);
+}
+// Mean and 1 / standard deviation; false where they are to be taken from the row times a power of two.
+template <int TPR, int VECS, int PAIRS>
+__device__ __forceinline__ bool row_statistics(const NormFwd &p, const Pair (&h)[VECS][PAIRS], int left, float &mean, float &rstd, float2 *part2)
+{
+    const float2 q = row_deviations<TPR, false>(p, h, left, 1.0f, mean, part2);
+    const float var = variance(q.y, p.inv_cols, p.eps);
+    mean = q.x;
+    rstd = __frsqrt_rn(var);
+    return held_by_fp32(var);
+}
+// (behind row_statistics; shared memory is used in the same order, a barrier lies between two uses of a word)
+template <int TPR, int VECS, int PAIRS>
+__device__ __forceinline__ void far_row_statistics(const NormFwd &p, const Pair (&h)[VECS][PAIRS], int left, float &mean, float &rstd, float *part,
+                                                   float2 *part2)
+{
+    const float by = far_factor(rstd);
+    const Pair by2 = pair_of(by);
+    Pair s = pair_of(0.0f);
+#pragma unroll
+    for (int i = 0; i < VECS; ++i) {
+        if (i * TPR >= left) continue;
+#pragma unroll
+        for (int k = 0; k < PAIRS; ++k) s = fma(h[i][k], by2, s);
     }
-    rstd = inverse_deviation(q.y, p.inv_cols, p.eps);
+    const float sum = block_sum<TPR>(sum_of(s), part);
+    float2 q = row_deviations<TPR, true>(p, h, left, by, p.layer ? average(sum, p.inv_cols) : 0.0f, part2);
+    q = far_statistics(by, q.x, q.y, p.inv_cols, p.eps);
+    mean = q.x;
+    rstd = q.y;
 }
 
 // Few rows whose bytes are wanted: the blocks are one cluster that knows the amax when its rows are done, and casts them from
@@ -422,7 +483,7 @@ __global__ void __launch_bounds__(kRowBlock<TPR>) norm_fwd_cluster_kernel(const 
             for (int k = 0; k < kPairs; ++k) s = s + h[i][k];
         }
         float mean = p.layer ? average(block_sum<TPR>(sum_of(s), part), p.inv_cols) : 0.0f, rstd;
-        row_statistics<TPR, kVecs, kPairs>(p, h, row_vecs - t, mean, rstd, part2[turn]);
+        if (!row_statistics<TPR>(p, h, row_vecs - t, mean, rstd, part2[turn])) far_row_statistics<TPR>(p, h, row_vecs - t, mean, rstd, part, part2[turn]);
         if (t == 0) {
             if (p.mean) p.mean[r] = mean;
             if (p.rstd) p.rstd[r] = rstd;
@@ -498,7 +559,29 @@ __global__ void __launch_bounds__(kRowBlock<TPR>, kResident<TPR, EPT>) norm_fwd_
     const bool bytes = p.y8 && p.bias, want_y = p.y || bytes || p.sink.slot;
     const ByteScale scale(bytes ? *p.bias + p.delta : 0);
     const HeldCoefficients<DT, WF32, kVecs> weight(p.w, 1.0f, t, TPR, row_vecs), shift(p.b, 0.0f, t, TPR, row_vecs);
-    int64_t r = (int64_t)blockIdx.x * kGroups + group;
+    auto write = [&](int64_t r, const Pair(&h)[kVecs][kPairs], float mean, float rstd, bool again) {
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) {
+            const int v = t + i * TPR;
+            if (v >= row_vecs) continue;
+            Pair w[kPairs], b[kPairs];
+            if (again) {   // (the others are held for the loop's sake)
+                asm volatile("" ::: "memory");
+                load_coefficients<DT, WF32>(p.w, v * kN, 1.0f, w);
+                load_coefficients<DT, WF32>(p.b, v * kN, 0.0f, b);
+            } else {
+                weight.get(i, v * kN, w);
+                shift.get(i, v * kN, b);
+            }
+            const uint4 y = normalise_vector<DT>(h[i], mean, rstd, w, b);
+            if (p.sink.slot) acc = fold_vector<DT>(acc, y);
+            if (p.y) reinterpret_cast<uint4 *>(static_cast<uint8_t *>(p.y) + r * p.ld_y * kSize)[v] = y;
+            if (bytes) scale.store<DT>(p.y8, r * p.cols + v * kN, y, peak);
+        }
+    };
+    const int64_t first = (int64_t)blockIdx.x * kGroups + group;
+    int64_t r = first;
+    bool far = false;
     if (t == 0)
         for (int i = 0; i < depth && r + i * step < p.rows; ++i) walk.start(r + i * step, i);
     for (; r < p.rows; r += step, turn ^= 1) {
@@ -516,7 +599,8 @@ __global__ void __launch_bounds__(kRowBlock<TPR>, kResident<TPR, EPT>) norm_fwd_
             for (int k = 0; k < kPairs; ++k) s = s + h[i][k];
         }
         float mean = p.layer ? average(block_sum<TPR>(sum_of(s), part), p.inv_cols) : 0.0f, rstd;
-        row_statistics<TPR, kVecs, kPairs>(p, h, row_vecs - t, mean, rstd, part2[turn]);
+        const bool held = row_statistics<TPR>(p, h, row_vecs - t, mean, rstd, part2[turn]);
+        far = far || !held;
         // every thread has read its part of the slot (a barrier, or the warp's exchange, lies behind it)
         if (TPR == 32) __syncwarp();
         if (t == 0) {
@@ -528,22 +612,37 @@ __global__ void __launch_bounds__(kRowBlock<TPR>, kResident<TPR, EPT>) norm_fwd_
             slot = 0;
             parity ^= 1u;
         }
-        if (want_y) {
+        if (want_y && held) write(r, h, mean, rstd, false);
+    }
+    walk.finish();
+    // rows with statistics that FP32 does not hold, if there were some: once more, from memory, behind the loop that the others
+    // run in (there, their code made 8192 x 4096 with bytes 3 % slower)
+    if (far) {
+        for (r = first; r < p.rows; r += step, turn ^= 1) {
+            const uint8_t *from = static_cast<const uint8_t *>(p.h ? p.h : p.x) + r * (p.h ? p.ld_h : p.ld_x) * kSize;
+            const uint8_t *res = p.h ? nullptr : static_cast<const uint8_t *>(p.res);
+            Pair h[kVecs][kPairs], s = pair_of(0.0f);
 #pragma unroll
             for (int i = 0; i < kVecs; ++i) {
                 const int v = t + i * TPR;
                 if (v >= row_vecs) continue;
-                Pair w[kPairs], b[kPairs];
-                weight.get(i, v * kN, w);
-                shift.get(i, v * kN, b);
-                const uint4 y = normalise_vector<DT>(h[i], mean, rstd, w, b);
-                if (p.sink.slot) acc = fold_vector<DT>(acc, y);
-                if (p.y) reinterpret_cast<uint4 *>(static_cast<uint8_t *>(p.y) + r * p.ld_y * kSize)[v] = y;
-                if (bytes) scale.store<DT>(p.y8, r * p.cols + v * kN, y, peak);
+                uint4 x = reinterpret_cast<const uint4 *>(from)[v];
+                if (res) sum_vector<DT>(x, reinterpret_cast<const uint4 *>(res + r * p.ld_res * kSize)[v], h[i], x);
+                else unpack_pairs<DT>(x, h[i]);
+#pragma unroll
+                for (int k = 0; k < kPairs; ++k) s = s + h[i][k];
+                asm volatile("" ::: "memory");   // (vector by vector: registers are short)
             }
+            float mean = p.layer ? average(block_sum<TPR>(sum_of(s), part), p.inv_cols) : 0.0f, rstd;
+            if (row_statistics<TPR>(p, h, row_vecs - t, mean, rstd, part2[turn])) continue;
+            far_row_statistics<TPR>(p, h, row_vecs - t, mean, rstd, part, part2[turn]);
+            if (t == 0) {
+                if (p.mean) p.mean[r] = mean;
+                if (p.rstd) p.rstd[r] = rstd;
+            }
+            if (want_y) write(r, h, mean, rstd, true);
         }
     }
-    walk.finish();
     if (scale.clipped<DT>(peak)) raise_flags(p.sink.d_status, FP8_FLAG_SATURATED);
     sink_amax(folded_key<DT>(acc), p.sink);
 }

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 import head_reference as R
-from test_gpu_norm import BF16, F16, F32, inputs, new
+from test_gpu_norm import BF16, F16, F32, check_norm, inputs, new
 
 pytestmark = pytest.mark.gpu
 
@@ -55,3 +55,49 @@ def test_rows_that_are_no_numbers(L, ctx, rows, cols, dtype, layer):
         ctx.cast_e4(y, bias, y=want)
         assert torch.equal(y8, want)
     ctx.device_flags()
+
+
+@pytest.mark.parametrize("rows,cols,dtype", [(r, c, BF16 if d == F16 else d) for r, c, d in ROWS])
+@pytest.mark.parametrize("layer", [True, False])
+def test_rows_whose_squares_fp32_does_not_hold(L, ctx, rows, cols, dtype, layer):
+    """Without eps a norm does not know its input's scale: a row times 2^k gives the same bits, its statistics times 2^k and
+    2^-k, whether the squares pass FP32 (k = 70, 110), are subnormal (-75) or nothing (-100).  Rows of ordinary size beside them
+    are what they were, and with an eps the definition holds."""
+    x, res, w, b = inputs(rows, cols, dtype, dtype, 2 * cols, True)
+    x, res = (torch.where(t.abs() < 2.0 ** -10, torch.ones_like(t), t) for t in (x, res))   # (nothing becomes subnormal)
+    kind, b = (L.NORM_LAYER, b) if layer else (L.NORM_RMS, None)
+
+    def run(x, res, eps):
+        out = dict(h=new(rows, cols, dtype=dtype), y=new(rows, cols, dtype=dtype), d_mean=new(rows), d_rstd=new(rows),
+                   y8=new(rows, cols, dtype=torch.uint8), d_bias_out=new(1, dtype=torch.int32))
+        ctx.norm_fwd(x, w, b, residual=res, kind=kind, eps=eps, **out)
+        return out
+    want = run(x, res, 0.0)
+    check_norm(*R.norm(x, w, b, res, eps=0.0, layer=layer), w, b, layer, dtype, want["h"], want["y"], want["d_mean"], want["d_rstd"])
+    for k in (70, 110, -75, -100):
+        by = torch.ones((rows, 1), device="cuda")
+        by[1::2] = 2.0 ** k
+        got = run((x.float() * by).to(dtype), (res.float() * by).to(dtype), 0.0)
+        assert torch.equal(got["h"].float(), want["h"].float() * by)
+        assert torch.equal(got["d_mean"], want["d_mean"] * by[:, 0]) and torch.equal(got["d_rstd"] * by[:, 0], want["d_rstd"])
+        assert all(torch.equal(got[n], want[n]) for n in ("y", "y8", "d_bias_out")), k
+        place, y = (x.float() * by).to(dtype), new(rows, cols, dtype=dtype)   # (the sum in x's place, and only y beside it)
+        ctx.norm_fwd(place, w, b, residual=(res.float() * by).to(dtype), kind=kind, eps=0.0, h=place, y=y)
+        assert torch.equal(place, got["h"]) and torch.equal(y, want["y"])
+    large = (x.float() * 2.0 ** 100).to(dtype)
+    got = run(large, None, 1e-5)
+    check_norm(*R.norm(large, w, b, layer=layer), w, b, layer, dtype, None, got["y"], got["d_mean"], got["d_rstd"])
+
+
+def test_sums_that_fp32_does_not_hold(L, ctx):
+    """Rows whose plain sum passes FP32, up to the type's largest number."""
+    for cols in (512, 4096, 1027):
+        x = torch.linspace(0.5, 1.0, cols, device="cuda").repeat(3, 1)
+        x[1] *= torch.finfo(BF16).max
+        x[2] = torch.finfo(BF16).max
+        x = x.to(BF16)
+        y, mean, rstd = new(3, cols, dtype=BF16), new(3), new(3)
+        ctx.norm_fwd(x, y=y, d_mean=mean, d_rstd=rstd)
+        assert bool(torch.isinf(x[1:].float().sum(-1)).all())
+        check_norm(*R.norm(x), None, None, True, BF16, None, y, mean, rstd)
+        assert bool((y[2] == 0).all()) and float(mean[2]) == torch.finfo(BF16).max
