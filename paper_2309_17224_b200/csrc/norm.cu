@@ -1134,7 +1134,7 @@ template <int DT, bool WF32>
 static unsigned launch_bwd(const fp8_ctx *ctx, NormBwd p, bool want_w, bool want_b, cudaStream_t st)
 {
     auto row = [&](const void *q, int64_t ld) { return !q || row_aligned(q, ld, DT, 16); };
-    const int sums = 2;   // (one output alone takes the same blocks, and gives the same bits)
+    const int sums = want_w || want_b ? 2 : 0;   // (one of the two alone takes the same blocks, and gives the same bits; dx needs no place)
     const bool fast = p.cols % kPerVec<DT> == 0 && p.cols <= kMostHeld && row(p.dy, p.ld_dy) && row(p.h, p.ld_h) && row(p.dh, p.ld_dh) &&
                       row(p.dx, p.ld_dx) && row(p.w, 0);
     unsigned grid = 0;

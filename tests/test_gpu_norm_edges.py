@@ -3,7 +3,7 @@ import pytest
 import torch
 
 import head_reference as R
-from test_gpu_norm import BF16, F16, F32, check_norm, inputs, new
+from test_gpu_norm import BF16, F16, F32, check_grad, check_norm, inputs, new
 
 pytestmark = pytest.mark.gpu
 
@@ -101,3 +101,14 @@ def test_sums_that_fp32_does_not_hold(L, ctx):
         assert bool(torch.isinf(x[1:].float().sum(-1)).all())
         check_norm(*R.norm(x), None, None, True, BF16, None, y, mean, rstd)
         assert bool((y[2] == 0).all()) and float(mean[2]) == torch.finfo(BF16).max
+
+
+@pytest.mark.parametrize("rows,cols", [(1, (1 << 23) + 8), (3, (1 << 24) + 1), (2, 1 << 22)])
+@pytest.mark.parametrize("layer", [True, False])
+def test_gradient_of_very_long_rows(L, ctx, rows, cols, layer):
+    """Without dw and db no workspace is asked for, and rows are as long as they like."""
+    h, dy, _, _ = inputs(rows, cols, BF16, BF16, 21, True)
+    _, _, mean, rstd = R.norm(h, layer=layer)
+    dx = new(rows, cols, dtype=BF16)
+    ctx.norm_bwd(dy, h, None, mean.float() if layer else None, rstd.float(), dx, kind=L.NORM_LAYER if layer else L.NORM_RMS)
+    check_grad(dx, R.norm_grad(dy, h, None, layer=layer)[0], None, dy, h, None, rstd, BF16)
