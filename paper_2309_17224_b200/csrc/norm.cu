@@ -955,8 +955,9 @@ struct RowHold {
     static constexpr int kThreads = TPR, kElements = EPT;
 };
 constexpr int kMostHeld = 16384;
-// A warp per row as long as 32 elements a lane hold it, then as few threads as that allow.  All kernels for whole rows share the
-// shapes, so that a row's sums are taken in one order, whatever is asked for and however many rows there are.
+// A warp per row as long as 32 elements a lane hold it, then as few threads as that allow.  The forward kernels for rows of whole
+// aligned vectors share the shapes, so that such a row's sums are taken in one order, however many rows there are and whether bytes are
+// asked for or not.  (A call in which some tensor is not aligned goes to the kernel by elements.)
 template <typename F>
 static void by_row_shape(int cols, F f)
 {
@@ -1001,6 +1002,9 @@ template <int DT, bool WF32>
 static bool launch_fwd_cluster(const NormFwd &p, cudaStream_t st, cudaError_t &e)
 {
     bool done = false;
+    // (rows that the kernel for many of them does not take: theirs have to come from the same sums)
+    int resident, depth;
+    if (!ring_size(1, 1, (int64_t)p.cols * InType<DT>::kBytes * (p.res ? 2 : 1), resident, depth)) return false;
     by_row_shape(p.cols, [&](auto s) {
         constexpr int kThreads = decltype(s)::kThreads, kBlock = kRowBlock<kThreads>, kGroups = kBlock / kThreads;
         const int64_t blocks = (p.rows + kGroups - 1) / kGroups;

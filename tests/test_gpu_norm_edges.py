@@ -112,3 +112,21 @@ def test_gradient_of_very_long_rows(L, ctx, rows, cols, layer):
     dx = new(rows, cols, dtype=BF16)
     ctx.norm_bwd(dy, h, None, mean.float() if layer else None, rstd.float(), dx, kind=L.NORM_LAYER if layer else L.NORM_RMS)
     check_grad(dx, R.norm_grad(dy, h, None, layer=layer)[0], None, dy, h, None, rstd, BF16)
+
+
+@pytest.mark.parametrize("cols,dtype", [(512, BF16), (4096, F16), (14272, F32), (16384, F32), (16384, BF16)])
+def test_a_row_has_the_same_bits_in_every_call(L, ctx, cols, dtype):
+    """Aligned rows with a residual: statistics and output do not depend on how many rows the call has, nor on whether bytes are
+    asked for beside it."""
+    x, res, w, b = inputs(40, cols, dtype, dtype, 22, True)
+    y, mean, rstd = new(40, cols, dtype=dtype), new(40), new(40)
+    ctx.norm_fwd(x, w, b, residual=res, y=y, d_mean=mean, d_rstd=rstd)
+    for n in (1, 2, 8, 40):
+        got, m, s, y8, bias = new(n, cols, dtype=dtype), new(n), new(n), new(n, cols, dtype=torch.uint8), new(1, dtype=torch.int32)
+        ctx.norm_fwd(x[:n], w, b, residual=res[:n], d_mean=m, d_rstd=s, y8=y8, d_bias_out=bias)
+        want = new(n, cols, dtype=torch.uint8)
+        ctx.cast_e4(y[:n], bias, y=want)
+        assert torch.equal(m, mean[:n]) and torch.equal(s, rstd[:n]) and torch.equal(y8, want), n
+        ctx.norm_fwd(x[:n], w, b, residual=res[:n], y=got)
+        assert torch.equal(got, y[:n]), n
+    ctx.device_flags()
