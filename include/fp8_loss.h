@@ -27,7 +27,7 @@ typedef enum { FP8_I32 = 0, FP8_I64 = 1 } fp8_itype_t;
 /* What the forward calls leave for the backward ones, four floats a row:
  *   [0] the largest logit m (not scaled)   [1] ln sum_j exp(scale (x_j - m))
  *   [2] the entropy (token log probabilities only)   [3] [1] with the listed tokens left out (distillation only)
- * lse is scale * [0] + [1]. */
+ * lse is scale * [0] + [1].  A row of nothing but -infinity has 0 and +infinity there. */
 #define FP8_LOSS_SAVED 4
 #define FP8_LOSS_TOP_MAX 128     /* top tokens of fp8_token_logprobs */
 #define FP8_LOSS_LISTED_MAX 256  /* listed tokens a row of the distillation calls */
@@ -52,7 +52,8 @@ FP8_API fp8_status_t fp8_token_logprobs(fp8_ctx *ctx, const void *logits, fp8_dt
  *     dlogits_j = scale * (g_logprob (1[j = t] - p_j) - g_entropy p_j (lp_j + entropy))
  *   g_logprob, g_entropy   in float, elements g_logprob_stride / g_entropy_stride apart (0: one number for all rows);
  *               NULL counts as zero, not both.  A row without a valid given token has no part of g_logprob.
- *   dlogits     out, of dt, rows ld_d apart; may be logits itself (ld_d = ld then)
+ *   dlogits     out, of dt, rows ld_d apart; may be logits itself (ld_d = ld then).  Where its rows do not lie like those of
+ *               logits relative to 16 bytes, they are written element by element.
  *   d_amax      NULL, or out: amax of dlogits (for the E5 cast of the linear below)
  * Rows whose gradients are zero are written as zeros and their logits are not read. */
 FP8_API fp8_status_t fp8_token_logprobs_bwd(fp8_ctx *ctx, const void *logits, fp8_dtype_t dt, int64_t ld, int64_t rows,

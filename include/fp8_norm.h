@@ -41,8 +41,9 @@ typedef enum { FP8_NORM_LAYER = 0, FP8_NORM_RMS = 1 } fp8_norm_kind_t;
  *   d_amax       NULL, or out: amax of y;   d_bias_out   NULL, or out: the bias of Eq. 3 (E4) for it, minus margin
  *   FP8_FLAG_NONFINITE_AMAX, FP8_FLAG_ZERO_AMAX and FP8_FLAG_SATURATED are raised as fp8_cast_e4 raises them.
  * At least one of h, y, d_mean, d_rstd, y8, d_amax, d_bias_out.  eps >= 0 and finite.  cols up to 2^30.  Pointers and
- * distances need the alignment of an element; rows that are 16-byte aligned with cols a multiple of 8 (4 in FP32) take
- * the fast kernels. */
+ * distances need the alignment of an element.  Rows of up to 16384 columns that are 16-byte aligned in all tensors (y8: 8-byte),
+ * with cols a multiple of 8 (4 in FP32), take the fast kernels; FP32 rows with a residual up to 14272 columns.  The other kernels
+ * go element by element.  Of the fast ones' statistics and output a row has the same bits in every call. */
 typedef struct {
     const void *x, *residual, *weight, *bias_vec;
     void *h, *y;
@@ -66,11 +67,13 @@ FP8_API fp8_status_t fp8_norm_fwd(fp8_ctx *ctx, const fp8_norm_fwd_t *args, void
  *   weight       NULL (ones), or in, of w_dt
  *   d_mean       in, float [rows] (not read for FP8_NORM_RMS, may be NULL);   d_rstd   in, float [rows]
  *   dx           NULL, or out, of dt.  May be dy or dh itself (rows as far apart).
- *   dw, db       NULL, or out, [cols] of w_dt.  Sums over rows are taken in an order that depends on the sizes only:
- *                equal inputs give equal bits.
+ *   dw, db       NULL, or out, [cols] of w_dt.  Sums over rows are taken in an order that depends on the sizes, the type, whether
+ *                there is dh and which kernel the alignment allows, not on the order in which blocks arrive: a call made again
+ *                gives the same bits.
  *   d_amax       NULL, or out: amax of dx (its E5 cast in the linear below needs no pass of its own; needs dx)
  * At least one of dx, dw, db.  dw and db use the context's workspace: calls that share one fp8_ctx must not overlap on the
- * device, like decode-size matmuls.  cols up to 2^22 where dw or db is asked for. */
+ * device, like decode-size matmuls.  cols up to 2^22 where dw or db is asked for.  Fast kernels as above, FP32 rows up to 14272
+ * columns, 9512 with dh. */
 typedef struct {
     const void *dy, *h, *dh, *weight;
     const float *d_mean, *d_rstd;

@@ -112,7 +112,7 @@ def top_tokens(logits, k: int, scale: float = 1.0, vocab: Optional[int] = None, 
 def distill_loss(logits, index, value, scale: float = 1.0, rest: bool = True, vocab: Optional[int] = None, ctx=None):
     """Divergence of the student's logits from the teacher's lists, float32, one a row: index (int32 or int64, negative:
     padding) and value (float32 log probabilities), [..., listed].  ``rest``: all other tokens are one more outcome with what
-    the list leaves; otherwise the listed ones share everything."""
+    the list leaves; otherwise the listed ones share everything.  The lists are the teacher's: no gradient reaches them."""
     if index.shape[:-1] != logits.shape[:-1] or value.shape != index.shape:
         raise ValueError(f"index and value {tuple(logits.shape[:-1])} + (listed,) expected, got {tuple(index.shape)}, {tuple(value.shape)}")
     return _DistillFn.apply(logits, index, value, vocab, scale, rest, _context(logits, ctx))

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 import head_reference as R
-from test_gpu_norm import BF16, F16, F32, check_grad, check_norm, inputs, new
+from test_gpu_norm import BF16, F16, F32, U, check_grad, check_norm, inputs, new
 
 pytestmark = pytest.mark.gpu
 
@@ -130,3 +130,20 @@ def test_a_row_has_the_same_bits_in_every_call(L, ctx, cols, dtype):
         ctx.norm_fwd(x[:n], w, b, residual=res[:n], y=got)
         assert torch.equal(got, y[:n]), n
     ctx.device_flags()
+
+
+@pytest.mark.parametrize("rows,cols,dtype", [(300, 512, BF16), (700, 4096, F32), (300, 8192, F16), (40, 16384, F32), (60, 1027, BF16)])
+def test_row_sums_with_and_without_a_joining_gradient(L, ctx, rows, cols, dtype):
+    """dw and db do not contain dh.  (Which rows are summed together may depend on it: FP32 rows leave room for fewer groups.)"""
+    h, dy, w, _ = inputs(rows, cols, dtype, dtype, 23, True)
+    dh = inputs(rows, cols, dtype, dtype, 24, False)[0]
+    _, _, mean, rstd = (t.float() for t in R.norm(h))
+    _, want_w, want_b = R.norm_grad(dy, h, w)
+    xh = ((h.double() - mean.double().unsqueeze(-1)).abs() + h.double().abs()) * rstd.double().unsqueeze(-1)
+    for join in (None, dh):
+        dx, dw, db = new(rows, cols, dtype=dtype), new(cols, dtype=dtype), new(cols, dtype=dtype)
+        ctx.norm_bwd(dy, h, w, mean, rstd, dx, dh=join, dw=dw, db=db)
+        check_grad(dx, R.norm_grad(dy, h, w, join)[0], join, dy, h, w, rstd, dtype)
+        for got, ref, size in ((dw, want_w, (dy.double().abs() * xh).sum(0)), (db, want_b, dy.double().abs().sum(0))):
+            d = size * (rows + 40) * U + ref.abs() * R.HALF[dtype] + R.TINY[dtype]
+            assert bool(((got.double() - ref).abs() <= d).all())
