@@ -10,6 +10,7 @@ namespace fp8lin {
 
 constexpr int kTopBuffer = 2048;     // candidates for the top tokens of a row
 constexpr float kFloor = -200.0f;    // exponents (base 2) below it are zeros: 2^-200 is none of an FP32 sum
+constexpr float kFarRest = -64.0f;   // ln of the unlisted tokens' sum (relative to the row's largest logit) that is good to 2^-16 of a share
 constexpr float kLn2 = 0.693147180559945309f, kLog2e = 1.44269504088896341f;
 
 __device__ __forceinline__ float exp2_approx(float x)
@@ -859,6 +860,39 @@ __global__ void __launch_bounds__(T) token_logprobs_bwd_kernel(const Logits p, c
     sink_amax(key, o.sink);
 }
 
+// Unlisted tokens far below the row's largest logit (a finite mask on all of them): of the difference of two such distances no digit
+// may be left, so their own largest and sum are taken again, by all parts of the row, before one of them writes: dx_j = a s_j.
+// (Element by element and a call: few rows come here, and the others' code stays as it is.)
+template <int DT, int T>
+__device__ __noinline__ uint32_t write_far_rest(const Row<DT> row, const uint32_t *bits, void *out, int64_t at, int blocks, float c, float a,
+                                                JoinShared<T> &joint, float4 &word)
+{
+    uint32_t key = 0;
+    Sums others = no_sums();
+    float top = -INFINITY;
+    for (int j = threadIdx.x; j < row.n; j += T) {
+        if (is_listed<DT>(bits, row, j)) continue;
+        const float x = row.at(j);
+        add_element<false>(others, x, c);
+        top = fmaxf(top, x);
+    }
+    others = block_join<T>(others, top, c, joint);
+    if (blocks > 1) {
+        cluster_note(others, word);
+        cluster_sync();
+        others = cluster_join(blocks, c, word);
+    }
+    const float log2sum = logf(others.s) * kLog2e;
+    for (int j = threadIdx.x; j < row.n; j += T) {
+        if (is_listed<DT>(bits, row, j)) continue;
+        const uint32_t v = element_bits<DT>(a * exp2_approx(__fmaf_rn(row.at(j) - others.m, c, -log2sum)));
+        key = max(key, magnitude_key(element_value<DT>(v)));
+        store_bits<DT>(out, at + j, v);
+    }
+    if (blocks > 1) cluster_sync();   // (no block leaves while another reads its word)
+    return key;
+}
+
 // 2048 x 50257 FP16 with lists of 32, 412 MB read and written: 73 us (5.6 TB/s), bound by the memory and the list's latency.
 template <int DT, int T>
 __global__ void __launch_bounds__(T) distill_bwd_kernel(const Logits p, const TeacherList l, const float *saved,
@@ -866,6 +900,8 @@ __global__ void __launch_bounds__(T) distill_bwd_kernel(const Logits p, const Te
 {
     extern __shared__ __align__(16) uint32_t listed_bits[];
     __shared__ ListShared<T> sh;
+    __shared__ JoinShared<T> joint;
+    __shared__ float4 word;
     const int64_t r = blockIdx.x / (unsigned)o.blocks;
     const int part = (int)(blockIdx.x % (unsigned)o.blocks), from = part_start(p.vocab, o.blocks, part);
     const int count = part_start(p.vocab, o.blocks, part + 1) - from;
@@ -897,12 +933,16 @@ __global__ void __launch_bounds__(T) distill_bwd_kernel(const Logits p, const Te
             own = element_bits<DT>(g * __fmaf_rn(e.total, prob, -e.q));
         }
         // the others: p_j Q, or with s_j = p_j / p_r, s_j (Q p_r - q_r): s_j is one of a sum of 1 however small p_r is
-        const float logsum = e.rest == 0.0f ? keep.y : keep.w;
         const float a = e.rest == 0.0f ? e.total : __fmaf_rn(e.total, expf(keep.w - keep.y), -e.rest);
-        const ListedVectors<DT> listed(listed_bits, row);
-        write_row<DT, T, false>(row, raw, o.dx, at, o.same, keep.x, p.c, logsum * kLog2e, g * a, 0.0f, key,
-                             [&](int ahead, uint4 &raw) { listed.hide(ahead, raw); },
-                             [&](int j) { return is_listed<DT>(listed_bits, row, j); });
+        if (e.rest != 0.0f && keep.w < kFarRest) {
+            key = write_far_rest<DT, T>(row, listed_bits, o.dx, at, o.blocks, p.c, g * a, joint, word);
+        } else {
+            const float logsum = e.rest == 0.0f ? keep.y : keep.w;
+            const ListedVectors<DT> listed(listed_bits, row);
+            write_row<DT, T, false>(row, raw, o.dx, at, o.same, keep.x, p.c, logsum * kLog2e, g * a, 0.0f, key,
+                                 [&](int ahead, uint4 &raw) { listed.hide(ahead, raw); },
+                                 [&](int j) { return is_listed<DT>(listed_bits, row, j); });
+        }
         __syncthreads();
         if (own_j >= 0) {
             store_bits<DT>(o.dx, at + own_j, own);
@@ -1117,9 +1157,10 @@ fp8_status_t fp8_distill_bwd(fp8_ctx *ctx, const void *logits, fp8_dtype_t dt, i
     const GradOut o = make_grad(ctx, logits, ld, (int)dt, dlogits, ld_d, d_amax, blocks);
     const unsigned shared = list_words((int)vocab) * 4u;
     // (64 threads: 76 us for 2048 rows of 50257 FP16, by 128 they take 72)
+    const bool cluster = l.rest;   // (the parts of a row may have to meet)
     return row_threads(std::max(128, (int)listed), shared) == 128
-               ? FP8LIN_LAUNCH_BY_TYPE(128, distill_bwd_kernel, rows, blocks, false, shared, stream, p, l, saved, g_loss, g_loss_stride, o)
-               : FP8LIN_LAUNCH_BY_TYPE(256, distill_bwd_kernel, rows, blocks, false, shared, stream, p, l, saved, g_loss, g_loss_stride, o);
+               ? FP8LIN_LAUNCH_BY_TYPE(128, distill_bwd_kernel, rows, blocks, cluster, shared, stream, p, l, saved, g_loss, g_loss_stride, o)
+               : FP8LIN_LAUNCH_BY_TYPE(256, distill_bwd_kernel, rows, blocks, cluster, shared, stream, p, l, saved, g_loss, g_loss_stride, o);
 }
 
 }  // extern "C"
