@@ -88,7 +88,8 @@ FP8_API fp8_status_t fp8_distill_fwd(fp8_ctx *ctx, const void *logits, fp8_dtype
 /* Its gradient, g the gradient of the row's loss and Q the sum of the row's q:
  *     dlogits_j = g * scale * (Q p_j - q_j)   for listed tokens,   g * scale * p_j (Q - q_r / p_r)   for the others
  * (q_r = 0 with FP8_DISTILL_TOP); zeros where no entry counts.  p_j / p_r keeps its digits however small p_r is: where all of
- * the others carry a finite mask, too (which does not rule them out: the loss is q_r times its depth then).  g_loss, dlogits, d_amax as in fp8_token_logprobs_bwd. */
+ * the others carry a finite mask, too (which does not rule them out: the loss is q_r times its depth then).  g_loss, dlogits,
+ * d_amax as in fp8_token_logprobs_bwd. */
 FP8_API fp8_status_t fp8_distill_bwd(fp8_ctx *ctx, const void *logits, fp8_dtype_t dt, int64_t ld, int64_t rows,
                                      int64_t vocab, float scale, const void *index, fp8_itype_t it, int64_t ld_index,
                                      const float *value, int64_t ld_value, int32_t listed, fp8_distill_mode_t mode,
