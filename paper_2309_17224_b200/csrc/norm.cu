@@ -38,20 +38,34 @@ __device__ __forceinline__ float2 corrected(float estimate, float2 sums, int col
 
 __device__ __forceinline__ float variance(float squares, double inv_cols, float eps) { return (float)((double)squares * inv_cols + (double)eps); }
 // Squares that FP32 holds, with their digits.  Where they pass it, or come near its subnormal numbers, a row's statistics are taken
-// again from its elements times a power of two (2^-96, 2^96), which is exact for all that count: a row of any finite size is
-// normalised.  (NaN goes the same way and comes back.)
+// again from its deviations times a power of two (2^-96, 2^96), which is exact for all that count: a row of any finite size is
+// normalised.  (Of small squares the mean is good; of large ones it is taken again too.  NaN goes the same way and comes back.)
 constexpr float kLeastVariance = 0x1p-90f, kFarDown = 0x1p-96f, kFarUp = 0x1p96f;
 __device__ __forceinline__ bool held_by_fp32(float variance)   // (from kLeastVariance to FLT_MAX: one comparison of the bits)
 {
     return __builtin_expect(__float_as_uint(variance) - __float_as_uint(kLeastVariance) <= __float_as_uint(FLT_MAX) - __float_as_uint(kLeastVariance), 1);
 }
 __device__ __forceinline__ float far_factor(float rstd) { return rstd >= 0x1p45f ? kFarUp : kFarDown; }   // (rstd: of such a variance)
-// {mean, 1 / standard deviation} from what the row times `by` has: mean and sum of squared deviations.
-__device__ __forceinline__ float2 far_statistics(float by, float mean, float squares, double inv_cols, float eps)
+// The estimate of the mean to go on from; `sum`: of the row times 2^-96.
+__device__ __forceinline__ float far_estimate(float by, float estimate, float sum, double inv_cols)
+{
+    return by == kFarUp ? estimate : average(sum, inv_cols) * kFarUp;
+}
+// `corrected` of sums over deviations times `by`; the estimate and the mean are as they are.
+__device__ __forceinline__ float2 corrected_far(float by, float estimate, float2 sums, int cols, double inv_cols)
+{
+    const float scaled = estimate * by;
+    if (scaled * scaled <= 64.0f * average(sums.y, inv_cols)) return make_float2(estimate, sums.y);
+    const float mean = estimate + average(sums.x, inv_cols) * (by == kFarUp ? kFarDown : kFarUp), e = (mean - estimate) * by;
+    const float squares = __fmaf_rn(-e, __fmaf_rn(-(float)cols, e, 2.0f * sums.x), sums.y);
+    return make_float2(mean, squares < 0.0f ? 0.0f : squares);
+}
+// 1 / standard deviation from a sum of squared deviations times `by`.
+__device__ __forceinline__ float far_inverse(float by, float squares, double inv_cols, float eps)
 {
     const double back = 1.0 / (double)by, var = (double)squares * inv_cols * back * back + (double)eps;
     const float f = var < (double)kLeastVariance ? kFarUp : var > (double)FLT_MAX ? kFarDown : 1.0f;
-    return make_float2((float)((double)mean * back), __frsqrt_rn((float)(var * (double)f * (double)f)) * f);
+    return __frsqrt_rn((float)(var * (double)f * (double)f)) * f;
 }
 
 template <int DT>
@@ -164,22 +178,20 @@ __global__ void __launch_bounds__(T, 1024 / T) norm_fwd_any_kernel(const NormFwd
             if (!held_by_fp32(var)) {
                 const float by = far_factor(rstd);
                 s = 0.0f;
-                each([&](float v, int, int) { s = __fmaf_rn(v, by, s); });
+                each([&](float v, int, int) { s = __fmaf_rn(v, kFarDown, s); });
                 s = block_sum<T>(s, part);
-                mean = p.layer ? average(s, p.inv_cols) : 0.0f;
+                if (p.layer) mean = far_estimate(by, mean, s, p.inv_cols);
                 q = make_float2(0.0f, 0.0f);
                 each([&](float v, int, int) {
-                    const float d = __fmaf_rn(v, by, -mean);
+                    const float d = (v - mean) * by;
                     q = make_float2(q.x + d, __fmaf_rn(d, d, q.y));
                 });
                 q = block_sum2<T>(q, part2);
                 if (p.layer) {
-                    q = corrected(mean, q, p.cols, p.inv_cols);
+                    q = corrected_far(by, mean, q, p.cols, p.inv_cols);
                     mean = q.x;
                 }
-                q = far_statistics(by, mean, q.y, p.inv_cols, p.eps);
-                mean = q.x;
-                rstd = q.y;
+                rstd = far_inverse(by, q.y, p.inv_cols, p.eps);
             }
             if (threadIdx.x == 0) {
                 if (p.mean) p.mean[r] = mean;
@@ -392,10 +404,9 @@ struct ByteScale {
     __device__ __forceinline__ bool clipped(uint32_t peak) const { return clips<FP8_E4>(of(packed_top<DT>(peak))); }
 };
 
-// From a row's elements and the first estimate of its mean: mean and sum of squared deviations.  FAR: elements times `by`.
-// `left`: row_vecs - t.
+// From a row's elements and an estimate of its mean: sums of deviations (FAR: times `by`) and of their squares.  `left`: row_vecs - t.
 template <int TPR, bool FAR, int VECS, int PAIRS>
-__device__ __forceinline__ float2 row_deviations(const NormFwd &p, const Pair (&h)[VECS][PAIRS], int left, float by, float mean, float2 *part)
+__device__ __forceinline__ float2 row_deviations(const Pair (&h)[VECS][PAIRS], int left, float mean, float by, float2 *part)
 {
     const Pair less = pair_of(-mean), by2 = pair_of(by);
     Pair d1 = pair_of(0.0f), d2 = d1;
@@ -404,21 +415,24 @@ __device__ __forceinline__ float2 row_deviations(const NormFwd &p, const Pair (&
         if (i * TPR >= left) continue;
 #pragma unroll
         for (int k = 0; k < PAIRS; ++k) {
-            const Pair d = FAR ? fma(h[i][k], by2, less) : h[i][k] + less;
+            Pair d = h[i][k] + less;
+            if (FAR) d = d * by2;
             d1 = d1 + d;
             d2 = fma(d, d, d2);
         }
     }
-    const float2 q = block_sum2<TPR>(make_float2(sum_of(d1), sum_of(d2)), part);
-    return p.layer ? corrected(mean, q, p.cols, p.inv_cols) : make_float2(0.0f, q.y);
+    return block_sum2<TPR>(make_float2(sum_of(d1), sum_of(d2)), part);
 }
-// Mean and 1 / standard deviation; false where they are to be taken from the row times a power of two.
+// Mean and 1 / standard deviation; false where they are to be taken again.
 template <int TPR, int VECS, int PAIRS>
 __device__ __forceinline__ bool row_statistics(const NormFwd &p, const Pair (&h)[VECS][PAIRS], int left, float &mean, float &rstd, float2 *part2)
 {
-    const float2 q = row_deviations<TPR, false>(p, h, left, 1.0f, mean, part2);
+    float2 q = row_deviations<TPR, false>(h, left, mean, 1.0f, part2);
+    if (p.layer) {
+        q = corrected(mean, q, p.cols, p.inv_cols);
+        mean = q.x;
+    }
     const float var = variance(q.y, p.inv_cols, p.eps);
-    mean = q.x;
     rstd = __frsqrt_rn(var);
     return held_by_fp32(var);
 }
@@ -428,19 +442,22 @@ __device__ __forceinline__ void far_row_statistics(const NormFwd &p, const Pair 
                                                    float2 *part2)
 {
     const float by = far_factor(rstd);
-    const Pair by2 = pair_of(by);
+    const Pair down = pair_of(kFarDown);
     Pair s = pair_of(0.0f);
 #pragma unroll
     for (int i = 0; i < VECS; ++i) {
         if (i * TPR >= left) continue;
 #pragma unroll
-        for (int k = 0; k < PAIRS; ++k) s = fma(h[i][k], by2, s);
+        for (int k = 0; k < PAIRS; ++k) s = fma(h[i][k], down, s);
     }
     const float sum = block_sum<TPR>(sum_of(s), part);
-    float2 q = row_deviations<TPR, true>(p, h, left, by, p.layer ? average(sum, p.inv_cols) : 0.0f, part2);
-    q = far_statistics(by, q.x, q.y, p.inv_cols, p.eps);
-    mean = q.x;
-    rstd = q.y;
+    if (p.layer) mean = far_estimate(by, mean, sum, p.inv_cols);
+    float2 q = row_deviations<TPR, true>(h, left, mean, by, part2);
+    if (p.layer) {
+        q = corrected_far(by, mean, q, p.cols, p.inv_cols);
+        mean = q.x;
+    }
+    rstd = far_inverse(by, q.y, p.inv_cols, p.eps);
 }
 
 // Few rows whose bytes are wanted: the blocks are one cluster that knows the amax when its rows are done, and casts them from

@@ -147,3 +147,23 @@ def test_row_sums_with_and_without_a_joining_gradient(L, ctx, rows, cols, dtype)
         for got, ref, size in ((dw, want_w, (dy.double().abs() * xh).sum(0)), (db, want_b, dy.double().abs().sum(0))):
             d = size * (rows + 40) * U + ref.abs() * R.HALF[dtype] + R.TINY[dtype]
             assert bool(((got.double() - ref).abs() <= d).all())
+
+
+@pytest.mark.parametrize("rows,cols,dtype", [(r, c, BF16 if d == F16 else d) for r, c, d in ROWS])
+def test_large_numbers_of_little_spread(L, ctx, rows, cols, dtype):
+    """No spread to speak of is not the same as small numbers: rows of one number, 2^-40 to 2^120, keep their mean and, with any
+    eps, give zeros; rows of numbers below 2^-60 with a mean far above their spread."""
+    x = torch.exp2(torch.linspace(-40, 120, rows, device="cuda")).unsqueeze(1).expand(rows, cols).to(dtype).contiguous()
+    for eps in (1e-30, 1e-5):
+        y, mean, rstd = new(rows, cols, dtype=dtype), new(rows), new(rows)
+        ctx.norm_fwd(x, eps=eps, y=y, d_mean=mean, d_rstd=rstd, y8=new(rows, cols, dtype=torch.uint8), d_bias_out=new(1, dtype=torch.int32))
+        assert bool((y == 0).all()) and torch.equal(mean, x[:, 0].float())
+        assert bool(((rstd.double() * eps ** 0.5 - 1).abs() <= 4 * U).all())
+    ctx.norm_fwd(x, eps=0.0, d_mean=mean)
+    assert torch.equal(mean, x[:, 0].float())
+    g = torch.Generator(device="cuda").manual_seed(cols)
+    x = ((1 + torch.randn((rows, cols), generator=g, device="cuda") / 32) * 2.0 ** -70).to(dtype)
+    ctx.norm_fwd(x, eps=0.0, y=y, d_mean=mean, d_rstd=rstd)
+    # (the mean's own rounding, 32 spreads of it, is what `path` allows relative to the size)
+    check_norm(*R.norm(x, eps=0.0), None, None, True, dtype, None, y, mean, rstd)
+    ctx.device_flags()
