@@ -13,8 +13,8 @@
  *     y    = (h - mean) * rstd * weight + bias_vec      in FP32, rounded once to the tensors' type
  *     y8   = RNE_E4(y * 2^(bias + delta)), saturating, exactly what fp8_cast_e4 makes of y
  * Sums are FP32; the variance is taken from deviations from the mean.  A row whose sum or squares FP32 does not hold is summed
- * again, its deviations times 2^-96 or 2^96.  A row with a NaN gives NaN, the statistics too; so does one with an infinity in a layer norm.
- * FP8_NORM_RMS has rstd = 1 / infinity = 0 there: y is bias_vec, NaN where the infinity is.
+ * again, its deviations times 2^-96 or 2^96.  A row with a NaN gives NaN, the statistics too; so does one with an infinity in a
+ * layer norm.  FP8_NORM_RMS has rstd = 1 / infinity = 0 there: y is bias_vec, NaN where the infinity is.
  */
 #ifndef FP8_NORM_H
 #define FP8_NORM_H
